@@ -559,6 +559,134 @@ BCP_API int bcp_ipc_close(void* ptr);
 BCP_API int bcp_pack_static(const void* const* tensors, const bcp_pack_meta* metas, size_t n, void* blob,
                             uint64_t blob_bytes, void* stream);
 
+/*
+ * Decoding operators: what a job that runs the resharded parameters needs next (the hand-over to an
+ * evaluation job, Sec. 3.3).  The paper has no counterpart; the formulas are the ones written here.
+ * Rotary positions, a paged key-value cache (optionally in 8 bits) that is written and read back, and
+ * the attention of one new token per sequence over that cache.
+ *
+ * All data pointers in this part are DEVICE pointers; descriptors are host structures that are read
+ * during the call.  Every call is asynchronous on `stream`, allocates nothing, and may be recorded
+ * by a stream capture.  Strides count ELEMENTS; the elements of one head vector are contiguous.
+ * Index arrays live on the device, so the kernels check them: an index outside its range is skipped
+ * as each call describes and a bit is set in the caller's status word, which bcp_decode_status reads.
+ */
+typedef enum { BCP_F32 = 1, BCP_BF16 = 2, BCP_F16 = 3, BCP_E4M3 = 4, BCP_I8 = 5 } bcp_type;
+typedef enum { BCP_ROPE_HALF = 0, BCP_ROPE_PAIRS = 1 } bcp_rope_layout;
+
+#define BCP_MAX_HEAD_DIM 256u /* head_dim: multiple of 16, at most this */
+
+/* n_heads vectors for each token: element e of head h of token t is data[t*token_stride + h*head_stride + e]. */
+typedef struct {
+  void* data;
+  int64_t token_stride; /* >= 0; an input may use 0 (one token or head for all) */
+  int64_t head_stride;
+  uint32_t n_heads;
+  uint32_t type;        /* BCP_F32, BCP_BF16 or BCP_F16 */
+} bcp_heads;
+
+/*
+ * Cosines and sines of the rotation angles: table[p][0][i] = a cos(p f_i), table[p][1][i] = a sin(p f_i)
+ * for positions p < n_positions and pairs i < rot_dim / 2, binary32, dense.  The frequencies f and the
+ * factor a hold whatever scaling a long context needs; the kernels only read the table.
+ * Pair i of a head vector x is (x[i], x[rot_dim/2 + i]) with BCP_ROPE_HALF and (x[2i], x[2i+1]) with
+ * BCP_ROPE_PAIRS; elements from rot_dim on are not rotated.
+ */
+typedef struct {
+  const float* table;   /* 16-byte aligned */
+  int64_t n_positions;  /* 1 .. 2^31-1 */
+  uint32_t rot_dim;     /* even, 2 .. BCP_MAX_HEAD_DIM */
+  uint32_t layout;      /* bcp_rope_layout */
+  uint32_t* status;     /* device word, may be NULL */
+} bcp_rope_table;
+
+/*
+ * A key-value cache in pages.  Element e of head h of the token at `offset` in `page` is
+ * k[page*page_stride + h*head_stride + offset*token_stride + e], the same for v.  A slot names a token's
+ * place: slot = page * page_size + offset.
+ * format BCP_BF16 / BCP_F16: elements are stored as they are.  BCP_E4M3 (no infinities, largest 448) and
+ * BCP_I8 (-127..127): every head vector has a binary32 scale, k_scale[(page*n_heads + h)*page_size + offset],
+ * and stands for element * scale.
+ */
+typedef struct {
+  void* k;               /* 16-byte aligned */
+  void* v;
+  float* k_scale;        /* 8-bit formats; NULL otherwise */
+  float* v_scale;
+  int64_t page_stride;   /* > 0, multiples of 16 bytes */
+  int64_t head_stride;
+  int64_t token_stride;
+  uint32_t n_pages;      /* n_pages * page_size < 2^31 */
+  uint32_t page_size;    /* any number of tokens >= 1 */
+  uint32_t n_heads;
+  uint32_t head_dim;
+  uint32_t format;       /* BCP_BF16, BCP_F16, BCP_E4M3 or BCP_I8 */
+  uint32_t reserved;     /* must be 0 */
+  uint32_t* status;      /* device word, may be NULL */
+} bcp_kv_cache;
+
+#define BCP_BAD_POSITION 1u /* bits of a status word */
+#define BCP_BAD_SLOT 2u
+#define BCP_BAD_PAGE 4u
+#define BCP_BAD_LENGTH 8u
+
+/*
+ * Rotates the heads of n_tokens tokens: (y1, y2) = (x1 c - x2 s, x2 c + x1 s) for every pair, with
+ * the row of the table at positions[t]; computed in binary32 and rounded once.  transpose != 0 applies the
+ * transposed rotation (y1 c + y2 s, y2 c - y1 s), which is the gradient.  q is required; k may be NULL (both
+ * go through one launch: the same tokens and head_dim, the same type).  An output may be its input's own
+ * memory (same data and strides), but must not overlap it in another way.
+ * head_dim is 2 .. BCP_MAX_HEAD_DIM, any number here.  A negative position marks padding: the row is written
+ * as zeros; so is a row whose position is >= n_positions, which also sets BCP_BAD_POSITION.
+ */
+BCP_API int bcp_rope(const bcp_heads* q_in, const bcp_heads* q_out, const bcp_heads* k_in, const bcp_heads* k_out,
+                     uint32_t head_dim, int64_t n_tokens, const bcp_rope_table* rope, const int64_t* positions,
+                     int transpose, void* stream);
+
+/*
+ * Writes the keys and values of n_tokens tokens into their slots; with rope != NULL the keys are rotated on
+ * the way (positions[t], in binary32, not rounded before they are stored).
+ * 8-bit formats: scale = max(max|x| / qmax, 2^-96) with qmax 448 or 127, stored element = x * (1/scale) rounded
+ * to nearest even and limited to +-qmax.  A vector that holds a NaN or an infinity gets a NaN scale, so all
+ * of it reads back as NaN.  A negative slot: the token is skipped.  A slot past the cache (BCP_BAD_SLOT) or a
+ * position outside the table (BCP_BAD_POSITION): the token is skipped.  Slots within one call must differ.
+ */
+BCP_API int bcp_kv_write(const bcp_kv_cache* cache, const bcp_heads* k, const bcp_heads* v, const int64_t* slots,
+                         int64_t n_tokens, const bcp_rope_table* rope, const int64_t* positions, void* stream);
+
+/*
+ * Reads n_tokens tokens back from their slots: element * scale in binary32, rounded once to the outputs' type.
+ * A negative slot, or one past the cache (BCP_BAD_SLOT), gives zeros.
+ */
+BCP_API int bcp_kv_read(const bcp_kv_cache* cache, const int64_t* slots, int64_t n_tokens, const bcp_heads* k_out,
+                        const bcp_heads* v_out, void* stream);
+
+/*
+ * Attention of one new token per sequence.  Sequence b has lengths[b] tokens in the cache, token p at offset
+ * p % page_size of page block_table[b*table_stride + p / page_size].  Query head h reads cache head
+ * h / (q.n_heads / cache.n_heads).  Over the tokens first <= p < lengths[b], first = max(0, lengths[b] - window)
+ * (window 0: all of them):  s_p = scale * q . k_p,  out = sum_p softmax(s)_p v_p,  lse = ln sum_p exp(s_p).
+ * A sequence without tokens (length <= 0) gives zeros and lse = -infinity.
+ * q and out: n_seqs tokens of one type; BCP_BF16 or BCP_F16, the cache's own type unless that has 8 bits.
+ * lse (binary32, [n_seqs][q heads], dense) may be NULL.  Rows of q and out start on 8-byte boundaries.
+ * Scores and sums are binary32; the weights are rounded to 16 bits for the product with the values.
+ * Tokens whose page is outside the cache (BCP_BAD_PAGE) are left out; a length past table_width * page_size
+ * counts as that many (BCP_BAD_LENGTH).
+ * workspace: device memory of at least bcp_kv_attend_workspace bytes, 16-byte aligned, whose first use finds
+ * it zeroed; every call leaves it ready for the next one.  It serves one call at a time: calls that may
+ * overlap on the GPU need a workspace each.
+ */
+BCP_API int bcp_kv_attend_workspace(const bcp_kv_cache* cache, uint32_t n_q_heads, uint32_t max_seqs, uint64_t* bytes);
+BCP_API int bcp_kv_attend(const bcp_kv_cache* cache, const bcp_heads* q, const bcp_heads* out, float* lse, uint32_t n_seqs,
+                          const int32_t* block_table, int64_t table_stride, uint32_t table_width, const int32_t* lengths,
+                          float scale, uint32_t window, void* workspace, uint64_t workspace_bytes, void* stream);
+
+/*
+ * Waits for `stream`, reads the status word of a table or cache, sets it back to zero, and returns BCP_OK or
+ * BCP_ERR_BOUNDS with a message that names the bits.
+ */
+BCP_API int bcp_decode_status(uint32_t* status, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -91,6 +91,21 @@ class PackMetaC(C.Structure):
     _fields_ = [("byte_offset", C.c_uint64), ("byte_length", C.c_uint64)]
 
 
+class HeadsC(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("token_stride", C.c_int64), ("head_stride", C.c_int64), ("n_heads", C.c_uint32), ("type", C.c_uint32)]
+
+
+class RopeTableC(C.Structure):
+    _fields_ = [("table", C.c_void_p), ("n_positions", C.c_int64), ("rot_dim", C.c_uint32), ("layout", C.c_uint32), ("status", C.c_void_p)]
+
+
+class KvCacheC(C.Structure):
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("k_scale", C.c_void_p), ("v_scale", C.c_void_p),
+                ("page_stride", C.c_int64), ("head_stride", C.c_int64), ("token_stride", C.c_int64),
+                ("n_pages", C.c_uint32), ("page_size", C.c_uint32), ("n_heads", C.c_uint32), ("head_dim", C.c_uint32),
+                ("format", C.c_uint32), ("reserved", C.c_uint32), ("status", C.c_void_p)]
+
+
 _VP = C.c_void_p
 _PROTOS = {
     "bcp_version": (C.c_int, []),
@@ -131,6 +146,13 @@ _PROTOS = {
     "bcp_ipc_export": (C.c_int, [_VP, C.POINTER(IpcHandleC)]),
     "bcp_ipc_open": (C.c_int, [C.POINTER(IpcHandleC), C.POINTER(_VP)]),
     "bcp_ipc_close": (C.c_int, [_VP]),
+    "bcp_rope": (C.c_int, [_VP, _VP, _VP, _VP, C.c_uint32, C.c_int64, _VP, _VP, C.c_int, _VP]),
+    "bcp_kv_write": (C.c_int, [_VP, _VP, _VP, _VP, C.c_int64, _VP, _VP, _VP]),
+    "bcp_kv_read": (C.c_int, [_VP, _VP, C.c_int64, _VP, _VP, _VP]),
+    "bcp_kv_attend_workspace": (C.c_int, [_VP, C.c_uint32, C.c_uint32, C.POINTER(C.c_uint64)]),
+    "bcp_kv_attend": (C.c_int, [_VP, _VP, _VP, _VP, C.c_uint32, _VP, C.c_int64, C.c_uint32, _VP, C.c_float, C.c_uint32, _VP,
+                                C.c_uint64, _VP]),
+    "bcp_decode_status": (C.c_int, [_VP, _VP]),
     "bcp_pack_static": (C.c_int, [C.POINTER(_VP), C.POINTER(PackMetaC), C.c_size_t, _VP, C.c_uint64, _VP]),
 }
 

@@ -1,0 +1,775 @@
+// Attention of one new token per sequence over the paged key-value cache.
+//
+// Mathematics.  For one query head the pass over the tokens keeps a reference r, l = sum exp2(s - r) and
+// o = sum exp2(s - r) v, with s = q.k scale log2 e; whenever a score exceeds r by more than 8 the sums are
+// multiplied by exp2(r - r') and r' takes its place.  Any r gives the same o / l; parts of a sequence are
+// joined by bringing their sums to the largest r.  Each key and value is read once, for all query heads
+// that share its cache head.
+//
+// What bounds it: reading the cache.  A byte of 16-bit cache is used in `group` multiply-adds (at most a
+// few dozen), so the matrix instructions only have to keep out of the way.  The products are taken as
+// S^T = K Q^T and O^T = V^T P^T with mma.m16n8k16: tokens (or head dimensions) fill the 16 rows and eight
+// query heads the 8 columns, so that a group of up to eight heads costs one instruction per 16 x 16 block
+// of the cache.  (A tcgen05 product has at least 64 rows: over eight heads it would be filled for an
+// eighth, and its operands would have to be laid out in shared memory first, 8-bit ones converted.)
+//
+// A warp is a worker of its own: it takes 16 tokens at a time through a ring of shared-memory stages that
+// it fills itself with 16-byte asynchronous copies, several stages ahead and across the borders of
+// sequences, so no barrier of the CTA stands in the stream.  The four warps of a CTA take the four quarters
+// of each 64-token step and add up at the end of a stretch of one sequence and cache head.
+//
+// Split.  All steps of all sequences and heads form one line that is cut into as many equal parts as CTAs
+// fit on the GPU; lengths are only known on the device, so each CTA finds its part itself.  A sequence and
+// head that lies in one part is finished there; else every part leaves its sums in the workspace and the
+// one that comes last (a counter per sequence and head) joins them, in the order of the parts, so results
+// do not depend on which that is.
+#include <mutex>
+
+#include "decode.cuh"
+
+using namespace bcp;
+
+namespace {
+
+constexpr int kWarps = 4, kTok = 16, kStep = kWarps * kTok;  // tokens per warp and per step of a CTA
+constexpr float kNone = -3.0e38f;                             // reference before the first token: below every score
+constexpr float kLog2e = 1.4426950408889634f;
+
+struct AttendArgs {
+  const void *k, *v;
+  const float *k_scale, *v_scale;
+  int64_t page_stride, head_stride, token_stride;
+  uint32_t n_pages, n_heads, head_dim;
+  FastDiv page_size;
+  uint32_t* status;
+  const void* q;
+  void* out;
+  float* lse;
+  int64_t q_token, q_head, out_token, out_head;
+  uint32_t q_is_bf16, group, row_tiles, n_seqs;
+  const int32_t* block_table;
+  int64_t table_stride;
+  uint32_t capacity;  // tokens a row of the block table can hold
+  const int32_t* lengths;
+  float scale_log2;
+  uint32_t window;
+  uint32_t* counters;  // one per sequence, cache head and row tile: parts that have arrived
+  float* parts;        // two per CTA: sums, then references, then denominators
+};
+
+template <int FMT, int DP, int NT>
+struct Shape {
+  static constexpr bool quant = FMT == BCP_E4M3 || FMT == BCP_I8;
+  static constexpr int ES = quant ? 1 : 2;
+  static constexpr int ROW = DP * ES;        // bytes of a row in shared memory
+  static constexpr int CPR = ROW / 16;       // 16-byte chunks of a row
+  static constexpr int SIDE = kTok * ROW;
+  static constexpr int STAGE = 2 * SIDE + (quant ? 128 : 0) + 16;  // keys, values, their scales, the mask of live tokens
+  // About 20 KiB a warp (two CTAs of four warps on an SM): enough bytes in flight to cover the latency of HBM.
+  static constexpr int STAGES = STAGE <= 2400 ? 8 : STAGE <= 4400 ? 5 : 3;
+  static constexpr int ROWS = 8 * NT;
+  static constexpr int SMEM = kWarps * STAGES * STAGE + kWarps * 8 * DP * 4 + kWarps * ROWS * 8 + 64;
+  static constexpr int PART = ROWS * (DP + 2);  // floats of one part in the workspace
+};
+
+__device__ __forceinline__ void copy16(uint32_t to, const void* from, bool on) {
+  asm volatile("cp.async.cg.shared.global.L2::128B [%0], [%1], 16, %2;" ::"r"(to), "l"(from), "r"(on ? 16 : 0) : "memory");
+}
+__device__ __forceinline__ void copy4(uint32_t to, const void* from, bool on) {
+  asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(to), "l"(from), "r"(on ? 4 : 0) : "memory");
+}
+__device__ __forceinline__ void copies_end() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+
+__device__ __forceinline__ float exp2_fast(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+__device__ __forceinline__ uint32_t transpose8x8(uint32_t x) {
+  uint32_t y;
+  asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
+  return y;
+}
+__device__ __forceinline__ void load_transposed(uint32_t (&r)[4], uint32_t at) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0, %1, %2, %3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(at) : "memory");
+}
+__device__ __forceinline__ uint4 load_shared16(uint32_t at) {
+  uint4 v;
+  asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(at) : "memory");
+  return v;
+}
+__device__ __forceinline__ uint2 load_shared8(uint32_t at) {
+  uint2 v;
+  asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(at) : "memory");
+  return v;
+}
+__device__ __forceinline__ float load_shared_f32(uint32_t at) {
+  float v;
+  asm volatile("ld.shared.f32 %0, [%1];" : "=f"(v) : "r"(at) : "memory");
+  return v;
+}
+
+// d += a b, a 16 x 16 (row fragments), b 16 x 8; both operands bfloat16 or both binary16
+template <bool BF16>
+__device__ __forceinline__ void mma(float (&d)[4], const uint32_t (&a)[4], const uint32_t (&b)[2]) {
+  if constexpr (BF16)
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+                 : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+                 : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b[0]), "r"(b[1]));
+  else
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+                 : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+                 : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b[0]), "r"(b[1]));
+}
+
+// Two 8-bit elements (low 16 bits of w) as binary16, exactly.
+template <int FMT>
+__device__ __forceinline__ uint32_t widen2(uint32_t w) {
+  if constexpr (FMT == BCP_E4M3) {
+    const __half2_raw h = __nv_cvt_fp8x2_to_halfraw2(__nv_fp8x2_storage_t(w), __NV_E4M3);
+    return uint32_t(h.x) | uint32_t(h.y) << 16;
+  } else {
+    // bytes u = x + 128 under the exponent of 1024 read as 1024 + u; 1152 off gives x
+    const uint32_t biased = __byte_perm(w ^ 0x8080u, 0x64646464u, 0x4140);
+    const __half2 x = __hsub2(*reinterpret_cast<const __half2*>(&biased), __half2half2(__ushort_as_half(0x6480)));
+    return *reinterpret_cast<const uint32_t*>(&x);
+  }
+}
+
+template <bool BF16>
+__device__ __forceinline__ uint32_t pack16(float x, float y) {
+  if constexpr (BF16) {
+    const __nv_bfloat162 p = __floats2bfloat162_rn(x, y);
+    return *reinterpret_cast<const uint32_t*>(&p);
+  } else {
+    const __half2 p = __floats2half2_rn(x, y);
+    return *reinterpret_cast<const uint32_t*>(&p);
+  }
+}
+__device__ __forceinline__ float load16(const void* p, int64_t i, bool bf16) {
+  return bf16 ? __bfloat162float(static_cast<const __nv_bfloat16*>(p)[i]) : __half2float(static_cast<const __half*>(p)[i]);
+}
+
+// Where dimension d of head (column) n lies in a warp's block of sums: eight rows of dimensions and four
+// pairs of heads are written at a time, the exclusive-or spreads them over the banks.
+template <int DP>
+__device__ __forceinline__ uint32_t sum_at(uint32_t n, uint32_t d) {
+  return n * DP + (d ^ (n >> 1) << 3);
+}
+
+// Where 16-byte chunk c of row r lies in a side of a stage.  Keys are read as 16-byte vectors by 8 lanes
+// that hold two rows and four neighbouring chunks, values by 8 lanes with eight rows of one chunk
+// (16-bit, transposing loads) or the four rows 0, 2, 4, 6 (1, 3, 5, 7) and two neighbouring chunks: the
+// exclusive-or spreads each of these over the 32 banks.
+template <int CPR>
+__device__ __forceinline__ uint32_t key_at(uint32_t r, uint32_t c) {
+  if (CPR >= 8) c ^= (r & 1) << 2;
+  return (r * CPR + c) * 16;
+}
+template <int CPR, bool QUANT>
+__device__ __forceinline__ uint32_t value_at(uint32_t r, uint32_t c) {
+  const uint32_t linear = r * CPR + c;
+  if (!QUANT) return (linear ^ (r & 7)) * 16;
+  return (linear ^ ((CPR >= 8 ? r >> 1 : linear >> 3) & 3) << 1) * 16;
+}
+
+struct Span {  // the tokens of one sequence, and its steps
+  uint32_t first, len, base, steps;  // base: first token of step 0, a multiple of 16
+};
+__device__ __forceinline__ Span span_of(const AttendArgs& a, uint32_t b) {
+  Span s;
+  int32_t n = a.lengths[b];
+  n = n < 0 ? 0 : n;
+  s.len = uint32_t(n) > a.capacity ? a.capacity : uint32_t(n);
+  s.first = a.window && s.len > a.window ? s.len - a.window : 0;
+  s.base = s.first & ~15u;
+  s.steps = (s.len - s.base + kStep - 1) / kStep;
+  if (!s.steps) s.steps = 1;  // a sequence without tokens still has a result to write
+  return s;
+}
+
+// A place on the line of steps: sequence b, unit u (cache head and row tile) of it, step of the unit.
+struct Place {
+  uint32_t b, u, step;
+  Span span;
+};
+__device__ __forceinline__ void advance(Place& p, const AttendArgs& a, uint32_t units, bool more) {
+  if (++p.step < p.span.steps) return;
+  p.step = 0;
+  if (++p.u < units) return;
+  p.u = 0;
+  if (++p.b < a.n_seqs && more) p.span = span_of(a, p.b);
+}
+
+template <int FMT, int DP, int NT>
+__global__ void __launch_bounds__(kWarps * 32) bcp_kv_attend_kernel(const AttendArgs a) {
+  typedef Shape<FMT, DP, NT> S;
+  constexpr bool kBf16 = FMT == BCP_BF16;  // type of the products; 8-bit caches are widened to binary16
+  // binary16 weights underflow below 2^-24: lifting them by 2^6 (they stay below 2^16) moves that to 2^-30
+  constexpr float kLift = kBf16 ? 0.f : 6.f;
+  extern __shared__ __align__(128) unsigned char smem[];
+  const uint32_t tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, q4 = lane & 3;
+  const uint32_t ring = uint32_t(__cvta_generic_to_shared(smem)) + warp * (S::STAGES * S::STAGE);
+  unsigned char* const ring_ptr = smem + warp * (S::STAGES * S::STAGE);
+  float* const sum_o = reinterpret_cast<float*>(smem + kWarps * S::STAGES * S::STAGE);  // [warp][sum_at]
+  float* const sum_r = sum_o + kWarps * 8 * DP;                                         // [warp][ROWS] references
+  float* const sum_l = sum_r + kWarps * S::ROWS;                                        // [warp][ROWS] denominators
+  uint32_t* const shared_word = reinterpret_cast<uint32_t*>(sum_l + kWarps * S::ROWS);
+
+  // ---- this CTA's part of the line
+  const uint32_t units = a.n_heads * a.row_tiles;
+  Place at;
+  uint64_t n_line, s0, s1;
+  uint32_t n_parts;
+  {
+    // every thread counts the steps of a run of sequences; an exclusive scan over the threads
+    const uint32_t run = (a.n_seqs + kWarps * 32 - 1) / (kWarps * 32);
+    const uint32_t b0 = tid * run, b1 = min(b0 + run, a.n_seqs);
+    uint64_t mine = 0;
+    for (uint32_t b = b0; b < b1; ++b) mine += span_of(a, b).steps;
+    uint64_t before = mine;
+    for (uint32_t o = 1; o < 32; o <<= 1) {
+      const uint64_t x = __shfl_up_sync(0xffffffffu, before, o);
+      if (lane >= o) before += x;
+    }
+    uint64_t* const totals = reinterpret_cast<uint64_t*>(sum_o);
+    if (lane == 31) totals[warp] = before;
+    __syncthreads();
+    uint64_t all = 0;
+    before -= mine;
+    for (uint32_t w = 0; w < kWarps; ++w) {
+      if (w < warp) before += totals[w];
+      all += totals[w];
+    }
+    n_line = all * units;
+    n_parts = uint32_t(n_line < gridDim.x ? n_line : gridDim.x);
+    if (blockIdx.x >= n_parts) return;
+    s0 = blockIdx.x * n_line / n_parts;
+    s1 = (blockIdx.x + 1) * n_line / n_parts;
+    uint32_t* const found = reinterpret_cast<uint32_t*>(totals + kWarps);
+    if (s0 >= before * units && s0 < (before + mine) * units) {
+      uint64_t pre = before;
+      uint32_t b = b0;
+      for (;; ++b) {
+        const uint32_t n = span_of(a, b).steps;
+        if (s0 < (pre + n) * units) break;
+        pre += n;
+      }
+      const uint32_t steps = span_of(a, b).steps, r = uint32_t(s0 - pre * units);
+      found[0] = b, found[1] = r / steps, found[2] = r % steps;
+    }
+    __syncthreads();
+    at.b = found[0], at.u = found[1], at.step = found[2];
+    at.span = span_of(a, at.b);
+    __syncthreads();
+    if (a.status && blockIdx.x == 0)
+      for (uint32_t b = b0; b < b1; ++b)
+        if (a.lengths[b] > int32_t(a.capacity)) raise(a.status, BCP_BAD_LENGTH);
+  }
+  const uint32_t n_steps = uint32_t(s1 - s0);
+
+  // ---- filling the ring: the next 16 tokens of this warp
+  Place ahead = at;
+  uint32_t produced = 0, fill_stage = 0;
+  auto produce = [&]() {
+    if (produced < n_steps) {
+      const uint32_t stage = ring + fill_stage * S::STAGE;
+      const uint32_t h = NT * 8 >= a.group ? ahead.u : ahead.u / a.row_tiles;
+      const uint32_t r = lane & 15, pos = ahead.span.base + ahead.step * kStep + warp * kTok + r;
+      bool on = pos >= ahead.span.first && pos < ahead.span.len;
+      int64_t row = 0;
+      uint32_t page = 0, off = 0;
+      if (on) {
+        const uint32_t n = a.page_size.div(pos);
+        off = pos - n * a.page_size.d;
+        page = uint32_t(__ldg(a.block_table + ahead.b * a.table_stride + n));
+        if (page >= a.n_pages) {
+          raise(a.status, BCP_BAD_PAGE);
+          on = false, page = 0;
+        }
+        row = page * a.page_stride + h * a.head_stride + off * a.token_stride;
+      }
+      const uint32_t live = __ballot_sync(0xffffffffu, on) & 0xffffu;
+      if (live) {
+#pragma unroll
+        for (int i = 0; i < kTok * S::CPR / 32; ++i) {
+          const uint32_t n = i * 32 + lane, rr = n / S::CPR, c = n % S::CPR;
+          const int64_t from = __shfl_sync(0xffffffffu, row, rr) * S::ES + c * 16;
+          const bool copy = (live >> rr & 1) && c * 16 < a.head_dim * S::ES;
+          copy16(stage + key_at<S::CPR>(rr, c), static_cast<const char*>(a.k) + (copy ? from : 0), copy);
+          copy16(stage + S::SIDE + value_at<S::CPR, S::quant>(rr, c), static_cast<const char*>(a.v) + (copy ? from : 0), copy);
+        }
+        if (S::quant) {
+          const int64_t n = (int64_t(page) * a.n_heads + h) * a.page_size.d + off;
+          copy4(stage + 2 * S::SIDE + lane * 4, (lane < 16 ? a.k_scale : a.v_scale) + (on ? n : 0), on);
+        }
+      }
+      if (lane == 0) *reinterpret_cast<uint32_t*>(ring_ptr + fill_stage * S::STAGE + S::STAGE - 16) = live;
+      ++produced;
+      fill_stage = fill_stage + 1 == S::STAGES ? 0 : fill_stage + 1;
+      advance(ahead, a, units, produced < n_steps);
+    }
+    copies_end();  // one group per stage, empty ones at the end
+  };
+  for (int i = 0; i < S::STAGES - 1; ++i) produce();
+
+  uint32_t done = 0, use_stage = 0;
+  while (done < n_steps) {
+    // ---- one stretch: steps [at.step, at.step + n) of one sequence, cache head and row tile
+    const uint32_t n = min(at.span.steps - at.step, n_steps - done);
+    const uint32_t h = at.u / a.row_tiles, row0 = (at.u - h * a.row_tiles) * S::ROWS;
+    // the queries as column fragments; head dimensions in the order in which the key vectors give them
+    uint32_t qf[NT][DP / 16][2];
+    float factor[NT][2];  // what turns a raw product into a score, for columns 2 q4 and 2 q4 + 1
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+      const bool row_on = row0 + t * 8 + g < a.group;
+      const int64_t q0 = at.b * a.q_token + (h * a.group + row0 + t * 8 + g) * a.q_head;
+      float up = 1.f, down = 1.f;
+      uint2 raw[DP / 16];
+#pragma unroll
+      for (int s = 0; s < DP / 16; ++s) {
+        // 16-byte key vectors hold two (16-bit) or four (8-bit) such groups of four dimensions
+        const uint32_t d = S::quant ? 64 * (s / 4) + 16 * q4 + 4 * (s % 4) : 32 * (s / 2) + 8 * q4 + 4 * (s % 2);
+        raw[s] = row_on && d < a.head_dim ? *reinterpret_cast<const uint2*>(static_cast<const char*>(a.q) + (q0 + d) * 2) : make_uint2(0, 0);
+      }
+      if (S::quant) {
+        // a power of two brings the largest element into [1, 2): bfloat16 queries then fit binary16 with
+        // an error of at most 2^-25 of the largest element
+        uint32_t top = 0;
+        float x[DP / 16][4];
+#pragma unroll
+        for (int s = 0; s < DP / 16; ++s)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            x[s][i] = load16(&raw[s], i, a.q_is_bf16);
+            top = max(top, __float_as_uint(x[s][i]) & 0x7fffffffu);
+          }
+        top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
+        top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
+        const uint32_t e = top >> 23 == 254 ? 253 : top >> 23;
+        if (e >= 1 && e <= 253) up = __uint_as_float((254 - e) << 23), down = __uint_as_float(e << 23);
+#pragma unroll
+        for (int s = 0; s < DP / 16; ++s) {
+          qf[t][s][0] = pack16<false>(x[s][0] * up, x[s][1] * up);
+          qf[t][s][1] = pack16<false>(x[s][2] * up, x[s][3] * up);
+        }
+      } else {
+#pragma unroll
+        for (int s = 0; s < DP / 16; ++s) qf[t][s][0] = raw[s].x, qf[t][s][1] = raw[s].y;
+      }
+      factor[t][0] = __shfl_sync(0xffffffffu, down, 8 * q4) * a.scale_log2;  // lane 4 n holds column n
+      factor[t][1] = __shfl_sync(0xffffffffu, down, 8 * q4 + 4) * a.scale_log2;
+    }
+    float o[NT][DP / 16][4], ref[NT][2], l[NT][2];
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+      ref[t][0] = ref[t][1] = kNone, l[t][0] = l[t][1] = 0.f;
+#pragma unroll
+      for (int m = 0; m < DP / 16; ++m) o[t][m][0] = o[t][m][1] = o[t][m][2] = o[t][m][3] = 0.f;
+    }
+
+    for (uint32_t i = 0; i < n; ++i) {
+      copies_wait<S::STAGES - 2>();
+      __syncwarp();  // every lane's copies have landed, and every lane is done with the stage that is filled next
+      const uint32_t stage = ring + use_stage * S::STAGE;
+      const uint32_t live = *reinterpret_cast<const volatile uint32_t*>(ring_ptr + use_stage * S::STAGE + S::STAGE - 16);
+      use_stage = use_stage + 1 == S::STAGES ? 0 : use_stage + 1;
+      produce();
+      if (!live) continue;
+
+      // scores of 16 tokens (rows) and 8 NT heads (columns)
+      float s[NT][4];
+#pragma unroll
+      for (int t = 0; t < NT; ++t) s[t][0] = s[t][1] = s[t][2] = s[t][3] = 0.f;
+      if constexpr (!S::quant) {
+#pragma unroll
+        for (int j = 0; j < DP / 32; ++j) {
+          const uint4 x = load_shared16(stage + key_at<S::CPR>(g, 4 * j + q4)), y = load_shared16(stage + key_at<S::CPR>(g + 8, 4 * j + q4));
+          const uint32_t a0[4] = {x.x, y.x, x.y, y.y}, a1[4] = {x.z, y.z, x.w, y.w};
+#pragma unroll
+          for (int t = 0; t < NT; ++t) {
+            mma<kBf16>(s[t], a0, qf[t][2 * j]);
+            mma<kBf16>(s[t], a1, qf[t][2 * j + 1]);
+          }
+        }
+      } else {
+#pragma unroll
+        for (int j = 0; j < DP / 64; ++j) {
+          const uint4 x = load_shared16(stage + key_at<S::CPR>(g, 4 * j + q4)), y = load_shared16(stage + key_at<S::CPR>(g + 8, 4 * j + q4));
+          const uint32_t xs[4] = {x.x, x.y, x.z, x.w}, ys[4] = {y.x, y.y, y.z, y.w};
+#pragma unroll
+          for (int w = 0; w < 4; ++w) {
+            const uint32_t f[4] = {widen2<FMT>(xs[w] & 0xffffu), widen2<FMT>(ys[w] & 0xffffu), widen2<FMT>(xs[w] >> 16), widen2<FMT>(ys[w] >> 16)};
+#pragma unroll
+            for (int t = 0; t < NT; ++t) mma<kBf16>(s[t], f, qf[t][4 * j + w]);
+          }
+        }
+      }
+      // scores of tokens g and g + 8; 8-bit values: their scale 2^e f goes into the weight, e into its
+      // exponent and f into the factor, so that the weights of the product stay in range whatever the scales
+      float vf[2] = {1.f, 1.f}, ve[2] = {0.f, 0.f}, ks[2] = {1.f, 1.f};
+      if constexpr (S::quant) {
+#pragma unroll
+        for (int r = 0; r < 2; ++r) {
+          ks[r] = load_shared_f32(stage + 2 * S::SIDE + (g + 8 * r) * 4);
+          const float x = load_shared_f32(stage + 2 * S::SIDE + 64 + (g + 8 * r) * 4);
+          const uint32_t v = __float_as_uint(x), e = v >> 23 & 255u;
+          ve[r] = float(int(max(e, 31u)) - 127);  // scales below 2^-96 (a zero, too) keep the exponent of that
+          vf[r] = e < 31 ? x * 0x1p96f : e == 255 ? __uint_as_float(0x7fc00000u) : __uint_as_float((v & 0x807fffffu) | 0x3f800000u);
+        }
+      }
+      bool above = false;
+#pragma unroll
+      for (int t = 0; t < NT; ++t)
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+          const bool in = live >> (g + 8 * (c >> 1)) & 1;
+          s[t][c] = in ? s[t][c] * factor[t][c & 1] * ks[c >> 1] : -INFINITY;
+          above |= s[t][c] + ve[c >> 1] > ref[t][c & 1] + 8.f;
+        }
+      if (__any_sync(0xffffffffu, above)) {
+#pragma unroll
+        for (int t = 0; t < NT; ++t)
+#pragma unroll
+          for (int c = 0; c < 2; ++c) {
+            float m = fmaxf(s[t][c] + ve[0], s[t][c + 2] + ve[1]);
+            m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 4));
+            m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 8));
+            m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 16));
+            m = fmaxf(m, ref[t][c]);
+            const float down = exp2_fast(ref[t][c] - m);
+            ref[t][c] = m;
+            l[t][c] *= down;
+#pragma unroll
+            for (int k = 0; k < DP / 16; ++k) o[t][k][c] *= down, o[t][k][c + 2] *= down;
+          }
+      }
+      uint32_t pf[NT][2];
+#pragma unroll
+      for (int t = 0; t < NT; ++t) {
+        float p[4];
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+          const float x = s[t][c] - ref[t][c & 1] + kLift;
+          if constexpr (S::quant) {
+            l[t][c & 1] += exp2_fast(x);
+            p[c] = exp2_fast(x + ve[c >> 1]) * vf[c >> 1];
+            if (!(live >> (g + 8 * (c >> 1)) & 1)) p[c] = 0.f;
+          } else {
+            p[c] = exp2_fast(x);
+            l[t][c & 1] += p[c];
+          }
+        }
+        pf[t][0] = transpose8x8(pack16<kBf16>(p[0], p[1]));
+        pf[t][1] = transpose8x8(pack16<kBf16>(p[2], p[3]));
+      }
+      // sums over the values: rows are head dimensions
+      if constexpr (!S::quant) {
+#pragma unroll
+        for (int m = 0; m < DP / 16; ++m) {
+          uint32_t f[4];
+          load_transposed(f, stage + S::SIDE + value_at<S::CPR, false>((lane & 7) + (lane >> 4 << 3), 2 * m + (lane >> 3 & 1)));
+#pragma unroll
+          for (int t = 0; t < NT; ++t) mma<kBf16>(o[t][m], f, pf[t]);
+        }
+      } else {
+        constexpr int kWords = DP >= 128 ? 4 : DP / 32;  // words a lane takes of each of its four tokens at once
+#pragma unroll
+        for (int j = 0; j < (DP + 127) / 128; ++j) {
+          uint32_t w[4][kWords];
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            const uint32_t token = 2 * q4 + (r & 1) + 8 * (r >> 1);
+            if constexpr (kWords == 4) {
+              const uint4 x = load_shared16(stage + S::SIDE + value_at<S::CPR, true>(token, 8 * j + g));
+              w[r][0] = x.x, w[r][1] = x.y, w[r][2] = x.z, w[r][3] = x.w;
+            } else {
+              const uint2 x = load_shared8(stage + S::SIDE + value_at<S::CPR, true>(token, g >> 1) + (g & 1) * 8);
+              w[r][0] = x.x, w[r][1] = x.y;
+            }
+          }
+#pragma unroll
+          for (int x = 0; x < kWords; ++x) {
+#pragma unroll
+            for (int half = 0; half < 2; ++half) {
+              const uint32_t pick = half ? 0x7362 : 0x5140;
+              const uint32_t lo = __byte_perm(w[0][x], w[1][x], pick), hi = __byte_perm(w[2][x], w[3][x], pick);
+              const uint32_t f[4] = {widen2<FMT>(lo & 0xffffu), widen2<FMT>(lo >> 16), widen2<FMT>(hi & 0xffffu), widen2<FMT>(hi >> 16)};
+#pragma unroll
+              for (int t = 0; t < NT; ++t) mma<kBf16>(o[t][8 * j + 2 * x + half], f, pf[t]);
+            }
+          }
+        }
+      }
+    }
+    done += n;
+
+    // ---- the four warps' sums together
+    const bool starts = at.step == 0, ends = at.step + n == at.span.steps;
+#pragma unroll
+    for (int t = 0; t < NT; ++t)
+#pragma unroll
+      for (int c = 0; c < 2; ++c) {
+        float x = l[t][c];
+        x += __shfl_xor_sync(0xffffffffu, x, 4);
+        x += __shfl_xor_sync(0xffffffffu, x, 8);
+        x += __shfl_xor_sync(0xffffffffu, x, 16);
+        if (g == 0) {
+          sum_r[warp * S::ROWS + t * 8 + 2 * q4 + c] = ref[t][c];
+          sum_l[warp * S::ROWS + t * 8 + 2 * q4 + c] = x;
+        }
+      }
+    __syncthreads();
+    const uint64_t place = s0 + done - n;  // of the stretch's first step on the line
+    float* const part = a.parts + (uint64_t(blockIdx.x) * 2 + (place != s0)) * S::PART;
+    const uint32_t head = tid >> 4, sub = tid & 15;  // in the sums: 16 threads per head, four dimensions at a time
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+#pragma unroll
+      for (int c = 0; c < 2; ++c) {
+        const uint32_t col = t * 8 + 2 * q4 + c;
+        float m = sum_r[col];
+#pragma unroll
+        for (int w = 1; w < kWarps; ++w) m = fmaxf(m, sum_r[w * S::ROWS + col]);
+        const float down = exp2_fast(ref[t][c] - m);
+#pragma unroll
+        for (int k = 0; k < DP / 16; ++k)
+#pragma unroll
+          for (int r = 0; r < 2; ++r) {
+            const uint32_t d = !S::quant ? 16 * k + 8 * r + g : DP >= 128 ? 128 * (k / 8) + 16 * g + 2 * (k % 8) + r : (DP / 8) * g + 2 * k + r;
+            sum_o[warp * 8 * DP + sum_at<DP>(2 * q4 + c, d)] = o[t][k][c + 2 * r] * down;
+          }
+      }
+      __syncthreads();
+      const uint32_t col = t * 8 + head;
+      float m = sum_r[col], den = 0.f;
+#pragma unroll
+      for (int w = 1; w < kWarps; ++w) m = fmaxf(m, sum_r[w * S::ROWS + col]);
+#pragma unroll
+      for (int w = 0; w < kWarps; ++w) den += sum_l[w * S::ROWS + col] * exp2_fast(sum_r[w * S::ROWS + col] - m);
+      const bool whole = starts && ends, row_on = row0 + col < a.group;
+      const uint32_t qh = h * a.group + row0 + col;
+#pragma unroll
+      for (int i = 0; i < DP / 64; ++i) {
+        const uint32_t d = 64 * i + 4 * sub;
+        float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+        for (int w = 0; w < kWarps; ++w) {
+          const float4 y = *reinterpret_cast<const float4*>(sum_o + w * 8 * DP + sum_at<DP>(head, d));
+          x.x += y.x, x.y += y.y, x.z += y.z, x.w += y.w;
+        }
+        if (!whole) {
+          __stcg(reinterpret_cast<float4*>(part + col * DP + d), x);
+        } else if (row_on && d < a.head_dim) {
+          const float inv = den == 0.f ? 0.f : 1.f / den;
+          uint2 y;
+          y.x = a.q_is_bf16 ? pack16<true>(x.x * inv, x.y * inv) : pack16<false>(x.x * inv, x.y * inv);
+          y.y = a.q_is_bf16 ? pack16<true>(x.z * inv, x.w * inv) : pack16<false>(x.z * inv, x.w * inv);
+          *reinterpret_cast<uint2*>(static_cast<char*>(a.out) + (at.b * a.out_token + qh * a.out_head + d) * 2) = y;
+        }
+      }
+      if (sub == 0) {
+        if (!whole) {
+          __stcg(part + S::ROWS * DP + col, m);
+          __stcg(part + S::ROWS * (DP + 1) + col, den);
+        } else if (row_on && a.lse) {
+          a.lse[uint64_t(at.b) * (a.n_heads * a.group) + qh] = den == 0.f ? -INFINITY : (m - kLift + log2f(den)) * 0.6931471805599453f;
+        }
+      }
+      __syncthreads();
+    }
+
+    if (!(starts && ends)) {
+      // ---- the unit lies in several parts: the last one to arrive joins them
+      const uint64_t u0 = place - at.step, u1 = u0 + at.span.steps;  // the unit on the line
+      const uint32_t c0 = uint32_t(((u0 + 1) * n_parts - 1) / n_line), c1 = uint32_t((u1 * n_parts - 1) / n_line);
+      uint32_t* const counter = a.counters + uint64_t(at.b) * units + at.u;
+      __threadfence();
+      __syncthreads();
+      if (tid == 0) {
+        const uint32_t arrived = atomicAdd(counter, 1u);
+        *shared_word = arrived == c1 - c0;
+        if (arrived == c1 - c0) *counter = 0;  // ready for the next call
+      }
+      __syncthreads();
+      if (*shared_word) {
+        __threadfence();
+        // the first part lies in its CTA's second place unless the unit begins where that CTA does
+        const bool second = c0 * n_line / n_parts != u0;
+        for (int t = 0; t < NT; ++t) {
+          const uint32_t col = t * 8 + head, qh = h * a.group + row0 + col;
+          float m = kNone;
+          for (uint32_t c = c0; c <= c1; ++c) m = fmaxf(m, __ldcg(a.parts + (uint64_t(c) * 2 + (c == c0 && second)) * S::PART + S::ROWS * DP + col));
+          float den = 0.f;
+          float4 x[DP / 64];
+#pragma unroll
+          for (int i = 0; i < DP / 64; ++i) x[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
+          for (uint32_t c = c0; c <= c1; ++c) {
+            const float* const from = a.parts + (uint64_t(c) * 2 + (c == c0 && second)) * S::PART;
+            const float down = exp2_fast(__ldcg(from + S::ROWS * DP + col) - m);
+            den += __ldcg(from + S::ROWS * (DP + 1) + col) * down;
+#pragma unroll
+            for (int i = 0; i < DP / 64; ++i) {
+              const float4 y = __ldcg(reinterpret_cast<const float4*>(from + col * DP + 64 * i + 4 * sub));
+              x[i].x += y.x * down, x[i].y += y.y * down, x[i].z += y.z * down, x[i].w += y.w * down;
+            }
+          }
+          if (row0 + col < a.group) {
+            const float inv = den == 0.f ? 0.f : 1.f / den;
+#pragma unroll
+            for (int i = 0; i < DP / 64; ++i) {
+              const uint32_t d = 64 * i + 4 * sub;
+              if (d >= a.head_dim) break;
+              uint2 y;
+              y.x = a.q_is_bf16 ? pack16<true>(x[i].x * inv, x[i].y * inv) : pack16<false>(x[i].x * inv, x[i].y * inv);
+              y.y = a.q_is_bf16 ? pack16<true>(x[i].z * inv, x[i].w * inv) : pack16<false>(x[i].z * inv, x[i].w * inv);
+              *reinterpret_cast<uint2*>(static_cast<char*>(a.out) + (at.b * a.out_token + qh * a.out_head + d) * 2) = y;
+            }
+            if (sub == 0 && a.lse)
+              a.lse[uint64_t(at.b) * (a.n_heads * a.group) + qh] = den == 0.f ? -INFINITY : (m - kLift + log2f(den)) * 0.6931471805599453f;
+          }
+        }
+      }
+    }
+    at.step += n - 1;
+    advance(at, a, units, done < n_steps);
+  }
+}
+
+// ------------------------------------------------------------------------------ launch
+typedef void (*Kernel)(AttendArgs);
+struct Variant {
+  Kernel kernel;
+  uint32_t smem, rows, part_floats;
+};
+
+template <int FMT, int DP, int NT>
+Variant variant() {
+  typedef Shape<FMT, DP, NT> S;
+  return Variant{bcp_kv_attend_kernel<FMT, DP, NT>, S::SMEM, S::ROWS, S::PART};
+}
+template <int FMT>
+Variant variant_of(uint32_t head_dim, uint32_t group) {
+  // Query heads of a group beyond eight take a second column block (16 rows share each key and value that
+  // was read); with 256 dimensions the sums of 16 rows would not fit the registers, more rows are more units.
+  if (head_dim <= 64) return group <= 8 ? variant<FMT, 64, 1>() : variant<FMT, 64, 2>();
+  if (head_dim <= 128) return group <= 8 ? variant<FMT, 128, 1>() : variant<FMT, 128, 2>();
+  return variant<FMT, 256, 1>();
+}
+Variant variant_of(uint32_t format, uint32_t head_dim, uint32_t group) {
+  switch (format) {
+    case BCP_BF16: return variant_of<BCP_BF16>(head_dim, group);
+    case BCP_F16: return variant_of<BCP_F16>(head_dim, group);
+    case BCP_E4M3: return variant_of<BCP_E4M3>(head_dim, group);
+    default: return variant_of<BCP_I8>(head_dim, group);
+  }
+}
+
+// CTAs of a kernel that fit on the current device, asked once per kernel and device.
+int resident_ctas(const Variant& v, uint32_t* out) {
+  struct Known {
+    Kernel kernel;
+    int device;
+    uint32_t ctas;
+  };
+  static std::mutex mu;
+  static Known known[256];
+  static int n_known = 0;
+  int device = 0;
+  BCP_CUDA(cudaGetDevice(&device));
+  std::lock_guard<std::mutex> lock(mu);
+  for (int i = 0; i < n_known; ++i)
+    if (known[i].kernel == v.kernel && known[i].device == device) {
+      *out = known[i].ctas;
+      return BCP_OK;
+    }
+  int per_sm = 0, sms = 0;
+  BCP_CUDA(cudaFuncSetAttribute(v.kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, int(v.smem)));
+  BCP_CUDA(cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, v.kernel, kWarps * 32, v.smem));
+  BCP_CUDA(cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, device));
+  if (per_sm < 1) return fail(BCP_ERR_CUDA, "bcp_kv_attend: the kernel does not fit on this device");
+  *out = uint32_t(per_sm * sms);
+  if (n_known < 256) known[n_known++] = Known{v.kernel, device, *out};
+  return BCP_OK;
+}
+
+uint64_t counter_bytes(uint64_t units) { return (units * 4 + 255) & ~uint64_t(255); }
+
+int check_group(const char* call, const bcp_kv_cache* c, uint32_t n_q_heads) {
+  if (!n_q_heads || n_q_heads > 65536 || n_q_heads % c->n_heads)
+    return fail(BCP_ERR_MISMATCH, "%s: %u query heads are not a multiple of %u cache heads", call, n_q_heads, c->n_heads);
+  return BCP_OK;
+}
+
+}  // namespace
+
+extern "C" int bcp_kv_attend_workspace(const bcp_kv_cache* cache, uint32_t n_q_heads, uint32_t max_seqs, uint64_t* bytes) {
+  const char* call = "bcp_kv_attend_workspace";
+  if (!bytes) return fail(BCP_ERR_INVALID, "%s: bytes is NULL", call);
+  if (int rc = check_cache(call, cache)) return rc;
+  if (int rc = check_group(call, cache, n_q_heads)) return rc;
+  const uint32_t group = n_q_heads / cache->n_heads;
+  const Variant v = variant_of(cache->format, cache->head_dim, group);
+  uint32_t ctas = 0;
+  if (int rc = resident_ctas(v, &ctas)) return rc;
+  const uint64_t units = uint64_t(max_seqs) * cache->n_heads * ((group + v.rows - 1) / v.rows);
+  *bytes = counter_bytes(units) + uint64_t(ctas) * 2 * v.part_floats * 4;
+  return BCP_OK;
+}
+
+extern "C" int bcp_kv_attend(const bcp_kv_cache* c, const bcp_heads* q, const bcp_heads* out, float* lse, uint32_t n_seqs,
+                             const int32_t* block_table, int64_t table_stride, uint32_t table_width, const int32_t* lengths, float scale,
+                             uint32_t window, void* workspace, uint64_t workspace_bytes, void* stream) {
+  const char* call = "bcp_kv_attend";
+  if (int rc = check_cache(call, c)) return rc;
+  if (int rc = check_heads(call, "q", q, false, c->head_dim, n_seqs)) return rc;
+  if (int rc = check_heads(call, "out", out, true, c->head_dim, n_seqs)) return rc;
+  if (int rc = check_group(call, c, q->n_heads)) return rc;
+  if (out->n_heads != q->n_heads || out->type != q->type) return fail(BCP_ERR_MISMATCH, "%s: out must have the heads and the type of q", call);
+  if (q->type == BCP_F32 || (!is_8bit(c->format) && q->type != c->format))
+    return fail(BCP_ERR_MISMATCH, "%s: queries of type %u over a cache of format %u (16-bit queries, of the cache's type unless that has 8 bits)", call,
+                q->type, c->format);
+  if (!rows_aligned(q, 8) || !rows_aligned(out, 8)) return fail(BCP_ERR_INVALID, "%s: rows of q and out must start on 8-byte boundaries", call);
+  if (n_seqs > 0x7fffffffu) return fail(BCP_ERR_INVALID, "%s: %u sequences", call, n_seqs);
+  if (n_seqs == 0) return BCP_OK;
+  if (!block_table || !lengths || table_stride < 0 || (n_seqs > 1 && table_stride < int64_t(table_width)))
+    return fail(BCP_ERR_INVALID, "%s: block_table or lengths is NULL, or rows of the table overlap", call);
+  if (!(scale == scale) || scale - scale != 0.f) return fail(BCP_ERR_INVALID, "%s: scale is not a finite number", call);
+
+  const uint32_t group = q->n_heads / c->n_heads;
+  const Variant v = variant_of(c->format, c->head_dim, group);
+  uint32_t ctas = 0;
+  if (int rc = resident_ctas(v, &ctas)) return rc;
+  AttendArgs a;
+  a.row_tiles = (group + v.rows - 1) / v.rows;
+  const uint64_t units = uint64_t(n_seqs) * c->n_heads * a.row_tiles;
+  const uint64_t need = counter_bytes(units) + uint64_t(ctas) * 2 * v.part_floats * 4;
+  if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 15)) return fail(BCP_ERR_INVALID, "%s: workspace is NULL or not 16-byte aligned", call);
+  if (workspace_bytes < need)
+    return fail(BCP_ERR_CAPACITY, "%s: a workspace of %llu bytes, %llu needed", call, (unsigned long long)workspace_bytes, (unsigned long long)need);
+  const uint64_t capacity = uint64_t(table_width) * c->page_size;
+  a.capacity = uint32_t(capacity < 0x7fffff00u ? capacity : 0x7fffff00u);
+  a.k = c->k, a.v = c->v, a.k_scale = c->k_scale, a.v_scale = c->v_scale;
+  a.page_stride = c->page_stride, a.head_stride = c->head_stride, a.token_stride = c->token_stride;
+  a.n_pages = c->n_pages, a.n_heads = c->n_heads, a.head_dim = c->head_dim;
+  a.page_size = FastDiv(c->page_size);
+  a.status = c->status;
+  a.q = q->data, a.out = out->data, a.lse = lse;
+  a.q_token = q->token_stride, a.q_head = q->head_stride, a.out_token = out->token_stride, a.out_head = out->head_stride;
+  a.q_is_bf16 = q->type == BCP_BF16, a.group = group, a.n_seqs = n_seqs;
+  a.block_table = block_table, a.table_stride = table_stride, a.lengths = lengths;
+  a.scale_log2 = scale * kLog2e, a.window = window;
+  a.counters = static_cast<uint32_t*>(workspace);
+  a.parts = reinterpret_cast<float*>(static_cast<char*>(workspace) + counter_bytes(units));
+  // no more CTAs than the longest lengths the table allows can use
+  uint32_t longest = a.capacity;
+  if (window && window < longest) longest = window + 15 < longest ? window + 15 : longest;
+  const uint64_t most = units * (longest / kStep + 1);
+  v.kernel<<<uint32_t(most < ctas ? most : ctas), kWarps * 32, v.smem, static_cast<cudaStream_t>(stream)>>>(a);
+  BCP_LAUNCHED(call);
+  return BCP_OK;
+}

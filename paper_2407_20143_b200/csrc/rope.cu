@@ -1,0 +1,180 @@
+// Rotary positions: every pair of a head vector is turned by the angle of its token's position.
+//
+// The arithmetic is six operations per pair, so the kernel is bound by memory: each element is read
+// once and written once.  A thread takes sixteen elements (eight pairs) of four heads of one token:
+// the cosines and sines, which all heads of a token share, are loaded once per four heads, and eight
+// 16-byte loads are in flight per thread (16-bit types).  Query and key heads go through one launch.
+#include "decode.cuh"
+
+using namespace bcp;
+
+namespace bcp {
+
+int check_heads(const char* call, const char* name, const bcp_heads* h, bool written, uint32_t head_dim, int64_t n_tokens) {
+  if (!h) return fail(BCP_ERR_INVALID, "%s: %s is NULL", call, name);
+  if (h->type != BCP_F32 && h->type != BCP_BF16 && h->type != BCP_F16)
+    return fail(BCP_ERR_INVALID, "%s: %s has type %u (binary32, bfloat16 or binary16 expected)", call, name, h->type);
+  if (!h->n_heads || h->n_heads > 65536) return fail(BCP_ERR_INVALID, "%s: %s has %u heads", call, name, h->n_heads);
+  if (h->token_stride < 0 || h->head_stride < 0) return fail(BCP_ERR_INVALID, "%s: %s has a negative stride", call, name);
+  if (n_tokens && !h->data) return fail(BCP_ERR_INVALID, "%s: %s has no data", call, name);
+  if (reinterpret_cast<uintptr_t>(h->data) & (type_size(h->type) - 1)) return fail(BCP_ERR_INVALID, "%s: %s is not aligned to its elements", call, name);
+  if (written) {  // the rows of an output must not share memory
+    const int64_t strides[2] = {h->token_stride, h->head_stride};
+    const uint32_t extents[2] = {uint32_t(n_tokens), h->n_heads};
+    if (rows_overlap(strides, extents, 2, head_dim))
+      return fail(BCP_ERR_DST_ALIAS, "%s: rows of %s overlap (strides %lld, %lld for vectors of %u)", call, name, (long long)h->token_stride,
+                  (long long)h->head_stride, head_dim);
+  }
+  return BCP_OK;
+}
+
+int check_rope(const char* call, const bcp_rope_table* r, uint32_t head_dim) {
+  if (!r->table || (reinterpret_cast<uintptr_t>(r->table) & 15)) return fail(BCP_ERR_INVALID, "%s: the table is NULL or not 16-byte aligned", call);
+  if (r->n_positions < 1 || r->n_positions > 0x7fffffff) return fail(BCP_ERR_INVALID, "%s: a table of %lld positions", call, (long long)r->n_positions);
+  if (r->rot_dim < 2 || (r->rot_dim & 1) || r->rot_dim > head_dim)
+    return fail(BCP_ERR_INVALID, "%s: rot_dim %u is not an even number from 2 to head_dim %u", call, r->rot_dim, head_dim);
+  if (r->layout > BCP_ROPE_PAIRS) return fail(BCP_ERR_INVALID, "%s: layout %u", call, r->layout);
+  return BCP_OK;
+}
+
+}  // namespace bcp
+
+namespace {
+
+constexpr int kHeads = 4;  // heads per thread
+
+struct RopeArgs {
+  const void* in[2];
+  void* out[2];
+  int64_t in_token[2], in_head[2], out_token[2], out_head[2];
+  uint32_t n_q, n_heads;  // heads [0, n_q) are q's, [n_q, n_heads) k's
+  uint32_t head_dim, rot_dim, layout;
+  float sign;
+  FastDiv per_token, per_group;  // threads per token; per group of kHeads heads
+  uint32_t n_threads;
+  const float* table;
+  int64_t n_positions;
+  const int64_t* positions;
+  uint32_t* status;
+};
+
+template <typename T, bool VEC>
+__global__ void __launch_bounds__(256) bcp_rope_kernel(const RopeArgs a) {
+  const uint32_t i = blockIdx.x * 256u + threadIdx.x;
+  if (i >= a.n_threads) return;
+  const uint32_t t = a.per_token.div(i), r = i - t * a.per_token.d;
+  const uint32_t g = a.per_group.div(r);
+  const Chunk k = chunk_at(r - g * a.per_group.d, a.head_dim, a.rot_dim, a.layout);
+  const int64_t position = a.positions[t];
+  const bool there = position >= 0 && position < a.n_positions;
+  if (position >= a.n_positions) raise(a.status, BCP_BAD_POSITION);
+
+  Elements<T, VEC> e[kHeads];
+  T* to[kHeads];
+#pragma unroll
+  for (int j = 0; j < kHeads; ++j) {
+    uint32_t h = g * kHeads + j;
+    const bool used = h < a.n_heads;
+    const int side = h >= a.n_q;
+    h -= side ? a.n_q : 0;
+    to[j] = used ? static_cast<T*>(a.out[side]) + t * a.out_token[side] + h * a.out_head[side] : nullptr;
+    if (used) e[j].load(static_cast<const T*>(a.in[side]) + t * a.in_token[side] + h * a.in_head[side], k);
+  }
+  Angles<VEC> w;
+  if (k.rotated) w.load(a.table, there ? position : 0, a.rot_dim, k);
+#pragma unroll
+  for (int j = 0; j < kHeads; ++j) {
+    if (!to[j]) continue;
+    if (k.rotated || !there) {
+      float x[8], y[8];
+      e[j].unpack(x, y, k);
+      if (k.rotated) w.rotate(x, y, a.sign);
+      if (!there) {
+#pragma unroll
+        for (int n = 0; n < 8; ++n) x[n] = y[n] = 0.f;
+      }
+      e[j].pack(x, y, k);
+    }
+    e[j].store(to[j], k);
+  }
+}
+
+template <typename T>
+void launch(const RopeArgs& a, bool vec, cudaStream_t stream) {
+  const uint32_t blocks = (a.n_threads + 255) / 256;
+  if (vec)
+    bcp_rope_kernel<T, true><<<blocks, 256, 0, stream>>>(a);
+  else
+    bcp_rope_kernel<T, false><<<blocks, 256, 0, stream>>>(a);
+}
+
+}  // namespace
+
+extern "C" int bcp_rope(const bcp_heads* q_in, const bcp_heads* q_out, const bcp_heads* k_in, const bcp_heads* k_out, uint32_t head_dim,
+                        int64_t n_tokens, const bcp_rope_table* rope, const int64_t* positions, int transpose, void* stream) {
+  const char* call = "bcp_rope";
+  if (!rope) return fail(BCP_ERR_INVALID, "%s: rope is NULL", call);
+  if (head_dim < 2 || head_dim > BCP_MAX_HEAD_DIM) return fail(BCP_ERR_INVALID, "%s: head_dim %u is not in 2..%u", call, head_dim, BCP_MAX_HEAD_DIM);
+  if (n_tokens < 0 || n_tokens > 0x7fffffff) return fail(BCP_ERR_INVALID, "%s: %lld tokens", call, (long long)n_tokens);
+  if (int rc = check_rope(call, rope, head_dim)) return rc;
+  if (int rc = check_heads(call, "q_in", q_in, false, head_dim, n_tokens)) return rc;
+  if (int rc = check_heads(call, "q_out", q_out, true, head_dim, n_tokens)) return rc;
+  if (!k_in != !k_out) return fail(BCP_ERR_INVALID, "%s: k_in and k_out go together", call);
+  if (k_in) {
+    if (int rc = check_heads(call, "k_in", k_in, false, head_dim, n_tokens)) return rc;
+    if (int rc = check_heads(call, "k_out", k_out, true, head_dim, n_tokens)) return rc;
+  }
+  const bcp_heads* in[2] = {q_in, k_in ? k_in : q_in};
+  const bcp_heads* out[2] = {q_out, k_in ? k_out : q_out};
+  for (int s = 0; s < 2; ++s) {
+    if (in[s]->type != q_in->type || out[s]->type != q_in->type) return fail(BCP_ERR_MISMATCH, "%s: all vectors must have one type", call);
+    if (in[s]->n_heads != out[s]->n_heads) return fail(BCP_ERR_MISMATCH, "%s: %u heads in, %u out", call, in[s]->n_heads, out[s]->n_heads);
+  }
+  if (n_tokens && !positions) return fail(BCP_ERR_INVALID, "%s: positions is NULL", call);
+
+  RopeArgs a;
+  bool vec = head_dim % 16 == 0 && rope->rot_dim % 16 == 0;
+  for (int s = 0; s < 2; ++s) {
+    a.in[s] = in[s]->data, a.in_token[s] = in[s]->token_stride, a.in_head[s] = in[s]->head_stride;
+    a.out[s] = out[s]->data, a.out_token[s] = out[s]->token_stride, a.out_head[s] = out[s]->head_stride;
+    vec = vec && rows_aligned(in[s], 16) && rows_aligned(out[s], 16);
+  }
+  a.n_q = q_in->n_heads;
+  a.n_heads = q_in->n_heads + (k_in ? k_in->n_heads : 0);
+  a.head_dim = head_dim, a.rot_dim = rope->rot_dim, a.layout = rope->layout;
+  a.sign = transpose ? -1.f : 1.f;
+  a.table = rope->table, a.n_positions = rope->n_positions, a.status = rope->status;
+  const uint32_t chunks = chunks_of(head_dim, rope->rot_dim), per_token = chunks * ((a.n_heads + kHeads - 1) / kHeads);
+  a.per_group = FastDiv(chunks), a.per_token = FastDiv(per_token);
+  // thread indices stay below 2^31: longer inputs take several launches
+  const int64_t most = 0x7fffff00 / per_token;
+  const uint32_t es = type_size(q_in->type);
+  for (int64_t t0 = 0; t0 < n_tokens; t0 += most) {
+    const int64_t n = n_tokens - t0 < most ? n_tokens - t0 : most;
+    a.n_threads = uint32_t(n) * per_token;
+    a.positions = positions + t0;
+    for (int s = 0; s < 2; ++s) {
+      a.in[s] = static_cast<const char*>(in[s]->data) + t0 * in[s]->token_stride * es;
+      a.out[s] = static_cast<char*>(out[s]->data) + t0 * out[s]->token_stride * es;
+    }
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    if (q_in->type == BCP_F32) launch<float>(a, vec, st);
+    if (q_in->type == BCP_BF16) launch<__nv_bfloat16>(a, vec, st);
+    if (q_in->type == BCP_F16) launch<__half>(a, vec, st);
+    BCP_LAUNCHED(call);
+  }
+  return BCP_OK;
+}
+
+extern "C" int bcp_decode_status(uint32_t* status, void* stream_) {
+  if (!status) return fail(BCP_ERR_INVALID, "bcp_decode_status: status is NULL");
+  cudaStream_t stream = static_cast<cudaStream_t>(stream_);
+  uint32_t bits = 0;
+  cudaError_t e = cudaMemcpyAsync(&bits, status, sizeof bits, cudaMemcpyDeviceToHost, stream);
+  if (e == cudaSuccess) e = cudaStreamSynchronize(stream);
+  if (e == cudaSuccess && bits) e = cudaMemsetAsync(status, 0, sizeof bits, stream);
+  if (e != cudaSuccess) return fail(BCP_ERR_CUDA, "bcp_decode_status: %s", cudaGetErrorString(e));
+  if (!bits) return BCP_OK;
+  return fail(BCP_ERR_BOUNDS, "an index was outside its range and was left out:%s%s%s%s", bits & BCP_BAD_POSITION ? " position" : "",
+              bits & BCP_BAD_SLOT ? " slot" : "", bits & BCP_BAD_PAGE ? " page" : "", bits & BCP_BAD_LENGTH ? " length" : "");
+}
