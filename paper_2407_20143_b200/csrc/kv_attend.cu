@@ -154,9 +154,9 @@ __device__ __forceinline__ float load16(const void* p, int64_t i, bool bf16) {
 
 // Where dimension d of head (column) n lies in a warp's block of sums: eight rows of dimensions and four
 // pairs of heads are written at a time, the exclusive-or spreads them over the banks.
-template <int DP>
+template <int DP, bool QUANT>
 __device__ __forceinline__ uint32_t sum_at(uint32_t n, uint32_t d) {
-  return n * DP + (d ^ (n >> 1) << 3);
+  return n * DP + (d ^ (n >> 1) << (QUANT ? 2 : 3));
 }
 
 // Where 16-byte chunk c of row r lies in a side of a stage.  Keys are read as 16-byte vectors by 8 lanes
@@ -270,36 +270,57 @@ __global__ void __launch_bounds__(kWarps * 32) bcp_kv_attend_kernel(const Attend
   }
   const uint32_t n_steps = uint32_t(s1 - s0);
 
-  // ---- filling the ring: the next 16 tokens of this warp
+  // ---- filling the ring: the next 16 tokens of this warp.  Lane r (and r + 16) looks up the page of token
+  // r one turn ahead, so that the copies do not wait for the block table.
   Place ahead = at;
-  uint32_t produced = 0, fill_stage = 0;
+  uint32_t produced = 0, fill_stage = 0, off = 0;
+  int32_t page = -1;
+  auto look_up = [&]() {
+    const uint32_t pos = ahead.span.base + ahead.step * kStep + warp * kTok + (lane & 15);
+    page = -1;
+    if (pos >= ahead.span.first && pos < ahead.span.len) {
+      const uint32_t n = a.page_size.div(pos);
+      off = pos - n * a.page_size.d;
+      page = __ldg(a.block_table + ahead.b * a.table_stride + n);
+      if (uint32_t(page) >= a.n_pages) {
+        raise(a.status, BCP_BAD_PAGE);
+        page = -1;
+      }
+    }
+  };
+  const int64_t v_from_k = static_cast<const char*>(a.v) - static_cast<const char*>(a.k);
   auto produce = [&]() {
     if (produced < n_steps) {
       const uint32_t stage = ring + fill_stage * S::STAGE;
       const uint32_t h = NT * 8 >= a.group ? ahead.u : ahead.u / a.row_tiles;
-      const uint32_t r = lane & 15, pos = ahead.span.base + ahead.step * kStep + warp * kTok + r;
-      bool on = pos >= ahead.span.first && pos < ahead.span.len;
-      int64_t row = 0;
-      uint32_t page = 0, off = 0;
-      if (on) {
-        const uint32_t n = a.page_size.div(pos);
-        off = pos - n * a.page_size.d;
-        page = uint32_t(__ldg(a.block_table + ahead.b * a.table_stride + n));
-        if (page >= a.n_pages) {
-          raise(a.status, BCP_BAD_PAGE);
-          on = false, page = 0;
-        }
-        row = page * a.page_stride + h * a.head_stride + off * a.token_stride;
-      }
+      const bool on = page >= 0;
       const uint32_t live = __ballot_sync(0xffffffffu, on) & 0xffffu;
       if (live) {
+        constexpr int kRows = 32 / S::CPR;  // rows that one turn of the copies covers
+        const uint32_t l = lane / S::CPR, c = lane % S::CPR;
+        const int64_t row = on ? page * a.page_stride + h * a.head_stride + off * a.token_stride : 0;
+        // Each lane copies one column of chunks.  In a tile that is live throughout and lies in one page
+        // (the offsets did not start again) rows are a stride apart; else each row is looked up.
+        const bool inside = c * 16 < a.head_dim * S::ES;
+        if (__all_sync(0xffffffffu, on && off >= (lane & 15))) {
+          const int64_t step = kRows * a.token_stride * S::ES;
+          const char* from = static_cast<const char*>(a.k) + (__shfl_sync(0xffffffffu, row, l) * S::ES + (inside ? c * 16 : 0));
 #pragma unroll
-        for (int i = 0; i < kTok * S::CPR / 32; ++i) {
-          const uint32_t n = i * 32 + lane, rr = n / S::CPR, c = n % S::CPR;
-          const int64_t from = __shfl_sync(0xffffffffu, row, rr) * S::ES + c * 16;
-          const bool copy = (live >> rr & 1) && c * 16 < a.head_dim * S::ES;
-          copy16(stage + key_at<S::CPR>(rr, c), static_cast<const char*>(a.k) + (copy ? from : 0), copy);
-          copy16(stage + S::SIDE + value_at<S::CPR, S::quant>(rr, c), static_cast<const char*>(a.v) + (copy ? from : 0), copy);
+          for (int i = 0; i < kTok / kRows; ++i) {
+            copy16(stage + key_at<S::CPR>(i * kRows + l, c), from, inside);
+            copy16(stage + S::SIDE + value_at<S::CPR, S::quant>(i * kRows + l, c), from + v_from_k, inside);
+            from += step;
+          }
+        } else {
+#pragma unroll
+          for (int i = 0; i < kTok / kRows; ++i) {
+            const uint32_t r = i * kRows + l;
+            const bool copy = (live >> r & 1) && inside;
+            const int64_t x = __shfl_sync(0xffffffffu, row, r) * S::ES + c * 16;
+            const char* const from = static_cast<const char*>(a.k) + (copy ? x : 0);
+            copy16(stage + key_at<S::CPR>(r, c), from, copy);
+            copy16(stage + S::SIDE + value_at<S::CPR, S::quant>(r, c), from + v_from_k, copy);
+          }
         }
         if (S::quant) {
           const int64_t n = (int64_t(page) * a.n_heads + h) * a.page_size.d + off;
@@ -307,12 +328,15 @@ __global__ void __launch_bounds__(kWarps * 32) bcp_kv_attend_kernel(const Attend
         }
       }
       if (lane == 0) *reinterpret_cast<uint32_t*>(ring_ptr + fill_stage * S::STAGE + S::STAGE - 16) = live;
-      ++produced;
       fill_stage = fill_stage + 1 == S::STAGES ? 0 : fill_stage + 1;
-      advance(ahead, a, units, produced < n_steps);
+      if (++produced < n_steps) {
+        advance(ahead, a, units, true);
+        look_up();
+      }
     }
     copies_end();  // one group per stage, empty ones at the end
   };
+  look_up();
   for (int i = 0; i < S::STAGES - 1; ++i) produce();
 
   uint32_t done = 0, use_stage = 0;
@@ -425,11 +449,20 @@ __global__ void __launch_bounds__(kWarps * 32) bcp_kv_attend_kernel(const Attend
 #pragma unroll
       for (int t = 0; t < NT; ++t)
 #pragma unroll
-        for (int c = 0; c < 4; ++c) {
-          const bool in = live >> (g + 8 * (c >> 1)) & 1;
-          s[t][c] = in ? s[t][c] * factor[t][c & 1] * ks[c >> 1] : -INFINITY;
-          above |= s[t][c] + ve[c >> 1] > ref[t][c & 1] + 8.f;
-        }
+        for (int c = 0; c < 4; ++c) s[t][c] *= factor[t][c & 1] * ks[c >> 1];
+      if (live != 0xffffu) {
+#pragma unroll
+        for (int r = 0; r < 2; ++r)
+          if (!(live >> (g + 8 * r) & 1)) {
+#pragma unroll
+            for (int t = 0; t < NT; ++t) s[t][2 * r] = s[t][2 * r + 1] = -INFINITY;
+            vf[r] = 1.f;
+          }
+      }
+#pragma unroll
+      for (int t = 0; t < NT; ++t)
+#pragma unroll
+        for (int c = 0; c < 4; ++c) above |= s[t][c] + ve[c >> 1] > ref[t][c & 1] + 8.f;
       if (__any_sync(0xffffffffu, above)) {
 #pragma unroll
         for (int t = 0; t < NT; ++t)
@@ -453,11 +486,10 @@ __global__ void __launch_bounds__(kWarps * 32) bcp_kv_attend_kernel(const Attend
         float p[4];
 #pragma unroll
         for (int c = 0; c < 4; ++c) {
-          const float x = s[t][c] - ref[t][c & 1] + kLift;
+          const float x = s[t][c] - (ref[t][c & 1] - kLift);
           if constexpr (S::quant) {
             l[t][c & 1] += exp2_fast(x);
             p[c] = exp2_fast(x + ve[c >> 1]) * vf[c >> 1];
-            if (!(live >> (g + 8 * (c >> 1)) & 1)) p[c] = 0.f;
           } else {
             p[c] = exp2_fast(x);
             l[t][c & 1] += p[c];
@@ -535,13 +567,20 @@ __global__ void __launch_bounds__(kWarps * 32) bcp_kv_attend_kernel(const Attend
 #pragma unroll
         for (int w = 1; w < kWarps; ++w) m = fmaxf(m, sum_r[w * S::ROWS + col]);
         const float down = exp2_fast(ref[t][c] - m);
+        float* const to = sum_o + warp * 8 * DP;
+        if constexpr (S::quant) {  // two blocks of rows hold four neighbouring dimensions
 #pragma unroll
-        for (int k = 0; k < DP / 16; ++k)
-#pragma unroll
-          for (int r = 0; r < 2; ++r) {
-            const uint32_t d = !S::quant ? 16 * k + 8 * r + g : DP >= 128 ? 128 * (k / 8) + 16 * g + 2 * (k % 8) + r : (DP / 8) * g + 2 * k + r;
-            sum_o[warp * 8 * DP + sum_at<DP>(2 * q4 + c, d)] = o[t][k][c + 2 * r] * down;
+          for (int k = 0; k < DP / 16; k += 2) {
+            const uint32_t d = DP >= 128 ? 128 * (k / 8) + 16 * g + 2 * (k % 8) : (DP / 8) * g + 2 * k;
+            *reinterpret_cast<float4*>(to + sum_at<DP, true>(2 * q4 + c, d)) =
+                make_float4(o[t][k][c] * down, o[t][k][c + 2] * down, o[t][k + 1][c] * down, o[t][k + 1][c + 2] * down);
           }
+        } else {
+#pragma unroll
+          for (int k = 0; k < DP / 16; ++k)
+#pragma unroll
+            for (int r = 0; r < 2; ++r) to[sum_at<DP, false>(2 * q4 + c, 16 * k + 8 * r + g)] = o[t][k][c + 2 * r] * down;
+        }
       }
       __syncthreads();
       const uint32_t col = t * 8 + head;
@@ -558,7 +597,7 @@ __global__ void __launch_bounds__(kWarps * 32) bcp_kv_attend_kernel(const Attend
         float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
         for (int w = 0; w < kWarps; ++w) {
-          const float4 y = *reinterpret_cast<const float4*>(sum_o + w * 8 * DP + sum_at<DP>(head, d));
+          const float4 y = *reinterpret_cast<const float4*>(sum_o + w * 8 * DP + sum_at<DP, S::quant>(head, d));
           x.x += y.x, x.y += y.y, x.z += y.z, x.w += y.w;
         }
         if (!whole) {
@@ -600,24 +639,38 @@ __global__ void __launch_bounds__(kWarps * 32) bcp_kv_attend_kernel(const Attend
         // the first part lies in its CTA's second place unless the unit begins where that CTA does
         const bool second = c0 * n_line / n_parts != u0;
         for (int t = 0; t < NT; ++t) {
+          // sixteen threads per head; each knows the weights of every sixteenth part
           const uint32_t col = t * 8 + head, qh = h * a.group + row0 + col;
+          auto part_of = [&](uint32_t c) { return a.parts + (uint64_t(c) * 2 + (c == c0 && second)) * S::PART; };
           float m = kNone;
-          for (uint32_t c = c0; c <= c1; ++c) m = fmaxf(m, __ldcg(a.parts + (uint64_t(c) * 2 + (c == c0 && second)) * S::PART + S::ROWS * DP + col));
+          for (uint32_t c = c0 + sub; c <= c1; c += 16) m = fmaxf(m, __ldcg(part_of(c) + S::ROWS * DP + col));
+#pragma unroll
+          for (int i = 1; i < 16; i <<= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, i));
           float den = 0.f;
           float4 x[DP / 64];
 #pragma unroll
           for (int i = 0; i < DP / 64; ++i) x[i] = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 4
-          for (uint32_t c = c0; c <= c1; ++c) {
-            const float* const from = a.parts + (uint64_t(c) * 2 + (c == c0 && second)) * S::PART;
-            const float down = exp2_fast(__ldcg(from + S::ROWS * DP + col) - m);
-            den += __ldcg(from + S::ROWS * (DP + 1) + col) * down;
+          for (uint32_t cb = c0; cb <= c1; cb += 16) {
+            float weight = 0.f;
+            if (cb + sub <= c1) {
+              const float* const from = part_of(cb + sub);
+              weight = exp2_fast(__ldcg(from + S::ROWS * DP + col) - m);
+              den += __ldcg(from + S::ROWS * (DP + 1) + col) * weight;
+            }
+#pragma unroll 8
+            for (uint32_t j = 0; j < 16; ++j) {
+              const uint32_t c = cb + j <= c1 ? cb + j : c1;
+              const float* const from = part_of(c);
+              const float w = __shfl_sync(0xffffffffu, weight, (lane & 16) + j);
 #pragma unroll
-            for (int i = 0; i < DP / 64; ++i) {
-              const float4 y = __ldcg(reinterpret_cast<const float4*>(from + col * DP + 64 * i + 4 * sub));
-              x[i].x += y.x * down, x[i].y += y.y * down, x[i].z += y.z * down, x[i].w += y.w * down;
+              for (int i = 0; i < DP / 64; ++i) {
+                const float4 y = __ldcg(reinterpret_cast<const float4*>(from + col * DP + 64 * i + 4 * sub));
+                if (cb + j <= c1) x[i].x += y.x * w, x[i].y += y.y * w, x[i].z += y.z * w, x[i].w += y.w * w;
+              }
             }
           }
+#pragma unroll
+          for (int i = 1; i < 16; i <<= 1) den += __shfl_xor_sync(0xffffffffu, den, i);
           if (row0 + col < a.group) {
             const float inv = den == 0.f ? 0.f : 1.f / den;
 #pragma unroll
