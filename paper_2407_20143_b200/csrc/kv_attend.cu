@@ -66,7 +66,7 @@ struct Shape {
   static constexpr int SIDE = kTok * ROW;
   static constexpr int STAGE = 2 * SIDE + (quant ? 128 : 0) + 16;  // keys, values, their scales, the mask of live tokens
   // About 20 KiB a warp (two CTAs of four warps on an SM): enough bytes in flight to cover the latency of HBM.
-  static constexpr int STAGES = STAGE <= 2400 ? 8 : STAGE <= 4400 ? 5 : 3;
+  static constexpr int STAGES = STAGE <= 2400 ? 5 : 3;
   static constexpr int ROWS = 8 * NT;
   static constexpr int SMEM = kWarps * STAGES * STAGE + kWarps * 8 * DP * 4 + kWarps * ROWS * 8 + 64;
   static constexpr int PART = ROWS * (DP + 2);  // floats of one part in the workspace
@@ -124,17 +124,17 @@ __device__ __forceinline__ void mma(float (&d)[4], const uint32_t (&a)[4], const
                  : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b[0]), "r"(b[1]));
 }
 
-// Two 8-bit elements (low 16 bits of w) as binary16, exactly.
+// Four 8-bit elements as two pairs of binary16, exactly.
 template <int FMT>
-__device__ __forceinline__ uint32_t widen2(uint32_t w) {
+__device__ __forceinline__ void widen4(uint32_t w, uint32_t& lo, uint32_t& hi) {
   if constexpr (FMT == BCP_E4M3) {
-    const __half2_raw h = __nv_cvt_fp8x2_to_halfraw2(__nv_fp8x2_storage_t(w), __NV_E4M3);
-    return uint32_t(h.x) | uint32_t(h.y) << 16;
+    asm("{\n.reg .b16 x, y;\nmov.b32 {x, y}, %2;\ncvt.rn.f16x2.e4m3x2 %0, x;\ncvt.rn.f16x2.e4m3x2 %1, y;\n}" : "=r"(lo), "=r"(hi) : "r"(w));
   } else {
     // bytes u = x + 128 under the exponent of 1024 read as 1024 + u; 1152 off gives x
-    const uint32_t biased = __byte_perm(w ^ 0x8080u, 0x64646464u, 0x4140);
-    const __half2 x = __hsub2(*reinterpret_cast<const __half2*>(&biased), __half2half2(__ushort_as_half(0x6480)));
-    return *reinterpret_cast<const uint32_t*>(&x);
+    const uint32_t u = w ^ 0x80808080u, a = __byte_perm(u, 0x64646464u, 0x4140), b = __byte_perm(u, 0x64646464u, 0x4342);
+    const __half2 bias = __half2half2(__ushort_as_half(0x6480));
+    const __half2 x = __hsub2(*reinterpret_cast<const __half2*>(&a), bias), y = __hsub2(*reinterpret_cast<const __half2*>(&b), bias);
+    lo = *reinterpret_cast<const uint32_t*>(&x), hi = *reinterpret_cast<const uint32_t*>(&y);
   }
 }
 
@@ -204,7 +204,7 @@ __device__ __forceinline__ void advance(Place& p, const AttendArgs& a, uint32_t 
 }
 
 template <int FMT, int DP, int NT>
-__global__ void __launch_bounds__(kWarps * 32) bcp_kv_attend_kernel(const AttendArgs a) {
+__global__ void __launch_bounds__(kWarps * 32, Shape<FMT, DP, NT>::SMEM <= 75 * 1024 ? 3 : Shape<FMT, DP, NT>::SMEM <= 113 * 1024 ? 2 : 1) bcp_kv_attend_kernel(const AttendArgs a) {
   typedef Shape<FMT, DP, NT> S;
   constexpr bool kBf16 = FMT == BCP_BF16;  // type of the products; 8-bit caches are widened to binary16
   // binary16 weights underflow below 2^-24: lifting them by 2^6 (they stay below 2^16) moves that to 2^-30
@@ -426,7 +426,9 @@ __global__ void __launch_bounds__(kWarps * 32) bcp_kv_attend_kernel(const Attend
           const uint32_t xs[4] = {x.x, x.y, x.z, x.w}, ys[4] = {y.x, y.y, y.z, y.w};
 #pragma unroll
           for (int w = 0; w < 4; ++w) {
-            const uint32_t f[4] = {widen2<FMT>(xs[w] & 0xffffu), widen2<FMT>(ys[w] & 0xffffu), widen2<FMT>(xs[w] >> 16), widen2<FMT>(ys[w] >> 16)};
+            uint32_t f[4];
+            widen4<FMT>(xs[w], f[0], f[2]);
+            widen4<FMT>(ys[w], f[1], f[3]);
 #pragma unroll
             for (int t = 0; t < NT; ++t) mma<kBf16>(s[t], f, qf[t][4 * j + w]);
           }
@@ -528,8 +530,9 @@ __global__ void __launch_bounds__(kWarps * 32) bcp_kv_attend_kernel(const Attend
 #pragma unroll
             for (int half = 0; half < 2; ++half) {
               const uint32_t pick = half ? 0x7362 : 0x5140;
-              const uint32_t lo = __byte_perm(w[0][x], w[1][x], pick), hi = __byte_perm(w[2][x], w[3][x], pick);
-              const uint32_t f[4] = {widen2<FMT>(lo & 0xffffu), widen2<FMT>(lo >> 16), widen2<FMT>(hi & 0xffffu), widen2<FMT>(hi >> 16)};
+              uint32_t f[4];
+              widen4<FMT>(__byte_perm(w[0][x], w[1][x], pick), f[0], f[1]);
+              widen4<FMT>(__byte_perm(w[2][x], w[3][x], pick), f[2], f[3]);
 #pragma unroll
               for (int t = 0; t < NT; ++t) mma<kBf16>(o[t][8 * j + 2 * x + half], f, pf[t]);
             }
