@@ -19,10 +19,11 @@
 // of each 64-token step and add up at the end of a stretch of one sequence and cache head.
 //
 // Split.  All steps of all sequences and heads form one line that is cut into as many equal parts as CTAs
-// fit on the GPU; lengths are only known on the device, so each CTA finds its part itself.  A sequence and
-// head that lies in one part is finished there; else every part leaves its sums in the workspace and the
-// one that comes last (a counter per sequence and head) joins them, in the order of the parts, so results
-// do not depend on which that is.
+// fit on the GPU; lengths are only known on the device, so each CTA finds its part itself.  One more step per
+// unit (sequence, cache head, row tile) stands for what its beginning and end cost.  A unit that lies in one
+// part is finished there; else every part leaves its sums in the workspace.  Of each 32 neighbouring parts the
+// one that comes last (a counter says which) joins them, and of these groups the last again, always in
+// the order of the parts, so results do not depend on which that is.
 #include <mutex>
 
 #include "decode.cuh"
@@ -53,8 +54,25 @@ struct AttendArgs {
   const int32_t* lengths;
   float scale_log2;
   uint32_t window;
-  uint32_t* counters;  // one per sequence, cache head and row tile: parts that have arrived
-  float* parts;        // two per CTA: sums, then references, then denominators
+  uint32_t* unit_count;  // one per sequence, cache head and row tile: groups of parts that have arrived
+  uint32_t* part_count;  // two per part: parts that have arrived, at the place of a unit's first part in a group
+  float* parts;          // two places per part: sums, then references, then denominators
+};
+
+constexpr uint32_t kGroup = 32;
+// The line of n steps is dealt out to the parts as evenly as whole steps allow.
+struct Cuts {
+  uint64_t n, each, longer;  // steps of the line, of a part; the first `longer` parts have one more
+  uint32_t parts;
+  __device__ __forceinline__ void cut(uint64_t steps, uint32_t ctas) {
+    n = steps, parts = uint32_t(n < ctas ? n : ctas);
+    each = n >> 32 ? n / parts : uint32_t(n) / parts, longer = n - each * parts;
+  }
+  __device__ __forceinline__ uint64_t begin(uint32_t p) const { return each * p + (p < longer ? p : longer); }
+  __device__ __forceinline__ uint32_t part_of(uint64_t x) const {  // the part that step x lies in
+    const uint64_t lower = longer * (each + 1), at = x < lower ? x : x - lower, size = each + (x < lower);
+    return (n >> 32 ? uint32_t(at / size) : uint32_t(at) / uint32_t(size)) + uint32_t(x < lower ? 0 : longer);
+  }
 };
 
 template <int FMT, int DP, int NT>
@@ -68,7 +86,7 @@ struct Shape {
   // About 20 KiB a warp (two CTAs of four warps on an SM): enough bytes in flight to cover the latency of HBM.
   static constexpr int STAGES = STAGE <= 2400 ? 5 : 3;
   static constexpr int ROWS = 8 * NT;
-  static constexpr int SMEM = kWarps * STAGES * STAGE + kWarps * 8 * DP * 4 + kWarps * ROWS * 8 + 64;
+  static constexpr int SMEM = kWarps * STAGES * STAGE + kWarps * 8 * DP * 4 + kWarps * ROWS * 8 + 128;
   static constexpr int PART = ROWS * (DP + 2);  // floats of one part in the workspace
 };
 
@@ -89,37 +107,21 @@ __device__ __forceinline__ float exp2_fast(float x) {
 }
 __device__ __forceinline__ uint32_t transpose8x8(uint32_t x) {
   uint32_t y;
-  asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
+  asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
   return y;
 }
 __device__ __forceinline__ void load_transposed(uint32_t (&r)[4], uint32_t at) {
-  asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0, %1, %2, %3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(at) : "memory");
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0, %1, %2, %3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(at));
 }
-__device__ __forceinline__ uint4 load_shared16(uint32_t at) {
-  uint4 v;
-  asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(at) : "memory");
-  return v;
-}
-__device__ __forceinline__ uint2 load_shared8(uint32_t at) {
-  uint2 v;
-  asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(at) : "memory");
-  return v;
-}
-__device__ __forceinline__ float load_shared_f32(uint32_t at) {
-  float v;
-  asm volatile("ld.shared.f32 %0, [%1];" : "=f"(v) : "r"(at) : "memory");
-  return v;
-}
-
 // d += a b, a 16 x 16 (row fragments), b 16 x 8; both operands bfloat16 or both binary16
 template <bool BF16>
 __device__ __forceinline__ void mma(float (&d)[4], const uint32_t (&a)[4], const uint32_t (&b)[2]) {
   if constexpr (BF16)
-    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
                  : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
                  : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b[0]), "r"(b[1]));
   else
-    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
                  : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
                  : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b[0]), "r"(b[1]));
 }
@@ -148,7 +150,7 @@ __device__ __forceinline__ uint32_t pack16(float x, float y) {
     return *reinterpret_cast<const uint32_t*>(&p);
   }
 }
-__device__ __forceinline__ float load16(const void* p, int64_t i, bool bf16) {
+__device__ __forceinline__ float query_at(const void* p, int i, bool bf16) {
   return bf16 ? __bfloat162float(static_cast<const __nv_bfloat16*>(p)[i]) : __half2float(static_cast<const __half*>(p)[i]);
 }
 
@@ -176,9 +178,10 @@ __device__ __forceinline__ uint32_t value_at(uint32_t r, uint32_t c) {
 }
 
 struct Span {  // the tokens of one sequence, and its steps
-  uint32_t first, len, base, steps;  // base: first token of step 0, a multiple of 16
+  uint32_t first, len, base, steps;  // base: first token of step 0, a multiple of 16 (less a step, modulo 2^32, if that has none)
 };
-__device__ __forceinline__ Span span_of(const AttendArgs& a, uint32_t b) {
+// extra: 1 if every unit begins with a step without tokens
+__device__ __forceinline__ Span span_of(const AttendArgs& a, uint32_t b, uint32_t extra) {
   Span s;
   int32_t n = a.lengths[b];
   n = n < 0 ? 0 : n;
@@ -187,6 +190,7 @@ __device__ __forceinline__ Span span_of(const AttendArgs& a, uint32_t b) {
   s.base = s.first & ~15u;
   s.steps = (s.len - s.base + kStep - 1) / kStep;
   if (!s.steps) s.steps = 1;  // a sequence without tokens still has a result to write
+  s.steps += extra, s.base -= extra * kStep;
   return s;
 }
 
@@ -195,12 +199,12 @@ struct Place {
   uint32_t b, u, step;
   Span span;
 };
-__device__ __forceinline__ void advance(Place& p, const AttendArgs& a, uint32_t units, bool more) {
+__device__ __forceinline__ void advance(Place& p, const AttendArgs& a, uint32_t units, uint32_t extra, bool more) {
   if (++p.step < p.span.steps) return;
   p.step = 0;
   if (++p.u < units) return;
   p.u = 0;
-  if (++p.b < a.n_seqs && more) p.span = span_of(a, p.b);
+  if (++p.b < a.n_seqs && more) p.span = span_of(a, p.b, extra);
 }
 
 template <int FMT, int DP, int NT>
@@ -218,18 +222,17 @@ __global__ void __launch_bounds__(kWarps * 32, Shape<FMT, DP, NT>::SMEM <= 75 * 
   float* const sum_l = sum_r + kWarps * S::ROWS;                                        // [warp][ROWS] denominators
   uint32_t* const shared_word = reinterpret_cast<uint32_t*>(sum_l + kWarps * S::ROWS);
 
-  // ---- this CTA's part of the line
+  // ---- the line, and this CTA's part of it
   const uint32_t units = a.n_heads * a.row_tiles;
-  Place at;
-  uint64_t n_line, s0, s1;
-  uint32_t n_parts;
+  // every thread counts the steps of a run of sequences; an exclusive scan over the threads
+  const uint32_t run = (a.n_seqs + kWarps * 32 - 1) / (kWarps * 32);
+  const uint32_t run0 = min(tid * run, a.n_seqs), run1 = min(run0 + run, a.n_seqs);
+  uint64_t mine = 0, before;
+  Cuts cuts;
+  uint32_t extra;
   {
-    // every thread counts the steps of a run of sequences; an exclusive scan over the threads
-    const uint32_t run = (a.n_seqs + kWarps * 32 - 1) / (kWarps * 32);
-    const uint32_t b0 = tid * run, b1 = min(b0 + run, a.n_seqs);
-    uint64_t mine = 0;
-    for (uint32_t b = b0; b < b1; ++b) mine += span_of(a, b).steps;
-    uint64_t before = mine;
+    for (uint32_t b = run0; b < run1; ++b) mine += span_of(a, b, 0).steps;
+    before = mine;
     for (uint32_t o = 1; o < 32; o <<= 1) {
       const uint64_t x = __shfl_up_sync(0xffffffffu, before, o);
       if (lane >= o) before += x;
@@ -243,37 +246,40 @@ __global__ void __launch_bounds__(kWarps * 32, Shape<FMT, DP, NT>::SMEM <= 75 * 
       if (w < warp) before += totals[w];
       all += totals[w];
     }
-    n_line = all * units;
-    n_parts = uint32_t(n_line < gridDim.x ? n_line : gridDim.x);
-    if (blockIdx.x >= n_parts) return;
-    s0 = blockIdx.x * n_line / n_parts;
-    s1 = (blockIdx.x + 1) * n_line / n_parts;
-    uint32_t* const found = reinterpret_cast<uint32_t*>(totals + kWarps);
+    extra = all * units >= 2 * gridDim.x;
+    mine += extra * (run1 - run0), before += extra * run0;
+    cuts.cut((all + extra * a.n_seqs) * units, gridDim.x);
+  }
+  if (blockIdx.x >= cuts.parts) return;
+  const uint64_t s0 = cuts.begin(blockIdx.x);
+  const uint32_t n_steps = uint32_t(cuts.begin(blockIdx.x + 1) - s0);
+  Place at;
+  {
+    // the thread whose run of sequences holds the first step knows where that is
+    uint32_t* const found = shared_word;
     if (s0 >= before * units && s0 < (before + mine) * units) {
       uint64_t pre = before;
-      uint32_t b = b0;
+      uint32_t b = run0, steps;
       for (;; ++b) {
-        const uint32_t n = span_of(a, b).steps;
-        if (s0 < (pre + n) * units) break;
-        pre += n;
+        steps = span_of(a, b, extra).steps;
+        if (s0 < (pre + steps) * units) break;
+        pre += steps;
       }
-      const uint32_t steps = span_of(a, b).steps, r = uint32_t(s0 - pre * units);
+      const uint32_t r = uint32_t(s0 - pre * units);
       found[0] = b, found[1] = r / steps, found[2] = r % steps;
     }
     __syncthreads();
     at.b = found[0], at.u = found[1], at.step = found[2];
-    at.span = span_of(a, at.b);
-    __syncthreads();
-    if (a.status && blockIdx.x == 0)
-      for (uint32_t b = b0; b < b1; ++b)
-        if (a.lengths[b] > int32_t(a.capacity)) raise(a.status, BCP_BAD_LENGTH);
+    at.span = span_of(a, at.b, extra);
   }
-  const uint32_t n_steps = uint32_t(s1 - s0);
+  if (a.status && blockIdx.x == 0)
+    for (uint32_t b = run0; b < run1; ++b)
+      if (a.lengths[b] > int32_t(a.capacity)) raise(a.status, BCP_BAD_LENGTH);
 
   // ---- filling the ring: the next 16 tokens of this warp.  Lane r (and r + 16) looks up the page of token
   // r one turn ahead, so that the copies do not wait for the block table.
   Place ahead = at;
-  uint32_t produced = 0, fill_stage = 0, off = 0;
+  uint32_t left = n_steps, fill_stage = 0, off = 0;
   int32_t page = -1;
   auto look_up = [&]() {
     const uint32_t pos = ahead.span.base + ahead.step * kStep + warp * kTok + (lane & 15);
@@ -288,9 +294,17 @@ __global__ void __launch_bounds__(kWarps * 32, Shape<FMT, DP, NT>::SMEM <= 75 * 
       }
     }
   };
+  // The queries of a unit are brought to the L1 cache when its first tile is filled: a lane per 128 bytes.
+  auto touch_queries = [&]() {
+    const uint32_t h = ahead.u / a.row_tiles, r = (ahead.u - h * a.row_tiles) * S::ROWS + lane / (DP / 64), d = lane % (DP / 64) * 64;
+    if (lane < S::ROWS * (DP / 64) && r < a.group && d < a.head_dim) {
+      uint32_t ignored;
+      asm volatile("ld.global.ca.u32 %0, [%1];" : "=r"(ignored) : "l"(static_cast<const char*>(a.q) + (ahead.b * a.q_token + (h * a.group + r) * a.q_head + d) * 2));
+    }
+  };
   const int64_t v_from_k = static_cast<const char*>(a.v) - static_cast<const char*>(a.k);
   auto produce = [&]() {
-    if (produced < n_steps) {
+    if (left) {
       const uint32_t stage = ring + fill_stage * S::STAGE;
       const uint32_t h = NT * 8 >= a.group ? ahead.u : ahead.u / a.row_tiles;
       const bool on = page >= 0;
@@ -329,13 +343,15 @@ __global__ void __launch_bounds__(kWarps * 32, Shape<FMT, DP, NT>::SMEM <= 75 * 
       }
       if (lane == 0) *reinterpret_cast<uint32_t*>(ring_ptr + fill_stage * S::STAGE + S::STAGE - 16) = live;
       fill_stage = fill_stage + 1 == S::STAGES ? 0 : fill_stage + 1;
-      if (++produced < n_steps) {
-        advance(ahead, a, units, true);
+      if (--left) {
+        advance(ahead, a, units, extra, true);
         look_up();
+        if (ahead.step == 0) touch_queries();
       }
     }
     copies_end();  // one group per stage, empty ones at the end
   };
+  touch_queries();
   look_up();
   for (int i = 0; i < S::STAGES - 1; ++i) produce();
 
@@ -368,7 +384,7 @@ __global__ void __launch_bounds__(kWarps * 32, Shape<FMT, DP, NT>::SMEM <= 75 * 
         for (int s = 0; s < DP / 16; ++s)
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
-            x[s][i] = load16(&raw[s], i, a.q_is_bf16);
+            x[s][i] = query_at(&raw[s], i, a.q_is_bf16);
             top = max(top, __float_as_uint(x[s][i]) & 0x7fffffffu);
           }
         top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
@@ -399,30 +415,34 @@ __global__ void __launch_bounds__(kWarps * 32, Shape<FMT, DP, NT>::SMEM <= 75 * 
       copies_wait<S::STAGES - 2>();
       __syncwarp();  // every lane's copies have landed, and every lane is done with the stage that is filled next
       const uint32_t stage = ring + use_stage * S::STAGE;
-      const uint32_t live = *reinterpret_cast<const volatile uint32_t*>(ring_ptr + use_stage * S::STAGE + S::STAGE - 16);
+      const unsigned char* const tile = ring_ptr + use_stage * S::STAGE;
+      auto load16 = [&](uint32_t at) { return *reinterpret_cast<const uint4*>(tile + at); };
+      const uint32_t live = *reinterpret_cast<const uint32_t*>(tile + S::STAGE - 16);
       use_stage = use_stage + 1 == S::STAGES ? 0 : use_stage + 1;
       produce();
       if (!live) continue;
 
       // scores of 16 tokens (rows) and 8 NT heads (columns)
-      float s[NT][4];
+      float s[NT][4], s2[NT][4];  // two sums, so that no product waits for the one before it
 #pragma unroll
-      for (int t = 0; t < NT; ++t) s[t][0] = s[t][1] = s[t][2] = s[t][3] = 0.f;
+      for (int t = 0; t < NT; ++t)
+#pragma unroll
+        for (int c = 0; c < 4; ++c) s[t][c] = s2[t][c] = 0.f;
       if constexpr (!S::quant) {
 #pragma unroll
         for (int j = 0; j < DP / 32; ++j) {
-          const uint4 x = load_shared16(stage + key_at<S::CPR>(g, 4 * j + q4)), y = load_shared16(stage + key_at<S::CPR>(g + 8, 4 * j + q4));
+          const uint4 x = load16(key_at<S::CPR>(g, 4 * j + q4)), y = load16(key_at<S::CPR>(g + 8, 4 * j + q4));
           const uint32_t a0[4] = {x.x, y.x, x.y, y.y}, a1[4] = {x.z, y.z, x.w, y.w};
 #pragma unroll
           for (int t = 0; t < NT; ++t) {
             mma<kBf16>(s[t], a0, qf[t][2 * j]);
-            mma<kBf16>(s[t], a1, qf[t][2 * j + 1]);
+            mma<kBf16>(s2[t], a1, qf[t][2 * j + 1]);
           }
         }
       } else {
 #pragma unroll
         for (int j = 0; j < DP / 64; ++j) {
-          const uint4 x = load_shared16(stage + key_at<S::CPR>(g, 4 * j + q4)), y = load_shared16(stage + key_at<S::CPR>(g + 8, 4 * j + q4));
+          const uint4 x = load16(key_at<S::CPR>(g, 4 * j + q4)), y = load16(key_at<S::CPR>(g + 8, 4 * j + q4));
           const uint32_t xs[4] = {x.x, x.y, x.z, x.w}, ys[4] = {y.x, y.y, y.z, y.w};
 #pragma unroll
           for (int w = 0; w < 4; ++w) {
@@ -430,7 +450,7 @@ __global__ void __launch_bounds__(kWarps * 32, Shape<FMT, DP, NT>::SMEM <= 75 * 
             widen4<FMT>(xs[w], f[0], f[2]);
             widen4<FMT>(ys[w], f[1], f[3]);
 #pragma unroll
-            for (int t = 0; t < NT; ++t) mma<kBf16>(s[t], f, qf[t][4 * j + w]);
+            for (int t = 0; t < NT; ++t) mma<kBf16>(w & 1 ? s2[t] : s[t], f, qf[t][4 * j + w]);
           }
         }
       }
@@ -440,8 +460,8 @@ __global__ void __launch_bounds__(kWarps * 32, Shape<FMT, DP, NT>::SMEM <= 75 * 
       if constexpr (S::quant) {
 #pragma unroll
         for (int r = 0; r < 2; ++r) {
-          ks[r] = load_shared_f32(stage + 2 * S::SIDE + (g + 8 * r) * 4);
-          const float x = load_shared_f32(stage + 2 * S::SIDE + 64 + (g + 8 * r) * 4);
+          ks[r] = *reinterpret_cast<const float*>(tile + 2 * S::SIDE + (g + 8 * r) * 4);
+          const float x = *reinterpret_cast<const float*>(tile + 2 * S::SIDE + 64 + (g + 8 * r) * 4);
           const uint32_t v = __float_as_uint(x), e = v >> 23 & 255u;
           ve[r] = float(int(max(e, 31u)) - 127);  // scales below 2^-96 (a zero, too) keep the exponent of that
           vf[r] = e < 31 ? x * 0x1p96f : e == 255 ? __uint_as_float(0x7fc00000u) : __uint_as_float((v & 0x807fffffu) | 0x3f800000u);
@@ -451,7 +471,7 @@ __global__ void __launch_bounds__(kWarps * 32, Shape<FMT, DP, NT>::SMEM <= 75 * 
 #pragma unroll
       for (int t = 0; t < NT; ++t)
 #pragma unroll
-        for (int c = 0; c < 4; ++c) s[t][c] *= factor[t][c & 1] * ks[c >> 1];
+        for (int c = 0; c < 4; ++c) s[t][c] = (s[t][c] + s2[t][c]) * (factor[t][c & 1] * ks[c >> 1]);
       if (live != 0xffffu) {
 #pragma unroll
         for (int r = 0; r < 2; ++r)
@@ -518,10 +538,10 @@ __global__ void __launch_bounds__(kWarps * 32, Shape<FMT, DP, NT>::SMEM <= 75 * 
           for (int r = 0; r < 4; ++r) {
             const uint32_t token = 2 * q4 + (r & 1) + 8 * (r >> 1);
             if constexpr (kWords == 4) {
-              const uint4 x = load_shared16(stage + S::SIDE + value_at<S::CPR, true>(token, 8 * j + g));
+              const uint4 x = load16(S::SIDE + value_at<S::CPR, true>(token, 8 * j + g));
               w[r][0] = x.x, w[r][1] = x.y, w[r][2] = x.z, w[r][3] = x.w;
             } else {
-              const uint2 x = load_shared8(stage + S::SIDE + value_at<S::CPR, true>(token, g >> 1) + (g & 1) * 8);
+              const uint2 x = *reinterpret_cast<const uint2*>(tile + S::SIDE + value_at<S::CPR, true>(token, g >> 1) + (g & 1) * 8);
               w[r][0] = x.x, w[r][1] = x.y;
             }
           }
@@ -625,56 +645,93 @@ __global__ void __launch_bounds__(kWarps * 32, Shape<FMT, DP, NT>::SMEM <= 75 * 
     }
 
     if (!(starts && ends)) {
-      // ---- the unit lies in several parts: the last one to arrive joins them
-      const uint64_t u0 = place - at.step, u1 = u0 + at.span.steps;  // the unit on the line
-      const uint32_t c0 = uint32_t(((u0 + 1) * n_parts - 1) / n_line), c1 = uint32_t((u1 * n_parts - 1) / n_line);
-      uint32_t* const counter = a.counters + uint64_t(at.b) * units + at.u;
-      __threadfence();
-      __syncthreads();
-      if (tid == 0) {
-        const uint32_t arrived = atomicAdd(counter, 1u);
-        *shared_word = arrived == c1 - c0;
-        if (arrived == c1 - c0) *counter = 0;  // ready for the next call
-      }
-      __syncthreads();
-      if (*shared_word) {
+      // ---- the unit lies in several parts
+      const uint64_t u0 = place - at.step;
+      const uint32_t p0 = cuts.part_of(u0), p1 = cuts.part_of(u0 + at.span.steps - 1);
+      // the first part has the unit in its second place unless it begins with it
+      const uint32_t first_place = 2 * p0 + (cuts.begin(p0) != u0);
+      auto place_in = [&](uint32_t p) { return p == p0 ? first_place : 2 * p; };
+      // Whether this CTA is the last of n to come to a counter; what the others wrote before is visible then.
+      auto last_of = [&](uint32_t* counter, uint32_t n) {
         __threadfence();
-        // the first part lies in its CTA's second place unless the unit begins where that CTA does
-        const bool second = c0 * n_line / n_parts != u0;
+        __syncthreads();
+        if (tid == 0) {
+          const bool last = atomicAdd(counter, 1u) + 1 == n;
+          *shared_word = last;
+          if (last) *counter = 0;  // ready for the next call
+        }
+        __syncthreads();
+        const bool last = *shared_word;
+        if (last) __threadfence();
+        return last;
+      };
+      const uint32_t group = blockIdx.x / kGroup, groups = p1 / kGroup - p0 / kGroup + 1;
+      uint32_t f = max(p0, group * kGroup), n_sums = min(p1, group * kGroup + kGroup - 1) - f + 1, apart = 1;
+      uint32_t* counter = a.part_count + place_in(f);
+      // first the parts of a group, then the groups of the unit, whose sums lie at their first parts
+#pragma unroll 1
+      for (bool last = groups == 1; last_of(counter, n_sums); last = true) {
+        // Sixteen threads per head; each knows the weights of every sixteenth of the n_sums sums.
+        const float* const first = a.parts + uint64_t(place_in(f)) * S::PART;
+        const float* const others = a.parts + uint64_t(2 * (f / apart * apart)) * S::PART;
+        auto from_of = [&](uint32_t i) { return i == 0 ? first : others + uint64_t(2 * apart * i) * S::PART; };
+#pragma unroll 1
         for (int t = 0; t < NT; ++t) {
-          // sixteen threads per head; each knows the weights of every sixteenth part
           const uint32_t col = t * 8 + head, qh = h * a.group + row0 + col;
-          auto part_of = [&](uint32_t c) { return a.parts + (uint64_t(c) * 2 + (c == c0 && second)) * S::PART; };
-          float m = kNone;
-          for (uint32_t c = c0 + sub; c <= c1; c += 16) m = fmaxf(m, __ldcg(part_of(c) + S::ROWS * DP + col));
+          // at most kGroup sums: those of parts sub and sub + 16 belong to this thread
+          float m = kNone, r[2], w[2], den = 0.f;
+#pragma unroll
+          for (int k = 0; k < 2; ++k) {
+            const bool mine = sub + 16 * k < n_sums;
+            const float* const from = from_of(mine ? sub + 16 * k : 0);
+            r[k] = __ldcg(from + S::ROWS * DP + col);
+            w[k] = __ldcg(from + S::ROWS * (DP + 1) + col);
+            if (!mine) r[k] = kNone, w[k] = 0.f;
+          }
+          float4 x[DP / 64], y[8][DP / 64];
+          auto load = [&](uint32_t i0) {
+#pragma unroll
+            for (uint32_t j = 0; j < 8; ++j) {
+              const float* const from = from_of(min(i0 + j, n_sums - 1)) + col * DP + 4 * sub;
+#pragma unroll
+              for (int i = 0; i < DP / 64; ++i) y[j][i] = __ldcg(reinterpret_cast<const float4*>(from + 64 * i));
+            }
+          };
+          load(0);  // under way while the weights are found
+          m = fmaxf(r[0], r[1]);
 #pragma unroll
           for (int i = 1; i < 16; i <<= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, i));
-          float den = 0.f;
-          float4 x[DP / 64];
 #pragma unroll
-          for (int i = 0; i < DP / 64; ++i) x[i] = make_float4(0.f, 0.f, 0.f, 0.f);
-          for (uint32_t cb = c0; cb <= c1; cb += 16) {
-            float weight = 0.f;
-            if (cb + sub <= c1) {
-              const float* const from = part_of(cb + sub);
-              weight = exp2_fast(__ldcg(from + S::ROWS * DP + col) - m);
-              den += __ldcg(from + S::ROWS * (DP + 1) + col) * weight;
-            }
-#pragma unroll 8
-            for (uint32_t j = 0; j < 16; ++j) {
-              const uint32_t c = cb + j <= c1 ? cb + j : c1;
-              const float* const from = part_of(c);
-              const float w = __shfl_sync(0xffffffffu, weight, (lane & 16) + j);
-#pragma unroll
-              for (int i = 0; i < DP / 64; ++i) {
-                const float4 y = __ldcg(reinterpret_cast<const float4*>(from + col * DP + 64 * i + 4 * sub));
-                if (cb + j <= c1) x[i].x += y.x * w, x[i].y += y.y * w, x[i].z += y.z * w, x[i].w += y.w * w;
-              }
-            }
+          for (int k = 0; k < 2; ++k) {
+            const float weight = exp2_fast(r[k] - m);
+            den += w[k] * weight;
+            w[k] = sub + 16 * k < n_sums ? weight : 0.f;
           }
 #pragma unroll
           for (int i = 1; i < 16; i <<= 1) den += __shfl_xor_sync(0xffffffffu, den, i);
-          if (row0 + col < a.group) {
+#pragma unroll
+          for (int i = 0; i < DP / 64; ++i) x[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 1
+          for (uint32_t i0 = 0;;) {
+#pragma unroll
+            for (uint32_t j = 0; j < 8; ++j) {
+              const float weight = __shfl_sync(0xffffffffu, i0 & 16 ? w[1] : w[0], (lane & 16) + (i0 & 8) + j);
+              if (i0 + j < n_sums) {
+#pragma unroll
+                for (int i = 0; i < DP / 64; ++i)
+                  x[i].x += y[j][i].x * weight, x[i].y += y[j][i].y * weight, x[i].z += y[j][i].z * weight, x[i].w += y[j][i].w * weight;
+              }
+            }
+            i0 += 8;
+            if (i0 >= n_sums) break;
+            load(i0);
+          }
+          if (!last) {  // these threads were the only ones to read this head's sums of the first part
+            float* const to = a.parts + uint64_t(place_in(f)) * S::PART;
+#pragma unroll
+            for (int i = 0; i < DP / 64; ++i) __stcg(reinterpret_cast<float4*>(to + col * DP + 64 * i + 4 * sub), x[i]);
+            if (sub == 0) __stcg(to + S::ROWS * DP + col, m), __stcg(to + S::ROWS * (DP + 1) + col, den);
+          } else if (row0 + col < a.group) {
             const float inv = den == 0.f ? 0.f : 1.f / den;
 #pragma unroll
             for (int i = 0; i < DP / 64; ++i) {
@@ -689,10 +746,13 @@ __global__ void __launch_bounds__(kWarps * 32, Shape<FMT, DP, NT>::SMEM <= 75 * 
               a.lse[uint64_t(at.b) * (a.n_heads * a.group) + qh] = den == 0.f ? -INFINITY : (m - kLift + log2f(den)) * 0.6931471805599453f;
           }
         }
+        if (last) break;
+        f = p0, n_sums = groups, apart = kGroup;
+        counter = a.unit_count + uint64_t(at.b) * units + at.u;
       }
     }
     at.step += n - 1;
-    advance(at, a, units, done < n_steps);
+    advance(at, a, units, extra, done < n_steps);
   }
 }
 
@@ -749,11 +809,22 @@ int resident_ctas(const Variant& v, uint32_t* out) {
   BCP_CUDA(cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, device));
   if (per_sm < 1) return fail(BCP_ERR_CUDA, "bcp_kv_attend: the kernel does not fit on this device");
   *out = uint32_t(per_sm * sms);
+  if (*out > kGroup * kGroup) *out = kGroup * kGroup;  // two rounds of joining
   if (n_known < 256) known[n_known++] = Known{v.kernel, device, *out};
   return BCP_OK;
 }
 
-uint64_t counter_bytes(uint64_t units) { return (units * 4 + 255) & ~uint64_t(255); }
+// The workspace: counters of the units, counters of the parts, sums of the parts.
+struct Layout {
+  uint64_t part_count, parts, bytes;
+  Layout(uint64_t units, uint32_t ctas, const Variant& v) {
+    auto up = [](uint64_t x) { return (x + 255) & ~uint64_t(255); };
+    const uint64_t places = uint64_t(ctas) * 2;
+    part_count = up(units * 4);
+    parts = up(part_count + places * 4);
+    bytes = parts + places * v.part_floats * 4;
+  }
+};
 
 int check_group(const char* call, const bcp_kv_cache* c, uint32_t n_q_heads) {
   if (!n_q_heads || n_q_heads > 65536 || n_q_heads % c->n_heads)
@@ -773,7 +844,7 @@ extern "C" int bcp_kv_attend_workspace(const bcp_kv_cache* cache, uint32_t n_q_h
   uint32_t ctas = 0;
   if (int rc = resident_ctas(v, &ctas)) return rc;
   const uint64_t units = uint64_t(max_seqs) * cache->n_heads * ((group + v.rows - 1) / v.rows);
-  *bytes = counter_bytes(units) + uint64_t(ctas) * 2 * v.part_floats * 4;
+  *bytes = Layout(units, ctas, v).bytes;
   return BCP_OK;
 }
 
@@ -803,10 +874,10 @@ extern "C" int bcp_kv_attend(const bcp_kv_cache* c, const bcp_heads* q, const bc
   AttendArgs a;
   a.row_tiles = (group + v.rows - 1) / v.rows;
   const uint64_t units = uint64_t(n_seqs) * c->n_heads * a.row_tiles;
-  const uint64_t need = counter_bytes(units) + uint64_t(ctas) * 2 * v.part_floats * 4;
+  const Layout at(units, ctas, v);
   if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 15)) return fail(BCP_ERR_INVALID, "%s: workspace is NULL or not 16-byte aligned", call);
-  if (workspace_bytes < need)
-    return fail(BCP_ERR_CAPACITY, "%s: a workspace of %llu bytes, %llu needed", call, (unsigned long long)workspace_bytes, (unsigned long long)need);
+  if (workspace_bytes < at.bytes)
+    return fail(BCP_ERR_CAPACITY, "%s: a workspace of %llu bytes, %llu needed", call, (unsigned long long)workspace_bytes, (unsigned long long)at.bytes);
   const uint64_t capacity = uint64_t(table_width) * c->page_size;
   a.capacity = uint32_t(capacity < 0x7fffff00u ? capacity : 0x7fffff00u);
   a.k = c->k, a.v = c->v, a.k_scale = c->k_scale, a.v_scale = c->v_scale;
@@ -819,8 +890,10 @@ extern "C" int bcp_kv_attend(const bcp_kv_cache* c, const bcp_heads* q, const bc
   a.q_is_bf16 = q->type == BCP_BF16, a.group = group, a.n_seqs = n_seqs;
   a.block_table = block_table, a.table_stride = table_stride, a.lengths = lengths;
   a.scale_log2 = scale * kLog2e, a.window = window;
-  a.counters = static_cast<uint32_t*>(workspace);
-  a.parts = reinterpret_cast<float*>(static_cast<char*>(workspace) + counter_bytes(units));
+  char* const w = static_cast<char*>(workspace);
+  a.unit_count = reinterpret_cast<uint32_t*>(w);
+  a.part_count = reinterpret_cast<uint32_t*>(w + at.part_count);
+  a.parts = reinterpret_cast<float*>(w + at.parts);
   // no more CTAs than the longest lengths the table allows can use
   uint32_t longest = a.capacity;
   if (window && window < longest) longest = window + 15 < longest ? window + 15 : longest;
