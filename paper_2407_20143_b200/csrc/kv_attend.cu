@@ -21,7 +21,7 @@
 // Split.  All steps of all sequences and heads form one line that is cut into as many equal parts as CTAs
 // fit on the GPU; lengths are only known on the device, so each CTA finds its part itself.  One more step per
 // unit (sequence, cache head, row tile) stands for what its beginning and end cost.  A unit that lies in one
-// part is finished there; else every part leaves its sums in the workspace.  Of each 32 neighbouring parts the
+// part is finished there; else every part leaves its sums in the workspace.  Of each 64 parts of a unit the
 // one that comes last (a counter says which) joins them, and of these groups the last again, always in
 // the order of the parts, so results do not depend on which that is.
 #include <mutex>
@@ -59,7 +59,7 @@ struct AttendArgs {
   float* parts;          // two places per part: sums, then references, then denominators
 };
 
-constexpr uint32_t kGroup = 32;
+constexpr uint32_t kGroup = 64;  // parts that are joined at once
 // The line of n steps is dealt out to the parts as evenly as whole steps allow.
 struct Cuts {
   uint64_t n, each, longer;  // steps of the line, of a part; the first `longer` parts have one more
@@ -83,8 +83,12 @@ struct Shape {
   static constexpr int CPR = ROW / 16;       // 16-byte chunks of a row
   static constexpr int SIDE = kTok * ROW;
   static constexpr int STAGE = 2 * SIDE + (quant ? 128 : 0) + 16;  // keys, values, their scales, the mask of live tokens
-  // About 20 KiB a warp (two CTAs of four warps on an SM): enough bytes in flight to cover the latency of HBM.
-  static constexpr int STAGES = STAGE <= 2400 ? 5 : 3;
+  // Bytes in flight, in all but one stage of each warp: about 64 KiB an SM cover the latency of HBM.  More only
+  // queue up, and unevenly: 16-bit caches with head_dim 128 take 95 us for 537 MB with two stages, 102 with three.
+  static constexpr int STAGES = STAGE <= 2400 ? 3 : 2;
+  // CTAs that share an SM, as many as registers (128, 168 or 255 a thread) and shared memory allow: 8-bit caches,
+  // whose elements cost conversions, gain from warps (int8 windows 46 us with four CTAs, 50 with three).
+  static constexpr int CTAS = DP == 64 ? (NT == 1 ? 4 : 3) : DP == 128 ? (!quant ? 2 : NT == 1 ? 4 : 3) : quant ? 2 : 1;
   static constexpr int ROWS = 8 * NT;
   static constexpr int SMEM = kWarps * STAGES * STAGE + kWarps * 8 * DP * 4 + kWarps * ROWS * 8 + 128;
   static constexpr int PART = ROWS * (DP + 2);  // floats of one part in the workspace
@@ -208,7 +212,7 @@ __device__ __forceinline__ void advance(Place& p, const AttendArgs& a, uint32_t 
 }
 
 template <int FMT, int DP, int NT>
-__global__ void __launch_bounds__(kWarps * 32, Shape<FMT, DP, NT>::SMEM <= 75 * 1024 ? 3 : Shape<FMT, DP, NT>::SMEM <= 113 * 1024 ? 2 : 1) bcp_kv_attend_kernel(const AttendArgs a) {
+__global__ void __launch_bounds__(kWarps * 32, Shape<FMT, DP, NT>::CTAS) bcp_kv_attend_kernel(const AttendArgs a) {
   typedef Shape<FMT, DP, NT> S;
   constexpr bool kBf16 = FMT == BCP_BF16;  // type of the products; 8-bit caches are widened to binary16
   // binary16 weights underflow below 2^-24: lifting them by 2^6 (they stay below 2^16) moves that to 2^-30
@@ -665,23 +669,20 @@ __global__ void __launch_bounds__(kWarps * 32, Shape<FMT, DP, NT>::SMEM <= 75 * 
         if (last) __threadfence();
         return last;
       };
-      const uint32_t group = blockIdx.x / kGroup, groups = p1 / kGroup - p0 / kGroup + 1;
-      uint32_t f = max(p0, group * kGroup), n_sums = min(p1, group * kGroup + kGroup - 1) - f + 1, apart = 1;
+      const uint32_t groups = (p1 - p0) / kGroup + 1;
+      uint32_t f = p0 + (blockIdx.x - p0) / kGroup * kGroup, n_sums = min(p1 - f + 1, kGroup), apart = 1;
       uint32_t* counter = a.part_count + place_in(f);
       // first the parts of a group, then the groups of the unit, whose sums lie at their first parts
 #pragma unroll 1
       for (bool last = groups == 1; last_of(counter, n_sums); last = true) {
-        // Sixteen threads per head; each knows the weights of every sixteenth of the n_sums sums.
-        const float* const first = a.parts + uint64_t(place_in(f)) * S::PART;
-        const float* const others = a.parts + uint64_t(2 * (f / apart * apart)) * S::PART;
-        auto from_of = [&](uint32_t i) { return i == 0 ? first : others + uint64_t(2 * apart * i) * S::PART; };
+        auto from_of = [&](uint32_t i) { return a.parts + uint64_t(place_in(f + apart * i)) * S::PART; };
 #pragma unroll 1
         for (int t = 0; t < NT; ++t) {
           const uint32_t col = t * 8 + head, qh = h * a.group + row0 + col;
-          // at most kGroup sums: those of parts sub and sub + 16 belong to this thread
-          float m = kNone, r[2], w[2], den = 0.f;
+          // Sixteen threads per head; of each sixteen sums one is this thread's to weigh.
+          float m = kNone, r[kGroup / 16], w[kGroup / 16], den = 0.f;
 #pragma unroll
-          for (int k = 0; k < 2; ++k) {
+          for (int k = 0; k < int(kGroup / 16); ++k) {
             const bool mine = sub + 16 * k < n_sums;
             const float* const from = from_of(mine ? sub + 16 * k : 0);
             r[k] = __ldcg(from + S::ROWS * DP + col);
@@ -698,14 +699,15 @@ __global__ void __launch_bounds__(kWarps * 32, Shape<FMT, DP, NT>::SMEM <= 75 * 
             }
           };
           load(0);  // under way while the weights are found
-          m = fmaxf(r[0], r[1]);
+#pragma unroll
+          for (int k = 0; k < int(kGroup / 16); ++k) m = fmaxf(m, r[k]);
 #pragma unroll
           for (int i = 1; i < 16; i <<= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, i));
 #pragma unroll
-          for (int k = 0; k < 2; ++k) {
+          for (int k = 0; k < int(kGroup / 16); ++k) {
             const float weight = exp2_fast(r[k] - m);
             den += w[k] * weight;
-            w[k] = sub + 16 * k < n_sums ? weight : 0.f;
+            w[k] = weight;
           }
 #pragma unroll
           for (int i = 1; i < 16; i <<= 1) den += __shfl_xor_sync(0xffffffffu, den, i);
@@ -713,9 +715,10 @@ __global__ void __launch_bounds__(kWarps * 32, Shape<FMT, DP, NT>::SMEM <= 75 * 
           for (int i = 0; i < DP / 64; ++i) x[i] = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll 1
           for (uint32_t i0 = 0;;) {
+            const float mine = i0 < 16 ? w[0] : i0 < 32 ? w[1] : i0 < 48 ? w[2] : w[3];
 #pragma unroll
             for (uint32_t j = 0; j < 8; ++j) {
-              const float weight = __shfl_sync(0xffffffffu, i0 & 16 ? w[1] : w[0], (lane & 16) + (i0 & 8) + j);
+              const float weight = __shfl_sync(0xffffffffu, mine, (lane & 16) + (i0 & 8) + j);
               if (i0 + j < n_sums) {
 #pragma unroll
                 for (int i = 0; i < DP / 64; ++i)
@@ -809,6 +812,7 @@ int resident_ctas(const Variant& v, uint32_t* out) {
   BCP_CUDA(cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, device));
   if (per_sm < 1) return fail(BCP_ERR_CUDA, "bcp_kv_attend: the kernel does not fit on this device");
   *out = uint32_t(per_sm * sms);
+  static_assert(kGroup == 64, "four weights a thread in the join");
   if (*out > kGroup * kGroup) *out = kGroup * kGroup;  // two rounds of joining
   if (n_known < 256) known[n_known++] = Known{v.kernel, device, *out};
   return BCP_OK;
