@@ -579,7 +579,7 @@ typedef enum { BCP_ROPE_HALF = 0, BCP_ROPE_PAIRS = 1 } bcp_rope_layout;
 /* n_heads vectors for each token: element e of head h of token t is data[t*token_stride + h*head_stride + e]. */
 typedef struct {
   void* data;
-  int64_t token_stride; /* >= 0; an input may use 0 (one token or head for all) */
+  int64_t token_stride; /* 0 .. 2^32-1; an input may use 0 (one token or head for all) */
   int64_t head_stride;
   uint32_t n_heads;
   uint32_t type;        /* BCP_F32, BCP_BF16 or BCP_F16 */
@@ -613,7 +613,7 @@ typedef struct {
   void* v;
   float* k_scale;        /* 8-bit formats; NULL otherwise */
   float* v_scale;
-  int64_t page_stride;   /* > 0, multiples of 16 bytes */
+  int64_t page_stride;   /* > 0, below 2^32, multiples of 16 bytes */
   int64_t head_stride;
   int64_t token_stride;
   uint32_t n_pages;      /* n_pages * page_size < 2^31 */

@@ -49,140 +49,185 @@ __device__ __forceinline__ __nv_bfloat16 from_f32<__nv_bfloat16>(float x) { retu
 template <>
 __device__ __forceinline__ __half from_f32<__half>(float x) { return __float2half_rn(x); }
 
-// Eight consecutive elements as they lie in memory: 16 bytes of a 16-bit type, 32 bytes of binary32.
-template <typename T>
-struct Raw8 {
-  uint4 w[sizeof(T) / 2];
+// N elements as they lie in memory, moved in the widest accesses of at most 16 bytes.
+template <typename T, int N>
+struct Raw {
+  static constexpr int kBytes = N * int(sizeof(T));
+  static_assert(kBytes == 4 || kBytes == 8 || kBytes % 16 == 0, "whole accesses");
+  uint32_t w[kBytes / 4];
   __device__ __forceinline__ void load(const T* p) {
+    if constexpr (kBytes == 4) w[0] = *reinterpret_cast<const uint32_t*>(p);
+    if constexpr (kBytes == 8) {
+      const uint2 v = *reinterpret_cast<const uint2*>(p);
+      w[0] = v.x, w[1] = v.y;
+    }
 #pragma unroll
-    for (int i = 0; i < int(sizeof(T) / 2); ++i) w[i] = *(reinterpret_cast<const uint4*>(p) + i);
+    for (int i = 0; i < kBytes / 16; ++i) {
+      const uint4 v = *(reinterpret_cast<const uint4*>(p) + i);
+      w[4 * i] = v.x, w[4 * i + 1] = v.y, w[4 * i + 2] = v.z, w[4 * i + 3] = v.w;
+    }
   }
   __device__ __forceinline__ void store(T* p) const {
+    if constexpr (kBytes == 4) *reinterpret_cast<uint32_t*>(p) = w[0];
+    if constexpr (kBytes == 8) *reinterpret_cast<uint2*>(p) = make_uint2(w[0], w[1]);
 #pragma unroll
-    for (int i = 0; i < int(sizeof(T) / 2); ++i) *(reinterpret_cast<uint4*>(p) + i) = w[i];
+    for (int i = 0; i < kBytes / 16; ++i) *(reinterpret_cast<uint4*>(p) + i) = make_uint4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]);
   }
   __device__ __forceinline__ T get(int i) const { return reinterpret_cast<const T*>(w)[i]; }
   __device__ __forceinline__ void set(int i, T x) { reinterpret_cast<T*>(w)[i] = x; }
 };
 
-// The sixteen elements of a head vector that one thread handles ("chunk" c): with a rotation, eight
-// pairs while c < ceil(rot/16), then sixteen unrotated elements; without one, sixteen in a row.
-// first(i) / second(i) are the places of the i-th element of either half; n is how many exist.
+// What one thread takes of a head vector, its "chunk": V pairs, or 2 V elements that are not rotated.
+// In vector form (VEC) V elements make 16 bytes, and a chunk is one vector of either half of a region, the
+// rotated dimensions or the rest, so that neighbouring threads touch neighbouring vectors whatever the
+// layout of the pairs: with the half layout the two vectors hold the first and second elements of V pairs,
+// else (PAIRS) each holds V/2 whole pairs.  It needs regions that are multiples of 2 V = 16 elements (8 of
+// binary32, held to 16 all the same) and rows on 16-byte boundaries.  The scalar form (V = 8) takes any
+// sizes: elements lo + i step and hi + i step, i < n_lo and n_hi.
+template <typename T, bool VEC>
+constexpr int kChunk = VEC ? 16 / int(sizeof(T)) : 8;
+
 struct Chunk {
-  uint32_t a, b, step, n_a, n_b;  // first(i) = a + i*step, second(i) = b + i*step
-  uint32_t pair;                  // index of the first pair (rotated chunks)
+  uint32_t lo, hi, step, n_lo, n_hi;
+  uint32_t pair, pair2;  // first pair of the chunk; in vector form with whole pairs, first pair of the second vector
   bool rotated;
 };
 
-__host__ __device__ __forceinline__ uint32_t chunks_of(uint32_t head_dim, uint32_t rot_dim) { return (rot_dim / 2 + 7) / 8 + (head_dim - rot_dim + 15) / 16; }
+__host__ __device__ __forceinline__ uint32_t chunks_of(uint32_t head_dim, uint32_t rot_dim, uint32_t v) {
+  return (rot_dim / 2 + v - 1) / v + (head_dim - rot_dim + 2 * v - 1) / (2 * v);
+}
 
-__device__ __forceinline__ Chunk chunk_at(uint32_t c, uint32_t head_dim, uint32_t rot_dim, uint32_t layout) {
+template <int V, bool VEC, bool PAIRS>
+__device__ __forceinline__ Chunk chunk_at(uint32_t c, uint32_t head_dim, uint32_t rot_dim) {
   Chunk k;
-  const uint32_t pairs = rot_dim / 2, n_rot = (pairs + 7) / 8;
+  const uint32_t pairs = rot_dim / 2, n_rot = (pairs + V - 1) / V;
   k.rotated = c < n_rot;
-  if (k.rotated) {
-    k.pair = 8 * c;
-    const uint32_t n = pairs - k.pair < 8 ? pairs - k.pair : 8;
-    k.n_a = k.n_b = n;
-    if (layout == BCP_ROPE_HALF) {
-      k.a = k.pair, k.b = pairs + k.pair, k.step = 1;
-    } else {
-      k.a = 2 * k.pair, k.b = 2 * k.pair + 1, k.step = 2;
-    }
+  k.pair = k.pair2 = 0;
+  k.step = 1;
+  if (VEC) {
+    const uint32_t begin = k.rotated ? 0 : rot_dim, size = k.rotated ? rot_dim : head_dim - rot_dim;
+    k.lo = begin + V * (k.rotated ? c : c - n_rot), k.hi = k.lo + size / 2;
+    k.n_lo = k.n_hi = V;
+    if (k.rotated) k.pair = PAIRS ? k.lo / 2 : k.lo, k.pair2 = k.hi / 2;
+  } else if (k.rotated) {
+    k.pair = V * c;
+    k.n_lo = k.n_hi = pairs - k.pair < V ? pairs - k.pair : V;
+    k.lo = PAIRS ? 2 * k.pair : k.pair, k.hi = PAIRS ? k.lo + 1 : k.lo + pairs, k.step = PAIRS ? 2 : 1;
   } else {
-    k.pair = 0;
-    k.a = rot_dim + 16 * (c - n_rot), k.b = k.a + 8, k.step = 1;
-    const uint32_t left = head_dim > k.a ? head_dim - k.a : 0;
-    k.n_a = left < 8 ? left : 8;
-    k.n_b = left <= 8 ? 0 : (left < 16 ? left - 8 : 8);
+    k.lo = rot_dim + 2 * V * (c - n_rot), k.hi = k.lo + V;
+    const uint32_t left = head_dim > k.lo ? head_dim - k.lo : 0;
+    k.n_lo = left < V ? left : V;
+    k.n_hi = left <= V ? 0 : (left < 2 * V ? left - V : V);
   }
   return k;
 }
 
-// Sixteen elements of a chunk.  VEC: whole 16-byte vectors (rot_dim and head_dim multiples of 16,
-// rows on 16-byte boundaries); neighbouring pairs then lie in two consecutive vectors.
 template <typename T, bool VEC>
 struct Elements {
-  Raw8<T> lo, hi;
+  static constexpr int V = kChunk<T, VEC>;
+  Raw<T, V> lo, hi;
   __device__ __forceinline__ void load(const T* row, const Chunk& k) {
     if (VEC) {
-      lo.load(row + k.a);
-      hi.load(row + (k.step == 2 ? k.a + 8 : k.b));
+      lo.load(row + k.lo);
+      hi.load(row + k.hi);
     } else {
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        lo.set(i, uint32_t(i) < k.n_a ? row[k.a + i * k.step] : from_f32<T>(0.f));
-        hi.set(i, uint32_t(i) < k.n_b ? row[k.b + i * k.step] : from_f32<T>(0.f));
+      for (int i = 0; i < V; ++i) {
+        lo.set(i, uint32_t(i) < k.n_lo ? row[k.lo + i * k.step] : from_f32<T>(0.f));
+        hi.set(i, uint32_t(i) < k.n_hi ? row[k.hi + i * k.step] : from_f32<T>(0.f));
       }
     }
   }
-  // x[i] is the first, y[i] the second element of pair i (or the two halves of an unrotated chunk)
-  __device__ __forceinline__ void unpack(float (&x)[8], float (&y)[8], const Chunk& k) const {
-    if (VEC && k.step == 2) {
+  __device__ __forceinline__ void unpack(float (&x)[V], float (&y)[V]) const {
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        x[i] = to_f32(lo.get(2 * i)), y[i] = to_f32(lo.get(2 * i + 1));
-        x[i + 4] = to_f32(hi.get(2 * i)), y[i + 4] = to_f32(hi.get(2 * i + 1));
-      }
-    } else {
-#pragma unroll
-      for (int i = 0; i < 8; ++i) x[i] = to_f32(lo.get(i)), y[i] = to_f32(hi.get(i));
-    }
+    for (int i = 0; i < V; ++i) x[i] = to_f32(lo.get(i)), y[i] = to_f32(hi.get(i));
   }
-  __device__ __forceinline__ void pack(const float (&x)[8], const float (&y)[8], const Chunk& k) {
-    if (VEC && k.step == 2) {
+  __device__ __forceinline__ void pack(const float (&x)[V], const float (&y)[V]) {
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        lo.set(2 * i, from_f32<T>(x[i])), lo.set(2 * i + 1, from_f32<T>(y[i]));
-        hi.set(2 * i, from_f32<T>(x[i + 4])), hi.set(2 * i + 1, from_f32<T>(y[i + 4]));
-      }
-    } else {
-#pragma unroll
-      for (int i = 0; i < 8; ++i) lo.set(i, from_f32<T>(x[i])), hi.set(i, from_f32<T>(y[i]));
-    }
+    for (int i = 0; i < V; ++i) lo.set(i, from_f32<T>(x[i])), hi.set(i, from_f32<T>(y[i]));
   }
   __device__ __forceinline__ void store(T* row, const Chunk& k) const {
     if (VEC) {
-      lo.store(row + k.a);
-      hi.store(row + (k.step == 2 ? k.a + 8 : k.b));
+      lo.store(row + k.lo);
+      hi.store(row + k.hi);
     } else {
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        if (uint32_t(i) < k.n_a) row[k.a + i * k.step] = lo.get(i);
-        if (uint32_t(i) < k.n_b) row[k.b + i * k.step] = hi.get(i);
+      for (int i = 0; i < V; ++i) {
+        if (uint32_t(i) < k.n_lo) row[k.lo + i * k.step] = lo.get(i);
+        if (uint32_t(i) < k.n_hi) row[k.hi + i * k.step] = hi.get(i);
       }
     }
   }
 };
 
-// Cosines and sines of a chunk's eight pairs.
-template <bool VEC>
+// Two binary32 operations at once (sm_100 has the packed forms).
+__device__ __forceinline__ float2 mul2(float2 a, float2 b) {
+  float2 r;
+  asm("{\n.reg .b64 x, y, z;\nmov.b64 x, {%2, %3};\nmov.b64 y, {%4, %5};\nmul.rn.f32x2 z, x, y;\nmov.b64 {%0, %1}, z;\n}"
+      : "=f"(r.x), "=f"(r.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+  return r;
+}
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
+  float2 r;
+  asm("{\n.reg .b64 x, y, z;\nmov.b64 x, {%2, %3};\nmov.b64 y, {%4, %5};\nmov.b64 z, {%6, %7};\nfma.rn.f32x2 z, x, y, z;\nmov.b64 {%0, %1}, z;\n}"
+      : "=f"(r.x), "=f"(r.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
+  return r;
+}
+
+// Cosines and sines of a chunk's V pairs.
+template <int V, bool VEC, bool PAIRS>
 struct Angles {
-  float c[8], s[8];
-  __device__ __forceinline__ void load(const float* table, int64_t position, uint32_t rot_dim, const Chunk& k) {
+  float c[V], s[V];
+  __device__ __forceinline__ void load(const float* table, int64_t position, uint32_t rot_dim, const Chunk& k, float sign) {
     const uint32_t pairs = rot_dim / 2;
-    const float* row = table + position * rot_dim;
+    const float* const row = table + position * rot_dim;
     if (VEC) {
-      const float4* pc = reinterpret_cast<const float4*>(row + k.pair);
-      const float4* ps = reinterpret_cast<const float4*>(row + pairs + k.pair);
-      const float4 c0 = __ldg(pc), c1 = __ldg(pc + 1), s0 = __ldg(ps), s1 = __ldg(ps + 1);
-      c[0] = c0.x, c[1] = c0.y, c[2] = c0.z, c[3] = c0.w, c[4] = c1.x, c[5] = c1.y, c[6] = c1.z, c[7] = c1.w;
-      s[0] = s0.x, s[1] = s0.y, s[2] = s0.z, s[3] = s0.w, s[4] = s1.x, s[5] = s1.y, s[6] = s1.z, s[7] = s1.w;
+      // with whole pairs the second vector's pairs are elsewhere
+      const uint32_t second = PAIRS ? k.pair2 : k.pair + V / 2;
+      part(row, row + pairs, k.pair, 0);
+      part(row, row + pairs, second, V / 2);
     } else {
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const bool in = uint32_t(i) < k.n_a;
+      for (int i = 0; i < V; ++i) {
+        const bool in = uint32_t(i) < k.n_lo;
         c[i] = in ? __ldg(row + k.pair + i) : 1.f;
         s[i] = in ? __ldg(row + pairs + k.pair + i) : 0.f;
       }
     }
-  }
-  __device__ __forceinline__ void rotate(float (&x)[8], float (&y)[8], float sign) const {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const float t = sign * s[i], u = x[i];
-      x[i] = u * c[i] - y[i] * t;
-      y[i] = y[i] * c[i] + u * t;
+    for (int i = 0; i < V; ++i) s[i] *= sign;
+  }
+  __device__ __forceinline__ void part(const float* pc, const float* ps, uint32_t from, int to) {
+    if constexpr (V == 8) {
+      const float4 a = __ldg(reinterpret_cast<const float4*>(pc + from)), b = __ldg(reinterpret_cast<const float4*>(ps + from));
+      c[to] = a.x, c[to + 1] = a.y, c[to + 2] = a.z, c[to + 3] = a.w;
+      s[to] = b.x, s[to + 1] = b.y, s[to + 2] = b.z, s[to + 3] = b.w;
+    } else {
+      const float2 a = __ldg(reinterpret_cast<const float2*>(pc + from)), b = __ldg(reinterpret_cast<const float2*>(ps + from));
+      c[to] = a.x, c[to + 1] = a.y;
+      s[to] = b.x, s[to + 1] = b.y;
+    }
+  }
+  // (u, v) = (u c - v s, v c + u s) for the pairs of the chunk, whose vectors are x and y
+  __device__ __forceinline__ void rotate(float (&x)[V], float (&y)[V]) const {
+    if constexpr (VEC && PAIRS) {
+      neighbours(x, 0);
+      neighbours(y, V / 2);
+    } else {
+#pragma unroll
+      for (int i = 0; i < V; i += 2) {
+        const float2 a = make_float2(x[i], x[i + 1]), b = make_float2(y[i], y[i + 1]), cc = make_float2(c[i], c[i + 1]), ss = make_float2(s[i], s[i + 1]);
+        const float2 p = fma2(a, cc, mul2(b, make_float2(-ss.x, -ss.y))), q = fma2(b, cc, mul2(a, ss));
+        x[i] = p.x, x[i + 1] = p.y, y[i] = q.x, y[i + 1] = q.y;
+      }
+    }
+  }
+  __device__ __forceinline__ void neighbours(float (&x)[V], int at) const {
+#pragma unroll
+    for (int i = 0; i < V; i += 2) {
+      const float cc = c[at + i / 2], ss = s[at + i / 2];
+      const float2 p = fma2(make_float2(x[i], x[i + 1]), make_float2(cc, cc), mul2(make_float2(x[i + 1], x[i]), make_float2(-ss, ss)));
+      x[i] = p.x, x[i + 1] = p.y;
     }
   }
 };

@@ -39,7 +39,7 @@ constexpr float kLog2e = 1.4426950408889634f;
 struct AttendArgs {
   const void *k, *v;
   const float *k_scale, *v_scale;
-  int64_t page_stride, head_stride, token_stride;
+  uint32_t page_stride, head_stride, token_stride;
   uint32_t n_pages, n_heads, head_dim;
   FastDiv page_size;
   uint32_t* status;
@@ -316,12 +316,12 @@ __global__ void __launch_bounds__(kWarps * 32, Shape<FMT, DP, NT>::CTAS) bcp_kv_
       if (live) {
         constexpr int kRows = 32 / S::CPR;  // rows that one turn of the copies covers
         const uint32_t l = lane / S::CPR, c = lane % S::CPR;
-        const int64_t row = on ? page * a.page_stride + h * a.head_stride + off * a.token_stride : 0;
+        const uint64_t row = on ? uint64_t(uint32_t(page)) * a.page_stride + uint64_t(h) * a.head_stride + uint64_t(off) * a.token_stride : 0;
         // Each lane copies one column of chunks.  In a tile that is live throughout and lies in one page
         // (the offsets did not start again) rows are a stride apart; else each row is looked up.
         const bool inside = c * 16 < a.head_dim * S::ES;
         if (__all_sync(0xffffffffu, on && off >= (lane & 15))) {
-          const int64_t step = kRows * a.token_stride * S::ES;
+          const uint64_t step = uint64_t(a.token_stride) * (kRows * S::ES);
           const char* from = static_cast<const char*>(a.k) + (__shfl_sync(0xffffffffu, row, l) * S::ES + (inside ? c * 16 : 0));
 #pragma unroll
           for (int i = 0; i < kTok / kRows; ++i) {
@@ -334,14 +334,14 @@ __global__ void __launch_bounds__(kWarps * 32, Shape<FMT, DP, NT>::CTAS) bcp_kv_
           for (int i = 0; i < kTok / kRows; ++i) {
             const uint32_t r = i * kRows + l;
             const bool copy = (live >> r & 1) && inside;
-            const int64_t x = __shfl_sync(0xffffffffu, row, r) * S::ES + c * 16;
+            const uint64_t x = __shfl_sync(0xffffffffu, row, r) * S::ES + c * 16;
             const char* const from = static_cast<const char*>(a.k) + (copy ? x : 0);
             copy16(stage + key_at<S::CPR>(r, c), from, copy);
             copy16(stage + S::SIDE + value_at<S::CPR, S::quant>(r, c), from + v_from_k, copy);
           }
         }
         if (S::quant) {
-          const int64_t n = (int64_t(page) * a.n_heads + h) * a.page_size.d + off;
+          const uint64_t n = uint64_t(uint32_t(page) * a.n_heads + h) * a.page_size.d + off;
           copy4(stage + 2 * S::SIDE + lane * 4, (lane < 16 ? a.k_scale : a.v_scale) + (on ? n : 0), on);
         }
       }
@@ -875,7 +875,7 @@ extern "C" int bcp_kv_attend(const bcp_kv_cache* c, const bcp_heads* q, const bc
   const Variant v = variant_of(c->format, c->head_dim, group);
   uint32_t ctas = 0;
   if (int rc = resident_ctas(v, &ctas)) return rc;
-  AttendArgs a;
+  AttendArgs a = {};
   a.row_tiles = (group + v.rows - 1) / v.rows;
   const uint64_t units = uint64_t(n_seqs) * c->n_heads * a.row_tiles;
   const Layout at(units, ctas, v);
@@ -885,7 +885,7 @@ extern "C" int bcp_kv_attend(const bcp_kv_cache* c, const bcp_heads* q, const bc
   const uint64_t capacity = uint64_t(table_width) * c->page_size;
   a.capacity = uint32_t(capacity < 0x7fffff00u ? capacity : 0x7fffff00u);
   a.k = c->k, a.v = c->v, a.k_scale = c->k_scale, a.v_scale = c->v_scale;
-  a.page_stride = c->page_stride, a.head_stride = c->head_stride, a.token_stride = c->token_stride;
+  a.page_stride = uint32_t(c->page_stride), a.head_stride = uint32_t(c->head_stride), a.token_stride = uint32_t(c->token_stride);
   a.n_pages = c->n_pages, a.n_heads = c->n_heads, a.head_dim = c->head_dim;
   a.page_size = FastDiv(c->page_size);
   a.status = c->status;

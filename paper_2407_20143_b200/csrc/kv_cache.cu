@@ -1,9 +1,9 @@
 // The paged key-value cache: new tokens written into their slots, slots read back.
 //
 // Both are bound by memory: a head vector is read once and written once.  A group of lanes (a power of
-// two, at least head_dim / 16) holds one vector, sixteen elements a lane, so the largest magnitude that
-// an 8-bit format's scale needs is a few shuffles away and the vector is never read twice.  A group
-// takes four heads of one token, whose loads are all in flight before the first one is used.
+// two) holds one head vector, a chunk a lane, so the largest magnitude that an 8-bit format's scale needs is a
+// few shuffles away and the vector is never read twice.  A group takes four heads of one token, whose loads
+// are all in flight before the first one is used.
 #include "decode.cuh"
 
 using namespace bcp;
@@ -38,8 +38,11 @@ int check_cache(const char* call, const bcp_kv_cache* c) {
   const uint64_t es = type_size(c->format);
   const uint64_t bits = reinterpret_cast<uintptr_t>(c->k) | reinterpret_cast<uintptr_t>(c->v) | uint64_t(c->page_stride) * es |
                         uint64_t(c->head_stride) * es | uint64_t(c->token_stride) * es;
-  if (c->page_stride <= 0 || c->head_stride <= 0 || c->token_stride <= 0 || (bits & 15))
-    return fail(BCP_ERR_INVALID, "%s: cache addresses and strides must be positive multiples of 16 bytes", call);
+  const int64_t most = 0xffffffffll;
+  if (c->page_stride <= 0 || c->head_stride <= 0 || c->token_stride <= 0 || c->page_stride > most || c->head_stride > most ||
+      c->token_stride > most || (bits & 15))
+    return fail(BCP_ERR_INVALID, "%s: cache addresses and strides must be positive multiples of 16 bytes, strides below 2^32 elements", call);
+  if (uint64_t(c->n_pages) * c->n_heads > uint64_t(most)) return fail(BCP_ERR_INVALID, "%s: %u pages of %u heads", call, c->n_pages, c->n_heads);
   const int64_t strides[3] = {c->page_stride, c->head_stride, c->token_stride};
   const uint32_t extents[3] = {c->n_pages, c->n_heads, c->page_size};
   if (rows_overlap(strides, extents, 3, c->head_dim)) return fail(BCP_ERR_DST_ALIAS, "%s: rows of the cache overlap", call);
@@ -54,19 +57,19 @@ int check_cache(const char* call, const bcp_kv_cache* c) {
 
 namespace {
 
-constexpr int kHeads = 4;            // heads per group of lanes
+constexpr int kHeads = 2;            // heads per group of lanes
 constexpr float kSmallestScale = 1.262177448353619e-29f;  // 2^-96: its reciprocal and sums of it stay finite
 
 struct CacheArgs {
   void* pages[2];
   float* scales[2];
-  int64_t page_stride, head_stride, token_stride;
+  uint32_t page_stride, head_stride, token_stride;
   uint32_t n_slots, n_heads, head_dim;
   FastDiv page_size;
   uint32_t* status;
   // the token-major side
   void* rows[2];
-  int64_t row_token[2], row_head[2];
+  uint32_t row_token[2], row_head[2];
   const int64_t* slots;
   uint32_t n_groups;      // groups of lanes
   FastDiv per_token;      // groups per token: 2 * ceil(n_heads / kHeads)
@@ -129,95 +132,125 @@ __device__ __forceinline__ Item item_of(const CacheArgs& a) {
   return it;
 }
 
-// Eight values of either half of a chunk, in an 8-bit format: two words per half, or four words of
-// neighbouring pairs.
-template <int FMT, bool VEC>
-__device__ __forceinline__ void store_8bit(uint8_t* row, const Chunk& k, const float (&x)[8], const float (&y)[8], float inv) {
+// The two halves of a chunk, multiplied by inv, in an 8-bit format.
+template <int FMT, int V, bool VEC>
+__device__ __forceinline__ void store_8bit(uint8_t* row, const Chunk& k, const float (&x)[V], const float (&y)[V], float inv) {
   typedef Format<FMT> F;
-  if (VEC && k.step == 2) {
-    uint32_t w[4];
+  uint32_t p[V / 2], q[V / 2];  // two elements each
+  const float2 inv2 = make_float2(inv, inv);
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
-      w[i] = F::pack2(x[2 * i] * inv, y[2 * i] * inv) | F::pack2(x[2 * i + 1] * inv, y[2 * i + 1] * inv) << 16;
-    *reinterpret_cast<uint4*>(row + k.a) = make_uint4(w[0], w[1], w[2], w[3]);
-    return;
-  }
-  uint32_t p[4], q[4];
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    p[i] = F::pack2(x[2 * i] * inv, x[2 * i + 1] * inv);
-    q[i] = F::pack2(y[2 * i] * inv, y[2 * i + 1] * inv);
+  for (int i = 0; i < V / 2; ++i) {
+    const float2 u = mul2(make_float2(x[2 * i], x[2 * i + 1]), inv2), v = mul2(make_float2(y[2 * i], y[2 * i + 1]), inv2);
+    p[i] = F::pack2(u.x, u.y), q[i] = F::pack2(v.x, v.y);
   }
   if (VEC) {
-    *reinterpret_cast<uint2*>(row + k.a) = make_uint2(p[0] | p[1] << 16, p[2] | p[3] << 16);
-    *reinterpret_cast<uint2*>(row + k.b) = make_uint2(q[0] | q[1] << 16, q[2] | q[3] << 16);
+    Raw<uint8_t, V> lo, hi;
+#pragma unroll
+    for (int i = 0; i < V / 4; ++i) lo.w[i] = p[2 * i] | p[2 * i + 1] << 16, hi.w[i] = q[2 * i] | q[2 * i + 1] << 16;
+    lo.store(row + k.lo);
+    hi.store(row + k.hi);
   } else {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      if (uint32_t(i) < k.n_a) row[k.a + i * k.step] = uint8_t(p[i / 2] >> (8 * (i & 1)));
-      if (uint32_t(i) < k.n_b) row[k.b + i * k.step] = uint8_t(q[i / 2] >> (8 * (i & 1)));
+    for (int i = 0; i < V; ++i) {
+      if (uint32_t(i) < k.n_lo) row[k.lo + i * k.step] = uint8_t(p[i / 2] >> (8 * (i & 1)));
+      if (uint32_t(i) < k.n_hi) row[k.hi + i * k.step] = uint8_t(q[i / 2] >> (8 * (i & 1)));
     }
   }
 }
 
-template <typename T, int FMT, bool VEC>
-__global__ void __launch_bounds__(256) bcp_kv_write_kernel(const CacheArgs a) {
+// x / qmax, correctly rounded, from the rounded reciprocal and the remainder of a first quotient (Markstein's
+// theorem on division).  The remainder is exact unless x is near the smallest numbers; what comes out there
+// is far below the smallest scale.
+template <int FMT>
+__device__ __forceinline__ float quotient(float x) {
+  constexpr float qmax = Format<FMT>::qmax, inverse = 1.f / qmax;
+  const float q = x * inverse;
+  return __fmaf_rn(__fmaf_rn(-qmax, q, x), inverse, q);
+}
+
+// The largest magnitude of three numbers, NaN if one is.
+__device__ __forceinline__ float largest(float a, float b, float c) {
+  float r;
+  asm("max.NaN.abs.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+  return r;
+}
+
+template <typename T, int FMT, bool VEC, bool PAIRS>
+__global__ void __launch_bounds__(256, 4) bcp_kv_write_kernel(const CacheArgs a) {
   typedef Format<FMT> F;
   typedef typename F::T C;
   const Item it = item_of(a);
   const uint32_t rot = it.side ? 0 : a.rot_dim;
-  const bool mine = it.lane < chunks_of(a.head_dim, rot);
-  const Chunk k = chunk_at(mine ? it.lane : 0, a.head_dim, rot, a.layout);
-  int64_t slot = it.used ? a.slots[it.t] : -1, position = 0;
+  constexpr int V = kChunk<T, VEC>;
+  const bool mine = it.lane < chunks_of(a.head_dim, rot, V);
+  const Chunk k = chunk_at<V, VEC, PAIRS>(mine ? it.lane : 0, a.head_dim, rot);
+  // nothing waits for the slot before the stores
+  Elements<T, VEC> e[kHeads];
+  const T* from = static_cast<const T*>(a.rows[it.side]) + (uint64_t(it.t) * a.row_token[it.side] + uint64_t(it.h0) * a.row_head[it.side]);
+#pragma unroll
+  for (int j = 0; j < kHeads; ++j)
+    if (it.used && mine && it.h0 + j < a.n_heads) e[j].load(from + uint64_t(j) * a.row_head[it.side], k);
+  int64_t slot = it.used ? a.slots[it.t] : -1;
   if (slot >= int64_t(a.n_slots)) {
     raise(a.status, BCP_BAD_SLOT);
     slot = -1;
   }
-  if (slot >= 0 && a.rot_dim) {  // both sides look at the position: a token is written whole or not at all
-    position = a.positions[it.t];
+  Angles<V, VEC, PAIRS> w;
+  if (it.used && a.rot_dim) {  // both sides look at the position: a token is written whole or not at all
+    int64_t position = a.positions[it.t];
     if (position < 0 || position >= a.n_positions) {
-      raise(a.status, BCP_BAD_POSITION);
-      slot = -1;
+      if (slot >= 0) raise(a.status, BCP_BAD_POSITION);
+      slot = -1, position = 0;
     }
+    if (mine && k.rotated) w.load(a.table, position, rot, k, 1.f);
   }
   const bool live = slot >= 0 && mine;
-  const uint32_t page = a.page_size.div(uint32_t(slot >= 0 ? slot : 0)), off = uint32_t(slot) - page * a.page_size.d;
-  Elements<T, VEC> e[kHeads];
-  const T* from = static_cast<const T*>(a.rows[it.side]) + it.t * a.row_token[it.side] + it.h0 * a.row_head[it.side];
+  const uint32_t page = a.page_size.div(uint32_t(slot >= 0 ? slot : 0)), off = uint32_t(slot >= 0 ? slot : 0) - page * a.page_size.d;
+  C* to = static_cast<C*>(a.pages[it.side]) + (uint64_t(page) * a.page_stride + uint64_t(it.h0) * a.head_stride + uint64_t(off) * a.token_stride);
+  if constexpr (F::quantised) {
+    float x[kHeads][V], y[kHeads][V], m[kHeads];
 #pragma unroll
-  for (int j = 0; j < kHeads; ++j)
-    if (live && it.h0 + j < a.n_heads) e[j].load(from + j * a.row_head[it.side], k);
-  Angles<VEC> w;
-  if (live && k.rotated) w.load(a.table, position, rot, k);
-  C* to = static_cast<C*>(a.pages[it.side]) + page * a.page_stride + it.h0 * a.head_stride + off * a.token_stride;
+    for (int j = 0; j < kHeads; ++j) {
+      m[j] = 0.f;
+      if (live && it.h0 + j < a.n_heads) {
+        e[j].unpack(x[j], y[j]);
+        if (k.rotated) w.rotate(x[j], y[j]);
 #pragma unroll
-  for (int j = 0; j < kHeads; ++j) {
-    const bool on = live && it.h0 + j < a.n_heads;
-    float x[8], y[8];
-    if (on) {
-      e[j].unpack(x, y, k);
-      if (k.rotated) w.rotate(x, y, 1.f);
+        for (int i = 0; i < V; ++i)
+          if (VEC || uint32_t(i) < k.n_lo) m[j] = largest(m[j], x[j][i], VEC || uint32_t(i) < k.n_hi ? y[j][i] : 0.f);
+      }
     }
-    if constexpr (F::quantised) {
-      // magnitudes compare like their bit patterns, and a NaN's is above all of them
-      uint32_t m = 0;
-      if (on) {
+    for (uint32_t o = 1u << a.lanes_log2 >> 1; o; o >>= 1) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          if (VEC || uint32_t(i) < k.n_a) m = max(m, __float_as_uint(x[i]) & 0x7fffffffu);
-          if (VEC || uint32_t(i) < k.n_b) m = max(m, __float_as_uint(y[i]) & 0x7fffffffu);
-        }
+      for (int j = 0; j < kHeads; ++j) m[j] = largest(m[j], __shfl_xor_sync(0xffffffffu, m[j], o), 0.f);
+    }
+#pragma unroll
+    for (int j = 0; j < kHeads; ++j) {
+      const float scale = m[j] < INFINITY ? fmaxf(quotient<FMT>(m[j]), kSmallestScale) : __uint_as_float(0x7fc00000u);
+      if (live && it.h0 + j < a.n_heads) {
+        store_8bit<FMT, V, VEC>(reinterpret_cast<uint8_t*>(to + uint64_t(j) * a.head_stride), k, x[j], y[j], __frcp_rn(scale));
+        if (it.lane == 0) a.scales[it.side][uint64_t(page * a.n_heads + it.h0 + j) * a.page_size.d + off] = scale;
       }
-      for (uint32_t o = 1u << a.lanes_log2 >> 1; o; o >>= 1) m = max(m, __shfl_xor_sync(0xffffffffu, m, o));
-      const float scale = m >= 0x7f800000u ? __uint_as_float(0x7fc00000u) : fmaxf(__fdiv_rn(__uint_as_float(m), F::qmax), kSmallestScale);
-      if (on) {
-        store_8bit<FMT, VEC>(reinterpret_cast<uint8_t*>(to + j * a.head_stride), k, x, y, __frcp_rn(scale));
-        if (it.lane == 0) a.scales[it.side][(int64_t(page) * a.n_heads + it.h0 + j) * a.page_size.d + off] = scale;
+    }
+  } else {
+#pragma unroll
+    for (int j = 0; j < kHeads; ++j) {
+      if (!live || it.h0 + j >= a.n_heads) continue;
+      float x[V], y[V];
+      e[j].unpack(x, y);
+      if (k.rotated) w.rotate(x, y);
+      C* const row = to + uint64_t(j) * a.head_stride;
+      if constexpr (VEC) {
+        Raw<C, V> lo, hi;
+#pragma unroll
+        for (int i = 0; i < V; ++i) lo.set(i, from_f32<C>(x[i])), hi.set(i, from_f32<C>(y[i]));
+        lo.store(row + k.lo);
+        hi.store(row + k.hi);
+      } else {
+        Elements<C, false> c;
+        c.pack(x, y);
+        c.store(row, k);
       }
-    } else if (on) {
-      Elements<C, VEC> c;
-      c.pack(x, y, k);
-      c.store(to + j * a.head_stride, k);
     }
   }
 }
@@ -226,50 +259,58 @@ template <typename T, int FMT, bool VEC>
 __global__ void __launch_bounds__(256) bcp_kv_read_kernel(const CacheArgs a) {
   typedef Format<FMT> F;
   typedef typename F::T C;
-  constexpr int kWords = F::quantised ? 1 : 2;  // 16-byte vectors per sixteen elements
+  constexpr int V = VEC ? 16 / int(sizeof(T)) : 8;
   const Item it = item_of(a);
-  if (!it.used || it.lane * 16 >= a.head_dim) return;
+  if (!it.used || it.lane * (2 * V) >= a.head_dim) return;
   int64_t slot = a.slots[it.t];
   if (slot >= int64_t(a.n_slots)) {
     raise(a.status, BCP_BAD_SLOT);
     slot = -1;
   }
-  const Chunk k = chunk_at(it.lane, a.head_dim, 0, 0);
+  // one vector of either half of the head (whose dimension is a multiple of 16)
+  const uint32_t lo = V * it.lane, hi = lo + a.head_dim / 2;
   const uint32_t page = a.page_size.div(uint32_t(slot >= 0 ? slot : 0)), off = uint32_t(slot) - page * a.page_size.d;
-  const C* from = static_cast<const C*>(a.pages[it.side]) + page * a.page_stride + it.h0 * a.head_stride + off * a.token_stride + 16 * it.lane;
-  uint4 raw[kHeads][kWords];
+  const C* from = static_cast<const C*>(a.pages[it.side]) + (uint64_t(page) * a.page_stride + uint64_t(it.h0) * a.head_stride + uint64_t(off) * a.token_stride);
+  Raw<C, V> raw[kHeads][2];
   float scale[kHeads];
 #pragma unroll
   for (int j = 0; j < kHeads; ++j) {
-    const bool on = slot >= 0 && it.h0 + j < a.n_heads;
-#pragma unroll
-    for (int i = 0; i < kWords; ++i) raw[j][i] = on ? __ldg(reinterpret_cast<const uint4*>(from + j * a.head_stride) + i) : make_uint4(0, 0, 0, 0);
     scale[j] = 1.f;
-    if (F::quantised && on) scale[j] = __ldg(a.scales[it.side] + (int64_t(page) * a.n_heads + it.h0 + j) * a.page_size.d + off);
+    if (slot >= 0 && it.h0 + j < a.n_heads) {
+      raw[j][0].load(from + uint64_t(j) * a.head_stride + lo);
+      raw[j][1].load(from + uint64_t(j) * a.head_stride + hi);
+      if (F::quantised) scale[j] = __ldg(a.scales[it.side] + uint64_t(page * a.n_heads + it.h0 + j) * a.page_size.d + off);
+    } else {
+#pragma unroll
+      for (int i = 0; i < int(sizeof raw[0][0].w / 4); ++i) raw[j][0].w[i] = raw[j][1].w[i] = 0;
+    }
   }
-  T* to = static_cast<T*>(a.rows[it.side]) + it.t * a.row_token[it.side] + it.h0 * a.row_head[it.side];
+  T* to = static_cast<T*>(a.rows[it.side]) + (uint64_t(it.t) * a.row_token[it.side] + uint64_t(it.h0) * a.row_head[it.side]);
 #pragma unroll
   for (int j = 0; j < kHeads; ++j) {
     if (it.h0 + j >= a.n_heads) break;
-    float x[8], y[8];
-    if constexpr (F::quantised) {
-      const uint32_t w[4] = {raw[j][0].x, raw[j][0].y, raw[j][0].z, raw[j][0].w};
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const float2 p = F::unpack2(w[i / 2] >> (16 * (i & 1)) & 0xffffu), q = F::unpack2(w[2 + i / 2] >> (16 * (i & 1)) & 0xffffu);
-        x[2 * i] = p.x * scale[j], x[2 * i + 1] = p.y * scale[j];
-        y[2 * i] = q.x * scale[j], y[2 * i + 1] = q.y * scale[j];
+    for (int half = 0; half < 2; ++half) {
+      Raw<T, V> y;
+#pragma unroll
+      for (int i = 0; i < V; i += 2) {
+        float2 x;
+        if constexpr (F::quantised) {
+          x = F::unpack2(raw[j][half].w[i / 4] >> (8 * (i & 2)) & 0xffffu);
+          x.x *= scale[j], x.y *= scale[j];
+        } else {
+          x = make_float2(to_f32(raw[j][half].get(i)), to_f32(raw[j][half].get(i + 1)));
+        }
+        y.set(i, from_f32<T>(x.x)), y.set(i + 1, from_f32<T>(x.y));
       }
-    } else {
+      T* const row = to + uint64_t(j) * a.row_head[it.side] + (half ? hi : lo);
+      if (VEC) {
+        y.store(row);
+      } else {
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        x[i] = to_f32(reinterpret_cast<const C*>(raw[j])[i]);
-        y[i] = to_f32(reinterpret_cast<const C*>(raw[j])[8 + i]);
+        for (int i = 0; i < V; ++i) row[i] = y.get(i);
       }
     }
-    Elements<T, VEC> e;
-    e.pack(x, y, k);
-    e.store(to + j * a.row_head[it.side], k);
   }
 }
 
@@ -278,8 +319,10 @@ void launch(bool write, const CacheArgs& a, uint32_t format, cudaStream_t stream
   const uint32_t blocks = uint32_t(((uint64_t(a.n_groups) << a.lanes_log2) + 255) / 256);
 #define BCP_ON(F)                                                           \
   if (format == F) {                                                        \
-    if (write)                                                              \
-      bcp_kv_write_kernel<T, F, VEC><<<blocks, 256, 0, stream>>>(a);        \
+    if (write && a.layout == BCP_ROPE_PAIRS)                                \
+      bcp_kv_write_kernel<T, F, VEC, true><<<blocks, 256, 0, stream>>>(a);  \
+    else if (write)                                                         \
+      bcp_kv_write_kernel<T, F, VEC, false><<<blocks, 256, 0, stream>>>(a); \
     else                                                                    \
       bcp_kv_read_kernel<T, F, VEC><<<blocks, 256, 0, stream>>>(a);         \
   }
@@ -305,22 +348,23 @@ int move(const char* call, bool write, const bcp_kv_cache* c, const bcp_heads* k
   if (n_tokens && !slots) return fail(BCP_ERR_INVALID, "%s: slots is NULL", call);
   if (n_tokens && rope && !positions) return fail(BCP_ERR_INVALID, "%s: positions is NULL", call);
 
-  CacheArgs a;
+  CacheArgs a = {};
   a.pages[0] = c->k, a.pages[1] = c->v, a.scales[0] = c->k_scale, a.scales[1] = c->v_scale;
-  a.page_stride = c->page_stride, a.head_stride = c->head_stride, a.token_stride = c->token_stride;
+  a.page_stride = uint32_t(c->page_stride), a.head_stride = uint32_t(c->head_stride), a.token_stride = uint32_t(c->token_stride);
   a.n_slots = c->n_pages * c->page_size, a.n_heads = c->n_heads, a.head_dim = c->head_dim;
   a.page_size = FastDiv(c->page_size);
   a.status = c->status;
-  a.row_token[0] = k->token_stride, a.row_head[0] = k->head_stride;
-  a.row_token[1] = v->token_stride, a.row_head[1] = v->head_stride;
+  a.row_token[0] = uint32_t(k->token_stride), a.row_head[0] = uint32_t(k->head_stride);
+  a.row_token[1] = uint32_t(v->token_stride), a.row_head[1] = uint32_t(v->head_stride);
   a.rot_dim = rope ? rope->rot_dim : 0, a.layout = rope ? rope->layout : 0;
   a.table = rope ? rope->table : nullptr, a.n_positions = rope ? rope->n_positions : 0;
-  const uint32_t ck = chunks_of(c->head_dim, a.rot_dim), cv = chunks_of(c->head_dim, 0), lanes = ck > cv ? ck : cv;
-  a.lanes_log2 = 0;
+  const bool vec = a.rot_dim % 16 == 0 && rows_aligned(k, 16) && rows_aligned(v, 16);
+  const uint32_t size = vec ? 16 / type_size(k->type) : 8;  // of a chunk
+  const uint32_t ck = chunks_of(c->head_dim, a.rot_dim, size), cv = chunks_of(c->head_dim, 0, size), lanes = ck > cv ? ck : cv;
+  a.lanes_log2 = 0;  // at most 5: 32 chunks of 8 elements, or 17 of 16
   while ((1u << a.lanes_log2) < lanes) ++a.lanes_log2;
   const uint32_t per_token = 2 * ((c->n_heads + kHeads - 1) / kHeads);
   a.per_token = FastDiv(per_token);
-  const bool vec = a.rot_dim % 16 == 0 && rows_aligned(k, 16) && rows_aligned(v, 16);
   // thread indices stay below 2^31: longer inputs take several launches
   const int64_t most = 0x7fffff00 / (per_token << a.lanes_log2);
   const uint32_t es = type_size(k->type);

@@ -1,7 +1,7 @@
 // Rotary positions: every pair of a head vector is turned by the angle of its token's position.
 //
 // The arithmetic is six operations per pair, so the kernel is bound by memory: each element is read
-// once and written once.  A thread takes sixteen elements (eight pairs) of four heads of one token:
+// once and written once.  A thread takes one chunk (two 16-byte vectors) of four heads of one token:
 // the cosines and sines, which all heads of a token share, are loaded once per four heads, and eight
 // 16-byte loads are in flight per thread (16-bit types).  Query and key heads go through one launch.
 #include "decode.cuh"
@@ -15,7 +15,8 @@ int check_heads(const char* call, const char* name, const bcp_heads* h, bool wri
   if (h->type != BCP_F32 && h->type != BCP_BF16 && h->type != BCP_F16)
     return fail(BCP_ERR_INVALID, "%s: %s has type %u (binary32, bfloat16 or binary16 expected)", call, name, h->type);
   if (!h->n_heads || h->n_heads > 65536) return fail(BCP_ERR_INVALID, "%s: %s has %u heads", call, name, h->n_heads);
-  if (h->token_stride < 0 || h->head_stride < 0) return fail(BCP_ERR_INVALID, "%s: %s has a negative stride", call, name);
+  if (h->token_stride < 0 || h->head_stride < 0 || h->token_stride > 0xffffffffll || h->head_stride > 0xffffffffll)
+    return fail(BCP_ERR_INVALID, "%s: %s has a stride that is negative or past 2^32", call, name);
   if (n_tokens && !h->data) return fail(BCP_ERR_INVALID, "%s: %s has no data", call, name);
   if (reinterpret_cast<uintptr_t>(h->data) & (type_size(h->type) - 1)) return fail(BCP_ERR_INVALID, "%s: %s is not aligned to its elements", call, name);
   if (written) {  // the rows of an output must not share memory
@@ -41,16 +42,18 @@ int check_rope(const char* call, const bcp_rope_table* r, uint32_t head_dim) {
 
 namespace {
 
-constexpr int kHeads = 4;  // heads per thread
+// Heads per thread: four share the loads of the table and keep eight 16-byte loads in flight, which a long
+// input needs (16k tokens of 40 heads: 52 us, 56 with two); where that leaves SMs without work, one.
+constexpr uint32_t kManyHeads = 4, kFewThreads = 1024;  // per SM, with a thread for every head
 
 struct RopeArgs {
   const void* in[2];
   void* out[2];
-  int64_t in_token[2], in_head[2], out_token[2], out_head[2];
-  uint32_t n_q, n_heads;  // heads [0, n_q) are q's, [n_q, n_heads) k's
-  uint32_t head_dim, rot_dim, layout;
+  uint32_t in_token[2], in_head[2], out_token[2], out_head[2];
+  uint32_t n_heads[2], q_groups;  // groups of heads: first those of q, then k's
+  uint32_t head_dim, rot_dim;
   float sign;
-  FastDiv per_token, per_group;  // threads per token; per group of kHeads heads
+  FastDiv per_token, per_group;  // threads per token; per group
   uint32_t n_threads;
   const float* table;
   int64_t n_positions;
@@ -58,54 +61,59 @@ struct RopeArgs {
   uint32_t* status;
 };
 
-template <typename T, bool VEC>
-__global__ void __launch_bounds__(256) bcp_rope_kernel(const RopeArgs a) {
+template <typename T, bool VEC, bool PAIRS, int HEADS>
+__global__ void __launch_bounds__(256, 3) bcp_rope_kernel(const RopeArgs a) {
   const uint32_t i = blockIdx.x * 256u + threadIdx.x;
   if (i >= a.n_threads) return;
   const uint32_t t = a.per_token.div(i), r = i - t * a.per_token.d;
   const uint32_t g = a.per_group.div(r);
-  const Chunk k = chunk_at(r - g * a.per_group.d, a.head_dim, a.rot_dim, a.layout);
+  constexpr int V = kChunk<T, VEC>;
+  const Chunk k = chunk_at<V, VEC, PAIRS>(r - g * a.per_group.d, a.head_dim, a.rot_dim);
   const int64_t position = a.positions[t];
   const bool there = position >= 0 && position < a.n_positions;
   if (position >= a.n_positions) raise(a.status, BCP_BAD_POSITION);
 
-  Elements<T, VEC> e[kHeads];
-  T* to[kHeads];
+  const int side = g >= a.q_groups;
+  const uint32_t h0 = (side ? g - a.q_groups : g) * HEADS, n = min(a.n_heads[side] - h0, uint32_t(HEADS));
+  const T* from = static_cast<const T*>(a.in[side]) + (uint64_t(t) * a.in_token[side] + uint64_t(h0) * a.in_head[side]);
+  T* to = static_cast<T*>(a.out[side]) + (uint64_t(t) * a.out_token[side] + uint64_t(h0) * a.out_head[side]);
+  Elements<T, VEC> e[HEADS];
 #pragma unroll
-  for (int j = 0; j < kHeads; ++j) {
-    uint32_t h = g * kHeads + j;
-    const bool used = h < a.n_heads;
-    const int side = h >= a.n_q;
-    h -= side ? a.n_q : 0;
-    to[j] = used ? static_cast<T*>(a.out[side]) + t * a.out_token[side] + h * a.out_head[side] : nullptr;
-    if (used) e[j].load(static_cast<const T*>(a.in[side]) + t * a.in_token[side] + h * a.in_head[side], k);
-  }
-  Angles<VEC> w;
-  if (k.rotated) w.load(a.table, there ? position : 0, a.rot_dim, k);
+  for (int j = 0; j < HEADS; ++j, from += a.in_head[side])
+    if (j < n) e[j].load(from, k);
+  Angles<V, VEC, PAIRS> w;
+  if (k.rotated) w.load(a.table, there ? position : 0, a.rot_dim, k, a.sign);
 #pragma unroll
-  for (int j = 0; j < kHeads; ++j) {
-    if (!to[j]) continue;
+  for (int j = 0; j < HEADS; ++j, to += a.out_head[side]) {
+    if (j >= n) break;
     if (k.rotated || !there) {
-      float x[8], y[8];
-      e[j].unpack(x, y, k);
-      if (k.rotated) w.rotate(x, y, a.sign);
+      float x[V], y[V];
+      e[j].unpack(x, y);
+      if (k.rotated) w.rotate(x, y);
       if (!there) {
 #pragma unroll
-        for (int n = 0; n < 8; ++n) x[n] = y[n] = 0.f;
+        for (int i = 0; i < V; ++i) x[i] = y[i] = 0.f;
       }
-      e[j].pack(x, y, k);
+      e[j].pack(x, y);
     }
-    e[j].store(to[j], k);
+    e[j].store(to, k);
   }
 }
 
-template <typename T>
-void launch(const RopeArgs& a, bool vec, cudaStream_t stream) {
+template <typename T, bool VEC, bool PAIRS>
+void launch(const RopeArgs& a, uint32_t heads, cudaStream_t stream) {
   const uint32_t blocks = (a.n_threads + 255) / 256;
-  if (vec)
-    bcp_rope_kernel<T, true><<<blocks, 256, 0, stream>>>(a);
+  if (heads == 1)
+    bcp_rope_kernel<T, VEC, PAIRS, 1><<<blocks, 256, 0, stream>>>(a);
   else
-    bcp_rope_kernel<T, false><<<blocks, 256, 0, stream>>>(a);
+    bcp_rope_kernel<T, VEC, PAIRS, kManyHeads><<<blocks, 256, 0, stream>>>(a);
+}
+template <typename T>
+void launch(const RopeArgs& a, bool vec, bool pairs, uint32_t heads, cudaStream_t stream) {
+  if (vec && pairs) launch<T, true, true>(a, heads, stream);
+  if (vec && !pairs) launch<T, true, false>(a, heads, stream);
+  if (!vec && pairs) launch<T, false, true>(a, heads, stream);
+  if (!vec && !pairs) launch<T, false, false>(a, heads, stream);
 }
 
 }  // namespace
@@ -132,23 +140,28 @@ extern "C" int bcp_rope(const bcp_heads* q_in, const bcp_heads* q_out, const bcp
   }
   if (n_tokens && !positions) return fail(BCP_ERR_INVALID, "%s: positions is NULL", call);
 
-  RopeArgs a;
+  RopeArgs a = {};
   bool vec = head_dim % 16 == 0 && rope->rot_dim % 16 == 0;
   for (int s = 0; s < 2; ++s) {
-    a.in[s] = in[s]->data, a.in_token[s] = in[s]->token_stride, a.in_head[s] = in[s]->head_stride;
-    a.out[s] = out[s]->data, a.out_token[s] = out[s]->token_stride, a.out_head[s] = out[s]->head_stride;
+    a.in_token[s] = uint32_t(in[s]->token_stride), a.in_head[s] = uint32_t(in[s]->head_stride);
+    a.out_token[s] = uint32_t(out[s]->token_stride), a.out_head[s] = uint32_t(out[s]->head_stride);
     vec = vec && rows_aligned(in[s], 16) && rows_aligned(out[s], 16);
   }
-  a.n_q = q_in->n_heads;
-  a.n_heads = q_in->n_heads + (k_in ? k_in->n_heads : 0);
-  a.head_dim = head_dim, a.rot_dim = rope->rot_dim, a.layout = rope->layout;
+  a.n_heads[0] = q_in->n_heads, a.n_heads[1] = k_in ? k_in->n_heads : 0;
+  a.head_dim = head_dim, a.rot_dim = rope->rot_dim;
   a.sign = transpose ? -1.f : 1.f;
   a.table = rope->table, a.n_positions = rope->n_positions, a.status = rope->status;
-  const uint32_t chunks = chunks_of(head_dim, rope->rot_dim), per_token = chunks * ((a.n_heads + kHeads - 1) / kHeads);
+  int sms = 0, device = 0;
+  BCP_CUDA(cudaGetDevice(&device));
+  BCP_CUDA(cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, device));
+  const uint32_t es = type_size(q_in->type), chunks = chunks_of(head_dim, rope->rot_dim, vec ? 16 / es : 8);
+  const uint64_t all_heads = uint64_t(a.n_heads[0]) + a.n_heads[1];
+  const uint32_t heads = uint64_t(n_tokens) * all_heads * chunks < uint64_t(sms) * kFewThreads ? 1 : kManyHeads;
+  a.q_groups = (a.n_heads[0] + heads - 1) / heads;
+  const uint32_t per_token = chunks * (a.q_groups + (a.n_heads[1] + heads - 1) / heads);
   a.per_group = FastDiv(chunks), a.per_token = FastDiv(per_token);
   // thread indices stay below 2^31: longer inputs take several launches
   const int64_t most = 0x7fffff00 / per_token;
-  const uint32_t es = type_size(q_in->type);
   for (int64_t t0 = 0; t0 < n_tokens; t0 += most) {
     const int64_t n = n_tokens - t0 < most ? n_tokens - t0 : most;
     a.n_threads = uint32_t(n) * per_token;
@@ -158,9 +171,9 @@ extern "C" int bcp_rope(const bcp_heads* q_in, const bcp_heads* q_out, const bcp
       a.out[s] = static_cast<char*>(out[s]->data) + t0 * out[s]->token_stride * es;
     }
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    if (q_in->type == BCP_F32) launch<float>(a, vec, st);
-    if (q_in->type == BCP_BF16) launch<__nv_bfloat16>(a, vec, st);
-    if (q_in->type == BCP_F16) launch<__half>(a, vec, st);
+    if (q_in->type == BCP_F32) launch<float>(a, vec, rope->layout == BCP_ROPE_PAIRS, heads, st);
+    if (q_in->type == BCP_BF16) launch<__nv_bfloat16>(a, vec, rope->layout == BCP_ROPE_PAIRS, heads, st);
+    if (q_in->type == BCP_F16) launch<__half>(a, vec, rope->layout == BCP_ROPE_PAIRS, heads, st);
     BCP_LAUNCHED(call);
   }
   return BCP_OK;
