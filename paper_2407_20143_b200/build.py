@@ -15,6 +15,9 @@ SOURCES = ["planner.cpp", "units.cpp", "api.cu", "plan_image.cu", "host_path.cu"
 HEADERS = ["plan.hpp", "kernels.cuh", "host_threads.hpp", "plan_object.hpp", "tma_ptx.cuh", "copy_loops.cuh", "decode.cuh"]
 
 
+BINDING = os.path.join(CSRC, "binding.cpp")
+
+
 def nvcc_path() -> str:
     for cand in (os.environ.get("NVCC"), shutil.which("nvcc"), "/usr/local/cuda/bin/nvcc"):
         if cand and os.path.exists(cand):
@@ -48,5 +51,40 @@ def build_library(force: bool = False, verbose: bool = False) -> str:
     return LIB
 
 
+def binding_path() -> str:
+    """The module that takes torch tensors: one file per torch and Python version, whose headers it was built with."""
+    import torch
+
+    tag = "".join(c if c.isalnum() else "_" for c in f"{torch.__version__}_py{sys.version_info[0]}{sys.version_info[1]}")
+    return os.path.join(HERE, f"_binding_{tag}.so")
+
+
+def build_binding(force: bool = False) -> str:
+    """Compile csrc/binding.cpp against the installed torch, if there is no newer module; returns its path."""
+    import sysconfig
+
+    import torch
+
+    path = binding_path()
+    if not force and os.path.exists(path) and all(os.path.getmtime(d) <= os.path.getmtime(path) for d in (BINDING, os.path.join(INCLUDE, "bcp.h"))):
+        return path
+    root = os.path.dirname(torch.__file__)
+    cuda = os.path.dirname(os.path.dirname(nvcc_path()))
+    include = [INCLUDE, os.path.join(root, "include"), os.path.join(root, "include", "torch", "csrc", "api", "include"),
+               os.path.join(cuda, "include"), sysconfig.get_paths()["include"]]
+    cmd = [os.environ.get("CXX") or shutil.which("g++") or "c++", "-O2", "-std=c++17", "-fPIC", "-shared", "-fvisibility=hidden", "-w",
+           f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}"]
+    for d in include:
+        cmd += ["-isystem" if d != INCLUDE else "-I", d]
+    partial = f"{path}.{os.getpid()}"
+    cmd += [BINDING, "-o", partial, "-L" + os.path.join(root, "lib"), "-lc10", "-lc10_cuda", "-ltorch_cpu", "-ltorch_python"]
+    r = subprocess.run(cmd, capture_output=True, text=True)
+    if r.returncode != 0:
+        raise RuntimeError("the binding does not compile:\n" + " ".join(cmd) + "\n" + r.stdout + r.stderr)
+    os.replace(partial, path)
+    return path
+
+
 if __name__ == "__main__":
     print(build_library(force=True, verbose="-v" in sys.argv))
+    print(build_binding(force=True))

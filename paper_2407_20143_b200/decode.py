@@ -1,6 +1,6 @@
 """Decoding operators on torch tensors: rotary positions, the paged key-value cache and the attention of
-one new token over it.  The C calls and their formulas are in include/bcp.h; this module checks and
-marshals their arguments.
+one new token over it.  The C calls and their formulas are in include/bcp.h; this module has the handles and
+defaults, csrc/binding.cpp checks the tensors and turns them into the calls' descriptors.
 
     table = RopeTable.build(rope_frequencies(128, base=500000.0), n_positions=8192)
     cache = KvCache.empty(n_pages=1024, n_heads=8, page_size=16, head_dim=128, dtype=torch.float8_e4m3fn)
@@ -18,13 +18,16 @@ Handles keep the tensors they were made from alive.  Nothing here synchronises e
 from __future__ import annotations
 
 import ctypes as C
+import importlib.machinery
+import importlib.util
 import math
-from typing import Optional, Sequence, Tuple
+from typing import Optional, Sequence
 
 import torch
 
 from . import _lib as L
-from .api import ERR_INVALID, ERR_MISMATCH, BcpError, _check
+from . import build as _build
+from .api import ERR_INVALID, BcpError, _check
 
 F32, BF16, F16, E4M3, I8 = 1, 2, 3, 4, 5
 ROPE_HALF, ROPE_PAIRS = 0, 1
@@ -32,18 +35,30 @@ BAD_POSITION, BAD_SLOT, BAD_PAGE, BAD_LENGTH = 1, 2, 4, 8
 MAX_HEAD_DIM = 256
 _LAYOUTS = {"half": ROPE_HALF, "pairs": ROPE_PAIRS}
 
-_TYPES = {torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16}
 _FORMATS = {torch.bfloat16: BF16, torch.float16: F16, torch.float8_e4m3fn: E4M3, torch.int8: I8}
+
+
+def _load_binding():
+    """The module built from csrc/binding.cpp (built now if it is missing or older than its source)."""
+    path = _build.build_binding()
+    loader = importlib.machinery.ExtensionFileLoader(__package__ + "._binding", path)
+    module = importlib.util.module_from_spec(importlib.util.spec_from_file_location(loader.name, path, loader=loader))
+    loader.exec_module(module)
+    calls = ("bcp_rope", "bcp_kv_write", "bcp_kv_read", "bcp_kv_attend", "bcp_last_error")
+    module.bind(BcpError, *(C.cast(getattr(L.lib(), name), C.c_void_p).value for name in calls))
+    return module
+
+
+_b = _load_binding()
 
 
 def _invalid(message: str, code: int = ERR_INVALID) -> BcpError:
     return BcpError(code, message)
 
 
-def _raw_stream(stream, device: int) -> int:
-    if stream is None:
-        return torch._C._cuda_getCurrentRawStream(device)
-    return stream if isinstance(stream, int) else stream.cuda_stream
+def _raw(stream):
+    """What the binding takes: None (the current stream of the tensors' device) or a raw handle."""
+    return stream if stream is None or isinstance(stream, int) else stream.cuda_stream
 
 
 def _empty(like, shape, dtype, stream):
@@ -54,43 +69,9 @@ def _empty(like, shape, dtype, stream):
         return torch.empty(shape, dtype=dtype, device=like.device)
 
 
-def _device(t, name: str) -> int:
-    """Index of the tensor's device, which has to be the current one."""
-    if not t.is_cuda:
-        raise _invalid(f"{name} is not on a CUDA device")
-    d = t.get_device()
-    if d != torch._C._cuda_getDevice():
-        raise _invalid(f"{name} is on cuda:{d}, but cuda:{torch._C._cuda_getDevice()} is the current device")
-    return d
-
-
-def _heads(t, name: str, device: int, tokens: int, dim: int) -> L.HeadsC:
-    if t.dim() != 3:
-        raise _invalid(f"{name} has {t.dim()} dimensions; [tokens, heads, head_dim] expected")
-    n, h, d = t.shape
-    ts, hs, es = t.stride()
-    typ = _TYPES.get(t.dtype)
-    if typ is None:
-        raise _invalid(f"{name} is {t.dtype}; float32, bfloat16 or float16 expected")
-    if t.get_device() != device:
-        raise _invalid(f"{name} is on another device")
-    if n != tokens or d != dim:
-        raise _invalid(f"{name} has shape {tuple(t.shape)}; {tokens} tokens and vectors of {dim} expected", ERR_MISMATCH)
-    if es != 1 and d > 1:
-        raise _invalid(f"the elements of {name}'s vectors are not contiguous")
-    return L.HeadsC(t.data_ptr(), ts, hs, h, typ)
-
-
-def _index(t, name: str, device: int, dtype, shape: Tuple[int, ...]) -> int:
-    if t.dtype != dtype or t.get_device() != device:
-        raise _invalid(f"{name} must be {dtype} on cuda:{device}")
-    if t.shape != shape or not t.is_contiguous():
-        raise _invalid(f"{name} has shape {tuple(t.shape)}; a contiguous {tuple(shape)} expected", ERR_MISMATCH)
-    return t.data_ptr()
-
-
 def _check_status(status, stream) -> None:
-    _check(L.lib().bcp_decode_status(status.data_ptr(), _raw_stream(stream, status.get_device())))
+    handle = _raw(torch.cuda.current_stream(status.device) if stream is None else stream)
+    _check(L.lib().bcp_decode_status(status.data_ptr(), handle))
 
 
 # ------------------------------------------------------------------ rotary positions
@@ -149,39 +130,32 @@ class RopeTable:
         _check_status(self.status, stream)
 
 
-def _rope(xs, table: RopeTable, positions, out, transpose: int, stream):
-    single = isinstance(xs, torch.Tensor)
-    xs = (xs,) if single else tuple(xs)
-    if not 1 <= len(xs) <= 2:
-        raise _invalid(f"{len(xs)} tensors: one, or queries and keys, expected")
-    device = _device(xs[0], "x")
-    if table.device != device:
-        raise _invalid("the table is on another device")
+def _rope(x, table: RopeTable, positions, out, transpose: bool, stream):
+    if isinstance(x, torch.Tensor):
+        if out is None:
+            out = _empty(x, x.shape, x.dtype, stream)
+        elif not isinstance(out, torch.Tensor):
+            out, = out
+        _b.rope(table.address, table.device, x, None, out, None, positions, transpose, _raw(stream))
+        return out
+    if len(x) == 1:
+        return (_rope(x[0], table, positions, out if out is None else out[0], transpose, stream),)
+    q, k = x
     if out is None:
-        outs = tuple(_empty(x, x.shape, x.dtype, stream) for x in xs)
-    else:
-        outs = (out,) if isinstance(out, torch.Tensor) else tuple(out)
-    if len(outs) != len(xs):
-        raise _invalid(f"{len(outs)} outputs for {len(xs)} inputs")
-    if xs[0].dim() != 3:
-        raise _invalid(f"x has {xs[0].dim()} dimensions; [tokens, heads, head_dim] expected")
-    n, _, d = xs[0].shape
-    c = [_heads(t, name, device, n, d) for x, o in zip(xs, outs) for t, name in ((x, "x"), (o, "out"))]
-    where = [C.addressof(h) for h in c] + [None, None]
-    p = _index(positions, "positions", device, torch.int64, (n,))
-    _check(L.lib().bcp_rope(where[0], where[1], where[2], where[3], d, n, table.address, p, transpose, _raw_stream(stream, device)))
-    return outs[0] if single and isinstance(outs[0], torch.Tensor) else outs
+        out = (_empty(q, q.shape, q.dtype, stream), _empty(k, k.shape, k.dtype, stream))
+    _b.rope(table.address, table.device, q, k, out[0], out[1], positions, transpose, _raw(stream))
+    return out
 
 
 def bcp_rope(x, table: RopeTable, positions, out=None, stream=None):
     """x [tokens, heads, head_dim], or a pair (queries, keys), rotated by the tokens' positions (int64 [tokens]; negative:
-    zeros).  `out` may be x itself.  Returns the output, or the tuple of them."""
-    return _rope(x, table, positions, out, 0, stream)
+    zeros).  `out` may be x itself.  Returns the output, or the pair of them."""
+    return _rope(x, table, positions, out, False, stream)
 
 
 def bcp_rope_backward(grad, table: RopeTable, positions, out=None, stream=None):
     """The gradient of bcp_rope: the transposed rotation of the outputs' gradient."""
-    return _rope(grad, table, positions, out, 1, stream)
+    return _rope(grad, table, positions, out, True, stream)
 
 
 class _Rope(torch.autograd.Function):
@@ -189,14 +163,14 @@ class _Rope(torch.autograd.Function):
     def forward(ctx, table, positions, *xs):
         ctx.table = table
         ctx.save_for_backward(positions)
-        return _rope(xs, table, positions, None, 0, None)
+        return _rope(xs, table, positions, None, False, None)
 
     @staticmethod
     def backward(ctx, *grads):
         positions, = ctx.saved_tensors
         # an expanded gradient (of a sum, say) has no contiguous vectors
         grads = [g if g.stride(-1) == 1 else g.contiguous() for g in grads]
-        return (None, None) + tuple(_rope(grads, ctx.table, positions, None, 1, None))
+        return (None, None) + tuple(_rope(grads, ctx.table, positions, None, True, None))
 
 
 def rope(x, table: RopeTable, positions):
@@ -218,9 +192,9 @@ class KvCache:
             raise _invalid(f"a cache of {k.dtype} and {v.dtype}; bfloat16, float16, float8_e4m3fn or int8 expected, the same for both")
         if k.dim() != 4 or v.shape != k.shape or v.stride() != k.stride() or (k.stride(3) != 1 and k.shape[3] > 1):
             raise _invalid("k and v must be [pages, heads, page_size, head_dim] with the same strides and contiguous vectors")
-        device = _device(k, "k")
-        if v.get_device() != device:
-            raise _invalid("v is on another device")
+        if not k.is_cuda or v.get_device() != k.get_device():
+            raise _invalid("k and v must be on one CUDA device")
+        device = k.get_device()
         if (fmt in (E4M3, I8)) != (k_scale is not None) or (k_scale is None) != (v_scale is None):
             raise _invalid("8-bit caches have k_scale and v_scale, the others have none")
         for s, name in ((k_scale, "k_scale"), (v_scale, "v_scale")):
@@ -261,35 +235,20 @@ class KvCache:
 def bcp_kv_write(cache: KvCache, k, v, slots, rope: Optional[RopeTable] = None, positions=None, stream=None) -> None:
     """k, v [tokens, heads, head_dim] into their slots (int64 [tokens]; negative: skipped); with `rope`, the keys are rotated
     by positions (int64 [tokens]) on the way."""
-    device = _device(k, "k")
-    if cache.device != device or (rope is not None and rope.device != device):
-        raise _invalid("the cache or the table is on another device")
-    n = k.shape[0]
-    kc, vc = _heads(k, "k", device, n, cache.head_dim), _heads(v, "v", device, n, cache.head_dim)
-    s = _index(slots, "slots", device, torch.int64, (n,))
-    if (rope is None) != (positions is None):
-        raise _invalid("rope and positions go together")
-    p = _index(positions, "positions", device, torch.int64, (n,)) if rope is not None else None
-    _check(L.lib().bcp_kv_write(cache.address, C.addressof(kc), C.addressof(vc), s, n, rope.address if rope is not None else None, p,
-                                _raw_stream(stream, device)))
+    if rope is None:
+        _b.kv_write(cache.address, cache.device, k, v, slots, None, cache.device, positions, _raw(stream))
+    else:
+        _b.kv_write(cache.address, cache.device, k, v, slots, rope.address, rope.device, positions, _raw(stream))
 
 
 def bcp_kv_read(cache: KvCache, slots, out=None, dtype=None, stream=None):
     """Keys and values [tokens, heads, head_dim] at `slots` (int64 [tokens]; negative: zeros), in `dtype` (default bfloat16, or
     the cache's own 16-bit type) or into out = (k, v)."""
-    device = _device(slots, "slots")
-    if cache.device != device:
-        raise _invalid("the cache is on another device")
-    if slots.dim() != 1:
-        raise _invalid(f"slots has {slots.dim()} dimensions; one expected")
-    n = slots.shape[0]
     if out is None:
         dtype = dtype or (cache.k.dtype if cache.k_scale is None else torch.bfloat16)
-        out = tuple(_empty(slots, (n, cache.n_heads, cache.head_dim), dtype, stream) for _ in range(2))
+        out = tuple(_empty(slots, (slots.numel(), cache.n_heads, cache.head_dim), dtype, stream) for _ in range(2))
     k, v = out
-    kc, vc = _heads(k, "k", device, n, cache.head_dim), _heads(v, "v", device, n, cache.head_dim)
-    s = _index(slots, "slots", device, torch.int64, (n,))
-    _check(L.lib().bcp_kv_read(cache.address, s, n, C.addressof(kc), C.addressof(vc), _raw_stream(stream, device)))
+    _b.kv_read(cache.address, cache.device, slots, k, v, _raw(stream))
     return k, v
 
 
@@ -310,32 +269,14 @@ def bcp_kv_attend(cache: KvCache, q, block_table, lengths, scale: Optional[float
     `window` of them, whose pages are block_table[b] (int32 [sequences, width]).  scale defaults to head_dim^-0.5.
     Returns (out, lse); lse [sequences, query heads] is the natural logarithm of the sum of exponentials, -inf where a
     sequence has no tokens (its output is zeros)."""
-    device = _device(q, "q")
-    if cache.device != device:
-        raise _invalid("the cache is on another device")
-    if q.dim() != 3:
-        raise _invalid(f"q has {q.dim()} dimensions; [sequences, heads, head_dim] expected")
-    n, h, _ = q.shape
     if out is None:
         out = _empty(q, q.shape, q.dtype, stream)
     if lse is None:
-        lse = _empty(q, (n, h), torch.float32, stream)
+        lse = _empty(q, q.shape[:2], torch.float32, stream)
     if workspace is None:
-        workspace = _new_workspace(cache, h, n, stream)
-    elif workspace.device != device:
-        raise _invalid("the workspace is on another device")
-    qc, oc = _heads(q, "q", device, n, cache.head_dim), _heads(out, "out", device, n, cache.head_dim)
-    if block_table.dim() != 2 or block_table.shape[0] != n or block_table.dtype != torch.int32 or block_table.get_device() != device or (
-            block_table.shape[1] > 1 and block_table.stride(1) != 1):
-        raise _invalid(f"block_table must be an int32 tensor [{n}, width] on cuda:{device} with contiguous rows")
-    if window < 0:
-        raise _invalid(f"window {window} is negative")
-    lens = _index(lengths, "lengths", device, torch.int32, (n,))
-    sums = _index(lse, "lse", device, torch.float32, (n, h))
-    width = block_table.shape[1]
-    _check(L.lib().bcp_kv_attend(cache.address, C.addressof(qc), C.addressof(oc), sums, n, block_table.data_ptr(),
-                                 block_table.stride(0) if n > 1 else width, width, lens, cache.head_dim ** -0.5 if scale is None else scale,
-                                 min(window, 0x7fffffff), workspace.address, workspace.bytes, _raw_stream(stream, device)))
+        workspace = _new_workspace(cache, q.shape[1], q.shape[0], stream)
+    _b.kv_attend(cache.address, cache.device, q, out, lse, block_table, lengths, cache.head_dim ** -0.5 if scale is None else scale, window,
+                 workspace.address, workspace.bytes, workspace.device, _raw(stream))
     return out, lse
 
 
