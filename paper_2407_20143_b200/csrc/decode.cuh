@@ -232,6 +232,25 @@ struct Angles {
   }
 };
 
+// Kernels of a decoding step are a few microseconds long, of which the gap between two launches is a good part.
+// They are launched so that their blocks may take their places while the kernel before them on the
+// stream ends (launch_early), and begin with after_previous(): the next kernel may do the same, and
+// nothing is read or written before the one before has completed and its memory is visible.
+__device__ __forceinline__ void after_previous() {
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+}
+template <typename Args>
+cudaError_t launch_early(void (*kernel)(Args), uint32_t blocks, uint32_t threads, uint32_t shared_bytes, cudaStream_t stream, const Args& args) {
+  cudaLaunchAttribute early;
+  early.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  early.val.programmaticStreamSerializationAllowed = 1;
+  cudaLaunchConfig_t config = {};
+  config.gridDim = dim3(blocks), config.blockDim = dim3(threads), config.dynamicSmemBytes = shared_bytes, config.stream = stream;
+  config.attrs = &early, config.numAttrs = 1;
+  return cudaLaunchKernelEx(&config, kernel, args);
+}
+
 __device__ __forceinline__ void raise(uint32_t* status, uint32_t bit) {
   if (status) atomicOr(status, bit);
 }
@@ -251,11 +270,5 @@ inline bool rows_aligned(const bcp_heads* h, uint32_t bytes) {
   const uint64_t es = type_size(h->type);
   return ((reinterpret_cast<uintptr_t>(h->data) | uint64_t(h->token_stride) * es | uint64_t(h->head_stride) * es) & (bytes - 1)) == 0;
 }
-
-#define BCP_LAUNCHED(call)                                                                     \
-  do {                                                                                         \
-    cudaError_t e_ = cudaGetLastError();                                                       \
-    if (e_ != cudaSuccess) return bcp::fail(BCP_ERR_CUDA, "%s: %s", call, cudaGetErrorString(e_)); \
-  } while (0)
 
 }  // namespace bcp

@@ -226,6 +226,7 @@ __global__ void __launch_bounds__(kWarps * 32, Shape<FMT, DP, NT>::CTAS) bcp_kv_
   float* const sum_l = sum_r + kWarps * S::ROWS;                                        // [warp][ROWS] denominators
   uint32_t* const shared_word = reinterpret_cast<uint32_t*>(sum_l + kWarps * S::ROWS);
 
+  after_previous();
   // ---- the line, and this CTA's part of it
   const uint32_t units = a.n_heads * a.row_tiles;
   // every thread counts the steps of a run of sequences; an exclusive scan over the threads
@@ -902,7 +903,6 @@ extern "C" int bcp_kv_attend(const bcp_kv_cache* c, const bcp_heads* q, const bc
   uint32_t longest = a.capacity;
   if (window && window < longest) longest = window + 15 < longest ? window + 15 : longest;
   const uint64_t most = units * (longest / kStep + 1);
-  v.kernel<<<uint32_t(most < ctas ? most : ctas), kWarps * 32, v.smem, static_cast<cudaStream_t>(stream)>>>(a);
-  BCP_LAUNCHED(call);
+  BCP_CUDA(launch_early(v.kernel, uint32_t(most < ctas ? most : ctas), kWarps * 32, v.smem, static_cast<cudaStream_t>(stream), a));
   return BCP_OK;
 }

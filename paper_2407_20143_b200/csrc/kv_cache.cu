@@ -177,6 +177,7 @@ __device__ __forceinline__ float largest(float a, float b, float c) {
 
 template <typename T, int FMT, bool VEC, bool PAIRS>
 __global__ void __launch_bounds__(256, 4) bcp_kv_write_kernel(const CacheArgs a) {
+  after_previous();
   typedef Format<FMT> F;
   typedef typename F::T C;
   const Item it = item_of(a);
@@ -257,6 +258,7 @@ __global__ void __launch_bounds__(256, 4) bcp_kv_write_kernel(const CacheArgs a)
 
 template <typename T, int FMT, bool VEC>
 __global__ void __launch_bounds__(256) bcp_kv_read_kernel(const CacheArgs a) {
+  after_previous();
   typedef Format<FMT> F;
   typedef typename F::T C;
   constexpr int V = VEC ? 16 / int(sizeof(T)) : 8;
@@ -314,23 +316,21 @@ __global__ void __launch_bounds__(256) bcp_kv_read_kernel(const CacheArgs a) {
   }
 }
 
-template <typename T, bool VEC>
-void launch(bool write, const CacheArgs& a, uint32_t format, cudaStream_t stream) {
+template <typename T, int FMT, bool VEC>
+cudaError_t launch(bool write, const CacheArgs& a, cudaStream_t stream) {
   const uint32_t blocks = uint32_t(((uint64_t(a.n_groups) << a.lanes_log2) + 255) / 256);
-#define BCP_ON(F)                                                           \
-  if (format == F) {                                                        \
-    if (write && a.layout == BCP_ROPE_PAIRS)                                \
-      bcp_kv_write_kernel<T, F, VEC, true><<<blocks, 256, 0, stream>>>(a);  \
-    else if (write)                                                         \
-      bcp_kv_write_kernel<T, F, VEC, false><<<blocks, 256, 0, stream>>>(a); \
-    else                                                                    \
-      bcp_kv_read_kernel<T, F, VEC><<<blocks, 256, 0, stream>>>(a);         \
+  void (*kernel)(CacheArgs) = bcp_kv_read_kernel<T, FMT, VEC>;
+  if (write) kernel = a.layout == BCP_ROPE_PAIRS ? bcp_kv_write_kernel<T, FMT, VEC, true> : bcp_kv_write_kernel<T, FMT, VEC, false>;
+  return launch_early(kernel, blocks, 256, 0, stream, a);
+}
+template <typename T>
+cudaError_t launch(bool write, const CacheArgs& a, uint32_t format, bool vec, cudaStream_t stream) {
+  switch (format) {
+    case BCP_BF16: return vec ? launch<T, BCP_BF16, true>(write, a, stream) : launch<T, BCP_BF16, false>(write, a, stream);
+    case BCP_F16: return vec ? launch<T, BCP_F16, true>(write, a, stream) : launch<T, BCP_F16, false>(write, a, stream);
+    case BCP_E4M3: return vec ? launch<T, BCP_E4M3, true>(write, a, stream) : launch<T, BCP_E4M3, false>(write, a, stream);
+    default: return vec ? launch<T, BCP_I8, true>(write, a, stream) : launch<T, BCP_I8, false>(write, a, stream);
   }
-  BCP_ON(BCP_BF16)
-  BCP_ON(BCP_F16)
-  BCP_ON(BCP_E4M3)
-  BCP_ON(BCP_I8)
-#undef BCP_ON
 }
 
 int move(const char* call, bool write, const bcp_kv_cache* c, const bcp_heads* k, const bcp_heads* v, const int64_t* slots, int64_t n_tokens,
@@ -376,18 +376,9 @@ int move(const char* call, bool write, const bcp_kv_cache* c, const bcp_heads* k
     a.positions = positions ? positions + t0 : nullptr;
     a.rows[0] = static_cast<char*>(k->data) + t0 * k->token_stride * es;
     a.rows[1] = static_cast<char*>(v->data) + t0 * v->token_stride * es;
-#define BCP_ON(TYPE, T)                                        \
-  if (k->type == TYPE) {                                       \
-    if (vec)                                                   \
-      launch<T, true>(write, a, c->format, st);                \
-    else                                                       \
-      launch<T, false>(write, a, c->format, st);               \
-  }
-    BCP_ON(BCP_F32, float)
-    BCP_ON(BCP_BF16, __nv_bfloat16)
-    BCP_ON(BCP_F16, __half)
-#undef BCP_ON
-    BCP_LAUNCHED(call);
+    if (k->type == BCP_F32) BCP_CUDA(launch<float>(write, a, c->format, vec, st));
+    if (k->type == BCP_BF16) BCP_CUDA(launch<__nv_bfloat16>(write, a, c->format, vec, st));
+    if (k->type == BCP_F16) BCP_CUDA(launch<__half>(write, a, c->format, vec, st));
   }
   return BCP_OK;
 }

@@ -63,6 +63,7 @@ struct RopeArgs {
 
 template <typename T, bool VEC, bool PAIRS, int HEADS>
 __global__ void __launch_bounds__(256, 3) bcp_rope_kernel(const RopeArgs a) {
+  after_previous();
   const uint32_t i = blockIdx.x * 256u + threadIdx.x;
   if (i >= a.n_threads) return;
   const uint32_t t = a.per_token.div(i), r = i - t * a.per_token.d;
@@ -101,19 +102,13 @@ __global__ void __launch_bounds__(256, 3) bcp_rope_kernel(const RopeArgs a) {
 }
 
 template <typename T, bool VEC, bool PAIRS>
-void launch(const RopeArgs& a, uint32_t heads, cudaStream_t stream) {
-  const uint32_t blocks = (a.n_threads + 255) / 256;
-  if (heads == 1)
-    bcp_rope_kernel<T, VEC, PAIRS, 1><<<blocks, 256, 0, stream>>>(a);
-  else
-    bcp_rope_kernel<T, VEC, PAIRS, kManyHeads><<<blocks, 256, 0, stream>>>(a);
+cudaError_t launch(const RopeArgs& a, uint32_t heads, cudaStream_t stream) {
+  return launch_early(heads == 1 ? bcp_rope_kernel<T, VEC, PAIRS, 1> : bcp_rope_kernel<T, VEC, PAIRS, kManyHeads>, (a.n_threads + 255) / 256, 256, 0, stream, a);
 }
 template <typename T>
-void launch(const RopeArgs& a, bool vec, bool pairs, uint32_t heads, cudaStream_t stream) {
-  if (vec && pairs) launch<T, true, true>(a, heads, stream);
-  if (vec && !pairs) launch<T, true, false>(a, heads, stream);
-  if (!vec && pairs) launch<T, false, true>(a, heads, stream);
-  if (!vec && !pairs) launch<T, false, false>(a, heads, stream);
+cudaError_t launch(const RopeArgs& a, bool vec, bool pairs, uint32_t heads, cudaStream_t stream) {
+  if (vec) return pairs ? launch<T, true, true>(a, heads, stream) : launch<T, true, false>(a, heads, stream);
+  return pairs ? launch<T, false, true>(a, heads, stream) : launch<T, false, false>(a, heads, stream);
 }
 
 }  // namespace
@@ -171,10 +166,10 @@ extern "C" int bcp_rope(const bcp_heads* q_in, const bcp_heads* q_out, const bcp
       a.out[s] = static_cast<char*>(out[s]->data) + t0 * out[s]->token_stride * es;
     }
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    if (q_in->type == BCP_F32) launch<float>(a, vec, rope->layout == BCP_ROPE_PAIRS, heads, st);
-    if (q_in->type == BCP_BF16) launch<__nv_bfloat16>(a, vec, rope->layout == BCP_ROPE_PAIRS, heads, st);
-    if (q_in->type == BCP_F16) launch<__half>(a, vec, rope->layout == BCP_ROPE_PAIRS, heads, st);
-    BCP_LAUNCHED(call);
+    const bool pairs = rope->layout == BCP_ROPE_PAIRS;
+    if (q_in->type == BCP_F32) BCP_CUDA(launch<float>(a, vec, pairs, heads, st));
+    if (q_in->type == BCP_BF16) BCP_CUDA(launch<__nv_bfloat16>(a, vec, pairs, heads, st));
+    if (q_in->type == BCP_F16) BCP_CUDA(launch<__half>(a, vec, pairs, heads, st));
   }
   return BCP_OK;
 }
