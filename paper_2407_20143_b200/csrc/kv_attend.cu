@@ -109,6 +109,16 @@ __device__ __forceinline__ float exp2_fast(float x) {
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
 }
+__device__ __forceinline__ float log2_fast(float x) {
+  float y;
+  asm("lg2.approx.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+__device__ __forceinline__ float reciprocal_fast(float x) {
+  float y;
+  asm("rcp.approx.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
 __device__ __forceinline__ uint32_t transpose8x8(uint32_t x) {
   uint32_t y;
   asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
@@ -459,43 +469,42 @@ __global__ void __launch_bounds__(kWarps * 32, Shape<FMT, DP, NT>::CTAS) bcp_kv_
           }
         }
       }
-      // scores of tokens g and g + 8; 8-bit values: their scale 2^e f goes into the weight, e into its
-      // exponent and f into the factor, so that the weights of the product stay in range whatever the scales
-      float vf[2] = {1.f, 1.f}, ve[2] = {0.f, 0.f}, ks[2] = {1.f, 1.f};
+      // Scores of tokens g and g + 8.  The scale f of 8-bit values goes into the weight as log2 f in its exponent, so
+      // that the weights of the product stay in range whatever the scales; the denominators get weight / f.
+      float vlog[2] = {0.f, 0.f}, vinv[2] = {1.f, 1.f}, ks[2] = {1.f, 1.f};
       if constexpr (S::quant) {
 #pragma unroll
         for (int r = 0; r < 2; ++r) {
           ks[r] = *reinterpret_cast<const float*>(tile + 2 * S::SIDE + (g + 8 * r) * 4);
-          const float x = *reinterpret_cast<const float*>(tile + 2 * S::SIDE + 64 + (g + 8 * r) * 4);
-          const uint32_t v = __float_as_uint(x), e = v >> 23 & 255u;
-          ve[r] = float(int(max(e, 31u)) - 127);  // scales below 2^-96 (a zero, too) keep the exponent of that
-          vf[r] = e < 31 ? x * 0x1p96f : e == 255 ? __uint_as_float(0x7fc00000u) : __uint_as_float((v & 0x807fffffu) | 0x3f800000u);
+          // scales below 2^-96 (a zero, too) count as that; a NaN stays one
+          float f = *reinterpret_cast<const float*>(tile + 2 * S::SIDE + 64 + (g + 8 * r) * 4);
+          if (f < 0x1p-96f) f = 0x1p-96f;
+          vlog[r] = log2_fast(f), vinv[r] = reciprocal_fast(f);
         }
       }
-      bool above = false;
 #pragma unroll
       for (int t = 0; t < NT; ++t)
 #pragma unroll
-        for (int c = 0; c < 4; ++c) s[t][c] = (s[t][c] + s2[t][c]) * (factor[t][c & 1] * ks[c >> 1]);
+        for (int c = 0; c < 4; ++c) s[t][c] = fmaf(s[t][c] + s2[t][c], factor[t][c & 1] * ks[c >> 1], vlog[c >> 1]);
       if (live != 0xffffu) {
 #pragma unroll
         for (int r = 0; r < 2; ++r)
           if (!(live >> (g + 8 * r) & 1)) {
 #pragma unroll
             for (int t = 0; t < NT; ++t) s[t][2 * r] = s[t][2 * r + 1] = -INFINITY;
-            vf[r] = 1.f;
           }
       }
+      bool above = false;
 #pragma unroll
       for (int t = 0; t < NT; ++t)
 #pragma unroll
-        for (int c = 0; c < 4; ++c) above |= s[t][c] + ve[c >> 1] > ref[t][c & 1] + 8.f;
+        for (int c = 0; c < 2; ++c) above |= fmaxf(s[t][c], s[t][c + 2]) > ref[t][c] + 8.f;
       if (__any_sync(0xffffffffu, above)) {
 #pragma unroll
         for (int t = 0; t < NT; ++t)
 #pragma unroll
           for (int c = 0; c < 2; ++c) {
-            float m = fmaxf(s[t][c] + ve[0], s[t][c + 2] + ve[1]);
+            float m = fmaxf(s[t][c], s[t][c + 2]);
             m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 4));
             m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 8));
             m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 16));
@@ -513,14 +522,8 @@ __global__ void __launch_bounds__(kWarps * 32, Shape<FMT, DP, NT>::CTAS) bcp_kv_
         float p[4];
 #pragma unroll
         for (int c = 0; c < 4; ++c) {
-          const float x = s[t][c] - (ref[t][c & 1] - kLift);
-          if constexpr (S::quant) {
-            l[t][c & 1] += exp2_fast(x);
-            p[c] = exp2_fast(x + ve[c >> 1]) * vf[c >> 1];
-          } else {
-            p[c] = exp2_fast(x);
-            l[t][c & 1] += p[c];
-          }
+          p[c] = exp2_fast(s[t][c] - (ref[t][c & 1] - kLift));
+          l[t][c & 1] = S::quant ? fmaf(p[c], vinv[c >> 1], l[t][c & 1]) : l[t][c & 1] + p[c];
         }
         pf[t][0] = transpose8x8(pack16<kBf16>(p[0], p[1]));
         pf[t][1] = transpose8x8(pack16<kBf16>(p[2], p[3]));
