@@ -60,18 +60,19 @@ struct AttendArgs {
 };
 
 constexpr uint32_t kGroup = 64;  // parts that are joined at once
-// The line of n steps is dealt out to the parts as evenly as whole steps allow.
+// The line of n steps is dealt out to the parts as evenly as whole steps allow.  (Fewer than 2^31 steps: the host
+// refuses more.)
 struct Cuts {
-  uint64_t n, each, longer;  // steps of the line, of a part; the first `longer` parts have one more
+  uint32_t n, each, longer;  // steps of the line, of a part; the first `longer` parts have one more
   uint32_t parts;
-  __device__ __forceinline__ void cut(uint64_t steps, uint32_t ctas) {
-    n = steps, parts = uint32_t(n < ctas ? n : ctas);
-    each = n >> 32 ? n / parts : uint32_t(n) / parts, longer = n - each * parts;
+  __device__ __forceinline__ void cut(uint32_t steps, uint32_t ctas) {
+    n = steps, parts = n < ctas ? n : ctas;
+    each = n / parts, longer = n - each * parts;
   }
-  __device__ __forceinline__ uint64_t begin(uint32_t p) const { return each * p + (p < longer ? p : longer); }
-  __device__ __forceinline__ uint32_t part_of(uint64_t x) const {  // the part that step x lies in
-    const uint64_t lower = longer * (each + 1), at = x < lower ? x : x - lower, size = each + (x < lower);
-    return (n >> 32 ? uint32_t(at / size) : uint32_t(at) / uint32_t(size)) + uint32_t(x < lower ? 0 : longer);
+  __device__ __forceinline__ uint32_t begin(uint32_t p) const { return each * p + (p < longer ? p : longer); }
+  __device__ __forceinline__ uint32_t part_of(uint32_t x) const {  // the part that step x lies in
+    const uint32_t lower = longer * (each + 1);
+    return x < lower ? x / (each + 1) : longer + (x - lower) / each;
   }
 };
 
@@ -90,8 +91,8 @@ struct Shape {
   // whose elements cost conversions, gain from warps (int8 windows 46 us with four CTAs, 50 with three).
   static constexpr int CTAS = DP == 64 ? (NT == 1 ? 4 : 3) : DP == 128 ? (!quant ? 2 : NT == 1 ? 4 : 3) : quant ? 2 : 1;
   static constexpr int ROWS = 8 * NT;
-  static constexpr int SMEM = kWarps * STAGES * STAGE + kWarps * 8 * DP * 4 + kWarps * ROWS * 8 + 128;
-  static constexpr int PART = ROWS * (DP + 2);  // floats of one part in the workspace
+  static constexpr int PART = ROWS * (DP + 2);  // floats of one set of sums: dimensions of the heads (sum_at), references, denominators
+  static constexpr int SMEM = kWarps * STAGES * STAGE + kWarps * PART * 4 + 16;
 };
 
 __device__ __forceinline__ void copy16(uint32_t to, const void* from, bool on) {
@@ -168,12 +169,19 @@ __device__ __forceinline__ float query_at(const void* p, int i, bool bf16) {
   return bf16 ? __bfloat162float(static_cast<const __nv_bfloat16*>(p)[i]) : __half2float(static_cast<const __half*>(p)[i]);
 }
 
-// Where dimension d of head (column) n lies in a warp's block of sums: eight rows of dimensions and four
-// pairs of heads are written at a time, the exclusive-or spreads them over the banks.
+// Where dimension d of head (column) n lies in a set of sums: eight rows of dimensions and four pairs of heads
+// are written at a time by a warp, the exclusive-or spreads them over the banks.
 template <int DP, bool QUANT>
 __device__ __forceinline__ uint32_t sum_at(uint32_t n, uint32_t d) {
-  return n * DP + (d ^ (n >> 1) << (QUANT ? 2 : 3));
+  return n * DP + (d ^ (n >> 1 & 3) << (QUANT ? 2 : 3));
 }
+// Sums lie in shared memory or in the workspace, where other CTAs wrote them: generic loads that no cache keeps.
+__device__ __forceinline__ float4 load_sums4(const float* p) {
+  float4 v;
+  asm volatile("ld.volatile.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "l"(p) : "memory");
+  return v;
+}
+__device__ __forceinline__ float load_sums(const float* p) { return *static_cast<const volatile float*>(p); }
 
 // Where 16-byte chunk c of row r lies in a side of a stage.  Keys are read as 16-byte vectors by 8 lanes
 // that hold two rows and four neighbouring chunks, values by 8 lanes with eight rows of one chunk
@@ -231,10 +239,8 @@ __global__ void __launch_bounds__(kWarps * 32, Shape<FMT, DP, NT>::CTAS) bcp_kv_
   const uint32_t tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, q4 = lane & 3;
   const uint32_t ring = uint32_t(__cvta_generic_to_shared(smem)) + warp * (S::STAGES * S::STAGE);
   unsigned char* const ring_ptr = smem + warp * (S::STAGES * S::STAGE);
-  float* const sum_o = reinterpret_cast<float*>(smem + kWarps * S::STAGES * S::STAGE);  // [warp][sum_at]
-  float* const sum_r = sum_o + kWarps * 8 * DP;                                         // [warp][ROWS] references
-  float* const sum_l = sum_r + kWarps * S::ROWS;                                        // [warp][ROWS] denominators
-  uint32_t* const shared_word = reinterpret_cast<uint32_t*>(sum_l + kWarps * S::ROWS);
+  float* const sums = reinterpret_cast<float*>(smem + kWarps * S::STAGES * S::STAGE);  // a part's worth for each warp
+  uint32_t* const shared_word = reinterpret_cast<uint32_t*>(sums + kWarps * S::PART);
 
   after_previous();
   // ---- the line, and this CTA's part of it
@@ -242,21 +248,24 @@ __global__ void __launch_bounds__(kWarps * 32, Shape<FMT, DP, NT>::CTAS) bcp_kv_
   // every thread counts the steps of a run of sequences; an exclusive scan over the threads
   const uint32_t run = (a.n_seqs + kWarps * 32 - 1) / (kWarps * 32);
   const uint32_t run0 = min(tid * run, a.n_seqs), run1 = min(run0 + run, a.n_seqs);
-  uint64_t mine = 0, before;
+  uint32_t mine = 0, before;
   Cuts cuts;
   uint32_t extra;
   {
+#pragma unroll 1
     for (uint32_t b = run0; b < run1; ++b) mine += span_of(a, b, 0).steps;
     before = mine;
+#pragma unroll
     for (uint32_t o = 1; o < 32; o <<= 1) {
-      const uint64_t x = __shfl_up_sync(0xffffffffu, before, o);
+      const uint32_t x = __shfl_up_sync(0xffffffffu, before, o);
       if (lane >= o) before += x;
     }
-    uint64_t* const totals = reinterpret_cast<uint64_t*>(sum_o);
+    uint32_t* const totals = reinterpret_cast<uint32_t*>(sums);
     if (lane == 31) totals[warp] = before;
     __syncthreads();
-    uint64_t all = 0;
+    uint32_t all = 0;
     before -= mine;
+#pragma unroll
     for (uint32_t w = 0; w < kWarps; ++w) {
       if (w < warp) before += totals[w];
       all += totals[w];
@@ -266,21 +275,20 @@ __global__ void __launch_bounds__(kWarps * 32, Shape<FMT, DP, NT>::CTAS) bcp_kv_
     cuts.cut((all + extra * a.n_seqs) * units, gridDim.x);
   }
   if (blockIdx.x >= cuts.parts) return;
-  const uint64_t s0 = cuts.begin(blockIdx.x);
-  const uint32_t n_steps = uint32_t(cuts.begin(blockIdx.x + 1) - s0);
+  const uint32_t s0 = cuts.begin(blockIdx.x), n_steps = cuts.begin(blockIdx.x + 1) - s0;
   Place at;
   {
     // the thread whose run of sequences holds the first step knows where that is
     uint32_t* const found = shared_word;
     if (s0 >= before * units && s0 < (before + mine) * units) {
-      uint64_t pre = before;
-      uint32_t b = run0, steps;
+      uint32_t pre = before, b = run0, steps;
+#pragma unroll 1
       for (;; ++b) {
         steps = span_of(a, b, extra).steps;
         if (s0 < (pre + steps) * units) break;
         pre += steps;
       }
-      const uint32_t r = uint32_t(s0 - pre * units);
+      const uint32_t r = s0 - pre * units;
       found[0] = b, found[1] = r / steps, found[2] = r % steps;
     }
     __syncthreads();
@@ -288,6 +296,7 @@ __global__ void __launch_bounds__(kWarps * 32, Shape<FMT, DP, NT>::CTAS) bcp_kv_
     at.span = span_of(a, at.b, extra);
   }
   if (a.status && blockIdx.x == 0)
+#pragma unroll 1
     for (uint32_t b = run0; b < run1; ++b)
       if (a.lengths[b] > int32_t(a.capacity)) raise(a.status, BCP_BAD_LENGTH);
 
@@ -341,7 +350,7 @@ __global__ void __launch_bounds__(kWarps * 32, Shape<FMT, DP, NT>::CTAS) bcp_kv_
             from += step;
           }
         } else {
-#pragma unroll
+#pragma unroll 2
           for (int i = 0; i < kTok / kRows; ++i) {
             const uint32_t r = i * kRows + l;
             const bool copy = (live >> r & 1) && inside;
@@ -368,6 +377,7 @@ __global__ void __launch_bounds__(kWarps * 32, Shape<FMT, DP, NT>::CTAS) bcp_kv_
   };
   touch_queries();
   look_up();
+#pragma unroll 1
   for (int i = 0; i < S::STAGES - 1; ++i) produce();
 
   uint32_t done = 0, use_stage = 0;
@@ -570,194 +580,144 @@ __global__ void __launch_bounds__(kWarps * 32, Shape<FMT, DP, NT>::CTAS) bcp_kv_
     }
     done += n;
 
-    // ---- the four warps' sums together
-    const bool starts = at.step == 0, ends = at.step + n == at.span.steps;
+    // ---- The end of a stretch: the four warps' sums are added up, and where the unit lies in several parts
+    // those of the parts.  One piece of code does both, and its loops are kept short: it runs a few times per
+    // CTA, and fetching instructions for the first time costs more than executing them.
+    const bool whole = at.step == 0 && at.step + n == at.span.steps;
+    float* const own = sums + warp * S::PART;
 #pragma unroll
     for (int t = 0; t < NT; ++t)
 #pragma unroll
       for (int c = 0; c < 2; ++c) {
+        const uint32_t col = t * 8 + 2 * q4 + c;
         float x = l[t][c];
         x += __shfl_xor_sync(0xffffffffu, x, 4);
         x += __shfl_xor_sync(0xffffffffu, x, 8);
         x += __shfl_xor_sync(0xffffffffu, x, 16);
-        if (g == 0) {
-          sum_r[warp * S::ROWS + t * 8 + 2 * q4 + c] = ref[t][c];
-          sum_l[warp * S::ROWS + t * 8 + 2 * q4 + c] = x;
-        }
-      }
-    __syncthreads();
-    const uint64_t place = s0 + done - n;  // of the stretch's first step on the line
-    float* const part = a.parts + (uint64_t(blockIdx.x) * 2 + (place != s0)) * S::PART;
-    const uint32_t head = tid >> 4, sub = tid & 15;  // in the sums: 16 threads per head, four dimensions at a time
-#pragma unroll
-    for (int t = 0; t < NT; ++t) {
-#pragma unroll
-      for (int c = 0; c < 2; ++c) {
-        const uint32_t col = t * 8 + 2 * q4 + c;
-        float m = sum_r[col];
-#pragma unroll
-        for (int w = 1; w < kWarps; ++w) m = fmaxf(m, sum_r[w * S::ROWS + col]);
-        const float down = exp2_fast(ref[t][c] - m);
-        float* const to = sum_o + warp * 8 * DP;
+        if (g == 0) own[S::ROWS * DP + col] = ref[t][c], own[S::ROWS * (DP + 1) + col] = x;
         if constexpr (S::quant) {  // two blocks of rows hold four neighbouring dimensions
 #pragma unroll
           for (int k = 0; k < DP / 16; k += 2) {
             const uint32_t d = DP >= 128 ? 128 * (k / 8) + 16 * g + 2 * (k % 8) : (DP / 8) * g + 2 * k;
-            *reinterpret_cast<float4*>(to + sum_at<DP, true>(2 * q4 + c, d)) =
-                make_float4(o[t][k][c] * down, o[t][k][c + 2] * down, o[t][k + 1][c] * down, o[t][k + 1][c + 2] * down);
+            *reinterpret_cast<float4*>(own + sum_at<DP, true>(col, d)) = make_float4(o[t][k][c], o[t][k][c + 2], o[t][k + 1][c], o[t][k + 1][c + 2]);
           }
         } else {
 #pragma unroll
           for (int k = 0; k < DP / 16; ++k)
 #pragma unroll
-            for (int r = 0; r < 2; ++r) to[sum_at<DP, false>(2 * q4 + c, 16 * k + 8 * r + g)] = o[t][k][c + 2 * r] * down;
+            for (int r = 0; r < 2; ++r) own[sum_at<DP, false>(col, 16 * k + 8 * r + g)] = o[t][k][c + 2 * r];
         }
       }
-      __syncthreads();
-      const uint32_t col = t * 8 + head;
-      float m = sum_r[col], den = 0.f;
+    __syncthreads();
+    const uint32_t place = s0 + done - n;                                                         // of the stretch's first step on the line
+    float* to = a.parts + (uint64_t(blockIdx.x) * 2 + (place != s0)) * S::PART;                   // where the sums go
+    const float *first = sums, *rest = sums;                                                      // the sums to add: first, rest + i * apart
+    uint64_t apart = S::PART;
+    uint32_t n_sums = kWarps, f = 0, groups = 0, first_place = 0, p0 = 0;
+    bool last = whole;
+#pragma unroll 1
+    for (int round = 0;; ++round) {  // the warps, the parts of a group, the groups
+      // Sixteen threads per head, four dimensions at a time; of each sixteen sums one is this thread's to weigh.
+      const uint32_t sub = tid & 15;
+#pragma unroll 1
+      for (uint32_t col = tid >> 4; col < S::ROWS; col += 8) {
+        const bool on = row0 + col < a.group;
+        float m = kNone, den = 0.f, r[kGroup / 16], w[kGroup / 16];
+        auto from_of = [&](uint32_t i) { return i ? rest + i * apart : first; };
 #pragma unroll
-      for (int w = 1; w < kWarps; ++w) m = fmaxf(m, sum_r[w * S::ROWS + col]);
-#pragma unroll
-      for (int w = 0; w < kWarps; ++w) den += sum_l[w * S::ROWS + col] * exp2_fast(sum_r[w * S::ROWS + col] - m);
-      const bool whole = starts && ends, row_on = row0 + col < a.group;
-      const uint32_t qh = h * a.group + row0 + col;
-#pragma unroll
-      for (int i = 0; i < DP / 64; ++i) {
-        const uint32_t d = 64 * i + 4 * sub;
-        float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll
-        for (int w = 0; w < kWarps; ++w) {
-          const float4 y = *reinterpret_cast<const float4*>(sum_o + w * 8 * DP + sum_at<DP, S::quant>(head, d));
-          x.x += y.x, x.y += y.y, x.z += y.z, x.w += y.w;
+        for (int k = 0; k < int(kGroup / 16); ++k) {
+          r[k] = kNone, w[k] = 0.f;
+          if (sub + 16 * k < n_sums && on) {
+            const float* const from = from_of(sub + 16 * k) + S::ROWS * DP + col;
+            r[k] = load_sums(from), w[k] = load_sums(from + S::ROWS);
+          }
+          m = fmaxf(m, r[k]);
         }
-        if (!whole) {
-          __stcg(reinterpret_cast<float4*>(part + col * DP + d), x);
-        } else if (row_on && d < a.head_dim) {
-          const float inv = den == 0.f ? 0.f : 1.f / den;
+#pragma unroll
+        for (int i = 1; i < 16; i <<= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, i));
+#pragma unroll
+        for (int k = 0; k < int(kGroup / 16); ++k) {
+          const float weight = exp2_fast(r[k] - m);
+          den += w[k] * weight;
+          w[k] = weight;
+        }
+#pragma unroll
+        for (int i = 1; i < 16; i <<= 1) den += __shfl_xor_sync(0xffffffffu, den, i);
+        float4 x[DP / 64];
+#pragma unroll
+        for (int i = 0; i < DP / 64; ++i) x[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 1
+        for (uint32_t i0 = 0; i0 < n_sums; i0 += 4) {
+          const float mine = i0 < 16 ? w[0] : i0 < 32 ? w[1] : i0 < 48 ? w[2] : w[3];
+          float4 y[4][DP / 64];
+          if (on) {
+#pragma unroll
+            for (uint32_t j = 0; j < 4; ++j) {
+              const float* const from = from_of(min(i0 + j, n_sums - 1));
+#pragma unroll
+              for (int i = 0; i < DP / 64; ++i) y[j][i] = load_sums4(from + sum_at<DP, S::quant>(col, 64 * i + 4 * sub));
+            }
+          }
+#pragma unroll
+          for (uint32_t j = 0; j < 4; ++j) {
+            const float weight = __shfl_sync(0xffffffffu, mine, (lane & 16) + (i0 & 15) + j);
+            if (on && i0 + j < n_sums) {
+#pragma unroll
+              for (int i = 0; i < DP / 64; ++i)
+                x[i].x += y[j][i].x * weight, x[i].y += y[j][i].y * weight, x[i].z += y[j][i].z * weight, x[i].w += y[j][i].w * weight;
+            }
+          }
+        }
+        if (!on) continue;
+        if (!last) {  // in the second round over the first part's own sums, which these threads alone have read
+#pragma unroll
+          for (int i = 0; i < DP / 64; ++i) __stcg(reinterpret_cast<float4*>(to + sum_at<DP, S::quant>(col, 64 * i + 4 * sub)), x[i]);
+          if (sub == 0) __stcg(to + S::ROWS * DP + col, m), __stcg(to + S::ROWS * (DP + 1) + col, den);
+          continue;
+        }
+        const uint32_t qh = h * a.group + row0 + col;
+        const float inv = den == 0.f ? 0.f : __fdividef(1.f, den);
+#pragma unroll
+        for (int i = 0; i < DP / 64; ++i) {
+          const uint32_t d = 64 * i + 4 * sub;
+          if (d >= a.head_dim) break;
           uint2 y;
-          y.x = a.q_is_bf16 ? pack16<true>(x.x * inv, x.y * inv) : pack16<false>(x.x * inv, x.y * inv);
-          y.y = a.q_is_bf16 ? pack16<true>(x.z * inv, x.w * inv) : pack16<false>(x.z * inv, x.w * inv);
+          y.x = a.q_is_bf16 ? pack16<true>(x[i].x * inv, x[i].y * inv) : pack16<false>(x[i].x * inv, x[i].y * inv);
+          y.y = a.q_is_bf16 ? pack16<true>(x[i].z * inv, x[i].w * inv) : pack16<false>(x[i].z * inv, x[i].w * inv);
           *reinterpret_cast<uint2*>(static_cast<char*>(a.out) + (at.b * a.out_token + qh * a.out_head + d) * 2) = y;
         }
+        if (sub == 0 && a.lse)
+          a.lse[uint64_t(at.b) * (a.n_heads * a.group) + qh] = den == 0.f ? -INFINITY : (m - kLift + log2_fast(den)) * 0.6931471805599453f;
       }
-      if (sub == 0) {
-        if (!whole) {
-          __stcg(part + S::ROWS * DP + col, m);
-          __stcg(part + S::ROWS * (DP + 1) + col, den);
-        } else if (row_on && a.lse) {
-          a.lse[uint64_t(at.b) * (a.n_heads * a.group) + qh] = den == 0.f ? -INFINITY : (m - kLift + log2f(den)) * 0.6931471805599453f;
-        }
+      if (last) break;
+      // the parts that the unit lies in; the first has it in its second place unless it begins with it
+      if (round == 0) {
+        const uint32_t u0 = place - at.step, p1 = cuts.part_of(u0 + at.span.steps - 1);
+        p0 = cuts.part_of(u0);
+        first_place = 2 * p0 + (cuts.begin(p0) != u0);
+        groups = (p1 - p0) / kGroup + 1;
+        f = p0 + (blockIdx.x - p0) / kGroup * kGroup;
+        n_sums = min(p1 - f + 1, kGroup), apart = 2 * S::PART;
+      } else {
+        f = p0, n_sums = groups, apart = 2 * kGroup * S::PART;
+      }
+      const uint32_t place_of_f = f == p0 ? first_place : 2 * f;
+      uint32_t* const counter = round == 0 ? a.part_count + place_of_f : a.unit_count + (uint64_t(at.b) * units + at.u);
+      // Goes on if this CTA is the last to come to the counter; what the others wrote before is visible then.
+      __threadfence();
+      __syncthreads();
+      if (tid == 0) {
+        const bool complete = atomicAdd(counter, 1u) + 1 == n_sums;
+        *shared_word = complete;
+        if (complete) *counter = 0;  // ready for the next call
       }
       __syncthreads();
+      if (!*static_cast<volatile uint32_t*>(shared_word)) break;
+      __threadfence();
+      last = round == 1 || groups == 1;
+      to = a.parts + uint64_t(place_of_f) * S::PART, first = to, rest = a.parts + uint64_t(2 * f) * S::PART;
     }
-
-    if (!(starts && ends)) {
-      // ---- the unit lies in several parts
-      const uint64_t u0 = place - at.step;
-      const uint32_t p0 = cuts.part_of(u0), p1 = cuts.part_of(u0 + at.span.steps - 1);
-      // the first part has the unit in its second place unless it begins with it
-      const uint32_t first_place = 2 * p0 + (cuts.begin(p0) != u0);
-      auto place_in = [&](uint32_t p) { return p == p0 ? first_place : 2 * p; };
-      // Whether this CTA is the last of n to come to a counter; what the others wrote before is visible then.
-      auto last_of = [&](uint32_t* counter, uint32_t n) {
-        __threadfence();
-        __syncthreads();
-        if (tid == 0) {
-          const bool last = atomicAdd(counter, 1u) + 1 == n;
-          *shared_word = last;
-          if (last) *counter = 0;  // ready for the next call
-        }
-        __syncthreads();
-        const bool last = *shared_word;
-        if (last) __threadfence();
-        return last;
-      };
-      const uint32_t groups = (p1 - p0) / kGroup + 1;
-      uint32_t f = p0 + (blockIdx.x - p0) / kGroup * kGroup, n_sums = min(p1 - f + 1, kGroup), apart = 1;
-      uint32_t* counter = a.part_count + place_in(f);
-      // first the parts of a group, then the groups of the unit, whose sums lie at their first parts
-#pragma unroll 1
-      for (bool last = groups == 1; last_of(counter, n_sums); last = true) {
-        auto from_of = [&](uint32_t i) { return a.parts + uint64_t(place_in(f + apart * i)) * S::PART; };
-#pragma unroll 1
-        for (int t = 0; t < NT; ++t) {
-          const uint32_t col = t * 8 + head, qh = h * a.group + row0 + col;
-          // Sixteen threads per head; of each sixteen sums one is this thread's to weigh.
-          float m = kNone, r[kGroup / 16], w[kGroup / 16], den = 0.f;
-#pragma unroll
-          for (int k = 0; k < int(kGroup / 16); ++k) {
-            const bool mine = sub + 16 * k < n_sums;
-            const float* const from = from_of(mine ? sub + 16 * k : 0);
-            r[k] = __ldcg(from + S::ROWS * DP + col);
-            w[k] = __ldcg(from + S::ROWS * (DP + 1) + col);
-            if (!mine) r[k] = kNone, w[k] = 0.f;
-          }
-          float4 x[DP / 64], y[8][DP / 64];
-          auto load = [&](uint32_t i0) {
-#pragma unroll
-            for (uint32_t j = 0; j < 8; ++j) {
-              const float* const from = from_of(min(i0 + j, n_sums - 1)) + col * DP + 4 * sub;
-#pragma unroll
-              for (int i = 0; i < DP / 64; ++i) y[j][i] = __ldcg(reinterpret_cast<const float4*>(from + 64 * i));
-            }
-          };
-          load(0);  // under way while the weights are found
-#pragma unroll
-          for (int k = 0; k < int(kGroup / 16); ++k) m = fmaxf(m, r[k]);
-#pragma unroll
-          for (int i = 1; i < 16; i <<= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, i));
-#pragma unroll
-          for (int k = 0; k < int(kGroup / 16); ++k) {
-            const float weight = exp2_fast(r[k] - m);
-            den += w[k] * weight;
-            w[k] = weight;
-          }
-#pragma unroll
-          for (int i = 1; i < 16; i <<= 1) den += __shfl_xor_sync(0xffffffffu, den, i);
-#pragma unroll
-          for (int i = 0; i < DP / 64; ++i) x[i] = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 1
-          for (uint32_t i0 = 0;;) {
-            const float mine = i0 < 16 ? w[0] : i0 < 32 ? w[1] : i0 < 48 ? w[2] : w[3];
-#pragma unroll
-            for (uint32_t j = 0; j < 8; ++j) {
-              const float weight = __shfl_sync(0xffffffffu, mine, (lane & 16) + (i0 & 8) + j);
-              if (i0 + j < n_sums) {
-#pragma unroll
-                for (int i = 0; i < DP / 64; ++i)
-                  x[i].x += y[j][i].x * weight, x[i].y += y[j][i].y * weight, x[i].z += y[j][i].z * weight, x[i].w += y[j][i].w * weight;
-              }
-            }
-            i0 += 8;
-            if (i0 >= n_sums) break;
-            load(i0);
-          }
-          if (!last) {  // these threads were the only ones to read this head's sums of the first part
-            float* const to = a.parts + uint64_t(place_in(f)) * S::PART;
-#pragma unroll
-            for (int i = 0; i < DP / 64; ++i) __stcg(reinterpret_cast<float4*>(to + col * DP + 64 * i + 4 * sub), x[i]);
-            if (sub == 0) __stcg(to + S::ROWS * DP + col, m), __stcg(to + S::ROWS * (DP + 1) + col, den);
-          } else if (row0 + col < a.group) {
-            const float inv = den == 0.f ? 0.f : 1.f / den;
-#pragma unroll
-            for (int i = 0; i < DP / 64; ++i) {
-              const uint32_t d = 64 * i + 4 * sub;
-              if (d >= a.head_dim) break;
-              uint2 y;
-              y.x = a.q_is_bf16 ? pack16<true>(x[i].x * inv, x[i].y * inv) : pack16<false>(x[i].x * inv, x[i].y * inv);
-              y.y = a.q_is_bf16 ? pack16<true>(x[i].z * inv, x[i].w * inv) : pack16<false>(x[i].z * inv, x[i].w * inv);
-              *reinterpret_cast<uint2*>(static_cast<char*>(a.out) + (at.b * a.out_token + qh * a.out_head + d) * 2) = y;
-            }
-            if (sub == 0 && a.lse)
-              a.lse[uint64_t(at.b) * (a.n_heads * a.group) + qh] = den == 0.f ? -INFINITY : (m - kLift + log2f(den)) * 0.6931471805599453f;
-          }
-        }
-        if (last) break;
-        f = p0, n_sums = groups, apart = kGroup;
-        counter = a.unit_count + uint64_t(at.b) * units + at.u;
-      }
-    }
+    __syncthreads();  // the sums have been read
     at.step += n - 1;
     advance(at, a, units, extra, done < n_steps);
   }
@@ -902,10 +862,12 @@ extern "C" int bcp_kv_attend(const bcp_kv_cache* c, const bcp_heads* q, const bc
   a.unit_count = reinterpret_cast<uint32_t*>(w);
   a.part_count = reinterpret_cast<uint32_t*>(w + at.part_count);
   a.parts = reinterpret_cast<float*>(w + at.parts);
-  // no more CTAs than the longest lengths the table allows can use
+  // steps are counted in 32 bits, one more for each unit included; no more CTAs than the longest lengths the table
+  // allows can use
   uint32_t longest = a.capacity;
   if (window && window < longest) longest = window + 15 < longest ? window + 15 : longest;
   const uint64_t most = units * (longest / kStep + 1);
+  if (most + units > 0x7fffffffull) return fail(BCP_ERR_CAPACITY, "%s: %u sequences of up to %u tokens are too many for one call", call, n_seqs, longest);
   BCP_CUDA(launch_early(v.kernel, uint32_t(most < ctas ? most : ctas), kWarps * 32, v.smem, static_cast<cudaStream_t>(stream), a));
   return BCP_OK;
 }
