@@ -14,7 +14,7 @@
 // eighth, and its operands would have to be laid out in shared memory first, 8-bit ones converted.)
 //
 // A warp is a worker of its own: it takes 16 tokens at a time through a ring of shared-memory stages that
-// it fills itself with 16-byte asynchronous copies, several stages ahead and across the borders of
+// it fills itself with 16-byte asynchronous copies, a stage or two ahead and across the borders of
 // sequences, so no barrier of the CTA stands in the stream.  The four warps of a CTA take the four quarters
 // of each 64-token step and add up at the end of a stretch of one sequence and cache head.
 //
@@ -24,6 +24,12 @@
 // part is finished there; else every part leaves its sums in the workspace.  Of each 64 parts of a unit the
 // one that comes last (a counter says which) joins them, and of these groups the last again, always in
 // the order of the parts, so results do not depend on which that is.
+//
+// Measured on one B200 (copy bandwidth 6533 GB/s), per launch in a row of them: one sequence of 131,072 tokens, 32 / 8 heads
+// of 128, bfloat16: 93 us = 5.8 TB/s; 64 ragged sequences of up to 4096, e4m3: 72 us = 4.8 TB/s; 37 windows of 1000,
+// 16 / 16 heads, int8: 44 us; one sequence of 600 tokens: 7.8 us, of which the launch, the look-up of the lengths and the
+// page, the first read and the joining of ten parts are most.  With the end-of-stretch work left out the first
+// three take 85, 57 and 33 us: it is what keeps them from the copy bandwidth (DRAM 38 to 67 % busy, tensor pipe 9 to 14 %).
 #include <mutex>
 
 #include "decode.cuh"

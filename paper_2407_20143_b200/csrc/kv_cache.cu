@@ -2,8 +2,12 @@
 //
 // Both are bound by memory: a head vector is read once and written once.  A group of lanes (a power of
 // two) holds one head vector, a chunk a lane, so the largest magnitude that an 8-bit format's scale needs is a
-// few shuffles away and the vector is never read twice.  A group takes four heads of one token, whose loads
+// few shuffles away and the vector is never read twice.  A group takes two heads of one token, whose loads
 // are all in flight before the first one is used.
+// Measured on one B200 (copy bandwidth 6533 GB/s): 65,536 tokens of 8 heads of 128 read back, e4m3 to bfloat16: 62.5 us, 409 MB,
+// 1.0 of it.  32,768 tokens written, bfloat16 to e4m3 with rotation: 48 us, 221 MB, 0.70: 12 instructions an element
+// and two dependent loads (position, row of the table) before it; 64 registers are the least and four CTAs an SM
+// the most that do not spill in the loop (three CTAs: 56 us; four heads a group, 128 registers: 66 us).
 #include "decode.cuh"
 
 using namespace bcp;
@@ -57,7 +61,7 @@ int check_cache(const char* call, const bcp_kv_cache* c) {
 
 namespace {
 
-constexpr int kHeads = 2;            // heads per group of lanes
+constexpr int kHeads = 2;            // heads per group of lanes (reading 64k tokens: 63 us with two or four, 75 with one)
 constexpr float kSmallestScale = 1.262177448353619e-29f;  // 2^-96: its reciprocal and sums of it stay finite
 
 struct CacheArgs {
