@@ -6,7 +6,7 @@ defaults, csrc/binding.cpp checks the tensors and turns them into the calls' des
     cache = KvCache.empty(n_pages=1024, n_heads=8, page_size=16, head_dim=128, dtype=torch.float8_e4m3fn)
     work = KvWorkspace(cache, n_q_heads=32, max_seqs=64)
     slots = cache.slots(block_table, sequences, positions)     # where each new token goes
-    q, = bcp_rope((q,), table, positions)
+    q = bcp_rope(q, table, positions)
     bcp_kv_write(cache, k, v, slots, rope=table, positions=positions)
     out, lse = bcp_kv_attend(cache, q, block_table, lengths, workspace=work)
     cache.check()                                               # raises if an index was out of range
