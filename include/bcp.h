@@ -673,8 +673,9 @@ BCP_API int bcp_kv_read(const bcp_kv_cache* cache, const int64_t* slots, int64_t
  * Tokens whose page is outside the cache (BCP_BAD_PAGE) are left out; a length past table_width * page_size
  * counts as that many (BCP_BAD_LENGTH).
  * workspace: device memory of at least bcp_kv_attend_workspace bytes, 16-byte aligned, whose first use finds
- * it zeroed; every call leaves it ready for the next one.  It serves one call at a time: calls that may
- * overlap on the GPU need a workspace each.
+ * it zeroed; every call leaves it ready for the next one, which may have other shapes if it is large enough for
+ * them.  It serves one call at a time: calls that may overlap on the GPU need a workspace each.  (max_seqs: how
+ * many sequences a call may have; the size does not depend on it at present.)
  */
 BCP_API int bcp_kv_attend_workspace(const bcp_kv_cache* cache, uint32_t n_q_heads, uint32_t max_seqs, uint64_t* bytes);
 BCP_API int bcp_kv_attend(const bcp_kv_cache* cache, const bcp_heads* q, const bcp_heads* out, float* lse, uint32_t n_seqs,

@@ -60,8 +60,8 @@ struct AttendArgs {
   const int32_t* lengths;
   float scale_log2;
   uint32_t window;
-  uint32_t* unit_count;  // one per sequence, cache head and row tile: groups of parts that have arrived
-  uint32_t* part_count;  // two per part: parts that have arrived, at the place of a unit's first part in a group
+  uint32_t* part_count;   // two per part: parts that have arrived, at the place of a unit's first part in a group
+  uint32_t* group_count;  // two per part: groups that have arrived, at the place of the unit's first part
   float* parts;          // two places per part: sums, then references, then denominators
 };
 
@@ -712,7 +712,7 @@ __global__ void __launch_bounds__(kWarps * 32, Shape<FMT, DP, NT>::CTAS) bcp_kv_
         f = p0, n_sums = groups, apart = 2 * kGroup * S::PART;
       }
       const uint32_t place_of_f = f == p0 ? first_place : 2 * f;
-      uint32_t* const counter = round == 0 ? a.part_count + place_of_f : a.unit_count + (uint64_t(at.b) * units + at.u);
+      uint32_t* const counter = round == 0 ? a.part_count + place_of_f : a.group_count + first_place;
       // Goes on if this CTA is the last to come to the counter; what the others wrote before is visible then.
       __threadfence();
       __syncthreads();
@@ -792,17 +792,10 @@ int resident_ctas(const Variant& v, uint32_t* out) {
   return BCP_OK;
 }
 
-// The workspace: counters of the units, counters of the parts, sums of the parts.
-struct Layout {
-  uint64_t part_count, parts, bytes;
-  Layout(uint64_t units, uint32_t ctas, const Variant& v) {
-    auto up = [](uint64_t x) { return (x + 255) & ~uint64_t(255); };
-    const uint64_t places = uint64_t(ctas) * 2;
-    part_count = up(units * 4);
-    parts = up(part_count + places * 4);
-    bytes = parts + places * v.part_floats * 4;
-  }
-};
+// The workspace: counters of the parts, of their groups, then the sums of the parts.  The counters have room for the most
+// parts there can be and lie at fixed places, so that calls of any shapes find them as the last one left them.
+constexpr uint64_t kCounterBytes = uint64_t(kGroup) * kGroup * 2 * 4;
+uint64_t workspace_bytes_of(uint32_t ctas, const Variant& v) { return 2 * kCounterBytes + uint64_t(ctas) * 2 * v.part_floats * 4; }
 
 int check_group(const char* call, const bcp_kv_cache* c, uint32_t n_q_heads) {
   if (!n_q_heads || n_q_heads > 65536 || n_q_heads % c->n_heads)
@@ -821,8 +814,8 @@ extern "C" int bcp_kv_attend_workspace(const bcp_kv_cache* cache, uint32_t n_q_h
   const Variant v = variant_of(cache->format, cache->head_dim, group);
   uint32_t ctas = 0;
   if (int rc = resident_ctas(v, &ctas)) return rc;
-  const uint64_t units = uint64_t(max_seqs) * cache->n_heads * ((group + v.rows - 1) / v.rows);
-  *bytes = Layout(units, ctas, v).bytes;
+  (void)max_seqs;  // the parts are as many as CTAs, however many sequences they come from
+  *bytes = workspace_bytes_of(ctas, v);
   return BCP_OK;
 }
 
@@ -852,10 +845,10 @@ extern "C" int bcp_kv_attend(const bcp_kv_cache* c, const bcp_heads* q, const bc
   AttendArgs a = {};
   a.row_tiles = (group + v.rows - 1) / v.rows;
   const uint64_t units = uint64_t(n_seqs) * c->n_heads * a.row_tiles;
-  const Layout at(units, ctas, v);
+  const uint64_t need = workspace_bytes_of(ctas, v);
   if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 15)) return fail(BCP_ERR_INVALID, "%s: workspace is NULL or not 16-byte aligned", call);
-  if (workspace_bytes < at.bytes)
-    return fail(BCP_ERR_CAPACITY, "%s: a workspace of %llu bytes, %llu needed", call, (unsigned long long)workspace_bytes, (unsigned long long)at.bytes);
+  if (workspace_bytes < need)
+    return fail(BCP_ERR_CAPACITY, "%s: a workspace of %llu bytes, %llu needed", call, (unsigned long long)workspace_bytes, (unsigned long long)need);
   const uint64_t capacity = uint64_t(table_width) * c->page_size;
   a.capacity = uint32_t(capacity < 0x7fffff00u ? capacity : 0x7fffff00u);
   a.k = c->k, a.v = c->v, a.k_scale = c->k_scale, a.v_scale = c->v_scale;
@@ -869,9 +862,9 @@ extern "C" int bcp_kv_attend(const bcp_kv_cache* c, const bcp_heads* q, const bc
   a.block_table = block_table, a.table_stride = table_stride, a.lengths = lengths;
   a.scale_log2 = scale * kLog2e, a.window = window;
   char* const w = static_cast<char*>(workspace);
-  a.unit_count = reinterpret_cast<uint32_t*>(w);
-  a.part_count = reinterpret_cast<uint32_t*>(w + at.part_count);
-  a.parts = reinterpret_cast<float*>(w + at.parts);
+  a.part_count = reinterpret_cast<uint32_t*>(w);
+  a.group_count = reinterpret_cast<uint32_t*>(w + kCounterBytes);
+  a.parts = reinterpret_cast<float*>(w + 2 * kCounterBytes);
   // steps are counted in 32 bits, kExtra more for each unit included; no more CTAs than the longest lengths the table
   // allows can use
   uint32_t longest = a.capacity;

@@ -526,6 +526,26 @@ def test_attend_values_that_are_not_finite(cuda_device, fmt):
         assert not out.any() and bool((lse == -math.inf).all())
 
 
+def test_one_workspace_for_calls_of_different_shapes(cuda_device):
+    # batches of one size after another, another head layout between them: what a call leaves must not disturb the next
+    work, cases = None, []
+    for i, (lengths, heads, group, dim, fmt) in enumerate([([500, 30, 700, 0, 64] * 12, 4, 8, 128, F16), ([9000], 2, 4, 128, F16),
+                                                           ([40000, 5], 1, 16, 128, F16), ([300] * 9, 2, 3, 64, I8)]):
+        table, lens, n_pages = _batch(lengths, 16, 5 + i)
+        cache = _filled(n_pages, heads, 16, dim, fmt, seed=i)
+        q = _randn((len(lengths), heads * group, dim), 9 + i, F16)
+        cases.append((cache, q, table, lens, bcp.bcp_kv_attend(cache, q, table, lens)))
+        w = bcp.KvWorkspace(cache, heads * group, len(lengths))
+        work = w if work is None or w.bytes > work.bytes else work
+    for order in ([0, 1, 2, 3], [3, 0, 2, 1], [1, 0, 3, 2]):
+        for i in order * 2:
+            cache, q, table, lens, (want, want_lse) = cases[i]
+            out, lse = bcp.bcp_kv_attend(cache, q, table, lens, workspace=work)
+            assert torch.equal(out, want) and torch.equal(lse, want_lse)
+            few, _ = bcp.bcp_kv_attend(cache, q[:1], table[:1], lens[:1], workspace=work)
+            assert_attended(few, _, cache, q[:1], table[:1], lens[:1], q.shape[2] ** -0.5, 0)
+
+
 def test_attend_reports_bad_pages_and_lengths(cuda_device):
     table, lens, n_pages = _batch([40, 64], 16, 5)
     cache = _filled(n_pages, 2, 16, 64, BF16)
