@@ -190,8 +190,8 @@ struct Angles {
 #pragma unroll
       for (int i = 0; i < V; ++i) {
         const bool in = uint32_t(i) < k.n_lo;
-        c[i] = in ? __ldg(row + k.pair + i) : 1.f;
-        s[i] = in ? __ldg(row + pairs + k.pair + i) : 0.f;
+        c[i] = in ? row[k.pair + i] : 1.f;
+        s[i] = in ? row[pairs + k.pair + i] : 0.f;
       }
     }
 #pragma unroll
@@ -199,11 +199,11 @@ struct Angles {
   }
   __device__ __forceinline__ void part(const float* pc, const float* ps, uint32_t from, int to) {
     if constexpr (V == 8) {
-      const float4 a = __ldg(reinterpret_cast<const float4*>(pc + from)), b = __ldg(reinterpret_cast<const float4*>(ps + from));
+      const float4 a = *reinterpret_cast<const float4*>(pc + from), b = *reinterpret_cast<const float4*>(ps + from);
       c[to] = a.x, c[to + 1] = a.y, c[to + 2] = a.z, c[to + 3] = a.w;
       s[to] = b.x, s[to + 1] = b.y, s[to + 2] = b.z, s[to + 3] = b.w;
     } else {
-      const float2 a = __ldg(reinterpret_cast<const float2*>(pc + from)), b = __ldg(reinterpret_cast<const float2*>(ps + from));
+      const float2 a = *reinterpret_cast<const float2*>(pc + from), b = *reinterpret_cast<const float2*>(ps + from);
       c[to] = a.x, c[to + 1] = a.y;
       s[to] = b.x, s[to + 1] = b.y;
     }
@@ -235,7 +235,8 @@ struct Angles {
 // Kernels of a decoding step are a few microseconds long, of which the gap between two launches is a good part.
 // They are launched so that their blocks may take their places while the kernel before them on the
 // stream ends (launch_early), and begin with after_previous(): the next kernel may do the same, and
-// nothing is read or written before the one before has completed and its memory is visible.
+// nothing is read or written before the one before has completed and its memory is visible.  (No load takes the
+// read-only path: what one kernel reads may be written while its blocks already wait.)
 __device__ __forceinline__ void after_previous() {
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   asm volatile("griddepcontrol.wait;" ::: "memory");

@@ -321,7 +321,7 @@ __global__ void __launch_bounds__(kWarps * 32, Shape<FMT, DP, NT>::CTAS) bcp_kv_
     if (pos >= ahead.span.first && pos < ahead.span.len) {
       const uint32_t n = a.page_size.div(pos);
       off = pos - n * a.page_size.d;
-      page = __ldg(a.block_table + ahead.b * a.table_stride + n);
+      page = a.block_table[ahead.b * a.table_stride + n];
       if (uint32_t(page) >= a.n_pages) {
         raise(a.status, BCP_BAD_PAGE);
         page = -1;

@@ -285,7 +285,7 @@ __global__ void __launch_bounds__(256) bcp_kv_read_kernel(const CacheArgs a) {
     if (slot >= 0 && it.h0 + j < a.n_heads) {
       raw[j][0].load(from + uint64_t(j) * a.head_stride + lo);
       raw[j][1].load(from + uint64_t(j) * a.head_stride + hi);
-      if (F::quantised) scale[j] = __ldg(a.scales[it.side] + uint64_t(page * a.n_heads + it.h0 + j) * a.page_size.d + off);
+      if (F::quantised) scale[j] = a.scales[it.side][uint64_t(page * a.n_heads + it.h0 + j) * a.page_size.d + off];
     } else {
 #pragma unroll
       for (int i = 0; i < int(sizeof raw[0][0].w / 4); ++i) raw[j][0].w[i] = raw[j][1].w[i] = 0;

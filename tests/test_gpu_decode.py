@@ -651,6 +651,59 @@ def test_streams_and_graphs(cuda_device):
     cache.check()
 
 
+@pytest.mark.parametrize("fmt", [BF16, E4M3, I8])
+def test_calls_in_a_row_see_what_the_ones_before_wrote(cuda_device, fmt):
+    # Steps without any wait between their kernels, on lines of memory that the kernels before have read: tokens
+    # join the pages (and rows of scales) that the last attention went over, a page table and the lengths change in
+    # place.  The same steps with a synchronisation after every call give the reference.
+    n, heads, group, dim, page, steps = 5, 2, 4, 64, 16, 60
+    table0, lens0, n_pages = _batch([20 + steps] * n, page, 5)
+    rot = bcp.RopeTable.build(bcp.rope_frequencies(dim), 128)
+    work_of = lambda c: bcp.KvWorkspace(c, heads * group, n)  # noqa: E731
+    q, k, v = (_randn((steps, n, h, dim), i, BF16 if fmt == BF16 else F16) for i, h in ((1, heads * group), (2, heads), (3, heads)))
+    positions = (torch.arange(steps, device="cuda")[:, None] + 20).expand(steps, n).contiguous()
+    rows = torch.arange(n, device="cuda")
+
+    def run(wait):
+        cache = _filled(n_pages, heads, page, dim, fmt)
+        work, table, lens = work_of(cache), table0.clone(), lens0.clone()
+        slots = [cache.slots(table0, rows, positions[s]) for s in range(steps)]
+        tables = [table0.clone() for _ in range(steps)]
+        for s in range(steps):
+            tables[s][:, 0] = tables[s][:, 0].roll(s)  # sequences exchange their first pages
+        lengths = [(positions[s] + 1).int() for s in range(steps)]
+        outs = [torch.empty_like(q[0]) for _ in range(steps)]
+        sums = [torch.empty((n, heads * group), device="cuda") for _ in range(steps)]
+        back = [(torch.empty((n, heads, dim), dtype=F32, device="cuda"), torch.empty((n, heads, dim), dtype=F32, device="cuda")) for _ in range(steps)]
+        turned = torch.empty_like(q[0])
+        torch.cuda.synchronize()
+        sync = torch.cuda.synchronize if wait else (lambda: None)
+        for s in range(steps):
+            bcp.bcp_rope(q[s], rot, positions[s], out=turned)
+            sync()
+            bcp.bcp_kv_write(cache, k[s], v[s], slots[s], rope=rot, positions=positions[s])
+            sync()
+            bcp.bcp_kv_read(cache, slots[s], out=back[s])
+            sync()
+            table.copy_(tables[s])
+            lens.copy_(lengths[s])
+            sync()
+            bcp.bcp_kv_attend(cache, turned, table, lens, out=outs[s], lse=sums[s], workspace=work)
+            sync()
+            bcp.bcp_kv_attend(cache, turned, tables[s], lengths[s], out=outs[s], lse=sums[s], workspace=work)
+            sync()
+        torch.cuda.synchronize()
+        cache.check()
+        return outs, sums, back
+
+    want = run(True)
+    for _ in range(4):
+        got = run(False)
+        for w, x in zip(want[:2], got[:2]):
+            assert all(torch.equal(a, b) for a, b in zip(w, x))
+        assert all(torch.equal(a, b) for w, x in zip(want[2], got[2]) for a, b in zip(w, x))
+
+
 def test_two_streams_with_a_workspace_each(cuda_device):
     table, lens, n_pages = _batch([2000, 64, 700], 16, 5)
     cache = _filled(n_pages, 2, 16, 128, BF16)
