@@ -76,7 +76,13 @@ struct Cuts {
   uint32_t n, each, longer;  // steps of the line, of a part; the first `longer` parts have one more
   uint32_t parts;
   __device__ __forceinline__ void cut(uint32_t steps, uint32_t ctas) {
+    // A line of a few steps per CTA is cut into parts of whole, equal numbers of them: the longest part decides, and
+    // fewer parts are joined sooner (one sequence of 4000 tokens 14.1 -> 12.9 us, of 3000 13.8 -> 12.4).
     n = steps, parts = n < ctas ? n : ctas;
+    if (n > ctas && n < 4 * ctas) {
+      const uint32_t most = (n + ctas - 1) / ctas;
+      parts = (n + most - 1) / most;
+    }
     each = n / parts, longer = n - each * parts;
   }
   __device__ __forceinline__ uint32_t begin(uint32_t p) const { return each * p + (p < longer ? p : longer); }
