@@ -26,8 +26,8 @@
 // the order of the parts, so results do not depend on which that is.
 //
 // Measured on one B200 (copy bandwidth 6533 GB/s), per launch in a row of them: one sequence of 131,072 tokens, 32 / 8 heads
-// of 128, bfloat16: 93 us = 5.8 TB/s; 64 ragged sequences of up to 4096, e4m3: 72 us = 4.8 TB/s; 37 windows of 1000,
-// 16 / 16 heads, int8: 44 us; one sequence of 600 tokens: 7.8 us, of which the launch, the look-up of the lengths and the
+// of 128, bfloat16: 94 us = 5.7 TB/s; 64 ragged sequences of up to 4096, e4m3: 70 us = 5.0 TB/s; 37 windows of 1000,
+// 16 / 16 heads, int8: 43 us; one sequence of 600 tokens: 7.8 us, of which the launch, the look-up of the lengths and the
 // page, the first read and the joining of ten parts are most.  With the end-of-stretch work left out the first
 // three take 85, 57 and 33 us: it is what keeps them from the copy bandwidth (DRAM 38 to 67 % busy, tensor pipe 9 to 14 %).
 #include <mutex>
