@@ -160,24 +160,26 @@ def bcp_rope_backward(grad, table: RopeTable, positions, out=None, stream=None):
 
 class _Rope(torch.autograd.Function):
     @staticmethod
-    def forward(ctx, table, positions, *xs):
-        ctx.table = table
+    def forward(ctx, table, positions, transpose, *xs):
+        ctx.table, ctx.transpose = table, transpose
         ctx.save_for_backward(positions)
-        return _rope(xs, table, positions, None, False, None)
+        return _rope(xs, table, positions, None, transpose, None)
 
     @staticmethod
     def backward(ctx, *grads):
         positions, = ctx.saved_tensors
         # an expanded gradient (of a sum, say) has no contiguous vectors
         grads = [g if g.stride(-1) == 1 else g.contiguous() for g in grads]
-        return (None, None) + tuple(_rope(grads, ctx.table, positions, None, True, None))
+        # the gradient of a linear map is its transpose: through this function again, so that it has gradients itself
+        return (None, None, None) + _Rope.apply(ctx.table, positions, not ctx.transpose, *grads)
 
 
 def rope(x, table: RopeTable, positions):
-    """bcp_rope as a differentiable function of x (a tensor, or a pair) on the current stream."""
+    """bcp_rope as a differentiable function of x (a tensor, or a pair) on the current stream; its gradients are differentiable
+    too."""
     if isinstance(x, torch.Tensor):
-        return _Rope.apply(table, positions, x)[0]
-    return _Rope.apply(table, positions, *x)
+        return _Rope.apply(table, positions, False, x)[0]
+    return _Rope.apply(table, positions, False, *x)
 
 
 # ------------------------------------------------------------------ cache

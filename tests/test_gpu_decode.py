@@ -143,6 +143,28 @@ def test_rope_gradient(cuda_device, layout):
     assert_rotated(z.grad, torch.ones_like(w), table.table, positions, layout, transposed=True)
 
 
+@pytest.mark.parametrize("layout", ["half", "pairs"])
+def test_rope_gradient_of_a_gradient(cuda_device, layout):
+    t, h, dim, rot = 7, 3, 48, 32
+    table = bcp.RopeTable.build(bcp.rope_frequencies(rot), 50, layout=layout, attention_factor=1.3)
+    positions = torch.randint(0, 50, (t,), generator=_gen(1), device="cuda")
+    x, w = _randn((t, h, dim), 2).requires_grad_(), _randn((t, h, dim), 4)
+    first = (bcp.rope(x, table, positions) ** 2 * w).sum()
+    g, = torch.autograd.grad(first, x, create_graph=True)
+    (first + (g ** 2).sum()).backward()
+    # J = 2 R^T w R is symmetric: the gradient is J x + 2 J J x
+    turn = lambda v, back=False: rotate64(v, table.table, positions, layout, back)  # noqa: E731
+    w64 = w.double().cpu()
+    through = lambda v: 2 * turn(w64 * turn(v)[0], True)[0]  # noqa: E731
+    want = through(x.detach()) + 2 * through(through(x.detach()))
+    # Every rotation rounds its terms (4 in binary32, of the sums of magnitudes that it adds), the products in between once or twice:
+    # 24 roundings along the longest way, of the same chain in magnitudes.
+    size = lambda v: 2 * 1.3 ** 2 * turn(w64.abs() * turn(v)[1])[1]  # noqa: E731
+    s1 = size(x.detach())
+    tol = 24 * F32_EPS * (s1 + 2 * size(s1))
+    assert bool(((x.grad.double().cpu() - want).abs() <= tol).all())
+
+
 def test_rope_long_positions_keep_their_angle(cuda_device):
     # 64-bit angles: at position 200,000 a binary32 product of position and frequency is off by up to 0.01
     f = bcp.rope_frequencies(64, base=500000.0, scaling="bands", factor=8.0, trained=8192)
