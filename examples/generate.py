@@ -69,8 +69,7 @@ class Decoder:
 
     def step(self, tokens, positions):
         """Logits (float32) after one more token for every sequence; a position of -1: the sequence has not begun."""
-        begun = positions >= 0
-        slots = torch.where(begun, self.caches[0].slots(self.block_table, self.rows, positions.clamp_min(0)), -1)
+        slots = self.caches[0].slots(self.block_table, self.rows, positions)
         lengths = (positions + 1).int()
         n = tokens.shape[0]
         x = self.w["embed_tokens.weight"][tokens]
@@ -79,7 +78,7 @@ class Decoder:
             qkv = (norm(x, self.w[p + "input_norm.weight"]) @ self.w[p + "attn.qkv.weight"].T).view(n, Q_HEADS + 2 * KV_HEADS, HEAD_DIM)
             q, k, v = qkv.split([Q_HEADS, KV_HEADS, KV_HEADS], 1)
             bcp.bcp_rope(q, self.rope, positions, out=q)
-            bcp.bcp_kv_write(cache, k, v, slots, rope=self.rope, positions=positions.clamp_min(0))
+            bcp.bcp_kv_write(cache, k, v, slots, rope=self.rope, positions=positions)
             out, _ = bcp.bcp_kv_attend(cache, q, self.block_table, lengths, workspace=self.work)
             x = x + out.view(n, HIDDEN) @ self.w[p + "attn.o.weight"].T
             gate, up = (norm(x, self.w[p + "post_norm.weight"]) @ self.w[p + "mlp.gate_up.weight"].T).split(FFN, -1)

@@ -225,9 +225,21 @@ class KvCache:
         return cls(k, v)
 
     def slots(self, block_table, sequences, positions):
-        """Slots (int64) of tokens at `positions` of `sequences` (rows of block_table), all on the device."""
+        """Slots (int64) of tokens at `positions` of `sequences` (rows of block_table), all on the device.  -1, which the calls
+        skip, for a negative position and where the table's page is negative; a slot past the cache, which they skip and
+        report, for a position past the table's width or a sequence that is no row of it."""
+        past = self.n_pages * self.page_size
         page = torch.div(positions, self.page_size, rounding_mode="floor")
-        return block_table[sequences, page].long() * self.page_size + (positions - page * self.page_size)
+        bad = page >= block_table.shape[1]
+        if not isinstance(sequences, int):
+            sequences = torch.as_tensor(sequences, device=block_table.device)
+            bad = bad | (sequences < 0) | (sequences >= block_table.shape[0])
+            sequences = sequences.clamp(0, max(0, block_table.shape[0] - 1))
+        if block_table.numel() == 0:  # nothing to look up
+            return torch.where(positions < 0, -1, torch.full_like(bad, past, dtype=torch.int64))
+        first = block_table[sequences, page.clamp(0, block_table.shape[1] - 1)].long() * self.page_size
+        slot = torch.where(bad, past, torch.where(first < 0, -1, first + (positions - page * self.page_size)))
+        return torch.where(positions < 0, -1, slot)
 
     def check(self, stream=None) -> None:
         """Waits for `stream`; raises BcpError (ERR_BOUNDS) if a call met a slot, page, length or position out of range."""

@@ -162,3 +162,38 @@ def test_the_host_only_calls_do_not_import_torch():
     root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
     r = subprocess.run([sys.executable, "-c", code_], capture_output=True, text=True, cwd=root, timeout=120)
     assert r.returncode == 0 and r.stdout.strip() == "ok", r.stderr
+
+
+def slots(table, sequences, positions, n_pages=12, page_size=16):
+    from types import SimpleNamespace
+
+    import torch
+
+    from paper_2407_20143_b200 import decode
+
+    row = lambda x: x if isinstance(x, int) else torch.tensor(x, dtype=torch.int64)  # noqa: E731
+    got = decode.KvCache.slots(SimpleNamespace(n_pages=n_pages, page_size=page_size), torch.tensor(table, dtype=torch.int32), row(sequences), row(positions))
+    assert got.dtype == torch.int64
+    return got.tolist()
+
+
+def test_slots_of_tokens():
+    table = [[5, 9], [3, -1]]
+    assert slots(table, [0, 0, 0, 1, 1], [0, 15, 16, 7, 15]) == [80, 95, 144, 55, 63]
+    assert slots(table, 1, [0, 3]) == [48, 51]  # one row for all
+    assert slots(table, [0, 0], [6, 7], page_size=7) == [41, 63]
+
+
+def test_slots_of_padding_are_skipped():
+    # position -1 marks padding everywhere else; it must not become the last slot of the last page
+    assert slots([[5, 9]], [0, 0, 0], [-1, -16, -(1 << 40)]) == [-1, -1, -1]
+    # a page that the table does not have yet
+    assert slots([[5, -1], [-7, 2]], [0, 1, 1], [17, 15, 16]) == [-1, -1, 32]
+
+
+def test_slots_past_the_table_are_past_the_cache():
+    # so that the write or read reports them (a plain index past the table's end would stop the whole GPU context)
+    assert slots([[5, 9], [5, -1]], [0, 1, 0], [32, 32, 1 << 40]) == [12 * 16] * 3
+    assert slots([[5, 9]], [1, -1, 0], [0, 0, 0]) == [12 * 16, 12 * 16, 80]
+    assert slots([[5, 9]], [1, 7], [-1, -1]) == [-1, -1]
+    assert slots([[]], [0, 0], [0, -1]) == [12 * 16, -1]

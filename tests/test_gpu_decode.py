@@ -340,6 +340,26 @@ def test_slots_out_of_the_cache(cuda_device):
         cache.check()
 
 
+def test_slots_of_padding_and_of_positions_past_the_table(cuda_device):
+    cache = _cache(4, 2, 5, 32, BF16)
+    table = torch.tensor([[2, 0], [3, -1]], dtype=torch.int32, device="cuda")
+    rows = torch.tensor([0, 0, 0, 1, 1, 0], device="cuda")
+    positions = torch.tensor([0, 9, -1, 4, 5, -7], device="cuda")
+    k = _randn((6, 2, 32), 1, BF16)
+    slots = cache.slots(table, rows, positions)
+    assert slots.tolist() == [10, 4, -1, 19, -1, -1]
+    bcp.bcp_kv_write(cache, k, k, slots)
+    cache.check()  # padding is no error
+    assert int((~cache.k.isnan()).sum()) == 3 * 2 * 32
+    rk, _ = bcp.bcp_kv_read(cache, slots)
+    assert torch.equal(rk[[0, 1, 3]], k[[0, 1, 3]]) and not rk[[2, 4, 5]].any()
+    past = cache.slots(table, torch.tensor([0, 2], device="cuda"), torch.tensor([10, 0], device="cuda"))
+    bcp.bcp_kv_write(cache, k[:2], k[:2], past)
+    with pytest.raises(bcp.BcpError, match="slot"):
+        cache.check()
+    assert int((~cache.k.isnan()).sum()) == 3 * 2 * 32
+
+
 @pytest.mark.parametrize("shift", [0, 1])
 def test_write_and_read_strided(cuda_device, shift):
     t, h, dim = 9, 5, 48
