@@ -606,7 +606,7 @@ typedef struct {
  * place: slot = page * page_size + offset.
  * format BCP_BF16 / BCP_F16: elements are stored as they are.  BCP_E4M3 (no infinities, largest 448) and
  * BCP_I8 (-127..127): every head vector has a binary32 scale, k_scale[(page*n_heads + h)*page_size + offset],
- * and stands for element * scale (scales are not negative; a zero is taken for 2^-96 by bcp_kv_attend).
+ * and stands for element * scale (scales are not negative; bcp_kv_attend takes those below 2^-96, zero included, for 2^-96).
  */
 typedef struct {
   void* k;               /* 16-byte aligned */

@@ -136,6 +136,14 @@ __device__ __forceinline__ float reciprocal_fast(float x) {
   asm("rcp.approx.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
 }
+// 2^x, x <= 0, for sums whose reference moves by x.  With scales in the exponents (WIDE) a reference can lie up to 2^247 above what
+// still counts in a denominator: that is multiplied in two steps, neither of which underflows.
+template <bool WIDE>
+struct Factor {
+  float root, all;
+  __device__ __forceinline__ explicit Factor(float x) : root(exp2_fast(WIDE ? 0.5f * x : x)), all(WIDE ? root * root : root) {}
+  __device__ __forceinline__ float denominator(float l) const { return WIDE ? l * root * root : l * root; }
+};
 __device__ __forceinline__ uint32_t transpose8x8(uint32_t x) {
   uint32_t y;
   asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
@@ -495,9 +503,11 @@ __global__ void __launch_bounds__(kWarps * 32, Shape<FMT, DP, NT>::CTAS) bcp_kv_
           }
         }
       }
-      // Scores of tokens g and g + 8.  The scale f of 8-bit values goes into the weight as log2 f in its exponent, so
-      // that the weights of the product stay in range whatever the scales; the denominators get weight / f.
-      float vlog[2] = {0.f, 0.f}, vinv[2] = {1.f, 1.f}, ks[2] = {1.f, 1.f};
+      // Scores of tokens g and g + 8.  The scale f of 8-bit values goes into the weight of the product as log2 f in its
+      // exponent, so that these weights stay in range whatever the scales; the reference is the largest of these exponents.
+      // The denominators get exp2(score - reference) without f: from the weight it could not be had back, for next to a scale
+      // of 2^40 the weight of a vector of zeros (f = 2^-96) underflows, though its score may be the largest.
+      float vlog[2] = {0.f, 0.f}, ks[2] = {1.f, 1.f};
       if constexpr (S::quant) {
 #pragma unroll
         for (int r = 0; r < 2; ++r) {
@@ -505,7 +515,7 @@ __global__ void __launch_bounds__(kWarps * 32, Shape<FMT, DP, NT>::CTAS) bcp_kv_
           // scales below 2^-96 (a zero, too) count as that; a NaN stays one
           float f = *reinterpret_cast<const float*>(tile + 2 * S::SIDE + 64 + (g + 8 * r) * 4);
           if (f < 0x1p-96f) f = 0x1p-96f;
-          vlog[r] = log2_fast(f), vinv[r] = reciprocal_fast(f);
+          vlog[r] = log2_fast(f);
         }
       }
 #pragma unroll
@@ -535,11 +545,11 @@ __global__ void __launch_bounds__(kWarps * 32, Shape<FMT, DP, NT>::CTAS) bcp_kv_
             m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 8));
             m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 16));
             m = fmaxf(m, ref[t][c]);
-            const float down = exp2_fast(ref[t][c] - m);
+            const Factor<S::quant> down(ref[t][c] - m);
             ref[t][c] = m;
-            l[t][c] *= down;
+            l[t][c] = down.denominator(l[t][c]);
 #pragma unroll
-            for (int k = 0; k < DP / 16; ++k) o[t][k][c] *= down, o[t][k][c + 2] *= down;
+            for (int k = 0; k < DP / 16; ++k) o[t][k][c] *= down.all, o[t][k][c + 2] *= down.all;
           }
       }
       uint32_t pf[NT][2];
@@ -548,8 +558,9 @@ __global__ void __launch_bounds__(kWarps * 32, Shape<FMT, DP, NT>::CTAS) bcp_kv_
         float p[4];
 #pragma unroll
         for (int c = 0; c < 4; ++c) {
-          p[c] = exp2_fast(s[t][c] - (ref[t][c & 1] - kLift));
-          l[t][c & 1] = S::quant ? fmaf(p[c], vinv[c >> 1], l[t][c & 1]) : l[t][c & 1] + p[c];
+          const float e = s[t][c] - (ref[t][c & 1] - kLift);
+          p[c] = exp2_fast(e);
+          l[t][c & 1] += S::quant ? exp2_fast(e - vlog[c >> 1]) : p[c];
         }
         pf[t][0] = transpose8x8(pack16<kBf16>(p[0], p[1]));
         pf[t][1] = transpose8x8(pack16<kBf16>(p[2], p[3]));
@@ -653,9 +664,9 @@ __global__ void __launch_bounds__(kWarps * 32, Shape<FMT, DP, NT>::CTAS) bcp_kv_
         for (int i = 1; i < 16; i <<= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, i));
 #pragma unroll
         for (int k = 0; k < int(kGroup / 16); ++k) {
-          const float weight = exp2_fast(r[k] - m);
-          den += w[k] * weight;
-          w[k] = weight;
+          const Factor<S::quant> down(r[k] - m);
+          den += down.denominator(w[k]);
+          w[k] = down.all;
         }
 #pragma unroll
         for (int i = 1; i < 16; i <<= 1) den += __shfl_xor_sync(0xffffffffu, den, i);
@@ -692,7 +703,7 @@ __global__ void __launch_bounds__(kWarps * 32, Shape<FMT, DP, NT>::CTAS) bcp_kv_
           continue;
         }
         const uint32_t qh = h * a.group + row0 + col;
-        const float inv = den == 0.f ? 0.f : __fdividef(1.f, den);
+        const float inv = den == 0.f ? 0.f : reciprocal_fast(den);  // up to 2^127, where the fast division gives zero
 #pragma unroll
         for (int i = 0; i < DP / 64; ++i) {
           const uint32_t d = 64 * i + 4 * sub;

@@ -544,6 +544,25 @@ def test_attend_scales_far_apart(cuda_device, fmt):
         assert_attended(out, lse, cache, q, table, lens, 1.0, 0)
 
 
+@pytest.mark.parametrize("fmt", [E4M3, I8])
+@pytest.mark.parametrize("top", [2.0 ** 45, 2.0 ** 100, 3.0e38])
+@pytest.mark.parametrize("n,zeros", [(1 + 16, [0]), (60, [5, 20, 59]), (3000, list(range(10))), (3000, list(range(2990, 3000))), (20000, [11000])])
+def test_attend_vectors_of_zeros_that_dominate(cuda_device, fmt, top, n, zeros):
+    # Tokens whose values are zero (scale 2^-96) have the largest scores by far, the others' values are near the largest numbers:
+    # what the zeros weigh has to stay in the denominator, whichever come first and whichever part of the sequence they are in.
+    dim, page = 64, 16
+    cache = _cache(-(-n // page), 1, page, dim, fmt)
+    k, v = _randn((n, 1, dim), 1) * 0.1, _randn((n, 1, dim), 2).clamp(-3, 3) * (top / 3)
+    k[zeros, 0, 0], v[zeros] = 30.0, 0.0
+    bcp.bcp_kv_write(cache, k, v, torch.arange(n, device="cuda"))
+    table = torch.arange(-(-n // page), dtype=torch.int32, device="cuda")[None]
+    lens = torch.tensor([n], dtype=torch.int32, device="cuda")
+    q = _randn((1, 4, dim), 3, BF16) * 0.1
+    q[0, :, 0] = torch.tensor([1.0, 0.5, 0.0, -1.0])
+    out, lse = bcp.bcp_kv_attend(cache, q, table, lens, scale=1.0)
+    assert_attended(out, lse, cache, q, table, lens, 1.0, 0)
+
+
 @pytest.mark.parametrize("fmt", [F16, E4M3])
 def test_attend_values_that_are_not_finite(cuda_device, fmt):
     table, lens, n_pages = _batch([40, 40], 16, 5)
