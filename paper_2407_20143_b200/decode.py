@@ -13,7 +13,10 @@ defaults, csrc/binding.cpp checks the tensors and turns them into the calls' des
 
 Head vectors are tensors [tokens, heads, head_dim] with any strides over tokens and heads.  `stream` is a torch
 stream, a raw handle, or None for the current stream of the tensors' device; that device must be current.
-Handles keep the tensors they were made from alive.  Nothing here synchronises except check().
+Handles keep the tensors they were made from alive, and a call with a `stream` records its tensors on it, so that torch's
+allocator does not hand out their memory before the work is done.  The order of work on different streams is the caller's:
+what another stream writes (a new handle's status word is zeroed on the stream that is current then) must be done before `stream`
+reads it.  Nothing here synchronises except check().
 """
 from __future__ import annotations
 
@@ -61,12 +64,24 @@ def _raw(stream):
     return stream if stream is None or isinstance(stream, int) else stream.cuda_stream
 
 
+def _torch_stream(stream, device):
+    return torch.cuda.ExternalStream(stream, device=device) if isinstance(stream, int) else stream
+
+
 def _empty(like, shape, dtype, stream):
     """Memory for an output that work on `stream` fills: taken from that stream's pool, so that it is not reused too early."""
     if stream is None:
         return torch.empty(shape, dtype=dtype, device=like.device)
-    with torch.cuda.stream(torch.cuda.ExternalStream(stream, device=like.device) if isinstance(stream, int) else stream):
+    with torch.cuda.stream(_torch_stream(stream, like.device)):
         return torch.empty(shape, dtype=dtype, device=like.device)
+
+
+def _record(stream, *tensors) -> None:
+    """Memory of `tensors`, which may belong to other streams, is not reused before the work now on `stream` is done."""
+    s = _torch_stream(stream, tensors[0].device)
+    for t in tensors:
+        if t is not None:
+            t.record_stream(s)
 
 
 def _check_status(status, stream) -> None:
@@ -114,6 +129,7 @@ class RopeTable:
             raise _invalid("a rotation table is a contiguous float32 CUDA tensor [positions, 2, rot_dim / 2]")
         self.table, self.layout, self.device = table, layout, table.get_device()
         self.status = torch.zeros(1, dtype=torch.int32, device=table.device)
+        self.tensors = (table, self.status)
         self.c = L.RopeTableC(table.data_ptr(), table.shape[0], 2 * table.shape[2], _LAYOUTS[layout], self.status.data_ptr())
         self.address = C.addressof(self.c)
 
@@ -137,6 +153,8 @@ def _rope(x, table: RopeTable, positions, out, transpose: bool, stream):
         elif not isinstance(out, torch.Tensor):
             out, = out
         _b.rope(table.address, table.device, x, None, out, None, positions, transpose, _raw(stream))
+        if stream is not None:
+            _record(stream, x, out, positions, *table.tensors)
         return out
     if len(x) == 1:
         return (_rope(x[0], table, positions, out if out is None else out[0], transpose, stream),)
@@ -144,6 +162,8 @@ def _rope(x, table: RopeTable, positions, out, transpose: bool, stream):
     if out is None:
         out = (_empty(q, q.shape, q.dtype, stream), _empty(k, k.shape, k.dtype, stream))
     _b.rope(table.address, table.device, q, k, out[0], out[1], positions, transpose, _raw(stream))
+    if stream is not None:
+        _record(stream, q, k, *out, positions, *table.tensors)
     return out
 
 
@@ -205,6 +225,7 @@ class KvCache:
         self.k, self.v, self.k_scale, self.v_scale, self.device = k, v, k_scale, v_scale, device
         self.n_pages, self.n_heads, self.page_size, self.head_dim = k.shape
         self.status = torch.zeros(1, dtype=torch.int32, device=k.device)
+        self.tensors = (k, v, k_scale, v_scale, self.status)
         # a dimension of one element may carry any stride: what the kernels get is that of a dense tensor
         strides, dense = [], self.head_dim
         for i in (2, 1, 0):
@@ -253,6 +274,8 @@ def bcp_kv_write(cache: KvCache, k, v, slots, rope: Optional[RopeTable] = None, 
         _b.kv_write(cache.address, cache.device, k, v, slots, None, cache.device, positions, _raw(stream))
     else:
         _b.kv_write(cache.address, cache.device, k, v, slots, rope.address, rope.device, positions, _raw(stream))
+    if stream is not None:
+        _record(stream, k, v, slots, positions, *cache.tensors, *(() if rope is None else rope.tensors))
 
 
 def bcp_kv_read(cache: KvCache, slots, out=None, dtype=None, stream=None):
@@ -263,17 +286,21 @@ def bcp_kv_read(cache: KvCache, slots, out=None, dtype=None, stream=None):
         out = tuple(_empty(slots, (slots.numel(), cache.n_heads, cache.head_dim), dtype, stream) for _ in range(2))
     k, v = out
     _b.kv_read(cache.address, cache.device, slots, k, v, _raw(stream))
+    if stream is not None:
+        _record(stream, slots, k, v, *cache.tensors)
     return k, v
 
 
 class KvWorkspace:
-    """Scratch memory of bcp_kv_attend for up to max_seqs sequences.  It serves one call at a time: calls that may overlap
-    on the GPU (other streams without ordering) need a workspace each."""
+    """Scratch memory of bcp_kv_attend for up to max_seqs sequences, zeroed on `stream`: a first use on another stream has to
+    be ordered behind that.  It serves one call at a time: calls that may overlap on the GPU (other streams without
+    ordering) need a workspace each."""
 
-    def __init__(self, cache: KvCache, n_q_heads: int, max_seqs: int):
+    def __init__(self, cache: KvCache, n_q_heads: int, max_seqs: int, stream=None):
         n = C.c_uint64()
         _check(L.lib().bcp_kv_attend_workspace(cache.address, n_q_heads, max_seqs, C.byref(n)))
-        self.memory = torch.zeros(n.value, dtype=torch.uint8, device=cache.k.device)
+        with torch.cuda.stream(_torch_stream(stream, cache.k.device)):  # None: the current one
+            self.memory = torch.zeros(n.value, dtype=torch.uint8, device=cache.k.device)
         self.address, self.bytes, self.device = self.memory.data_ptr(), n.value, cache.device
 
 
@@ -288,15 +315,10 @@ def bcp_kv_attend(cache: KvCache, q, block_table, lengths, scale: Optional[float
     if lse is None:
         lse = _empty(q, q.shape[:2], torch.float32, stream)
     if workspace is None:
-        workspace = _new_workspace(cache, q.shape[1], q.shape[0], stream)
+        workspace = KvWorkspace(cache, q.shape[1], q.shape[0], stream)
     _b.kv_attend(cache.address, cache.device, q, out, lse, block_table, lengths, cache.head_dim ** -0.5 if scale is None else scale, window,
                  workspace.address, workspace.bytes, workspace.device, _raw(stream))
+    if stream is not None:
+        _record(stream, q, out, lse, block_table, lengths, workspace.memory, *cache.tensors)
     return out, lse
 
-
-def _new_workspace(cache: KvCache, n_q_heads: int, max_seqs: int, stream) -> KvWorkspace:
-    """A workspace zeroed on the stream that will use it."""
-    if stream is None:
-        return KvWorkspace(cache, n_q_heads, max_seqs)
-    with torch.cuda.stream(torch.cuda.ExternalStream(stream, device=cache.k.device) if isinstance(stream, int) else stream):
-        return KvWorkspace(cache, n_q_heads, max_seqs)

@@ -781,6 +781,64 @@ def test_two_streams_with_a_workspace_each(cuda_device):
     assert all(torch.equal(x, want) for o in outs for x in o)
 
 
+@pytest.mark.parametrize("raw", [False, True])
+@pytest.mark.parametrize("call", ["rope", "rope_pair", "write", "write_rotated", "read", "attend"])
+def test_inputs_of_another_stream_are_not_reused_too_early(cuda_device, call, raw):
+    # Tensors that the current stream owns are handed to work on a stream that is still busy, and dropped: their memory must not be
+    # given to new tensors of the current stream before that work is done.
+    side = torch.cuda.Stream()
+    stream = side.cuda_stream if raw else side
+    table, lens, n_pages = _batch([300, 64, 7], 16, 5)
+    cache = _filled(n_pages, 2, 16, 64, E4M3)
+    rot = bcp.RopeTable.build(bcp.rope_frequencies(64), 512)
+    work = bcp.KvWorkspace(cache, 8, 3)
+    row = lambda i, h=2: _randn((3, h, 64), i, BF16)  # noqa: E731
+    index = lambda: torch.tensor([1, 20, 3], device="cuda")  # noqa: E731
+    given = {"rope": lambda: [row(1), index()], "rope_pair": lambda: [row(1, 8), row(2), index()], "write": lambda: [row(1), row(2), index()],
+             "write_rotated": lambda: [row(1), row(2), index(), index()], "read": lambda: [index(), row(1), row(2)],
+             "attend": lambda: [row(1, 8), row(2, 8), table.clone(), lens.clone(), torch.empty((3, 8), device="cuda")]}[call]
+    made = given()
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        torch.cuda._sleep(200_000_000)  # a tenth of a second
+    if call == "rope":
+        bcp.bcp_rope(made[0], rot, made[1], stream=stream)
+    elif call == "rope_pair":
+        bcp.bcp_rope(made[:2], rot, made[2], out=made[:2], stream=stream)
+    elif call == "write":
+        bcp.bcp_kv_write(cache, *made, stream=stream)
+    elif call == "write_rotated":
+        bcp.bcp_kv_write(cache, made[0], made[1], made[2], rope=rot, positions=made[3], stream=stream)
+    elif call == "read":
+        bcp.bcp_kv_read(cache, made[0], out=(made[1], made[2]), stream=stream)
+    else:
+        bcp.bcp_kv_attend(cache, made[0], made[2], made[3], out=made[1], lse=made[4], workspace=work, stream=stream)
+    was = {x.data_ptr() for x in made}
+    del made
+    again = given()
+    busy = not side.query()
+    side.synchronize()
+    assert busy and not was & {x.data_ptr() for x in again}
+
+
+def test_workspace_zeroed_on_the_stream_that_uses_it(cuda_device):
+    table, lens, n_pages = _batch([2000, 64, 700], 16, 5)
+    cache = _filled(n_pages, 2, 16, 128, BF16)
+    q = _randn((3, 8, 128), 9, BF16)
+    want, _ = bcp.bcp_kv_attend(cache, q, table, lens)
+    side = torch.cuda.Stream()
+    for stream in (side, side.cuda_stream):
+        with torch.cuda.stream(side):
+            junk = torch.full((bcp.KvWorkspace(cache, 8, 3).bytes,), 255, dtype=torch.uint8, device="cuda")  # what the memory may hold
+        torch.cuda.synchronize()
+        del junk
+        torch.cuda._sleep(200_000_000)  # zeroes on this stream would come too late
+        got, _ = bcp.bcp_kv_attend(cache, q, table, lens, workspace=bcp.KvWorkspace(cache, 8, 3, stream=stream), stream=stream)
+        side.synchronize()
+        assert torch.equal(got, want)
+        torch.cuda.synchronize()
+
+
 def test_python_refusals(cuda_device):
     cache = _cache(3, 2, 16, 64, E4M3)
     rot = bcp.RopeTable.build(bcp.rope_frequencies(64), 32)
