@@ -683,8 +683,8 @@ BCP_API int bcp_kv_attend(const bcp_kv_cache* cache, const bcp_heads* q, const b
                           float scale, uint32_t window, void* workspace, uint64_t workspace_bytes, void* stream);
 
 /*
- * Waits for `stream`, reads the status word of a table or cache, sets it back to zero, and returns BCP_OK or
- * BCP_ERR_BOUNDS with a message that names the bits.
+ * Waits for `stream`, reads the status word of a table or cache, clears the bits it read (others that work on another
+ * stream sets meanwhile stay for the next call), and returns BCP_OK or BCP_ERR_BOUNDS with a message that names the bits.
  */
 BCP_API int bcp_decode_status(uint32_t* status, void* stream);
 

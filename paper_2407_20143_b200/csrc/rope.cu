@@ -103,6 +103,8 @@ __global__ void __launch_bounds__(256, 3) bcp_rope_kernel(const RopeArgs a) {
   }
 }
 
+__global__ void bcp_clear_kernel(uint32_t* status, uint32_t bits) { atomicAnd(status, ~bits); }
+
 template <typename T, bool VEC, bool PAIRS>
 cudaError_t launch(const RopeArgs& a, uint32_t heads, cudaStream_t stream) {
   return launch_early(heads == 1 ? bcp_rope_kernel<T, VEC, PAIRS, 1> : bcp_rope_kernel<T, VEC, PAIRS, kManyHeads>, (a.n_threads + 255) / 256, 256, 0, stream, a);
@@ -182,7 +184,10 @@ extern "C" int bcp_decode_status(uint32_t* status, void* stream_) {
   uint32_t bits = 0;
   cudaError_t e = cudaMemcpyAsync(&bits, status, sizeof bits, cudaMemcpyDeviceToHost, stream);
   if (e == cudaSuccess) e = cudaStreamSynchronize(stream);
-  if (e == cudaSuccess && bits) e = cudaMemsetAsync(status, 0, sizeof bits, stream);
+  if (e == cudaSuccess && bits) {  // only what was read: another stream may have set more since
+    bcp_clear_kernel<<<1, 1, 0, stream>>>(status, bits);
+    e = cudaGetLastError();
+  }
   if (e != cudaSuccess) return fail(BCP_ERR_CUDA, "bcp_decode_status: %s", cudaGetErrorString(e));
   if (!bits) return BCP_OK;
   return fail(BCP_ERR_BOUNDS, "an index was outside its range and was left out:%s%s%s%s", bits & BCP_BAD_POSITION ? " position" : "",

@@ -839,6 +839,35 @@ def test_workspace_zeroed_on_the_stream_that_uses_it(cuda_device):
         torch.cuda.synchronize()
 
 
+def test_status_keeps_bits_that_are_set_while_it_is_read(cuda_device):
+    # a bad slot on one stream, a bad page on another, somewhere around the moment in which the status is read and cleared
+    table, lens, n_pages = _batch([40], 16, 5)
+    cache = _filled(n_pages, 2, 16, 64, BF16)
+    table[0, 1] = n_pages
+    x, slots = _randn((1, 2, 64), 1, BF16), torch.tensor([n_pages * 16], device="cuda")
+    q, out, lse = _randn((1, 4, 64), 9, BF16), torch.empty((1, 4, 64), dtype=BF16, device="cuda"), torch.empty((1, 4), device="cuda")
+    work, side = bcp.KvWorkspace(cache, 4, 1), torch.cuda.Stream()
+    torch.cuda.synchronize()
+
+    def read():
+        try:
+            cache.check()
+        except bcp.BcpError as e:
+            return str(e)
+        return ""
+
+    for i in range(500):
+        with torch.cuda.stream(side):
+            torch.cuda._sleep(1 + 211 * i % 120_000)  # up to some 60 us
+        bcp.bcp_kv_attend(cache, q, table, lens, out=out, lse=lse, workspace=work, stream=side.cuda_stream)
+        bcp.bcp_kv_write(cache, x, x, slots)
+        seen = read()
+        torch.cuda.synchronize()
+        seen += read()
+        assert "slot" in seen and "page" in seen, (i, seen)
+    assert read() == ""
+
+
 def test_python_refusals(cuda_device):
     cache = _cache(3, 2, 16, 64, E4M3)
     rot = bcp.RopeTable.build(bcp.rope_frequencies(64), 32)
