@@ -7,6 +7,7 @@
 #include <Python.h>
 
 #include <ATen/core/Tensor.h>
+#include <c10/core/GradMode.h>
 #include <c10/cuda/CUDAFunctions.h>
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/autograd/python_variable.h>
@@ -71,10 +72,29 @@ bool device_of(PyObject* o, const char* name, int* device) {
 
 bool on_device(const at::Tensor& t, int device) { return t.is_cuda() && t.get_device() == device; }
 
+// The calls leave no trace in autograd's graph: a result without history would end a gradient without a word.
+bool no_gradient(const at::Tensor& t, const char* name) {
+  if (!t.requires_grad() || !c10::GradMode::is_enabled()) return true;
+  raise(BCP_ERR_INVALID, "%s requires a gradient, which this call does not record (rope() does): detach it, or call under torch.no_grad()", name);
+  return false;
+}
+
+// Counts a write, so that autograd notices where the values from before are still wanted.
+void written(PyObject* o) {
+  const at::Tensor& t = THPVariable_Unpack(o);
+  if (!t.is_inference()) t.unsafeGetTensorImpl()->bump_version();
+}
+template <typename... Tensors>
+PyObject* result_in(int rc, Tensors... outputs) {
+  if (rc == BCP_OK) (written(outputs), ...);
+  return result(rc);
+}
+
 bool heads(PyObject* o, const char* name, int device, int64_t tokens, int64_t dim, bcp_heads* h) {
   const at::Tensor* p = tensor(o, name);
   if (!p) return false;
   const at::Tensor& t = *p;
+  if (!no_gradient(t, name)) return false;
   if (t.dim() != 3) {
     raise(BCP_ERR_INVALID, "%s has %d dimensions; [tokens, heads, head_dim] expected", name, int(t.dim()));
     return false;
@@ -118,6 +138,7 @@ void* index(PyObject* o, const char* name, int device, at::ScalarType type, int6
   const at::Tensor* p = tensor(o, name);
   if (!p) return nullptr;
   const at::Tensor& t = *p;
+  if (!no_gradient(t, name)) return nullptr;
   if (t.scalar_type() != type || !on_device(t, device)) {
     raise(BCP_ERR_INVALID, "%s must be %s on cuda:%d", name, c10::toString(type), device);
     return nullptr;
@@ -169,14 +190,15 @@ PyObject* py_rope(PyObject*, PyObject* const* a, Py_ssize_t n) {
   void* const positions = index(a[6], "positions", device, at::kLong, tokens);
   void* stream;
   if (!positions || !stream_of(a[8], device, &stream)) return nullptr;
-  return result(g_rope(&h[0], &h[1], two ? &h[2] : nullptr, two ? &h[3] : nullptr, uint32_t(dim), tokens,
+  const int rc = g_rope(&h[0], &h[1], two ? &h[2] : nullptr, two ? &h[3] : nullptr, uint32_t(dim), tokens,
                        static_cast<const bcp_rope_table*>(PyLong_AsVoidPtr(a[0])), static_cast<const int64_t*>(positions),
-                       a[7] == Py_True, stream));
+                       a[7] == Py_True, stream);
+  return two ? result_in(rc, a[4], a[5]) : result_in(rc, a[4]);
 }
 
-// kv_write(cache, cache device, k, v, slots, table or None, table device, positions or None, stream)
+// kv_write(cache, cache device, k, v, slots, table or None, table device, positions or None, stream, the cache's keys, its values)
 PyObject* py_kv_write(PyObject*, PyObject* const* a, Py_ssize_t n) {
-  if (!arguments(n, 9)) return nullptr;
+  if (!arguments(n, 11)) return nullptr;
   const bcp_kv_cache* cache = static_cast<const bcp_kv_cache*>(PyLong_AsVoidPtr(a[0]));
   int device;
   if (!device_of(a[2], "k", &device) || !same_device(device, a[1], "the cache")) return nullptr;
@@ -191,8 +213,9 @@ PyObject* py_kv_write(PyObject*, PyObject* const* a, Py_ssize_t n) {
   void* const positions = slots && turn ? index(a[7], "positions", device, at::kLong, tokens) : nullptr;
   void* stream;
   if (!slots || (turn && !positions) || !stream_of(a[8], device, &stream)) return nullptr;
-  return result(g_write(cache, &k, &v, static_cast<const int64_t*>(slots), tokens,
-                        turn ? static_cast<const bcp_rope_table*>(PyLong_AsVoidPtr(a[5])) : nullptr, static_cast<const int64_t*>(positions), stream));
+  return result_in(g_write(cache, &k, &v, static_cast<const int64_t*>(slots), tokens,
+                           turn ? static_cast<const bcp_rope_table*>(PyLong_AsVoidPtr(a[5])) : nullptr, static_cast<const int64_t*>(positions), stream),
+                   a[9], a[10]);
 }
 
 // kv_read(cache, cache device, slots, k, v, stream)
@@ -209,7 +232,7 @@ PyObject* py_kv_read(PyObject*, PyObject* const* a, Py_ssize_t n) {
   if (!slots || !heads(a[3], "k", device, tokens, cache->head_dim, &k) || !heads(a[4], "v", device, tokens, cache->head_dim, &v) ||
       !stream_of(a[5], device, &stream))
     return nullptr;
-  return result(g_read(cache, static_cast<const int64_t*>(slots), tokens, &k, &v, stream));
+  return result_in(g_read(cache, static_cast<const int64_t*>(slots), tokens, &k, &v, stream), a[3], a[4]);
 }
 
 // kv_attend(cache, cache device, q, out, lse, block_table, lengths, scale, window, workspace, its bytes, its device, stream)
@@ -239,10 +262,11 @@ PyObject* py_kv_attend(PyObject*, PyObject* const* a, Py_ssize_t n) {
   void* stream;
   if (!stream_of(a[12], device, &stream)) return nullptr;
   static int32_t no_pages[1];  // a table without columns is not read
-  return result(g_attend(cache, &q, &out, static_cast<float*>(lse), uint32_t(seqs),
-                         table->numel() ? static_cast<const int32_t*>(table->data_ptr()) : no_pages, seqs > 1 ? table->stride(0) : table->size(1),
-                         uint32_t(table->size(1)), static_cast<const int32_t*>(lengths), float(scale),
-                         uint32_t(window > 0x7fffffff ? 0x7fffffff : window), PyLong_AsVoidPtr(a[9]), bytes, stream));
+  return result_in(g_attend(cache, &q, &out, static_cast<float*>(lse), uint32_t(seqs),
+                            table->numel() ? static_cast<const int32_t*>(table->data_ptr()) : no_pages, seqs > 1 ? table->stride(0) : table->size(1),
+                            uint32_t(table->size(1)), static_cast<const int32_t*>(lengths), float(scale),
+                            uint32_t(window > 0x7fffffff ? 0x7fffffff : window), PyLong_AsVoidPtr(a[9]), bytes, stream),
+                   a[3], a[4]);
 }
 
 // bind(BcpError, addresses of bcp_rope, bcp_kv_write, bcp_kv_read, bcp_kv_attend, bcp_last_error)

@@ -11,6 +11,7 @@ defaults, csrc/binding.cpp checks the tensors and turns them into the calls' des
     out, lse = bcp_kv_attend(cache, q, block_table, lengths, workspace=work)
     cache.check()                                               # raises if an index was out of range
 
+rope() is differentiable; the bcp_ calls record no gradients and refuse tensors that require one (outside torch.no_grad()).
 Head vectors are tensors [tokens, heads, head_dim] with any strides over tokens and heads.  `stream` is a torch
 stream, a raw handle, or None for the current stream of the tensors' device; that device must be current.
 Handles keep the tensors they were made from alive, and a call with a `stream` records its tensors on it, so that torch's
@@ -271,9 +272,9 @@ def bcp_kv_write(cache: KvCache, k, v, slots, rope: Optional[RopeTable] = None, 
     """k, v [tokens, heads, head_dim] into their slots (int64 [tokens]; negative: skipped); with `rope`, the keys are rotated
     by positions (int64 [tokens]) on the way."""
     if rope is None:
-        _b.kv_write(cache.address, cache.device, k, v, slots, None, cache.device, positions, _raw(stream))
+        _b.kv_write(cache.address, cache.device, k, v, slots, None, cache.device, positions, _raw(stream), cache.k, cache.v)
     else:
-        _b.kv_write(cache.address, cache.device, k, v, slots, rope.address, rope.device, positions, _raw(stream))
+        _b.kv_write(cache.address, cache.device, k, v, slots, rope.address, rope.device, positions, _raw(stream), cache.k, cache.v)
     if stream is not None:
         _record(stream, k, v, slots, positions, *cache.tensors, *(() if rope is None else rope.tensors))
 

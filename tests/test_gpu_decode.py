@@ -868,6 +868,65 @@ def test_status_keeps_bits_that_are_set_while_it_is_read(cuda_device):
     assert read() == ""
 
 
+def test_tensors_that_require_gradients(cuda_device):
+    cache = _cache(3, 2, 16, 64, BF16)
+    rot = bcp.RopeTable.build(bcp.rope_frequencies(64), 32)
+    x, slots = _randn((4, 2, 64), 1, BF16), torch.arange(4, device="cuda")
+    g = x.clone().requires_grad_()
+    lens, table = torch.ones(4, dtype=torch.int32, device="cuda"), torch.zeros((4, 3), dtype=torch.int32, device="cuda")
+    calls = [
+        lambda a: bcp.bcp_rope(a, rot, slots),
+        lambda a: bcp.bcp_rope((x, a), rot, slots)[1],
+        lambda a: bcp.bcp_rope_backward(a, rot, slots),
+        lambda a: bcp.bcp_rope(x, rot, slots, out=a * 1),
+        lambda a: bcp.bcp_kv_write(cache, a, x, slots),
+        lambda a: bcp.bcp_kv_write(cache, x, a, slots, rope=rot, positions=slots),
+        lambda a: bcp.bcp_kv_read(cache, slots, out=(x.clone(), a * 1))[1],
+        lambda a: bcp.bcp_kv_attend(cache, a, table, lens)[0],
+        lambda a: bcp.bcp_kv_attend(cache, x, table, lens, lse=(a * 1).float().sum(-1))[1],
+    ]
+    for i, call in enumerate(calls):
+        with pytest.raises(bcp.BcpError, match="requires a gradient"):
+            call(g)
+            pytest.fail(f"call {i} was accepted")
+        want = call(x)
+        for mode in (torch.no_grad, torch.inference_mode):
+            with mode():
+                got = call(g)
+            assert want is None or torch.equal(got, want)
+    leaf = bcp.rope(g, rot, slots)  # the differentiable form takes it
+    leaf.float().sum().backward()
+    assert g.grad is not None
+
+
+def test_outputs_count_as_written(cuda_device):
+    # autograd keeps values for the backward pass: a call that overwrites them has to be noticed
+    cache = _cache(3, 2, 16, 64, F16)
+    rot = bcp.RopeTable.build(bcp.rope_frequencies(64), 32)
+    slots = torch.arange(4, device="cuda")
+    lens, table = torch.ones(4, dtype=torch.int32, device="cuda"), torch.zeros((4, 3), dtype=torch.int32, device="cuda")
+    x = [_randn((4, 2, 64), i, F16) for i in range(4)]
+    sums = torch.zeros((4, 2), device="cuda")
+    calls = [
+        (x[0], lambda: bcp.bcp_rope(x[0], rot, slots, out=x[0])),
+        (x[1], lambda: bcp.bcp_rope((x[0], x[1]), rot, slots, out=(x[0], x[1]))),
+        (cache.k, lambda: bcp.bcp_kv_write(cache, x[0], x[1], slots)),
+        (cache.v, lambda: bcp.bcp_kv_write(cache, x[0], x[1], slots, rope=rot, positions=slots)),
+        (x[2], lambda: bcp.bcp_kv_read(cache, slots, out=(x[2], x[3]))),
+        (x[3], lambda: bcp.bcp_kv_read(cache, slots, out=(x[2], x[3]))),
+        (x[2], lambda: bcp.bcp_kv_attend(cache, x[0], table, lens, out=x[2], lse=sums)),
+        (sums, lambda: bcp.bcp_kv_attend(cache, x[0], table, lens, out=x[2], lse=sums)),
+    ]
+    for kept, call in calls:
+        a = torch.ones_like(kept).requires_grad_()
+        y = (a * kept).float().sum()
+        version = kept._version
+        call()
+        assert kept._version > version
+        with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+            y.backward()
+
+
 def test_python_refusals(cuda_device):
     cache = _cache(3, 2, 16, 64, E4M3)
     rot = bcp.RopeTable.build(bcp.rope_frequencies(64), 32)
