@@ -197,3 +197,26 @@ def test_slots_past_the_table_are_past_the_cache():
     assert slots([[5, 9]], [1, -1, 0], [0, 0, 0]) == [12 * 16, 12 * 16, 80]
     assert slots([[5, 9]], [1, 7], [-1, -1]) == [-1, -1]
     assert slots([[]], [0, 0], [0, -1]) == [12 * 16, -1]
+
+
+def run_without_torch(code_):
+    import os
+    import subprocess
+    import sys
+
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    r = subprocess.run([sys.executable, "-c", "import sys; sys.modules['torch'] = None\n" + code_], capture_output=True, text=True, cwd=root, timeout=120)
+    assert r.returncode == 0 and r.stdout.strip().endswith("ok"), r.stdout + r.stderr
+
+
+def test_a_star_import_needs_no_torch():
+    run_without_torch("from paper_2407_20143_b200 import *\nassert bcp_decompose((4, 4), 1, 5) and bcp_plan and Plan; print('ok')")
+
+
+def test_the_lazy_names_are_listed_and_found():
+    import paper_2407_20143_b200 as bcp
+
+    names = {"KvCache", "KvWorkspace", "RopeTable", "bcp_kv_attend", "bcp_kv_read", "bcp_kv_write", "bcp_rope", "bcp_rope_backward", "rope", "rope_frequencies"}
+    assert names <= set(dir(bcp)) and all(callable(getattr(bcp, n)) for n in names)
+    with pytest.raises(AttributeError):
+        bcp.no_such_name
