@@ -85,6 +85,15 @@ def build_binding(force: bool = False) -> str:
     return path
 
 
+def build_all(force: bool = False, verbose: bool = False) -> list:
+    """The library and, where torch is installed, the module that takes its tensors (the decoding operators)."""
+    import importlib.util
+
+    paths = [build_library(force=force, verbose=verbose)]
+    if importlib.util.find_spec("torch") is not None:
+        paths.append(build_binding(force=force))
+    return paths
+
+
 if __name__ == "__main__":
-    print(build_library(force=True, verbose="-v" in sys.argv))
-    print(build_binding(force=True))
+    print("\n".join(build_all(force=True, verbose="-v" in sys.argv)))

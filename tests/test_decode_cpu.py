@@ -220,3 +220,19 @@ def test_the_lazy_names_are_listed_and_found():
     assert names <= set(dir(bcp)) and all(callable(getattr(bcp, n)) for n in names)
     with pytest.raises(AttributeError):
         bcp.no_such_name
+
+
+def test_the_library_is_built_without_torch():
+    run_without_torch("""
+from paper_2407_20143_b200 import build
+build.build_library = lambda force=False, verbose=False: "library"
+build.build_binding = lambda force=False: 1 / 0
+assert build.build_all(force=True) == ["library"]; print('ok')""")
+
+
+def test_all_is_built_with_torch(monkeypatch):
+    from paper_2407_20143_b200 import build
+
+    monkeypatch.setattr(build, "build_library", lambda force=False, verbose=False: "library")
+    monkeypatch.setattr(build, "build_binding", lambda force=False: "binding")
+    assert build.build_all() == ["library", "binding"]
