@@ -189,6 +189,12 @@ __device__ __forceinline__ uint32_t pack16(float x, float y) {
     return *reinterpret_cast<const uint32_t*>(&p);
   }
 }
+// A positive binary32 number as the sum of a bfloat16 that is its upper half and what remains, positive as well (its last bit is
+// set): the products of both with an infinite value are that infinity.
+__device__ __forceinline__ uint32_t upper_halves(float x, float y) { return __byte_perm(__float_as_uint(x), __float_as_uint(y), 0x7632); }
+__device__ __forceinline__ float lower_half(float x) {
+  return __uint_as_float(__float_as_uint(x) | 1u) - __uint_as_float(__float_as_uint(x) & 0xffff0000u);
+}
 __device__ __forceinline__ float query_at(const void* p, int i, bool bf16) {
   return bf16 ? __bfloat162float(static_cast<const __nv_bfloat16*>(p)[i]) : __half2float(static_cast<const __half*>(p)[i]);
 }
@@ -259,6 +265,11 @@ __global__ void __launch_bounds__(kWarps * 32, Shape<FMT, DP, NT>::CTAS) bcp_kv_
   constexpr bool kBf16 = FMT == BCP_BF16;  // type of the products; 8-bit caches are widened to binary16
   // binary16 weights underflow below 2^-24: lifting them by 2^6 (they stay below 2^16) moves that to 2^-30
   constexpr float kLift = kBf16 ? 0.f : 6.f;
+  // Over a bfloat16 cache a weight goes into the product as two bfloat16 numbers: one alone is rounded to 2^-9, as coarsely as the
+  // result (131,072 tokens: relative error 2.2e-3, 1.6e-3 with two, which is the rounding of the result; 96.0 and 96.6 us).  The
+  // weights over other caches are binary16, 2^-12: 8-bit caches would pay 4 to 5 % for the second product (windows 43.4 and 45.5 us,
+  // 2.4e-4 and 2.1e-4 with results in binary16), and are rounded to 2^-4 or 2^-8 of a vector's largest themselves.
+  constexpr bool kRest = kBf16;
   extern __shared__ __align__(128) unsigned char smem[];
   const uint32_t tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, q4 = lane & 3;
   const uint32_t ring = uint32_t(__cvta_generic_to_shared(smem)) + warp * (S::STAGES * S::STAGE);
@@ -552,7 +563,7 @@ __global__ void __launch_bounds__(kWarps * 32, Shape<FMT, DP, NT>::CTAS) bcp_kv_
             for (int k = 0; k < DP / 16; ++k) o[t][k][c] *= down.all, o[t][k][c + 2] *= down.all;
           }
       }
-      uint32_t pf[NT][2];
+      uint32_t pf[NT][2], rest[NT][2];
 #pragma unroll
       for (int t = 0; t < NT; ++t) {
         float p[4];
@@ -562,8 +573,16 @@ __global__ void __launch_bounds__(kWarps * 32, Shape<FMT, DP, NT>::CTAS) bcp_kv_
           p[c] = exp2_fast(e);
           l[t][c & 1] += S::quant ? exp2_fast(e - vlog[c >> 1]) : p[c];
         }
-        pf[t][0] = transpose8x8(pack16<kBf16>(p[0], p[1]));
-        pf[t][1] = transpose8x8(pack16<kBf16>(p[2], p[3]));
+#pragma unroll
+        for (int r = 0; r < 2; ++r) {
+          const float x = p[2 * r], y = p[2 * r + 1];
+          if constexpr (kRest) {
+            pf[t][r] = transpose8x8(upper_halves(x, y));
+            rest[t][r] = transpose8x8(pack16<kBf16>(lower_half(x), lower_half(y)));
+          } else {
+            pf[t][r] = transpose8x8(pack16<kBf16>(x, y));
+          }
+        }
       }
       // sums over the values: rows are head dimensions
       if constexpr (!S::quant) {
@@ -572,7 +591,10 @@ __global__ void __launch_bounds__(kWarps * 32, Shape<FMT, DP, NT>::CTAS) bcp_kv_
           uint32_t f[4];
           load_transposed(f, stage + S::SIDE + value_at<S::CPR, false>((lane & 7) + (lane >> 4 << 3), 2 * m + (lane >> 3 & 1)));
 #pragma unroll
-          for (int t = 0; t < NT; ++t) mma<kBf16>(o[t][m], f, pf[t]);
+          for (int t = 0; t < NT; ++t) {
+            mma<kBf16>(o[t][m], f, pf[t]);
+            if constexpr (kRest) mma<kBf16>(o[t][m], f, rest[t]);
+          }
         }
       } else {
         constexpr int kWords = DP >= 128 ? 4 : DP / 32;  // words a lane takes of each of its four tokens at once
@@ -599,7 +621,10 @@ __global__ void __launch_bounds__(kWarps * 32, Shape<FMT, DP, NT>::CTAS) bcp_kv_
               widen4<FMT>(__byte_perm(w[0][x], w[1][x], pick), f[0], f[1]);
               widen4<FMT>(__byte_perm(w[2][x], w[3][x], pick), f[2], f[3]);
 #pragma unroll
-              for (int t = 0; t < NT; ++t) mma<kBf16>(o[t][8 * j + 2 * x + half], f, pf[t]);
+              for (int t = 0; t < NT; ++t) {
+                mma<kBf16>(o[t][8 * j + 2 * x + half], f, pf[t]);
+                if constexpr (kRest) mma<kBf16>(o[t][8 * j + 2 * x + half], f, rest[t]);
+              }
             }
           }
         }

@@ -587,6 +587,39 @@ def test_attend_values_that_are_not_finite(cuda_device, fmt):
         assert not out.any() and bool((lse == -math.inf).all())
 
 
+@pytest.mark.parametrize("heads,group,dim,n", [(1, 4, 64, 300), (2, 16, 128, 2000), (1, 3, 256, 90)])
+def test_attend_weights_over_bfloat16_caches(cuda_device, heads, group, dim, n):
+    # Values that nearly cancel: neighbours are each other's negative, and their keys differ a little.  A weight reaches the product as the
+    # sum of two bfloat16 numbers, the second rounded to 2^-9 of at most 2^-7 of it: 2^-16, where one alone would be off by 2^-9.
+    page = 16
+    cache = _cache(-(-n // page), heads, page, dim, BF16)
+    k, v = _randn((n, heads, dim), 1), _randn((n, heads, dim), 2, BF16)
+    k[1::2], v[1::2] = k[0::2] * 1.004, -v[0::2]
+    bcp.bcp_kv_write(cache, k.to(BF16), v, torch.arange(n, device="cuda"))
+    table = torch.arange(-(-n // page), dtype=torch.int32, device="cuda")[None]
+    q, scale = _randn((1, heads * group, dim), 3, BF16), dim ** -0.5
+    lens = torch.tensor([n], dtype=torch.int32, device="cuda")
+    out, _ = bcp.bcp_kv_attend(cache, q, table, lens)
+    want, sums, mass, size = attend64(cache, q, table, lens, scale, 0)
+    # scores and exponentials as for any attention (rounded the same way for both neighbours or not)
+    score = (dim / 2 + 4) * F32_EPS * size + 2.0 ** -21 + 4 * F32_EPS * sums.abs()
+    tol = (1.01 * 2.0 ** -16 + 4 * score[..., None] + n * F32_EPS) * mass + U[BF16] * want.abs()
+    assert bool(((out.double().cpu() - want).abs() <= tol).all())
+
+
+def test_attend_infinite_values_stay_infinite(cuda_device):
+    table, lens, n_pages = _batch([40, 40], 16, 5)
+    cache = _filled(n_pages, 2, 16, 64, BF16)
+    q = _randn((2, 4, 64), 9, BF16)
+    q[0, 0] = 0  # equal weights, that are exact in few bits
+    page = int(table[0, 1])
+    cache.v[page, :, 3, 7], cache.v[page, :, 4, 9] = math.inf, -math.inf
+    out, _ = bcp.bcp_kv_attend(cache, q, table, lens)
+    assert bool((out[0, :, 7] == math.inf).all()) and bool((out[0, :, 9] == -math.inf).all())
+    out[0, :, 7] = out[0, :, 9] = 0
+    assert bool(out.isfinite().all())
+
+
 def test_one_workspace_for_calls_of_different_shapes(cuda_device):
     # batches of one size after another, another head layout between them: what a call leaves must not disturb the next
     work, cases = None, []
