@@ -265,9 +265,9 @@ __global__ void __launch_bounds__(kWarps * 32, Shape<FMT, DP, NT>::CTAS) bcp_kv_
   constexpr bool kBf16 = FMT == BCP_BF16;  // type of the products; 8-bit caches are widened to binary16
   // binary16 weights underflow below 2^-24: lifting them by 2^6 (they stay below 2^16) moves that to 2^-30
   constexpr float kLift = kBf16 ? 0.f : 6.f;
-  // Over a bfloat16 cache a weight goes into the product as two bfloat16 numbers: one alone is rounded to 2^-9, as coarsely as the
+  // Over a bfloat16 cache a weight goes into the product as two bfloat16 numbers: one alone is rounded to 2^-8, as coarsely as the
   // result (131,072 tokens: relative error 2.2e-3, 1.6e-3 with two, which is the rounding of the result; 96.0 and 96.6 us).  The
-  // weights over other caches are binary16, 2^-12: 8-bit caches would pay 4 to 5 % for the second product (windows 43.4 and 45.5 us,
+  // weights over other caches are binary16, 2^-11: 8-bit caches would pay 4 to 5 % for the second product (windows 43.4 and 45.5 us,
   // 2.4e-4 and 2.1e-4 with results in binary16), and are rounded to 2^-4 or 2^-8 of a vector's largest themselves.
   constexpr bool kRest = kBf16;
   extern __shared__ __align__(128) unsigned char smem[];

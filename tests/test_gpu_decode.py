@@ -590,7 +590,7 @@ def test_attend_values_that_are_not_finite(cuda_device, fmt):
 @pytest.mark.parametrize("heads,group,dim,n", [(1, 4, 64, 300), (2, 16, 128, 2000), (1, 3, 256, 90)])
 def test_attend_weights_over_bfloat16_caches(cuda_device, heads, group, dim, n):
     # Values that nearly cancel: neighbours are each other's negative, and their keys differ a little.  A weight reaches the product as the
-    # sum of two bfloat16 numbers, the second rounded to 2^-9 of at most 2^-7 of it: 2^-16, where one alone would be off by 2^-9.
+    # sum of two bfloat16 numbers, the second, below 2^-7 of it, rounded to nearest: 2^-16, where one alone would be off by 2^-8.
     page = 16
     cache = _cache(-(-n // page), heads, page, dim, BF16)
     k, v = _randn((n, heads, dim), 1), _randn((n, heads, dim), 2, BF16)
