@@ -184,15 +184,21 @@ class _Rope(torch.autograd.Function):
     def forward(ctx, table, positions, transpose, *xs):
         ctx.table, ctx.transpose = table, transpose
         ctx.save_for_backward(positions)
+        ctx.set_materialize_grads(False)
         return _rope(xs, table, positions, None, transpose, None)
 
     @staticmethod
     def backward(ctx, *grads):
         positions, = ctx.saved_tensors
-        # an expanded gradient (of a sum, say) has no contiguous vectors
-        grads = [g if g.stride(-1) == 1 else g.contiguous() for g in grads]
-        # the gradient of a linear map is its transpose: through this function again, so that it has gradients itself
-        return (None, None, None) + _Rope.apply(ctx.table, positions, not ctx.transpose, *grads)
+        wanted = [i for i, g in enumerate(grads) if g is not None and ctx.needs_input_grad[3 + i]]
+        out = [None] * len(grads)
+        if wanted:
+            # an expanded gradient (of a sum, say) has no contiguous vectors
+            given = [g if g.stride(-1) == 1 else g.contiguous() for g in (grads[i] for i in wanted)]
+            # the gradient of a linear map is its transpose: through this function again, so that it has gradients itself
+            for i, g in zip(wanted, _Rope.apply(ctx.table, positions, not ctx.transpose, *given)):
+                out[i] = g
+        return (None, None, None, *out)
 
 
 def rope(x, table: RopeTable, positions):

@@ -64,3 +64,17 @@ def test_a_penalty_on_the_gradient(stand_in):
     loss(lambda t: decode.rope(t, handle, positions), x).backward()
     loss(lambda t: turned(t, kernel.table, positions), y).backward()
     assert torch.allclose(x.grad, y.grad, rtol=1e-12, atol=1e-12)
+
+
+def test_only_the_gradients_that_are_asked_for(stand_in, monkeypatch):
+    kernel, handle, positions = stand_in
+    pairs, rope = [], kernel.rope
+    monkeypatch.setattr(kernel, "rope", lambda *a: (pairs.append(a[3] is not None), rope(*a)))
+    x, y = _x(1), _x(2, 1)
+    a, b = decode.rope((x, y), handle, positions)
+    b.sum().backward()  # the first output is not used
+    assert pairs == [True, False] and x.grad is None and torch.equal(y.grad, turned(torch.ones_like(y), kernel.table, positions, True).detach())
+    y.requires_grad_(False)  # the second input needs none
+    a, b = decode.rope((x, y), handle, positions)
+    (a.sum() + (b * 2).sum()).backward()
+    assert pairs == [True, False, True, False] and torch.equal(x.grad, turned(torch.ones_like(x), kernel.table, positions, True).detach())
