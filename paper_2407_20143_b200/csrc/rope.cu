@@ -45,8 +45,11 @@ int check_rope(const char* call, const bcp_rope_table* r, uint32_t head_dim) {
 namespace {
 
 // Heads per thread: four share the loads of the table and keep eight 16-byte loads in flight, which a long
-// input needs (16k tokens of 40 heads: 52 us, 56 with two); where that leaves SMs without work, one.
-constexpr uint32_t kManyHeads = 4, kFewThreads = 1024;  // per SM, with a thread for every head
+// input needs (16k tokens of 40 heads: 52 us, 56 with two); where that leaves SMs without work, one.  Microseconds with one
+// and with four, by threads an SM if each had one head: 540 (250 tokens of 40 heads, bf16) 2.5 / 2.6, 860 (400) 2.8 / 3.3, 1300 (600)
+// 3.7 / 4.3, 1500 (700) 4.8 / 4.4, 1700 (500 tokens of 32 heads, f32) 4.4 / 4.7, 2160 (1000 tokens of 40 heads) 5.9 / 5.5,
+// 4300 (2000) 9.8 / 8.7.
+constexpr uint32_t kManyHeads = 4, kFewThreads = 2048;  // per SM, with a thread for every head
 
 struct RopeArgs {
   const void* in[2];
