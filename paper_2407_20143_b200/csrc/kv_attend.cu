@@ -100,9 +100,10 @@ struct Shape {
   static constexpr int CPR = ROW / 16;       // 16-byte chunks of a row
   static constexpr int SIDE = kTok * ROW;
   static constexpr int STAGE = 2 * SIDE + (quant ? 128 : 0) + 16;  // keys, values, their scales, the mask of live tokens
-  // Bytes in flight, in all but one stage of each warp: about 64 KiB an SM cover the latency of HBM.  More only
-  // queue up, and unevenly: 16-bit caches with head_dim 128 take 95 us for 537 MB with two stages, 102 with three.
-  static constexpr int STAGES = STAGE <= 2400 ? 3 : 2;
+  // Bytes in flight, in all but one stage of each warp: 32 to 64 KiB an SM cover the latency of HBM.  More only
+  // queue up, and unevenly, or cost CTAs: microseconds with two and with three stages for 64 ragged sequences of up to 4096 tokens, 8 heads,
+  // 8-bit 64 dimensions 48.0 / 48.5, 128 70.9 / 83.7, 256 (4 heads) 68.9 / 102; 16-bit 64 58.8 / 61.4, 128 107 / 113.
+  static constexpr int STAGES = 2;
   // CTAs that share an SM, as many as registers (128, 168 or 255 a thread) and shared memory allow: 8-bit caches,
   // whose elements cost conversions, gain from warps (int8 windows 46 us with four CTAs, 50 with three).
   static constexpr int CTAS = DP == 64 ? (NT == 1 ? 4 : 3) : DP == 128 ? (!quant ? 2 : NT == 1 ? 4 : 3) : quant ? 2 : 1;
