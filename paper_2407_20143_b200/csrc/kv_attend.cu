@@ -104,9 +104,14 @@ struct Shape {
   // queue up, and unevenly, or cost CTAs: microseconds with two and with three stages for 64 ragged sequences of up to 4096 tokens, 8 heads,
   // 8-bit 64 dimensions 48.0 / 48.5, 128 70.9 / 83.7, 256 (4 heads) 68.9 / 102; 16-bit 64 58.8 / 61.4, 128 107 / 113.
   static constexpr int STAGES = 2;
-  // CTAs that share an SM, as many as registers (128, 168 or 255 a thread) and shared memory allow: 8-bit caches,
-  // whose elements cost conversions, gain from warps (int8 windows 46 us with four CTAs, 50 with three).
-  static constexpr int CTAS = DP == 64 ? (NT == 1 ? 4 : 3) : DP == 128 ? (!quant ? 2 : NT == 1 ? 4 : 3) : quant ? 2 : 1;
+  // CTAs that share an SM and bound the registers of a thread (128, 168 or 255 for four, three and two).  8-bit caches, whose
+  // elements cost conversions, gain from warps as long as little is spilled.  Microseconds for 64 ragged sequences of up to 4096
+  // tokens: 64 dimensions, up to 8 heads a group, 8 / 16 bits: 48.5 / 58.9 with four, 54.9 / 60.7 with three, 49.4 / 60.7 with five; 16
+  // heads 43.4 / 40.6 with three, 46.6 / 47.4 with two, 39.7 / 40.6 with four (but 8 sequences of 2000 17.7 against 15.5);
+  // 128 dimensions, 8 bits, up to 8 heads 70.8 with four, 72.7 with three (windows 43 and 50; but one sequence of 60,000 42.3
+  // and 36.7); 16 heads 65.4 with two, 73.2 with three; 16 bits, 16 heads 65.0 with two, 72.6 with three.  Of the others
+  // shared memory allows two (16 bits, 256 dimensions: one).
+  static constexpr int CTAS = DP == 64 ? (NT == 1 ? 4 : 3) : DP == 128 && quant && NT == 1 ? 4 : 2;
   static constexpr int ROWS = 8 * NT;
   static constexpr int PART = ROWS * (DP + 2);  // floats of one set of sums: dimensions of the heads (sum_at), references, denominators
   static constexpr int SMEM = kWarps * STAGES * STAGE + kWarps * PART * 4 + 16;
@@ -306,7 +311,9 @@ __global__ void __launch_bounds__(kWarps * 32, Shape<FMT, DP, NT>::CTAS) bcp_kv_
       if (w < warp) before += totals[w];
       all += totals[w];
     }
-    extra = all * units >= 2 * gridDim.x ? kExtra : 0;  // a short line is cut finely instead
+    // A short line is cut finely instead (us without and with: one sequence of 600 tokens 7.7 / 8.6, 4 of 500 9.5 / 10.5; one of
+    // 6000 16.1 / 15.1, 4 of 3000 19.6 / 18.0).
+    extra = all * units >= 2 * gridDim.x ? kExtra : 0;
     mine += extra * (run1 - run0), before += extra * run0;
     cuts.cut((all + extra * a.n_seqs) * units, gridDim.x);
   }
