@@ -48,7 +48,8 @@ namespace {
 // input needs (16k tokens of 40 heads: 52 us, 56 with two); where that leaves SMs without work, one.  Microseconds with one
 // and with four, by threads an SM if each had one head: 540 (250 tokens of 40 heads, bf16) 2.5 / 2.6, 860 (400) 2.8 / 3.3, 1300 (600)
 // 3.7 / 4.3, 1500 (700) 4.8 / 4.4, 1700 (500 tokens of 32 heads, f32) 4.4 / 4.7, 2160 (1000 tokens of 40 heads) 5.9 / 5.5,
-// 4300 (2000) 9.8 / 8.7.
+// 4300 (2000) 9.8 / 8.7.  The scalar form takes one head always: four spill (16,384 tokens of 40 heads of 80, 20 rotated, bf16 285 / 328,
+// 8192 of them in f32 124 / 164, 1000 in bf16 22 / 39).
 constexpr uint32_t kManyHeads = 4, kFewThreads = 2048;  // per SM, with a thread for every head
 
 struct RopeArgs {
@@ -110,7 +111,11 @@ __global__ void bcp_clear_kernel(uint32_t* status, uint32_t bits) { atomicAnd(st
 
 template <typename T, bool VEC, bool PAIRS>
 cudaError_t launch(const RopeArgs& a, uint32_t heads, cudaStream_t stream) {
-  return launch_early(heads == 1 ? bcp_rope_kernel<T, VEC, PAIRS, 1> : bcp_rope_kernel<T, VEC, PAIRS, kManyHeads>, (a.n_threads + 255) / 256, 256, 0, stream, a);
+  void (*kernel)(RopeArgs) = bcp_rope_kernel<T, VEC, PAIRS, 1>;
+  if constexpr (VEC) {
+    if (heads != 1) kernel = bcp_rope_kernel<T, VEC, PAIRS, kManyHeads>;
+  }
+  return launch_early(kernel, (a.n_threads + 255) / 256, 256, 0, stream, a);
 }
 template <typename T>
 cudaError_t launch(const RopeArgs& a, bool vec, bool pairs, uint32_t heads, cudaStream_t stream) {
@@ -158,7 +163,7 @@ extern "C" int bcp_rope(const bcp_heads* q_in, const bcp_heads* q_out, const bcp
   BCP_CUDA(cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, device));
   const uint32_t es = type_size(q_in->type), chunks = chunks_of(head_dim, rope->rot_dim, vec ? 16 / es : 8);
   const uint64_t all_heads = uint64_t(a.n_heads[0]) + a.n_heads[1];
-  const uint32_t heads = uint64_t(n_tokens) * all_heads * chunks < uint64_t(sms) * kFewThreads ? 1 : kManyHeads;
+  const uint32_t heads = !vec || uint64_t(n_tokens) * all_heads * chunks < uint64_t(sms) * kFewThreads ? 1 : kManyHeads;
   a.q_groups = (a.n_heads[0] + heads - 1) / heads;
   const uint32_t per_token = chunks * (a.q_groups + (a.n_heads[1] + heads - 1) / heads);
   a.per_group = FastDiv(chunks), a.per_token = FastDiv(per_token);
