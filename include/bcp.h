@@ -671,6 +671,7 @@ BCP_API int bcp_kv_read(const bcp_kv_cache* cache, const int64_t* slots, int64_t
  * lse (binary32, [n_seqs][q heads], dense) may be NULL.  Rows of q and out start on 8-byte boundaries.
  * Scores and sums are binary32.  For the product with the values a weight is rounded: over a bfloat16 cache to the sum of two
  * bfloat16 numbers (2^-16 of it), over the others to binary16 (2^-11).
+ * Rows of the block table must not overlap (table_stride >= table_width for more than one sequence); different rows may name the same pages.
  * Tokens whose page is outside the cache (BCP_BAD_PAGE) are left out; a length past table_width * page_size
  * counts as that many (BCP_BAD_LENGTH).
  * workspace: device memory of at least bcp_kv_attend_workspace bytes, 16-byte aligned, whose first use finds

@@ -3,8 +3,8 @@
 // Mathematics.  For one query head the pass over the tokens keeps a reference r, l = sum exp2(s - r) and
 // o = sum exp2(s - r) v, with s = q.k scale log2 e; whenever a score exceeds r by more than 8 the sums are
 // multiplied by exp2(r - r') and r' takes its place.  Any r gives the same o / l; parts of a sequence are
-// joined by bringing their sums to the largest r.  Each key and value is read once, for all query heads
-// that share its cache head.
+// joined by bringing their sums to the largest r.  Each key and value is read once for up to 16 query heads that
+// share its cache head (8 with more than 128 dimensions); larger groups are cut into row tiles, which each read it again.
 //
 // What bounds it: reading the cache.  A byte of 16-bit cache is used in `group` multiply-adds (at most a
 // few dozen), so the matrix instructions only have to keep out of the way.  The products are taken as
@@ -26,10 +26,13 @@
 // the order of the parts, so results do not depend on which that is.
 //
 // Measured on one B200 (copy bandwidth 6533 GB/s), per launch in a row of them: one sequence of 131,072 tokens, 32 / 8 heads
-// of 128, bfloat16: 94 us = 5.7 TB/s; 64 ragged sequences of up to 4096, e4m3: 70 us = 5.0 TB/s; 37 windows of 1000,
-// 16 / 16 heads, int8: 43 us; one sequence of 600 tokens: 7.8 us, of which the launch, the look-up of the lengths and the
-// page, the first read and the joining of ten parts are most.  With the end-of-stretch work left out the first
-// three take 85, 57 and 33 us: it is what keeps them from the copy bandwidth (DRAM 38 to 67 % busy, tensor pipe 9 to 14 %).
+// of 128, bfloat16: 92 us = 5.8 TB/s; 64 ragged sequences of up to 4096, bfloat16: 107.6 us = 6.1 TB/s, e4m3: 71.5 us =
+// 4.7 TB/s; 37 windows of 1000, 16 / 16 heads, int8: 42 us = 3.4 TB/s; one sequence of 600 tokens: 7.8 us, of which the launch, the
+// look-up of the lengths and the page, the first read and the joining of ten parts are most.  With the end-of-stretch work left out
+// (measured on an earlier form of the kernel) the first takes 85, the e4m3 batch 57 and the windows 33 us: it is what keeps
+// them from the copy bandwidth (DRAM 40 to 67 % busy, tensor pipe 10 to 14 %).  Not near it: 8000 sequences of up to 64 tokens,
+// one cache head, bfloat16: 127 us for 0.18 GB, as every CTA goes over all lengths; one cache head under 16 / 32 / 64 query
+// heads, 64 ragged sequences: 27 / 38 / 62 us for 84 MB (row tiles); 2 under 16 each with 256 dimensions 113 us for 0.34 GB, 62 under 8.
 #include <mutex>
 
 #include "decode.cuh"
@@ -66,7 +69,8 @@ struct AttendArgs {
 };
 
 // Steps that a unit counts for besides its own.  Microseconds with 0 / 1 / 2 / 3: 64 ragged sequences of up to 4k tokens,
-// e4m3 83 / 76 / 72 / 71; 37 windows of 1000, int8, 16 heads 67 / 44.6 / 44.1 / 45.2; 300 sequences of up to 500 72 / 67 / 65.5 / 65.8.
+// e4m3 82 / 77 / 71.6 / 69; 37 windows of 1000, int8, 16 heads 65 / 42.9 / 42.3 / 43.6; 300 sequences of up to 500, e4m3 71 / 64.6 / 63 / 63,
+// bfloat16 84.7 / 83.5 / 82.2 / 82.7; one sequence of 5000, bfloat16 15.2 / 14.6 / 14 / 14.2.
 constexpr uint32_t kExtra = 2;
 
 constexpr uint32_t kGroup = 64;  // parts that are joined at once
@@ -77,7 +81,8 @@ struct Cuts {
   uint32_t parts;
   __device__ __forceinline__ void cut(uint32_t steps, uint32_t ctas) {
     // A line of a few steps per CTA is cut into parts of whole, equal numbers of them: the longest part decides, and
-    // fewer parts are joined sooner (one sequence of 4000 tokens 14.1 -> 12.9 us, of 3000 13.8 -> 12.4).
+    // fewer parts are joined sooner (one sequence of 3000 tokens 13.5 us, 14.5 without; of 4000 14.6 and 15.2; of 5000 14.0 and
+    // 15.2).
     n = steps, parts = n < ctas ? n : ctas;
     if (n > ctas && n < 4 * ctas) {
       const uint32_t most = (n + ctas - 1) / ctas;

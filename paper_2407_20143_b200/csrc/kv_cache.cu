@@ -4,10 +4,13 @@
 // two) holds one head vector, a chunk a lane, so the largest magnitude that an 8-bit format's scale needs is a
 // few shuffles away and the vector is never read twice.  A group takes two heads of one token, whose loads
 // are all in flight before the first one is used.
-// Measured on one B200 (copy bandwidth 6533 GB/s): 65,536 tokens of 8 heads of 128 read back, e4m3 to bfloat16: 62.5 us, 409 MB,
-// 1.0 of it.  32,768 tokens written, bfloat16 to e4m3 with rotation: 48 us, 221 MB, 0.70: 12 instructions an element
-// and two dependent loads (position, row of the table) before it; 64 registers are the least and four CTAs an SM
-// the most that do not spill in the loop (three CTAs: 56 us; four heads a group, 128 registers: 66 us).
+// Measured on one B200 (copy bandwidth 6533 GB/s): 65,536 tokens of 8 heads of 128 read back, one in 17 slots empty, e4m3 to
+// bfloat16: 62.4 us, 399 MB, 0.98 of it.  32,768 tokens written with rotation, one in 17 skipped, bfloat16 to e4m3: 47.6 us for the 202 MB
+// that live tokens need, 0.65 of it (skipped tokens' vectors are read too: nothing waits for the slot), to int8 52 us, to a bfloat16
+// cache 47 us (0.86 for its 263 MB); neighbouring pairs 48.5.  It waits: half of the issue slots are used and DRAM is 46 % busy; a
+// group of lanes lives for one token, loads its position, then the row of the table, and has nothing else in flight meanwhile.  Four
+// CTAs an SM allow 64 registers (half layout without spills, neighbouring pairs with 44 bytes; three CTAs: 56 us; four heads a
+// group, 128 registers: 66 us).
 #include "decode.cuh"
 
 using namespace bcp;

@@ -4,8 +4,12 @@
 // once and written once.  A thread takes one chunk (two 16-byte vectors) of four heads of one token: the cosines
 // and sines, which all heads of a token share, are loaded once per four heads, and eight 16-byte loads
 // are in flight per thread (16-bit types).  Query and key heads go through one launch.
-// Measured on one B200 (copy bandwidth 6533 GB/s): 16,384 tokens of 32 + 8 heads of 128, bfloat16: 52 us, 344 MB, 1.0 of it; the
-// gradient of 8191 tokens of 16 + 16 heads, binary32, half of each rotated: 41 us, 271 MB, 1.0; 16 tokens: 1.6 us.
+// Measured on one B200 (copy bandwidth 6533 GB/s): 16,384 tokens of 32 + 8 heads of 128, bfloat16: 51.7 us for 342 MB, 1.01 of it (a
+// part of the output is still in the L2 cache when the launch ends); the gradient of 8191 tokens of 16 + 16 heads, binary32,
+// half of each rotated: 41.1 us for 270 MB, 1.0; 16 tokens: 1.6 us.
+// The scalar form, for rotated parts that are no multiple of 16 and for rows off the 16-byte boundaries, is bound by its
+// element-wise accesses: 16,384 tokens of 32 + 8 heads of 80, 20 of them rotated, bfloat16 285 us for 211 MB (32 rotated,
+// vector form: 36 us); 8192 tokens in binary32 124 us (16 rotated, vector form: 33 us).
 #include "decode.cuh"
 
 using namespace bcp;
