@@ -854,6 +854,33 @@ def test_inputs_of_another_stream_are_not_reused_too_early(cuda_device, call, ra
     assert busy and not was & {x.data_ptr() for x in again}
 
 
+def test_calls_that_name_the_capturing_stream(cuda_device):
+    # tensors are recorded on a stream that is being captured, some of them from the capture's own pool
+    table, lens, n_pages = _batch([300, 64, 7], 16, 5)
+    cache = _filled(n_pages, 2, 16, 64, E4M3)
+    rot = bcp.RopeTable.build(bcp.rope_frequencies(64), 512)
+    work = bcp.KvWorkspace(cache, 8, 3)
+    q, k, v = _randn((3, 8, 64), 9, BF16), _randn((3, 2, 64), 10, BF16), _randn((3, 2, 64), 11, BF16)
+    positions, rows = (lens - 1).long(), torch.arange(3, device="cuda")
+
+    def step(stream=None):
+        slots = cache.slots(table, rows, positions)
+        turned = bcp.bcp_rope(q, rot, positions, stream=stream)
+        bcp.bcp_kv_write(cache, k, v, slots, rope=rot, positions=positions, stream=stream)
+        return (*bcp.bcp_kv_attend(cache, turned, table, lens, workspace=work, stream=stream), bcp.bcp_kv_read(cache, slots, stream=stream)[0])
+
+    want = step()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = step(torch.cuda.current_stream())
+    for _ in range(2):
+        graph.replay()
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+    cache.check()
+
+
 def test_workspace_zeroed_on_the_stream_that_uses_it(cuda_device):
     table, lens, n_pages = _batch([2000, 64, 700], 16, 5)
     cache = _filled(n_pages, 2, 16, 128, BF16)
