@@ -256,18 +256,23 @@ class KvCache:
         """Slots (int64) of tokens at `positions` of `sequences` (rows of block_table), all on the device.  -1, which the calls
         skip, for a negative position and where the table's page is negative; a slot past the cache, which they skip and
         report, for a position past the table's width or a sequence that is no row of it."""
-        past = self.n_pages * self.page_size
+        rows, width = block_table.shape
+        positions = positions.long()
         page = torch.div(positions, self.page_size, rounding_mode="floor")
-        bad = page >= block_table.shape[1]
-        if not isinstance(sequences, int):
-            sequences = torch.as_tensor(sequences, device=block_table.device)
-            bad = bad | (sequences < 0) | (sequences >= block_table.shape[0])
-            sequences = sequences.clamp(0, max(0, block_table.shape[0] - 1))
-        if block_table.numel() == 0:  # nothing to look up
-            return torch.where(positions < 0, -1, torch.full_like(bad, past, dtype=torch.int64))
-        first = block_table[sequences, page.clamp(0, block_table.shape[1] - 1)].long() * self.page_size
-        slot = torch.where(bad, past, torch.where(first < 0, -1, first + (positions - page * self.page_size)))
-        return torch.where(positions < 0, -1, slot)
+        # the table as one line: what lies before or behind it, or behind its row, is past the table
+        if isinstance(sequences, int):
+            place = page + range(rows)[sequences] * width
+        else:
+            place = torch.add(page, torch.as_tensor(sequences, device=block_table.device), alpha=width)
+        slot = torch.remainder(positions, self.page_size)
+        if block_table.numel():  # else there is nothing to look up
+            there = place.clamp(0, rows * width - 1)
+            first = block_table.take(there)
+            slot = torch.add(slot, first, alpha=self.page_size).masked_fill_(first < 0, -1)
+            past = (page >= width).logical_or(place != there)
+        else:
+            slot, past = slot + 0 * place, torch.ones_like(place, dtype=torch.bool)
+        return slot.masked_fill_(past, self.n_pages * self.page_size).masked_fill_(positions < 0, -1)
 
     def check(self, stream=None) -> None:
         """Waits for `stream`; raises BcpError (ERR_BOUNDS) if a call met a slot, page, length or position out of range."""

@@ -199,6 +199,23 @@ def test_slots_past_the_table_are_past_the_cache():
     assert slots([[]], [0, 0], [0, -1]) == [12 * 16, -1]
 
 
+def test_slots_of_any_index_type():
+    from types import SimpleNamespace
+
+    import torch
+
+    from paper_2407_20143_b200 import decode
+
+    big = SimpleNamespace(n_pages=1 << 20, page_size=1 << 10)  # slots up to 2^30, products of int32 past 2^31
+    table = torch.tensor([[(1 << 20) - 1, 4]], dtype=torch.int32)
+    for typ in (torch.int32, torch.int64):
+        got = decode.KvCache.slots(big, table, torch.tensor([0, 0, 0], dtype=typ), torch.tensor([5, 1024, 2048], dtype=typ))
+        assert got.dtype == torch.int64 and got.tolist() == [((1 << 20) - 1) * 1024 + 5, 4096, 1 << 30]
+    assert decode.KvCache.slots(big, table.expand(3, 2), [2, 1], torch.tensor([7, 1025])).tolist() == [((1 << 20) - 1) * 1024 + 7, 4097]
+    with pytest.raises(IndexError):
+        decode.KvCache.slots(big, table, 1, torch.tensor([5]))
+
+
 def run_without_torch(code_):
     import os
     import subprocess
