@@ -644,6 +644,27 @@ BCP_API int bcp_rope(const bcp_heads* q_in, const bcp_heads* q_out, const bcp_he
                      int transpose, void* stream);
 
 /*
+ * Rotary positions with several axes (time, row and column of a patch, say): pair i of a token's heads goes by the position on
+ * axis axis_of_pair[i], that is by table[positions[axis_of_pair[i] * axis_stride + t]][.][i].  The table is the one above, so
+ * that axes may have frequencies of their own.
+ */
+#define BCP_MAX_AXES 4u
+typedef struct {
+  const uint8_t* axis_of_pair; /* HOST array of rot_dim / 2 entries below n_axes, read during the call */
+  int64_t axis_stride;         /* elements between the positions of two axes, 0 .. 2^40 (0: the same positions) */
+  uint32_t n_axes;             /* 1 .. BCP_MAX_AXES */
+  uint32_t reserved;           /* must be 0 */
+} bcp_rope_axes_map;
+
+/*
+ * bcp_rope with a position for every axis.  A token with a negative position on any axis is padding, whose rows are zeros; else one
+ * with a position past the table on any axis has rows of zeros and sets BCP_BAD_POSITION.
+ */
+BCP_API int bcp_rope_axes(const bcp_heads* q_in, const bcp_heads* q_out, const bcp_heads* k_in, const bcp_heads* k_out,
+                          uint32_t head_dim, int64_t n_tokens, const bcp_rope_table* rope, const bcp_rope_axes_map* axes,
+                          const int64_t* positions, int transpose, void* stream);
+
+/*
  * Writes the keys and values of n_tokens tokens into their slots; with rope != NULL the keys are rotated on
  * the way (positions[t], in binary32, not rounded before they are stored).
  * 8-bit formats: scale = max(max|x| / qmax, 2^-96) with qmax 448 or 127, stored element = x * (1/scale) rounded
@@ -653,6 +674,11 @@ BCP_API int bcp_rope(const bcp_heads* q_in, const bcp_heads* q_out, const bcp_he
  */
 BCP_API int bcp_kv_write(const bcp_kv_cache* cache, const bcp_heads* k, const bcp_heads* v, const int64_t* slots,
                          int64_t n_tokens, const bcp_rope_table* rope, const int64_t* positions, void* stream);
+
+/* bcp_kv_write with keys rotated by a position for every axis; a token with one outside the table is skipped (BCP_BAD_POSITION). */
+BCP_API int bcp_kv_write_axes(const bcp_kv_cache* cache, const bcp_heads* k, const bcp_heads* v, const int64_t* slots,
+                              int64_t n_tokens, const bcp_rope_table* rope, const bcp_rope_axes_map* axes,
+                              const int64_t* positions, void* stream);
 
 /*
  * Reads n_tokens tokens back from their slots: element * scale in binary32, rounded once to the outputs' type.
@@ -683,6 +709,33 @@ BCP_API int bcp_kv_attend_workspace(const bcp_kv_cache* cache, uint32_t n_q_head
 BCP_API int bcp_kv_attend(const bcp_kv_cache* cache, const bcp_heads* q, const bcp_heads* out, float* lse, uint32_t n_seqs,
                           const int32_t* block_table, int64_t table_stride, uint32_t table_width, const int32_t* lengths,
                           float scale, uint32_t window, void* workspace, uint64_t workspace_bytes, void* stream);
+
+/*
+ * Drafted tokens verified against a target's probabilities from given random numbers, so that what comes out is distributed as if
+ * the target had been sampled token by token; with n_drafts = 0 it samples the next token.
+ * Sequence b has drafts x_i = drafts[b*n_drafts + i], i < n_drafts; the first negative one ends them.  Row i of `target` is what the target says
+ * before draft i (n_drafts + 1 rows; the last behind all drafts), row i of `draft` what the drafts were drawn from; draft NULL: they were
+ * certain (looked up, say), q_i is 1 at x_i and 0 elsewhere.  Rows are logits, p = softmax(z / temperature[b]) (temperature NULL: 1; above
+ * 1e30: that; not above 1e-30: greedy, p is 1 at the lowest index of the largest logit), or, with probabilities != 0, weights that are taken as they are.
+ * Draft i is accepted iff all before it are and uniform[b*(n_drafts+1) + i] * q_i(x_i) < p_i(x_i); a draft past the vocabulary is not.  At the first
+ * one that is not, r = max(p_i - q_i, 0) (p_i, if that is zero throughout); if all n are, r = p_n.  The next token is the lowest j with
+ * sum_{l<=j} r(l) > uniform[b*(n_drafts+1) + n_drafts] * sum_l r(l) (should rounding leave none, the last with r > 0).
+ * tokens[b*(n_drafts+1) ..]: the accepted drafts, the next token, then -1.  accepted[b]: how many drafts.  The next token is -1 where its
+ * row has no weight, or one that is no finite number (all logits -infinity, a NaN, a logit of +infinity).
+ * Sums are held in 64 bits, their terms in 32.  Random numbers are at least 0 and below 1.
+ */
+#define BCP_MAX_DRAFTS 64u
+#define BCP_MAX_VOCAB (1u << 22)
+typedef struct {
+  const void* data;    /* element j of row i of sequence b: data[b*seq_stride + i*row_stride + j]; any alignment of elements */
+  int64_t seq_stride;  /* 0 .. 2^40 */
+  int64_t row_stride;
+  uint32_t type;       /* BCP_F32, BCP_BF16 or BCP_F16; target and draft alike */
+  uint32_t reserved;   /* must be 0 */
+} bcp_vocab_rows;
+BCP_API int bcp_verify_drafts(const bcp_vocab_rows* target, const bcp_vocab_rows* draft, uint32_t n_seqs, uint32_t n_drafts,
+                              uint32_t vocab, const int64_t* drafts, const float* uniform, const float* temperature,
+                              int probabilities, int64_t* tokens, int32_t* accepted, void* stream);
 
 /*
  * Waits for `stream`, reads the status word of a table or cache, clears the bits it read (others that work on another

@@ -5,13 +5,15 @@ import os
 import shutil
 import subprocess
 import sys
+import tempfile
+from concurrent.futures import ThreadPoolExecutor
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 INCLUDE = os.path.join(os.path.dirname(HERE), "include")
 LIB = os.path.join(HERE, "libbcp.so")
 SOURCES = ["planner.cpp", "units.cpp", "api.cu", "plan_image.cu", "host_path.cu", "kernels.cu", "tma_kernel.cu", "convert_kernel.cu", "static_pack.cu", "stager.cu", "export.cu", "ipc.cu",
-           "rope.cu", "kv_cache.cu", "kv_attend.cu"]
+           "rope.cu", "kv_cache.cu", "kv_attend.cu", "verify.cu"]
 HEADERS = ["plan.hpp", "kernels.cuh", "host_threads.hpp", "plan_object.hpp", "tma_ptx.cuh", "copy_loops.cuh", "decode.cuh"]
 
 
@@ -37,17 +39,23 @@ def build_library(force: bool = False, verbose: bool = False) -> str:
     """Compile for sm_100a only; returns the path of the shared library."""
     if not force and not is_stale():
         return LIB
-    cmd = [nvcc_path(), "-O3", "-std=c++17", "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo",
-           "-Xcompiler", "-fPIC,-fvisibility=hidden", "-shared", "-I", INCLUDE, "-I", CSRC, "-o", LIB]
-    if verbose:
-        cmd += ["-Xptxas", "-v"]
-    cmd += [os.path.join(CSRC, f) for f in SOURCES]
-    cmd += ["-lcuda"] if os.environ.get("BCP_LINK_DRIVER") else []
-    r = subprocess.run(cmd, capture_output=True, text=True)
-    if r.returncode != 0:
-        raise RuntimeError("nvcc failed:\n" + " ".join(cmd) + "\n" + r.stdout + r.stderr)
-    if verbose:
-        sys.stderr.write(r.stdout + r.stderr)
+    flags = ["-O3", "-std=c++17", "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-Xcompiler", "-fPIC,-fvisibility=hidden"]
+
+    def nvcc(*args):
+        cmd = [nvcc_path(), *flags, *args]
+        r = subprocess.run(cmd, capture_output=True, text=True)
+        if r.returncode != 0:
+            raise RuntimeError("nvcc failed:\n" + " ".join(cmd) + "\n" + r.stdout + r.stderr)
+        if verbose:
+            sys.stderr.write(r.stdout + r.stderr)
+
+    with tempfile.TemporaryDirectory() as tmp:
+        objects = [os.path.join(tmp, f + ".o") for f in SOURCES]
+        more = ["-Xptxas", "-v"] if verbose else []
+        with ThreadPoolExecutor(os.cpu_count()) as pool:  # the kernels take most of the time: a process for each file
+            for done in [pool.submit(nvcc, *more, "-c", "-I", INCLUDE, "-I", CSRC, os.path.join(CSRC, f), "-o", o) for f, o in zip(SOURCES, objects)]:
+                done.result()
+        nvcc("-shared", *objects, "-o", LIB, *(["-lcuda"] if os.environ.get("BCP_LINK_DRIVER") else []))
     return LIB
 
 

@@ -14,15 +14,19 @@
 
 #include <cstdarg>
 #include <cstdio>
+#include <type_traits>
 
 #include "bcp.h"
 
 namespace {
 
 decltype(&bcp_rope) g_rope;
+decltype(&bcp_rope_axes) g_rope_axes;
 decltype(&bcp_kv_write) g_write;
+decltype(&bcp_kv_write_axes) g_write_axes;
 decltype(&bcp_kv_read) g_read;
 decltype(&bcp_kv_attend) g_attend;
+decltype(&bcp_verify_drafts) g_verify;
 decltype(&bcp_last_error) g_last_error;
 PyObject* g_error;  // BcpError
 
@@ -174,9 +178,27 @@ bool arguments(Py_ssize_t n, Py_ssize_t want) {
   return n == want;
 }
 
-// rope(table, table device, x, x2 or None, out, out2 or None, positions, transpose, stream)
+// Positions of each axis, rows of [axes, tokens]; the map gets the stride between them.
+void* axis_positions(PyObject* o, int device, int64_t tokens, bcp_rope_axes_map* axes) {
+  static char empty[1];
+  const at::Tensor* p = tensor(o, "positions");
+  if (!p) return nullptr;
+  const at::Tensor& t = *p;
+  if (t.scalar_type() != at::kLong || !on_device(t, device)) {
+    raise(BCP_ERR_INVALID, "positions must be %s on cuda:%d", c10::toString(at::kLong), device);
+    return nullptr;
+  }
+  if (t.dim() != 2 || t.size(0) != axes->n_axes || t.size(1) != tokens || (tokens > 1 && t.stride(1) != 1)) {
+    raise(BCP_ERR_MISMATCH, "positions must be of shape [%u, %lld] with contiguous rows, one for each axis", axes->n_axes, (long long)tokens);
+    return nullptr;
+  }
+  axes->axis_stride = t.stride(0);
+  return t.numel() ? t.data_ptr() : empty;
+}
+
+// rope(table, table device, x, x2 or None, out, out2 or None, positions, transpose, stream[, axes])
 PyObject* py_rope(PyObject*, PyObject* const* a, Py_ssize_t n) {
-  if (!arguments(n, 9)) return nullptr;
+  if (!arguments(n, n == 10 ? 10 : 9)) return nullptr;
   int device;
   if (!device_of(a[2], "x", &device) || !same_device(device, a[1], "the table")) return nullptr;
   const at::Tensor& x = THPVariable_Unpack(a[2]);
@@ -187,18 +209,25 @@ PyObject* py_rope(PyObject*, PyObject* const* a, Py_ssize_t n) {
   const bool two = a[3] != Py_None;
   if (!heads(a[2], "x", device, tokens, dim, &h[0]) || !heads(a[4], "out", device, tokens, dim, &h[1])) return nullptr;
   if (two && (!heads(a[3], "x", device, tokens, dim, &h[2]) || !heads(a[5], "out", device, tokens, dim, &h[3]))) return nullptr;
-  void* const positions = index(a[6], "positions", device, at::kLong, tokens);
+  bcp_rope_axes_map axes;
+  const bool by_axes = n == 10;
+  if (by_axes) axes = *static_cast<const bcp_rope_axes_map*>(PyLong_AsVoidPtr(a[9]));
+  void* const positions = by_axes ? axis_positions(a[6], device, tokens, &axes) : index(a[6], "positions", device, at::kLong, tokens);
   void* stream;
   if (!positions || !stream_of(a[8], device, &stream)) return nullptr;
-  const int rc = g_rope(&h[0], &h[1], two ? &h[2] : nullptr, two ? &h[3] : nullptr, uint32_t(dim), tokens,
-                       static_cast<const bcp_rope_table*>(PyLong_AsVoidPtr(a[0])), static_cast<const int64_t*>(positions),
-                       a[7] == Py_True, stream);
+  const bcp_rope_table* const table = static_cast<const bcp_rope_table*>(PyLong_AsVoidPtr(a[0]));
+  const int64_t* const at = static_cast<const int64_t*>(positions);
+  const int rc = by_axes ? g_rope_axes(&h[0], &h[1], two ? &h[2] : nullptr, two ? &h[3] : nullptr, uint32_t(dim), tokens, table, &axes, at,
+                                       a[7] == Py_True, stream)
+                         : g_rope(&h[0], &h[1], two ? &h[2] : nullptr, two ? &h[3] : nullptr, uint32_t(dim), tokens, table, at,
+                                  a[7] == Py_True, stream);
   return two ? result_in(rc, a[4], a[5]) : result_in(rc, a[4]);
 }
 
-// kv_write(cache, cache device, k, v, slots, table or None, table device, positions or None, stream, the cache's keys, its values)
+// kv_write(cache, cache device, k, v, slots, table or None, table device, positions or None, stream, the cache's keys, its values
+// [, axes])
 PyObject* py_kv_write(PyObject*, PyObject* const* a, Py_ssize_t n) {
-  if (!arguments(n, 11)) return nullptr;
+  if (!arguments(n, n == 12 ? 12 : 11)) return nullptr;
   const bcp_kv_cache* cache = static_cast<const bcp_kv_cache*>(PyLong_AsVoidPtr(a[0]));
   int device;
   if (!device_of(a[2], "k", &device) || !same_device(device, a[1], "the cache")) return nullptr;
@@ -210,11 +239,16 @@ PyObject* py_kv_write(PyObject*, PyObject* const* a, Py_ssize_t n) {
   bcp_heads k, v;
   if (!heads(a[2], "k", device, tokens, cache->head_dim, &k) || !heads(a[3], "v", device, tokens, cache->head_dim, &v)) return nullptr;
   void* const slots = index(a[4], "slots", device, at::kLong, tokens);
-  void* const positions = slots && turn ? index(a[7], "positions", device, at::kLong, tokens) : nullptr;
+  bcp_rope_axes_map axes;
+  const bool by_axes = n == 12;
+  if (by_axes) axes = *static_cast<const bcp_rope_axes_map*>(PyLong_AsVoidPtr(a[11]));
+  void* positions = nullptr;
+  if (slots && turn) positions = by_axes ? axis_positions(a[7], device, tokens, &axes) : index(a[7], "positions", device, at::kLong, tokens);
   void* stream;
   if (!slots || (turn && !positions) || !stream_of(a[8], device, &stream)) return nullptr;
-  return result_in(g_write(cache, &k, &v, static_cast<const int64_t*>(slots), tokens,
-                           turn ? static_cast<const bcp_rope_table*>(PyLong_AsVoidPtr(a[5])) : nullptr, static_cast<const int64_t*>(positions), stream),
+  const bcp_rope_table* const table = turn ? static_cast<const bcp_rope_table*>(PyLong_AsVoidPtr(a[5])) : nullptr;
+  const int64_t *const to = static_cast<const int64_t*>(slots), *const at = static_cast<const int64_t*>(positions);
+  return result_in(by_axes ? g_write_axes(cache, &k, &v, to, tokens, table, &axes, at, stream) : g_write(cache, &k, &v, to, tokens, table, at, stream),
                    a[9], a[10]);
 }
 
@@ -269,20 +303,79 @@ PyObject* py_kv_attend(PyObject*, PyObject* const* a, Py_ssize_t n) {
                    a[3], a[4]);
 }
 
-// bind(BcpError, addresses of bcp_rope, bcp_kv_write, bcp_kv_read, bcp_kv_attend, bcp_last_error)
+// Rows over the vocabulary [sequences, rows, vocab].
+bool vocab_rows(PyObject* o, const char* name, int device, int64_t seqs, int64_t rows, int64_t vocab, bcp_vocab_rows* r) {
+  const at::Tensor* p = tensor(o, name);
+  if (!p) return false;
+  const at::Tensor& t = *p;
+  if (!no_gradient(t, name)) return false;
+  switch (t.scalar_type()) {
+    case at::kFloat: r->type = BCP_F32; break;
+    case at::kBFloat16: r->type = BCP_BF16; break;
+    case at::kHalf: r->type = BCP_F16; break;
+    default:
+      raise(BCP_ERR_INVALID, "%s is neither float32, bfloat16 nor float16", name);
+      return false;
+  }
+  if (!on_device(t, device)) {
+    raise(BCP_ERR_INVALID, "%s is on another device", name);
+    return false;
+  }
+  if (t.dim() != 3 || t.size(0) != seqs || t.size(1) != rows || t.size(2) != vocab || (vocab > 1 && t.stride(2) != 1)) {
+    raise(BCP_ERR_MISMATCH, "%s must be of shape [%lld, %lld, %lld] with contiguous rows", name, (long long)seqs, (long long)rows, (long long)vocab);
+    return false;
+  }
+  static char empty[16] __attribute__((aligned(16)));  // what a tensor without elements points to is not read
+  r->data = t.numel() ? t.data_ptr() : empty;
+  r->seq_stride = seqs > 1 ? t.stride(0) : 0, r->row_stride = rows > 1 ? t.stride(1) : 0;
+  r->reserved = 0;
+  return true;
+}
+
+// verify(target, draft or None, drafts, uniform, temperature or None, probabilities, tokens, accepted, stream)
+PyObject* py_verify(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  if (!arguments(n, 9)) return nullptr;
+  int device;
+  if (!device_of(a[0], "target", &device)) return nullptr;
+  const at::Tensor& z = THPVariable_Unpack(a[0]);
+  if (z.dim() != 3 || z.size(1) < 1) return raise(BCP_ERR_INVALID, "target must be [sequences, drafts + 1, vocabulary]");
+  const int64_t seqs = z.size(0), drafts = z.size(1) - 1, vocab = z.size(2);
+  if (seqs > 0x7fffffff || drafts > int64_t(BCP_MAX_DRAFTS) || vocab > int64_t(BCP_MAX_VOCAB))
+    return raise(BCP_ERR_INVALID, "%lld sequences of %lld drafts and a vocabulary of %lld; at most %u drafts and %u tokens", (long long)seqs,
+                 (long long)drafts, (long long)vocab, BCP_MAX_DRAFTS, BCP_MAX_VOCAB);
+  bcp_vocab_rows target, draft;
+  const bool certain = a[1] == Py_None;
+  if (!vocab_rows(a[0], "target", device, seqs, drafts + 1, vocab, &target)) return nullptr;
+  if (!certain && !vocab_rows(a[1], "draft", device, seqs, drafts, vocab, &draft)) return nullptr;
+  void* const x = index(a[2], "drafts", device, at::kLong, seqs, drafts);
+  void* const u = x ? index(a[3], "uniform", device, at::kFloat, seqs, drafts + 1) : nullptr;
+  void* const t = u && a[4] != Py_None ? index(a[4], "temperature", device, at::kFloat, seqs) : nullptr;
+  if (!u || (a[4] != Py_None && !t)) return nullptr;
+  void* const tokens = index(a[6], "out", device, at::kLong, seqs, drafts + 1);
+  void* const accepted = tokens ? index(a[7], "accepted", device, at::kInt, seqs) : nullptr;
+  const int probabilities = PyObject_IsTrue(a[5]);
+  void* stream;
+  if (!accepted || probabilities < 0 || !stream_of(a[8], device, &stream)) return nullptr;
+  return result_in(g_verify(&target, certain ? nullptr : &draft, uint32_t(seqs), uint32_t(drafts), uint32_t(vocab), static_cast<const int64_t*>(x),
+                            static_cast<const float*>(u), static_cast<const float*>(t), probabilities, static_cast<int64_t*>(tokens),
+                            static_cast<int32_t*>(accepted), stream),
+                   a[6], a[7]);
+}
+
+// bind(BcpError, addresses of bcp_rope, bcp_rope_axes, bcp_kv_write, bcp_kv_write_axes, bcp_kv_read, bcp_kv_attend, bcp_verify_drafts,
+// bcp_last_error)
 PyObject* py_bind(PyObject*, PyObject* const* a, Py_ssize_t n) {
-  if (!arguments(n, 6)) return nullptr;
-  void* f[5];
-  for (int i = 0; i < 5; ++i) f[i] = PyLong_AsVoidPtr(a[i + 1]);
+  constexpr int kCalls = 8;
+  if (!arguments(n, 1 + kCalls)) return nullptr;
+  void* f[kCalls];
+  for (int i = 0; i < kCalls; ++i) f[i] = PyLong_AsVoidPtr(a[i + 1]);
   if (PyErr_Occurred()) return nullptr;
   Py_INCREF(a[0]);
   Py_XDECREF(g_error);
   g_error = a[0];
-  g_rope = reinterpret_cast<decltype(g_rope)>(f[0]);
-  g_write = reinterpret_cast<decltype(g_write)>(f[1]);
-  g_read = reinterpret_cast<decltype(g_read)>(f[2]);
-  g_attend = reinterpret_cast<decltype(g_attend)>(f[3]);
-  g_last_error = reinterpret_cast<decltype(g_last_error)>(f[4]);
+  int i = 0;
+  auto next = [&](auto& call) { call = reinterpret_cast<std::remove_reference_t<decltype(call)>>(f[i++]); };
+  next(g_rope), next(g_rope_axes), next(g_write), next(g_write_axes), next(g_read), next(g_attend), next(g_verify), next(g_last_error);
   Py_RETURN_NONE;
 }
 
@@ -302,7 +395,8 @@ constexpr PyMethodDef method(const char* name) {
 }
 
 PyMethodDef g_methods[] = {method<py_bind>("bind"),       method<py_rope>("rope"),           method<py_kv_write>("kv_write"),
-                           method<py_kv_read>("kv_read"), method<py_kv_attend>("kv_attend"), {nullptr, nullptr, 0, nullptr}};
+                           method<py_kv_read>("kv_read"), method<py_kv_attend>("kv_attend"),
+                           method<py_verify>("verify"), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "_binding", nullptr, -1, g_methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

@@ -174,10 +174,79 @@ __device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
   return r;
 }
 
+// The positions of a token: one, or (AXES) one for each axis.
+struct AxisMap {
+  uint32_t w[BCP_MAX_HEAD_DIM / 2 / 16] = {};  // two bits for each pair: its axis
+  uint32_t n_axes = 1;
+  int64_t stride = 0;  // positions of axis a begin at a * stride
+};
+template <bool AXES>
+struct At {
+  int64_t p[AXES ? BCP_MAX_AXES : 1];
+  bool inside, padding;  // all positions are rows of the table; one is negative
+  __device__ __forceinline__ void load(const int64_t* positions, uint32_t t, int64_t n_positions, const AxisMap& m) {
+    p[0] = positions[t];
+    if constexpr (AXES) {
+#pragma unroll
+      for (uint32_t a = 1; a < BCP_MAX_AXES; ++a) p[a] = a < m.n_axes ? positions[a * m.stride + t] : p[0];
+    }
+    inside = true, padding = false;
+#pragma unroll
+    for (int a = 0; a < int(sizeof p / sizeof p[0]); ++a) {
+      padding |= p[a] < 0;
+      inside &= p[a] >= 0 && p[a] < n_positions;
+    }
+    if (!inside) {
+#pragma unroll
+      for (int a = 0; a < int(sizeof p / sizeof p[0]); ++a) p[a] = 0;
+    }
+  }
+  __device__ __forceinline__ int64_t of(uint32_t axis) const {
+    if constexpr (AXES) return axis < 2 ? (axis ? p[1] : p[0]) : (axis == 2 ? p[2] : p[3]);
+    return p[0];
+  }
+};
+
 // Cosines and sines of a chunk's V pairs.
 template <int V, bool VEC, bool PAIRS>
 struct Angles {
   float c[V], s[V];
+  __device__ __forceinline__ void load(const float* table, const At<false>& at, uint32_t rot_dim, const Chunk& k, float sign, const AxisMap&) {
+    load(table, at.p[0], rot_dim, k, sign);
+  }
+  // Each pair from the row of its axis.  V / 2 neighbouring pairs of one axis, as in parts of a multiple of that, are loaded as
+  // vectors; where axes take turns, element by element.
+  __device__ __forceinline__ void load(const float* table, const At<true>& at, uint32_t rot_dim, const Chunk& k, float sign, const AxisMap& m) {
+    const uint32_t pairs = rot_dim / 2;
+    if (VEC) {
+#pragma unroll
+      for (int half = 0; half < 2; ++half) {
+        constexpr uint32_t kAll = (1u << V) - 1, kOnes = 0x55555555u & kAll;  // two bits for each of V / 2 pairs
+        const uint32_t from = half ? (PAIRS ? k.pair2 : k.pair + V / 2) : k.pair, axes = m.w[from / 16] >> (2 * (from % 16)) & kAll;
+        if (axes == (axes & 3) * kOnes) {
+          const float* const row = table + at.of(axes & 3) * rot_dim;
+          part(row, row + pairs, from, half * (V / 2));
+        } else {
+#pragma unroll
+          for (int i = 0; i < V / 2; ++i) {
+            const float* const e = table + at.of(axes >> (2 * i) & 3) * rot_dim + from + i;
+            c[half * (V / 2) + i] = e[0], s[half * (V / 2) + i] = e[pairs];
+          }
+        }
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < V; ++i) {
+        const bool in = uint32_t(i) < k.n_lo;
+        const uint32_t pair = in ? k.pair + i : 0;
+        const float* const e = table + at.of(m.w[pair / 16] >> (2 * (pair % 16)) & 3) * rot_dim + pair;
+        c[i] = in ? e[0] : 1.f;
+        s[i] = in ? e[pairs] : 0.f;
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < V; ++i) s[i] *= sign;
+  }
   __device__ __forceinline__ void load(const float* table, int64_t position, uint32_t rot_dim, const Chunk& k, float sign) {
     const uint32_t pairs = rot_dim / 2;
     const float* const row = table + position * rot_dim;
@@ -265,6 +334,7 @@ inline bool is_8bit(uint32_t t) { return t == BCP_E4M3 || t == BCP_I8; }
 bool rows_overlap(const int64_t* strides, const uint32_t* extents, int n, uint32_t row);
 int check_heads(const char* call, const char* name, const bcp_heads* h, bool written, uint32_t head_dim, int64_t n_tokens);
 int check_rope(const char* call, const bcp_rope_table* r, uint32_t head_dim);
+int check_axes(const char* call, const bcp_rope_axes_map* axes, const bcp_rope_table* r, AxisMap* out);
 int check_cache(const char* call, const bcp_kv_cache* c);
 // Whether every row of h starts on a boundary of `bytes` bytes.
 inline bool rows_aligned(const bcp_heads* h, uint32_t bytes) {

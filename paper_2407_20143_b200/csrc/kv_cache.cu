@@ -86,6 +86,7 @@ struct CacheArgs {
   int64_t n_positions;
   const int64_t* positions;
   uint32_t rot_dim, layout;
+  AxisMap axes;
 };
 
 template <int FMT>
@@ -182,7 +183,7 @@ __device__ __forceinline__ float largest(float a, float b, float c) {
   return r;
 }
 
-template <typename T, int FMT, bool VEC, bool PAIRS>
+template <typename T, int FMT, bool VEC, bool PAIRS, bool AXES>
 __global__ void __launch_bounds__(256, 4) bcp_kv_write_kernel(const CacheArgs a) {
   after_previous();
   typedef Format<FMT> F;
@@ -205,12 +206,13 @@ __global__ void __launch_bounds__(256, 4) bcp_kv_write_kernel(const CacheArgs a)
   }
   Angles<V, VEC, PAIRS> w;
   if (it.used && a.rot_dim) {  // both sides look at the position: a token is written whole or not at all
-    int64_t position = a.positions[it.t];
-    if (position < 0 || position >= a.n_positions) {
+    At<AXES> at;
+    at.load(a.positions, it.t, a.n_positions, a.axes);
+    if (!at.inside) {
       if (slot >= 0) raise(a.status, BCP_BAD_POSITION);
-      slot = -1, position = 0;
+      slot = -1;
     }
-    if (mine && k.rotated) w.load(a.table, position, rot, k, 1.f);
+    if (mine && k.rotated) w.load(a.table, at, rot, k, 1.f, a.axes);
   }
   const bool live = slot >= 0 && mine;
   const uint32_t page = a.page_size.div(uint32_t(slot >= 0 ? slot : 0)), off = uint32_t(slot >= 0 ? slot : 0) - page * a.page_size.d;
@@ -323,11 +325,15 @@ __global__ void __launch_bounds__(256) bcp_kv_read_kernel(const CacheArgs a) {
   }
 }
 
+template <typename T, int FMT, bool VEC, bool AXES>
+auto write_kernel(const CacheArgs& a) {
+  return a.layout == BCP_ROPE_PAIRS ? bcp_kv_write_kernel<T, FMT, VEC, true, AXES> : bcp_kv_write_kernel<T, FMT, VEC, false, AXES>;
+}
 template <typename T, int FMT, bool VEC>
 cudaError_t launch(bool write, const CacheArgs& a, cudaStream_t stream) {
   const uint32_t blocks = uint32_t(((uint64_t(a.n_groups) << a.lanes_log2) + 255) / 256);
   void (*kernel)(CacheArgs) = bcp_kv_read_kernel<T, FMT, VEC>;
-  if (write) kernel = a.layout == BCP_ROPE_PAIRS ? bcp_kv_write_kernel<T, FMT, VEC, true> : bcp_kv_write_kernel<T, FMT, VEC, false>;
+  if (write) kernel = a.axes.n_axes > 1 ? write_kernel<T, FMT, VEC, true>(a) : write_kernel<T, FMT, VEC, false>(a);
   return launch_early(kernel, blocks, 256, 0, stream, a);
 }
 template <typename T>
@@ -341,7 +347,7 @@ cudaError_t launch(bool write, const CacheArgs& a, uint32_t format, bool vec, cu
 }
 
 int move(const char* call, bool write, const bcp_kv_cache* c, const bcp_heads* k, const bcp_heads* v, const int64_t* slots, int64_t n_tokens,
-         const bcp_rope_table* rope, const int64_t* positions, void* stream) {
+         const bcp_rope_table* rope, bool by_axes, const bcp_rope_axes_map* axes, const int64_t* positions, void* stream) {
   if (int rc = check_cache(call, c)) return rc;
   if (n_tokens < 0 || n_tokens > 0x7fffffff) return fail(BCP_ERR_INVALID, "%s: %lld tokens", call, (long long)n_tokens);
   if (int rc = check_heads(call, "k", k, !write, c->head_dim, n_tokens)) return rc;
@@ -356,6 +362,10 @@ int move(const char* call, bool write, const bcp_kv_cache* c, const bcp_heads* k
   if (n_tokens && rope && !positions) return fail(BCP_ERR_INVALID, "%s: positions is NULL", call);
 
   CacheArgs a = {};
+  if (by_axes) {
+    if (!rope) return fail(BCP_ERR_INVALID, "%s: rope is NULL", call);
+    if (int rc = check_axes(call, axes, rope, &a.axes)) return rc;
+  }
   a.pages[0] = c->k, a.pages[1] = c->v, a.scales[0] = c->k_scale, a.scales[1] = c->v_scale;
   a.page_stride = uint32_t(c->page_stride), a.head_stride = uint32_t(c->head_stride), a.token_stride = uint32_t(c->token_stride);
   a.n_slots = c->n_pages * c->page_size, a.n_heads = c->n_heads, a.head_dim = c->head_dim;
@@ -396,11 +406,16 @@ extern "C" {
 
 int bcp_kv_write(const bcp_kv_cache* cache, const bcp_heads* k, const bcp_heads* v, const int64_t* slots, int64_t n_tokens,
                  const bcp_rope_table* rope, const int64_t* positions, void* stream) {
-  return move("bcp_kv_write", true, cache, k, v, slots, n_tokens, rope, positions, stream);
+  return move("bcp_kv_write", true, cache, k, v, slots, n_tokens, rope, false, nullptr, positions, stream);
+}
+
+int bcp_kv_write_axes(const bcp_kv_cache* cache, const bcp_heads* k, const bcp_heads* v, const int64_t* slots, int64_t n_tokens,
+                      const bcp_rope_table* rope, const bcp_rope_axes_map* axes, const int64_t* positions, void* stream) {
+  return move("bcp_kv_write_axes", true, cache, k, v, slots, n_tokens, rope, true, axes, positions, stream);
 }
 
 int bcp_kv_read(const bcp_kv_cache* cache, const int64_t* slots, int64_t n_tokens, const bcp_heads* k_out, const bcp_heads* v_out, void* stream) {
-  return move("bcp_kv_read", false, cache, k_out, v_out, slots, n_tokens, nullptr, nullptr, stream);
+  return move("bcp_kv_read", false, cache, k_out, v_out, slots, n_tokens, nullptr, false, nullptr, nullptr, stream);
 }
 
 }  // extern "C"

@@ -44,6 +44,21 @@ int check_rope(const char* call, const bcp_rope_table* r, uint32_t head_dim) {
   return BCP_OK;
 }
 
+int check_axes(const char* call, const bcp_rope_axes_map* axes, const bcp_rope_table* r, AxisMap* out) {
+  if (!axes || !axes->axis_of_pair) return fail(BCP_ERR_INVALID, "%s: axes or their pairs are NULL", call);
+  if (!axes->n_axes || axes->n_axes > BCP_MAX_AXES) return fail(BCP_ERR_INVALID, "%s: %u axes; 1 to %u expected", call, axes->n_axes, BCP_MAX_AXES);
+  if (axes->reserved) return fail(BCP_ERR_INVALID, "%s: reserved field of the axes is not 0", call);
+  if (axes->n_axes > 1 && (axes->axis_stride < 0 || axes->axis_stride > (int64_t(1) << 40)))
+    return fail(BCP_ERR_INVALID, "%s: a stride of %lld between the axes' positions", call, (long long)axes->axis_stride);
+  *out = AxisMap();
+  out->n_axes = axes->n_axes, out->stride = axes->n_axes > 1 ? axes->axis_stride : 0;
+  for (uint32_t i = 0; i < r->rot_dim / 2; ++i) {
+    if (axes->axis_of_pair[i] >= axes->n_axes) return fail(BCP_ERR_INVALID, "%s: pair %u goes by axis %u of %u", call, i, axes->axis_of_pair[i], axes->n_axes);
+    out->w[i / 16] |= uint32_t(axes->axis_of_pair[i]) << (2 * (i % 16));
+  }
+  return BCP_OK;
+}
+
 }  // namespace bcp
 
 namespace {
@@ -69,9 +84,10 @@ struct RopeArgs {
   int64_t n_positions;
   const int64_t* positions;
   uint32_t* status;
+  AxisMap axes;
 };
 
-template <typename T, bool VEC, bool PAIRS, int HEADS>
+template <typename T, bool VEC, bool PAIRS, int HEADS, bool AXES>
 __global__ void __launch_bounds__(256, 3) bcp_rope_kernel(const RopeArgs a) {
   after_previous();
   const uint32_t i = blockIdx.x * 256u + threadIdx.x;
@@ -80,9 +96,10 @@ __global__ void __launch_bounds__(256, 3) bcp_rope_kernel(const RopeArgs a) {
   const uint32_t g = a.per_group.div(r);
   constexpr int V = kChunk<T, VEC>;
   const Chunk k = chunk_at<V, VEC, PAIRS>(r - g * a.per_group.d, a.head_dim, a.rot_dim);
-  const int64_t position = a.positions[t];
-  const bool there = position >= 0 && position < a.n_positions;
-  if (position >= a.n_positions) raise(a.status, BCP_BAD_POSITION);
+  At<AXES> at;
+  at.load(a.positions, t, a.n_positions, a.axes);
+  const bool there = at.inside;
+  if (!there && !at.padding) raise(a.status, BCP_BAD_POSITION);
 
   const int side = g >= a.q_groups;
   const uint32_t h0 = (side ? g - a.q_groups : g) * HEADS, n = min(a.n_heads[side] - h0, uint32_t(HEADS));
@@ -93,7 +110,7 @@ __global__ void __launch_bounds__(256, 3) bcp_rope_kernel(const RopeArgs a) {
   for (int j = 0; j < HEADS; ++j, from += a.in_head[side])
     if (j < n) e[j].load(from, k);
   Angles<V, VEC, PAIRS> w;
-  if (k.rotated) w.load(a.table, there ? position : 0, a.rot_dim, k, a.sign);
+  if (k.rotated) w.load(a.table, at, a.rot_dim, k, a.sign, a.axes);
 #pragma unroll
   for (int j = 0; j < HEADS; ++j, to += a.out_head[side]) {
     if (j >= n) break;
@@ -113,25 +130,27 @@ __global__ void __launch_bounds__(256, 3) bcp_rope_kernel(const RopeArgs a) {
 
 __global__ void bcp_clear_kernel(uint32_t* status, uint32_t bits) { atomicAnd(status, ~bits); }
 
-template <typename T, bool VEC, bool PAIRS>
+template <typename T, bool VEC, bool PAIRS, bool AXES>
 cudaError_t launch(const RopeArgs& a, uint32_t heads, cudaStream_t stream) {
-  void (*kernel)(RopeArgs) = bcp_rope_kernel<T, VEC, PAIRS, 1>;
+  void (*kernel)(RopeArgs) = bcp_rope_kernel<T, VEC, PAIRS, 1, AXES>;
   if constexpr (VEC) {
-    if (heads != 1) kernel = bcp_rope_kernel<T, VEC, PAIRS, kManyHeads>;
+    if (heads != 1) kernel = bcp_rope_kernel<T, VEC, PAIRS, kManyHeads, AXES>;
   }
   return launch_early(kernel, (a.n_threads + 255) / 256, 256, 0, stream, a);
 }
-template <typename T>
+template <typename T, bool AXES>
 cudaError_t launch(const RopeArgs& a, bool vec, bool pairs, uint32_t heads, cudaStream_t stream) {
-  if (vec) return pairs ? launch<T, true, true>(a, heads, stream) : launch<T, true, false>(a, heads, stream);
-  return pairs ? launch<T, false, true>(a, heads, stream) : launch<T, false, false>(a, heads, stream);
+  if (vec) return pairs ? launch<T, true, true, AXES>(a, heads, stream) : launch<T, true, false, AXES>(a, heads, stream);
+  return pairs ? launch<T, false, true, AXES>(a, heads, stream) : launch<T, false, false, AXES>(a, heads, stream);
+}
+template <typename T>
+cudaError_t launch(const RopeArgs& a, bool vec, bool pairs, bool axes, uint32_t heads, cudaStream_t stream) {
+  return axes ? launch<T, true>(a, vec, pairs, heads, stream) : launch<T, false>(a, vec, pairs, heads, stream);
 }
 
-}  // namespace
-
-extern "C" int bcp_rope(const bcp_heads* q_in, const bcp_heads* q_out, const bcp_heads* k_in, const bcp_heads* k_out, uint32_t head_dim,
-                        int64_t n_tokens, const bcp_rope_table* rope, const int64_t* positions, int transpose, void* stream) {
-  const char* call = "bcp_rope";
+int rotate(const char* call, const bcp_heads* q_in, const bcp_heads* q_out, const bcp_heads* k_in, const bcp_heads* k_out, uint32_t head_dim,
+           int64_t n_tokens, const bcp_rope_table* rope, bool by_axes, const bcp_rope_axes_map* axes, const int64_t* positions, int transpose,
+           void* stream) {
   if (!rope) return fail(BCP_ERR_INVALID, "%s: rope is NULL", call);
   if (head_dim < 2 || head_dim > BCP_MAX_HEAD_DIM) return fail(BCP_ERR_INVALID, "%s: head_dim %u is not in 2..%u", call, head_dim, BCP_MAX_HEAD_DIM);
   if (n_tokens < 0 || n_tokens > 0x7fffffff) return fail(BCP_ERR_INVALID, "%s: %lld tokens", call, (long long)n_tokens);
@@ -152,6 +171,9 @@ extern "C" int bcp_rope(const bcp_heads* q_in, const bcp_heads* q_out, const bcp
   if (n_tokens && !positions) return fail(BCP_ERR_INVALID, "%s: positions is NULL", call);
 
   RopeArgs a = {};
+  if (by_axes) {
+    if (int rc = check_axes(call, axes, rope, &a.axes)) return rc;
+  }
   bool vec = head_dim % 16 == 0 && rope->rot_dim % 16 == 0;
   for (int s = 0; s < 2; ++s) {
     a.in_token[s] = uint32_t(in[s]->token_stride), a.in_head[s] = uint32_t(in[s]->head_stride);
@@ -183,11 +205,24 @@ extern "C" int bcp_rope(const bcp_heads* q_in, const bcp_heads* q_out, const bcp
     }
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     const bool pairs = rope->layout == BCP_ROPE_PAIRS;
-    if (q_in->type == BCP_F32) BCP_CUDA(launch<float>(a, vec, pairs, heads, st));
-    if (q_in->type == BCP_BF16) BCP_CUDA(launch<__nv_bfloat16>(a, vec, pairs, heads, st));
-    if (q_in->type == BCP_F16) BCP_CUDA(launch<__half>(a, vec, pairs, heads, st));
+    if (q_in->type == BCP_F32) BCP_CUDA(launch<float>(a, vec, pairs, a.axes.n_axes > 1, heads, st));
+    if (q_in->type == BCP_BF16) BCP_CUDA(launch<__nv_bfloat16>(a, vec, pairs, a.axes.n_axes > 1, heads, st));
+    if (q_in->type == BCP_F16) BCP_CUDA(launch<__half>(a, vec, pairs, a.axes.n_axes > 1, heads, st));
   }
   return BCP_OK;
+}
+
+}  // namespace
+
+extern "C" int bcp_rope(const bcp_heads* q_in, const bcp_heads* q_out, const bcp_heads* k_in, const bcp_heads* k_out, uint32_t head_dim,
+                        int64_t n_tokens, const bcp_rope_table* rope, const int64_t* positions, int transpose, void* stream) {
+  return rotate("bcp_rope", q_in, q_out, k_in, k_out, head_dim, n_tokens, rope, false, nullptr, positions, transpose, stream);
+}
+
+extern "C" int bcp_rope_axes(const bcp_heads* q_in, const bcp_heads* q_out, const bcp_heads* k_in, const bcp_heads* k_out, uint32_t head_dim,
+                             int64_t n_tokens, const bcp_rope_table* rope, const bcp_rope_axes_map* axes, const int64_t* positions, int transpose,
+                             void* stream) {
+  return rotate("bcp_rope_axes", q_in, q_out, k_in, k_out, head_dim, n_tokens, rope, true, axes, positions, transpose, stream);
 }
 
 extern "C" int bcp_decode_status(uint32_t* status, void* stream_) {

@@ -36,7 +36,7 @@ from .api import ERR_INVALID, BcpError, _check
 F32, BF16, F16, E4M3, I8 = 1, 2, 3, 4, 5
 ROPE_HALF, ROPE_PAIRS = 0, 1
 BAD_POSITION, BAD_SLOT, BAD_PAGE, BAD_LENGTH = 1, 2, 4, 8
-MAX_HEAD_DIM = 256
+MAX_HEAD_DIM, MAX_AXES = 256, 4
 _LAYOUTS = {"half": ROPE_HALF, "pairs": ROPE_PAIRS}
 
 _FORMATS = {torch.bfloat16: BF16, torch.float16: F16, torch.float8_e4m3fn: E4M3, torch.int8: I8}
@@ -48,7 +48,8 @@ def _load_binding():
     loader = importlib.machinery.ExtensionFileLoader(__package__ + "._binding", path)
     module = importlib.util.module_from_spec(importlib.util.spec_from_file_location(loader.name, path, loader=loader))
     loader.exec_module(module)
-    calls = ("bcp_rope", "bcp_kv_write", "bcp_kv_read", "bcp_kv_attend", "bcp_last_error")
+    calls = ("bcp_rope", "bcp_rope_axes", "bcp_kv_write", "bcp_kv_write_axes", "bcp_kv_read", "bcp_kv_attend",
+             "bcp_verify_drafts", "bcp_last_error")
     module.bind(BcpError, *(C.cast(getattr(L.lib(), name), C.c_void_p).value for name in calls))
     return module
 
@@ -120,10 +121,23 @@ def rope_frequencies(rot_dim: int, base: float = 10000.0, *, scaling: Optional[s
     raise _invalid(f"scaling {scaling!r}: None, 'linear', 'base' or 'bands' expected")
 
 
-class RopeTable:
-    """Cosines and sines for bcp_rope and bcp_kv_write, over a float32 tensor [positions, 2, rot_dim / 2]."""
+def rope_axes(pairs: Sequence[int], interleaved: bool = False) -> Sequence[int]:
+    """The axis of every pair, for RopeTable: pairs[a] pairs go by axis a, one axis after the other, or (interleaved) dealt out in
+    turn as long as an axis has pairs left."""
+    pairs = list(pairs)
+    if not 1 <= len(pairs) <= MAX_AXES or any(n < 1 for n in pairs):
+        raise _invalid(f"pairs of axes {pairs}: 1 to {MAX_AXES} numbers above 0 expected")
+    if interleaved:
+        return [a for turn in range(max(pairs)) for a, n in enumerate(pairs) if turn < n]
+    return [a for a, n in enumerate(pairs) for _ in range(n)]
 
-    def __init__(self, table, layout: str = "half"):
+
+class RopeTable:
+    """Cosines and sines for bcp_rope and bcp_kv_write, over a float32 tensor [positions, 2, rot_dim / 2].  With `axes`, an axis for
+    every pair (rope_axes makes such lists), a token has a position for each axis: the calls then take positions [axes, tokens] (int64,
+    contiguous rows), and pair i goes by the one on axis axes[i]."""
+
+    def __init__(self, table, layout: str = "half", axes: Optional[Sequence[int]] = None):
         if layout not in _LAYOUTS:
             raise _invalid(f"layout {layout!r}: 'half' or 'pairs' expected")
         if table.dtype != torch.float32 or table.dim() != 3 or table.shape[1] != 2 or not table.is_contiguous() or not table.is_cuda:
@@ -133,18 +147,33 @@ class RopeTable:
         self.tensors = (table, self.status)
         self.c = L.RopeTableC(table.data_ptr(), table.shape[0], 2 * table.shape[2], _LAYOUTS[layout], self.status.data_ptr())
         self.address = C.addressof(self.c)
+        self.axes, self.axes_address = None, None
+        if axes is not None:
+            self.axes = tuple(axes)
+            if len(self.axes) != table.shape[2] or not all(a in range(MAX_AXES) for a in self.axes):
+                raise _invalid(f"axes {self.axes}: one from 0 to {MAX_AXES - 1} for each of {table.shape[2]} pairs expected")
+            self._of_pair = (C.c_uint8 * max(1, len(self.axes)))(*self.axes)
+            self.axes_c = L.RopeAxesC(C.addressof(self._of_pair), 0, 1 + max(self.axes, default=0), 0)
+            self.axes_address = C.addressof(self.axes_c)
 
     @classmethod
     def build(cls, frequencies: Sequence[float], n_positions: int, *, layout: str = "half", attention_factor: float = 1.0,
-              device="cuda") -> "RopeTable":
-        """Table of attention_factor * cos / sin of position * frequency, computed in 64 bits, rounded once."""
+              device="cuda", axes: Optional[Sequence[int]] = None) -> "RopeTable":
+        """Table of attention_factor * cos / sin of position * frequency, computed in 64 bits, rounded once.  The pairs of an axis may have
+        frequencies of their own: frequencies[i] is pair i's, whatever axis it goes by."""
         f = torch.tensor(list(frequencies), dtype=torch.float64, device=device)
         angle = torch.arange(n_positions, dtype=torch.float64, device=device)[:, None] * f
-        return cls((torch.stack([angle.cos(), angle.sin()], 1) * attention_factor).float(), layout)
+        return cls((torch.stack([angle.cos(), angle.sin()], 1) * attention_factor).float(), layout, axes)
 
     def check(self, stream=None) -> None:
         """Waits for `stream`; raises BcpError (ERR_BOUNDS) if a call met a position outside the table."""
         _check_status(self.status, stream)
+
+
+def _axes_of(table) -> tuple:
+    """What the binding takes besides, where a table has axes."""
+    axes = getattr(table, "axes_address", None)
+    return () if axes is None else (axes,)
 
 
 def _rope(x, table: RopeTable, positions, out, transpose: bool, stream):
@@ -153,7 +182,7 @@ def _rope(x, table: RopeTable, positions, out, transpose: bool, stream):
             out = _empty(x, x.shape, x.dtype, stream)
         elif not isinstance(out, torch.Tensor):
             out, = out
-        _b.rope(table.address, table.device, x, None, out, None, positions, transpose, _raw(stream))
+        _b.rope(table.address, table.device, x, None, out, None, positions, transpose, _raw(stream), *_axes_of(table))
         if stream is not None:
             _record(stream, x, out, positions, *table.tensors)
         return out
@@ -162,15 +191,15 @@ def _rope(x, table: RopeTable, positions, out, transpose: bool, stream):
     q, k = x
     if out is None:
         out = (_empty(q, q.shape, q.dtype, stream), _empty(k, k.shape, k.dtype, stream))
-    _b.rope(table.address, table.device, q, k, out[0], out[1], positions, transpose, _raw(stream))
+    _b.rope(table.address, table.device, q, k, out[0], out[1], positions, transpose, _raw(stream), *_axes_of(table))
     if stream is not None:
         _record(stream, q, k, *out, positions, *table.tensors)
     return out
 
 
 def bcp_rope(x, table: RopeTable, positions, out=None, stream=None):
-    """x [tokens, heads, head_dim], or a pair (queries, keys), rotated by the tokens' positions (int64 [tokens]; negative:
-    zeros).  `out` may be x itself.  Returns the output, or the pair of them."""
+    """x [tokens, heads, head_dim], or a pair (queries, keys), rotated by the tokens' positions (int64 [tokens], or [axes, tokens]
+    with a table that has axes; negative: zeros).  `out` may be x itself.  Returns the output, or the pair of them."""
     return _rope(x, table, positions, out, False, stream)
 
 
@@ -281,11 +310,11 @@ class KvCache:
 
 def bcp_kv_write(cache: KvCache, k, v, slots, rope: Optional[RopeTable] = None, positions=None, stream=None) -> None:
     """k, v [tokens, heads, head_dim] into their slots (int64 [tokens]; negative: skipped); with `rope`, the keys are rotated
-    by positions (int64 [tokens]) on the way."""
+    by positions (int64 [tokens], or [axes, tokens] with a table that has axes) on the way."""
     if rope is None:
         _b.kv_write(cache.address, cache.device, k, v, slots, None, cache.device, positions, _raw(stream), cache.k, cache.v)
     else:
-        _b.kv_write(cache.address, cache.device, k, v, slots, rope.address, rope.device, positions, _raw(stream), cache.k, cache.v)
+        _b.kv_write(cache.address, cache.device, k, v, slots, rope.address, rope.device, positions, _raw(stream), cache.k, cache.v, *_axes_of(rope))
     if stream is not None:
         _record(stream, k, v, slots, positions, *cache.tensors, *(() if rope is None else rope.tensors))
 
@@ -334,3 +363,24 @@ def bcp_kv_attend(cache: KvCache, q, block_table, lengths, scale: Optional[float
         _record(stream, q, out, lse, block_table, lengths, workspace.memory, *cache.tensors)
     return out, lse
 
+
+
+# ------------------------------------------------------------------ drafted tokens
+def bcp_verify_drafts(target, drafts, uniform, draft=None, temperature=None, probabilities: bool = False, out=None, accepted=None, stream=None):
+    """Drafts (int64 [sequences, n]; the first negative one of a sequence ends its drafts) verified against target [sequences, n + 1, vocabulary],
+    logits or (probabilities=True) weights, from random numbers uniform (float32 [sequences, n + 1], in [0, 1)): draft i is accepted if
+    uniform[:, i] * q < p, the next token is drawn with the last number from what p has over q at the first rejected draft, or from the row
+    behind the last one.  draft [sequences, n, vocabulary] is what the drafts were drawn from (None: they were certain); temperature
+    (float32 [sequences]; 0: greedy) goes for both.  n may be 0: the next token is sampled.
+    Returns (tokens int64 [sequences, n + 1]: the accepted drafts, the next token, then -1; accepted int32 [sequences]: how many drafts).  The
+    next token is -1 where its row has no weight or holds no number."""
+    if not isinstance(target, torch.Tensor):
+        raise _invalid("target is not a tensor")
+    if out is None:
+        out = _empty(target, target.shape[:2], torch.int64, stream)
+    if accepted is None:
+        accepted = _empty(target, target.shape[:1], torch.int32, stream)
+    _b.verify(target, draft, drafts, uniform, temperature, probabilities, out, accepted, _raw(stream))
+    if stream is not None:
+        _record(stream, target, draft, drafts, uniform, temperature, out, accepted)
+    return out, accepted
