@@ -629,6 +629,7 @@ typedef struct {
 #define BCP_BAD_SLOT 2u
 #define BCP_BAD_PAGE 4u
 #define BCP_BAD_LENGTH 8u
+#define BCP_TIMED_OUT 16u   /* a wait inside a kernel ran out (two seconds): the call's results are not to be used */
 
 /*
  * Rotates the heads of n_tokens tokens: (y1, y2) = (x1 c - x2 s, x2 c + x1 s) for every pair, with
@@ -709,6 +710,25 @@ BCP_API int bcp_kv_attend_workspace(const bcp_kv_cache* cache, uint32_t n_q_head
 BCP_API int bcp_kv_attend(const bcp_kv_cache* cache, const bcp_heads* q, const bcp_heads* out, float* lse, uint32_t n_seqs,
                           const int32_t* block_table, int64_t table_stride, uint32_t table_width, const int32_t* lengths,
                           float scale, uint32_t window, void* workspace, uint64_t workspace_bytes, void* stream);
+
+/*
+ * bcp_kv_attend for groups of sequences that share a prefix, which is read and multiplied once for all sequences of a group (samples of
+ * one prompt, questions about one document; the drafted tokens of one sequence, whose own tokens so far are the prefix).
+ * Sequences starts[g] <= b < starts[g+1] (n_prefixes + 1 numbers that do not decrease) attend over the first prefix_lengths[g] tokens of prefix g,
+ * whose pages are row g of prefix_table, and then over their own lengths[b] tokens, whose pages are row b of block_table: softmax and lse are
+ * those over both.  Sequences before starts[0] or from starts[n_prefixes] on have no prefix.  Everything else is as for bcp_kv_attend, without a
+ * window; of the prefix, weights over a bfloat16 or 8-bit cache are the sum of two bfloat16 numbers (2^-16; below 2^-86 of the largest they may count
+ * as nothing), over binary16 ones binary16.
+ * What of starts lies outside 0 .. n_seqs is cut off, and a group that ends before it starts has no sequences (BCP_BAD_LENGTH; results of sequences that two
+ * groups claim are not to be used).  Tokens whose page is outside the cache are left out (BCP_BAD_PAGE); a prefix length past prefix_width * page_size counts as that many (BCP_BAD_LENGTH).
+ * workspace: as for bcp_kv_attend, of at least bcp_kv_attend_shared_workspace bytes for n_seqs <= max_seqs; it also serves bcp_kv_attend.
+ */
+BCP_API int bcp_kv_attend_shared_workspace(const bcp_kv_cache* cache, uint32_t n_q_heads, uint32_t max_seqs, uint64_t* bytes);
+BCP_API int bcp_kv_attend_shared(const bcp_kv_cache* cache, const bcp_heads* q, const bcp_heads* out, float* lse, uint32_t n_seqs,
+                                 const int32_t* prefix_table, int64_t prefix_stride, uint32_t prefix_width,
+                                 const int32_t* prefix_lengths, const int32_t* starts, uint32_t n_prefixes,
+                                 const int32_t* block_table, int64_t table_stride, uint32_t table_width, const int32_t* lengths,
+                                 float scale, void* workspace, uint64_t workspace_bytes, void* stream);
 
 /*
  * Drafted tokens verified against a target's probabilities from given random numbers, so that what comes out is distributed as if

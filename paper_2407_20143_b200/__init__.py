@@ -4,7 +4,7 @@ from .api import (BcpError, Plan, Stager, bcp_decompose, bcp_dedup_assign, bcp_p
 
 # The decoding operators take torch tensors; torch is imported when the first of them is asked for by name, so
 # that the host-only calls (planning, layouts) load without it.  For the same reason a star import leaves them out.
-_DECODE = ("KvCache", "KvWorkspace", "RopeTable", "bcp_kv_attend", "bcp_kv_read", "bcp_kv_write", "bcp_rope", "bcp_rope_backward", "bcp_verify_drafts", "rope", "rope_axes",
+_DECODE = ("KvCache", "KvWorkspace", "RopeTable", "bcp_kv_attend", "bcp_kv_attend_shared", "bcp_kv_read", "bcp_kv_write", "bcp_rope", "bcp_rope_backward", "bcp_verify_drafts", "rope", "rope_axes",
            "rope_frequencies")
 
 __all__ = ["BcpError", "Plan", "Stager", "bcp_decompose", "bcp_dedup_assign", "bcp_pack", "bcp_pack_cache_clear", "bcp_pack_layout", "bcp_pack_static", "bcp_plan",

@@ -162,6 +162,9 @@ _PROTOS = {
     "bcp_kv_attend_workspace": (C.c_int, [_VP, C.c_uint32, C.c_uint32, C.POINTER(C.c_uint64)]),
     "bcp_kv_attend": (C.c_int, [_VP, _VP, _VP, _VP, C.c_uint32, _VP, C.c_int64, C.c_uint32, _VP, C.c_float, C.c_uint32, _VP,
                                 C.c_uint64, _VP]),
+    "bcp_kv_attend_shared_workspace": (C.c_int, [_VP, C.c_uint32, C.c_uint32, C.POINTER(C.c_uint64)]),
+    "bcp_kv_attend_shared": (C.c_int, [_VP, _VP, _VP, _VP, C.c_uint32, _VP, C.c_int64, C.c_uint32, _VP, _VP, C.c_uint32, _VP, C.c_int64, C.c_uint32, _VP,
+                                       C.c_float, _VP, C.c_uint64, _VP]),
     "bcp_verify_drafts": (C.c_int, [_VP, _VP, C.c_uint32, C.c_uint32, C.c_uint32, _VP, _VP, _VP, C.c_int, _VP, _VP, _VP]),
     "bcp_decode_status": (C.c_int, [_VP, _VP]),
     "bcp_pack_static": (C.c_int, [C.POINTER(_VP), C.POINTER(PackMetaC), C.c_size_t, _VP, C.c_uint64, _VP]),

@@ -13,8 +13,8 @@ CSRC = os.path.join(HERE, "csrc")
 INCLUDE = os.path.join(os.path.dirname(HERE), "include")
 LIB = os.path.join(HERE, "libbcp.so")
 SOURCES = ["planner.cpp", "units.cpp", "api.cu", "plan_image.cu", "host_path.cu", "kernels.cu", "tma_kernel.cu", "convert_kernel.cu", "static_pack.cu", "stager.cu", "export.cu", "ipc.cu",
-           "rope.cu", "kv_cache.cu", "kv_attend.cu", "verify.cu"]
-HEADERS = ["plan.hpp", "kernels.cuh", "host_threads.hpp", "plan_object.hpp", "tma_ptx.cuh", "copy_loops.cuh", "decode.cuh"]
+           "rope.cu", "kv_cache.cu", "kv_attend.cu", "kv_prefix.cu", "verify.cu"]
+HEADERS = ["plan.hpp", "kernels.cuh", "host_threads.hpp", "plan_object.hpp", "tma_ptx.cuh", "copy_loops.cuh", "decode.cuh", "attend.cuh"]
 
 
 BINDING = os.path.join(CSRC, "binding.cpp")

@@ -14,6 +14,7 @@
 
 #include <cstdarg>
 #include <cstdio>
+#include <string>
 #include <type_traits>
 
 #include "bcp.h"
@@ -26,6 +27,7 @@ decltype(&bcp_kv_write) g_write;
 decltype(&bcp_kv_write_axes) g_write_axes;
 decltype(&bcp_kv_read) g_read;
 decltype(&bcp_kv_attend) g_attend;
+decltype(&bcp_kv_attend_shared) g_shared;
 decltype(&bcp_verify_drafts) g_verify;
 decltype(&bcp_last_error) g_last_error;
 PyObject* g_error;  // BcpError
@@ -303,6 +305,60 @@ PyObject* py_kv_attend(PyObject*, PyObject* const* a, Py_ssize_t n) {
                    a[3], a[4]);
 }
 
+// A block table: int32 rows, contiguous; what a table without columns points to is not read.
+struct Table {
+  const int32_t* data;
+  int64_t stride;
+  uint32_t width;
+};
+bool block_table(PyObject* o, const char* name, int device, int64_t rows, Table* out) {
+  static int32_t no_pages[1];
+  const at::Tensor* const t = tensor(o, name);
+  if (!t) return false;
+  if (t->dim() != 2 || (rows >= 0 && t->size(0) != rows) || t->scalar_type() != at::kInt || !on_device(*t, device) ||
+      (t->size(1) > 1 && t->stride(1) != 1) || t->size(0) > 0x7fffffff || t->size(1) > 0x7fffffff) {
+    raise(BCP_ERR_INVALID, "%s must be an int32 tensor [%s, width] on cuda:%d with contiguous rows", name,
+          rows >= 0 ? std::to_string(rows).c_str() : "prefixes", device);
+    return false;
+  }
+  out->data = t->numel() ? static_cast<const int32_t*>(t->data_ptr()) : no_pages;
+  out->stride = t->size(0) > 1 ? t->stride(0) : t->size(1);
+  out->width = uint32_t(t->size(1));
+  return true;
+}
+
+// kv_attend_shared(cache, cache device, q, out, lse, prefix_table, prefix_lengths, starts, block_table, lengths, scale, workspace, its bytes,
+// its device, stream)
+PyObject* py_kv_attend_shared(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  if (!arguments(n, 15)) return nullptr;
+  const bcp_kv_cache* cache = static_cast<const bcp_kv_cache*>(PyLong_AsVoidPtr(a[0]));
+  int device;
+  if (!device_of(a[2], "q", &device) || !same_device(device, a[1], "the cache") || !same_device(device, a[13], "the workspace")) return nullptr;
+  const at::Tensor& t = THPVariable_Unpack(a[2]);
+  if (t.dim() != 3) return raise(BCP_ERR_INVALID, "q has %d dimensions; [sequences, heads, head_dim] expected", int(t.dim()));
+  const int64_t seqs = t.size(0);
+  if (seqs > 0x7fffffff) return raise(BCP_ERR_INVALID, "%lld sequences", (long long)seqs);
+  bcp_heads q, out;
+  if (!heads(a[2], "q", device, seqs, cache->head_dim, &q) || !heads(a[3], "out", device, seqs, cache->head_dim, &out)) return nullptr;
+  void* const lse = index(a[4], "lse", device, at::kFloat, seqs, t.size(1));
+  Table prefix, own;
+  if (!lse || !block_table(a[5], "prefix_table", device, -1, &prefix) || !block_table(a[8], "block_table", device, seqs, &own)) return nullptr;
+  const int64_t prefixes = THPVariable_Unpack(a[5]).size(0);
+  void* const prefix_lengths = index(a[6], "prefix_lengths", device, at::kInt, prefixes);
+  void* const starts = prefix_lengths ? index(a[7], "starts", device, at::kInt, prefixes + 1) : nullptr;
+  void* const lengths = starts ? index(a[9], "lengths", device, at::kInt, seqs) : nullptr;
+  if (!lengths) return nullptr;
+  const double scale = PyFloat_AsDouble(a[10]);
+  const uint64_t bytes = PyLong_AsUnsignedLongLong(a[12]);
+  if (PyErr_Occurred()) return nullptr;
+  void* stream;
+  if (!stream_of(a[14], device, &stream)) return nullptr;
+  return result_in(g_shared(cache, &q, &out, static_cast<float*>(lse), uint32_t(seqs), prefix.data, prefix.stride, prefix.width,
+                            static_cast<const int32_t*>(prefix_lengths), static_cast<const int32_t*>(starts), uint32_t(prefixes), own.data, own.stride,
+                            own.width, static_cast<const int32_t*>(lengths), float(scale), PyLong_AsVoidPtr(a[11]), bytes, stream),
+                   a[3], a[4]);
+}
+
 // Rows over the vocabulary [sequences, rows, vocab].
 bool vocab_rows(PyObject* o, const char* name, int device, int64_t seqs, int64_t rows, int64_t vocab, bcp_vocab_rows* r) {
   const at::Tensor* p = tensor(o, name);
@@ -362,10 +418,10 @@ PyObject* py_verify(PyObject*, PyObject* const* a, Py_ssize_t n) {
                    a[6], a[7]);
 }
 
-// bind(BcpError, addresses of bcp_rope, bcp_rope_axes, bcp_kv_write, bcp_kv_write_axes, bcp_kv_read, bcp_kv_attend, bcp_verify_drafts,
-// bcp_last_error)
+// bind(BcpError, addresses of bcp_rope, bcp_rope_axes, bcp_kv_write, bcp_kv_write_axes, bcp_kv_read, bcp_kv_attend,
+// bcp_kv_attend_shared, bcp_verify_drafts, bcp_last_error)
 PyObject* py_bind(PyObject*, PyObject* const* a, Py_ssize_t n) {
-  constexpr int kCalls = 8;
+  constexpr int kCalls = 9;
   if (!arguments(n, 1 + kCalls)) return nullptr;
   void* f[kCalls];
   for (int i = 0; i < kCalls; ++i) f[i] = PyLong_AsVoidPtr(a[i + 1]);
@@ -375,7 +431,7 @@ PyObject* py_bind(PyObject*, PyObject* const* a, Py_ssize_t n) {
   g_error = a[0];
   int i = 0;
   auto next = [&](auto& call) { call = reinterpret_cast<std::remove_reference_t<decltype(call)>>(f[i++]); };
-  next(g_rope), next(g_rope_axes), next(g_write), next(g_write_axes), next(g_read), next(g_attend), next(g_verify), next(g_last_error);
+  next(g_rope), next(g_rope_axes), next(g_write), next(g_write_axes), next(g_read), next(g_attend), next(g_shared), next(g_verify), next(g_last_error);
   Py_RETURN_NONE;
 }
 
@@ -396,7 +452,7 @@ constexpr PyMethodDef method(const char* name) {
 
 PyMethodDef g_methods[] = {method<py_bind>("bind"),       method<py_rope>("rope"),           method<py_kv_write>("kv_write"),
                            method<py_kv_read>("kv_read"), method<py_kv_attend>("kv_attend"),
-                           method<py_verify>("verify"), {nullptr, nullptr, 0, nullptr}};
+                           method<py_kv_attend_shared>("kv_attend_shared"), method<py_verify>("verify"), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "_binding", nullptr, -1, g_methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

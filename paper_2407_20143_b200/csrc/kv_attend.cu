@@ -35,15 +35,13 @@
 // heads, 64 ragged sequences: 27 / 38 / 62 us for 84 MB (row tiles); 2 under 16 each with 256 dimensions 113 us for 0.34 GB, 62 under 8.
 #include <mutex>
 
-#include "decode.cuh"
+#include "attend.cuh"
 
 using namespace bcp;
 
 namespace {
 
 constexpr int kWarps = 4, kTok = 16, kStep = kWarps * kTok;  // tokens per warp and per step of a CTA
-constexpr float kNone = -3.0e38f;                             // reference before the first token: below every score
-constexpr float kLog2e = 1.4426950408889634f;
 
 struct AttendArgs {
   const void *k, *v;
@@ -66,6 +64,7 @@ struct AttendArgs {
   uint32_t* part_count;   // two per part: parts that have arrived, at the place of a unit's first part in a group
   uint32_t* group_count;  // two per part: groups that have arrived, at the place of the unit's first part
   float* parts;          // two places per part: sums, then references, then denominators
+  Prior prior;           // what a shared prefix has left to join (PRIOR)
 };
 
 // Steps that a unit counts for besides its own.  Microseconds with 0 / 1 / 2 / 3: 64 ragged sequences of up to 4k tokens,
@@ -74,29 +73,6 @@ struct AttendArgs {
 constexpr uint32_t kExtra = 2;
 
 constexpr uint32_t kGroup = 64;  // parts that are joined at once
-// The line of n steps is dealt out to the parts as evenly as whole steps allow.  (Fewer than 2^31 steps: the host
-// refuses more.)
-struct Cuts {
-  uint32_t n, each, longer;  // steps of the line, of a part; the first `longer` parts have one more
-  uint32_t parts;
-  __device__ __forceinline__ void cut(uint32_t steps, uint32_t ctas) {
-    // A line of a few steps per CTA is cut into parts of whole, equal numbers of them: the longest part decides, and
-    // fewer parts are joined sooner (one sequence of 3000 tokens 13.5 us, 14.5 without; of 4000 14.6 and 15.2; of 5000 14.0 and
-    // 15.2).
-    n = steps, parts = n < ctas ? n : ctas;
-    if (n > ctas && n < 4 * ctas) {
-      const uint32_t most = (n + ctas - 1) / ctas;
-      parts = (n + most - 1) / most;
-    }
-    each = n / parts, longer = n - each * parts;
-  }
-  __device__ __forceinline__ uint32_t begin(uint32_t p) const { return each * p + (p < longer ? p : longer); }
-  __device__ __forceinline__ uint32_t part_of(uint32_t x) const {  // the part that step x lies in
-    const uint32_t lower = longer * (each + 1);
-    return x < lower ? x / (each + 1) : longer + (x - lower) / each;
-  }
-};
-
 template <int FMT, int DP, int NT>
 struct Shape {
   static constexpr bool quant = FMT == BCP_E4M3 || FMT == BCP_I8;
@@ -122,39 +98,6 @@ struct Shape {
   static constexpr int SMEM = kWarps * STAGES * STAGE + kWarps * PART * 4 + 16;
 };
 
-__device__ __forceinline__ void copy16(uint32_t to, const void* from, bool on) {
-  asm volatile("cp.async.cg.shared.global.L2::128B [%0], [%1], 16, %2;" ::"r"(to), "l"(from), "r"(on ? 16 : 0) : "memory");
-}
-__device__ __forceinline__ void copy4(uint32_t to, const void* from, bool on) {
-  asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(to), "l"(from), "r"(on ? 4 : 0) : "memory");
-}
-__device__ __forceinline__ void copies_end() { asm volatile("cp.async.commit_group;" ::: "memory"); }
-template <int N>
-__device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
-
-__device__ __forceinline__ float exp2_fast(float x) {
-  float y;
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-  return y;
-}
-__device__ __forceinline__ float log2_fast(float x) {
-  float y;
-  asm("lg2.approx.f32 %0, %1;" : "=f"(y) : "f"(x));
-  return y;
-}
-__device__ __forceinline__ float reciprocal_fast(float x) {
-  float y;
-  asm("rcp.approx.f32 %0, %1;" : "=f"(y) : "f"(x));
-  return y;
-}
-// 2^x, x <= 0, for sums whose reference moves by x.  With scales in the exponents (WIDE) a reference can lie up to 2^247 above what
-// still counts in a denominator: that is multiplied in two steps, neither of which underflows.
-template <bool WIDE>
-struct Factor {
-  float root, all;
-  __device__ __forceinline__ explicit Factor(float x) : root(exp2_fast(WIDE ? 0.5f * x : x)), all(WIDE ? root * root : root) {}
-  __device__ __forceinline__ float denominator(float l) const { return WIDE ? l * root * root : l * root; }
-};
 __device__ __forceinline__ uint32_t transpose8x8(uint32_t x) {
   uint32_t y;
   asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
@@ -174,40 +117,6 @@ __device__ __forceinline__ void mma(float (&d)[4], const uint32_t (&a)[4], const
     asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
                  : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
                  : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b[0]), "r"(b[1]));
-}
-
-// Four 8-bit elements as two pairs of binary16, exactly.
-template <int FMT>
-__device__ __forceinline__ void widen4(uint32_t w, uint32_t& lo, uint32_t& hi) {
-  if constexpr (FMT == BCP_E4M3) {
-    asm("{\n.reg .b16 x, y;\nmov.b32 {x, y}, %2;\ncvt.rn.f16x2.e4m3x2 %0, x;\ncvt.rn.f16x2.e4m3x2 %1, y;\n}" : "=r"(lo), "=r"(hi) : "r"(w));
-  } else {
-    // bytes u = x + 128 under the exponent of 1024 read as 1024 + u; 1152 off gives x
-    const uint32_t u = w ^ 0x80808080u, a = __byte_perm(u, 0x64646464u, 0x4140), b = __byte_perm(u, 0x64646464u, 0x4342);
-    const __half2 bias = __half2half2(__ushort_as_half(0x6480));
-    const __half2 x = __hsub2(*reinterpret_cast<const __half2*>(&a), bias), y = __hsub2(*reinterpret_cast<const __half2*>(&b), bias);
-    lo = *reinterpret_cast<const uint32_t*>(&x), hi = *reinterpret_cast<const uint32_t*>(&y);
-  }
-}
-
-template <bool BF16>
-__device__ __forceinline__ uint32_t pack16(float x, float y) {
-  if constexpr (BF16) {
-    const __nv_bfloat162 p = __floats2bfloat162_rn(x, y);
-    return *reinterpret_cast<const uint32_t*>(&p);
-  } else {
-    const __half2 p = __floats2half2_rn(x, y);
-    return *reinterpret_cast<const uint32_t*>(&p);
-  }
-}
-// A positive binary32 number as the sum of a bfloat16 that is its upper half and what remains, positive as well (its last bit is
-// set): the products of both with an infinite value are that infinity.
-__device__ __forceinline__ uint32_t upper_halves(float x, float y) { return __byte_perm(__float_as_uint(x), __float_as_uint(y), 0x7632); }
-__device__ __forceinline__ float lower_half(float x) {
-  return __uint_as_float(__float_as_uint(x) | 1u) - __uint_as_float(__float_as_uint(x) & 0xffff0000u);
-}
-__device__ __forceinline__ float query_at(const void* p, int i, bool bf16) {
-  return bf16 ? __bfloat162float(static_cast<const __nv_bfloat16*>(p)[i]) : __half2float(static_cast<const __half*>(p)[i]);
 }
 
 // Where dimension d of head (column) n lies in a set of sums: eight rows of dimensions and four pairs of heads
@@ -270,7 +179,63 @@ __device__ __forceinline__ void advance(Place& p, const AttendArgs& a, uint32_t 
   if (++p.b < a.n_seqs && more) p.span = span_of(a, p.b, extra);
 }
 
-template <int FMT, int DP, int NT>
+// The sums of one row, x relative to m for the dimensions of this thread and den, joined with the records that its prefix left.  Sixteen
+// threads a row (sub: which), each with its own records to weigh; the order is that of the records.
+template <bool WIDE, int N>
+__device__ __forceinline__ void join_prior(const Prior& prior, const int4 row, uint32_t sub, uint32_t lane, float& m, float& den, float4 (&x)[N]) {
+  const uint32_t both = row.w ? 2 : 1, n = min(uint32_t(row.z), prior.parts) * both, half = 0xffffu << (lane & 16);
+  auto record = [&](uint32_t i) {
+    const uint32_t part = i / both, r = uint32_t(part ? row.y + (part - 1) * prior.apart : row.x) + (i % both) * uint32_t(row.w);
+    return r < prior.records ? r : prior.records;
+  };
+  if (!n) return;
+  float top = den > 0.f ? m : kNone;
+  for (uint32_t i = sub; i < n; i += 16) {
+    const uint32_t r = record(i);
+    if (r < prior.records) {
+      const float2 ml = __ldcg(prior.ml + r);
+      if (ml.y > 0.f) top = fmaxf(top, ml.x);
+    }
+  }
+#pragma unroll
+  for (int o = 1; o < 16; o <<= 1) top = fmaxf(top, __shfl_xor_sync(half, top, o));
+  const Factor<WIDE> own(den > 0.f ? m - top : kNone);
+  float sum = 0.f;
+#pragma unroll
+  for (int k = 0; k < N; ++k) x[k].x *= own.all, x[k].y *= own.all, x[k].z *= own.all, x[k].w *= own.all;
+  for (uint32_t i0 = 0; i0 < n; i0 += 16) {
+    float weight = 0.f;
+    uint32_t place = 0;
+    if (i0 + sub < n) {
+      const uint32_t r = record(i0 + sub);
+      if (r < prior.records) {
+        const float2 ml = __ldcg(prior.ml + r);
+        const Factor<WIDE> down(ml.y > 0.f ? ml.x - top : kNone);
+        sum += down.denominator(ml.y), weight = down.all, place = r;
+        if (ml.y != ml.y) sum = weight = ml.y;  // a NaN stays one
+      }
+    }
+    const uint32_t here = n - i0 < 16 ? n - i0 : 16;
+#pragma unroll 4
+    for (uint32_t j = 0; j < here; ++j) {
+      const float w = __shfl_sync(half, weight, (lane & 16) + j);
+      const float* const from = prior.o + uint64_t(__shfl_sync(half, place, (lane & 16) + j)) * prior.dims;
+      if (w == 0.f) continue;  // an empty record has no sums
+#pragma unroll
+      for (int k = 0; k < N; ++k) {
+        const uint32_t d = 64 * k + 4 * sub;
+        if (d >= prior.dims) break;
+        const float4 y = __ldcg(reinterpret_cast<const float4*>(from + d));
+        x[k].x += y.x * w, x[k].y += y.y * w, x[k].z += y.z * w, x[k].w += y.w * w;
+      }
+    }
+  }
+#pragma unroll
+  for (int o = 1; o < 16; o <<= 1) sum += __shfl_xor_sync(half, sum, o);
+  den = own.denominator(den) + sum, m = top;
+}
+
+template <int FMT, int DP, int NT, bool PRIOR>
 __global__ void __launch_bounds__(kWarps * 32, Shape<FMT, DP, NT>::CTAS) bcp_kv_attend_kernel(const AttendArgs a) {
   typedef Shape<FMT, DP, NT> S;
   constexpr bool kBf16 = FMT == BCP_BF16;  // type of the products; 8-bit caches are widened to binary16
@@ -741,6 +706,11 @@ __global__ void __launch_bounds__(kWarps * 32, Shape<FMT, DP, NT>::CTAS) bcp_kv_
           continue;
         }
         const uint32_t qh = h * a.group + row0 + col;
+        if constexpr (PRIOR) {
+          m -= kLift;
+          join_prior<S::quant>(a.prior, a.prior.rows[uint64_t(at.b) * (a.n_heads * a.group) + qh], sub, lane, m, den, x);
+          m += kLift;
+        }
         const float inv = den == 0.f ? 0.f : reciprocal_fast(den);  // up to 2^127, where the fast division gives zero
 #pragma unroll
         for (int i = 0; i < DP / 64; ++i) {
@@ -796,24 +766,24 @@ struct Variant {
 };
 
 template <int FMT, int DP, int NT>
-Variant variant() {
+Variant variant(bool prior) {
   typedef Shape<FMT, DP, NT> S;
-  return Variant{bcp_kv_attend_kernel<FMT, DP, NT>, S::SMEM, S::ROWS, S::PART};
+  return Variant{prior ? bcp_kv_attend_kernel<FMT, DP, NT, true> : bcp_kv_attend_kernel<FMT, DP, NT, false>, S::SMEM, S::ROWS, S::PART};
 }
 template <int FMT>
-Variant variant_of(uint32_t head_dim, uint32_t group) {
+Variant variant_of(uint32_t head_dim, uint32_t group, bool prior) {
   // Query heads of a group beyond eight take a second column block (16 rows share each key and value that
   // was read); with 256 dimensions the sums of 16 rows would not fit the registers, more rows are more units.
-  if (head_dim <= 64) return group <= 8 ? variant<FMT, 64, 1>() : variant<FMT, 64, 2>();
-  if (head_dim <= 128) return group <= 8 ? variant<FMT, 128, 1>() : variant<FMT, 128, 2>();
-  return variant<FMT, 256, 1>();
+  if (head_dim <= 64) return group <= 8 ? variant<FMT, 64, 1>(prior) : variant<FMT, 64, 2>(prior);
+  if (head_dim <= 128) return group <= 8 ? variant<FMT, 128, 1>(prior) : variant<FMT, 128, 2>(prior);
+  return variant<FMT, 256, 1>(prior);
 }
-Variant variant_of(uint32_t format, uint32_t head_dim, uint32_t group) {
+Variant variant_of(uint32_t format, uint32_t head_dim, uint32_t group, bool prior) {
   switch (format) {
-    case BCP_BF16: return variant_of<BCP_BF16>(head_dim, group);
-    case BCP_F16: return variant_of<BCP_F16>(head_dim, group);
-    case BCP_E4M3: return variant_of<BCP_E4M3>(head_dim, group);
-    default: return variant_of<BCP_I8>(head_dim, group);
+    case BCP_BF16: return variant_of<BCP_BF16>(head_dim, group, prior);
+    case BCP_F16: return variant_of<BCP_F16>(head_dim, group, prior);
+    case BCP_E4M3: return variant_of<BCP_E4M3>(head_dim, group, prior);
+    default: return variant_of<BCP_I8>(head_dim, group, prior);
   }
 }
 
@@ -852,13 +822,17 @@ int resident_ctas(const Variant& v, uint32_t* out) {
 constexpr uint64_t kCounterBytes = uint64_t(kGroup) * kGroup * 2 * 4;
 uint64_t workspace_bytes_of(uint32_t ctas, const Variant& v) { return 2 * kCounterBytes + uint64_t(ctas) * 2 * v.part_floats * 4; }
 
+}  // namespace
+
+namespace bcp {
+
 int check_group(const char* call, const bcp_kv_cache* c, uint32_t n_q_heads) {
   if (!n_q_heads || n_q_heads > 65536 || n_q_heads % c->n_heads)
     return fail(BCP_ERR_MISMATCH, "%s: %u query heads are not a multiple of %u cache heads", call, n_q_heads, c->n_heads);
   return BCP_OK;
 }
 
-}  // namespace
+}  // namespace bcp
 
 extern "C" int bcp_kv_attend_workspace(const bcp_kv_cache* cache, uint32_t n_q_heads, uint32_t max_seqs, uint64_t* bytes) {
   const char* call = "bcp_kv_attend_workspace";
@@ -866,18 +840,23 @@ extern "C" int bcp_kv_attend_workspace(const bcp_kv_cache* cache, uint32_t n_q_h
   if (int rc = check_cache(call, cache)) return rc;
   if (int rc = check_group(call, cache, n_q_heads)) return rc;
   const uint32_t group = n_q_heads / cache->n_heads;
-  const Variant v = variant_of(cache->format, cache->head_dim, group);
-  uint32_t ctas = 0;
-  if (int rc = resident_ctas(v, &ctas)) return rc;
   (void)max_seqs;  // the parts are as many as CTAs, however many sequences they come from
-  *bytes = workspace_bytes_of(ctas, v);
+  *bytes = 0;
+  for (bool prior : {false, true}) {  // for either form of the kernel
+    const Variant v = variant_of(cache->format, cache->head_dim, group, prior);
+    uint32_t ctas = 0;
+    if (int rc = resident_ctas(v, &ctas)) return rc;
+    const uint64_t n = workspace_bytes_of(ctas, v);
+    if (n > *bytes) *bytes = n;
+  }
   return BCP_OK;
 }
 
-extern "C" int bcp_kv_attend(const bcp_kv_cache* c, const bcp_heads* q, const bcp_heads* out, float* lse, uint32_t n_seqs,
-                             const int32_t* block_table, int64_t table_stride, uint32_t table_width, const int32_t* lengths, float scale,
-                             uint32_t window, void* workspace, uint64_t workspace_bytes, void* stream) {
-  const char* call = "bcp_kv_attend";
+namespace bcp {
+
+int attend(const char* call, const bcp_kv_cache* c, const bcp_heads* q, const bcp_heads* out, float* lse, uint32_t n_seqs, const int32_t* block_table,
+           int64_t table_stride, uint32_t table_width, const int32_t* lengths, float scale, uint32_t window, void* workspace, uint64_t workspace_bytes,
+           const Prior* prior, bool launch, void* stream) {
   if (int rc = check_cache(call, c)) return rc;
   if (int rc = check_heads(call, "q", q, false, c->head_dim, n_seqs)) return rc;
   if (int rc = check_heads(call, "out", out, true, c->head_dim, n_seqs)) return rc;
@@ -894,7 +873,7 @@ extern "C" int bcp_kv_attend(const bcp_kv_cache* c, const bcp_heads* q, const bc
   if (!(scale == scale) || scale - scale != 0.f) return fail(BCP_ERR_INVALID, "%s: scale is not a finite number", call);
 
   const uint32_t group = q->n_heads / c->n_heads;
-  const Variant v = variant_of(c->format, c->head_dim, group);
+  const Variant v = variant_of(c->format, c->head_dim, group, prior != nullptr);
   uint32_t ctas = 0;
   if (int rc = resident_ctas(v, &ctas)) return rc;
   AttendArgs a = {};
@@ -916,6 +895,7 @@ extern "C" int bcp_kv_attend(const bcp_kv_cache* c, const bcp_heads* q, const bc
   a.q_is_bf16 = q->type == BCP_BF16, a.group = group, a.n_seqs = n_seqs;
   a.block_table = block_table, a.table_stride = table_stride, a.lengths = lengths;
   a.scale_log2 = scale * kLog2e, a.window = window;
+  if (prior) a.prior = *prior;
   char* const w = static_cast<char*>(workspace);
   a.part_count = reinterpret_cast<uint32_t*>(w);
   a.group_count = reinterpret_cast<uint32_t*>(w + kCounterBytes);
@@ -926,6 +906,15 @@ extern "C" int bcp_kv_attend(const bcp_kv_cache* c, const bcp_heads* q, const bc
   if (window && window < longest) longest = window + 15 < longest ? window + 15 : longest;
   const uint64_t most = units * (longest / kStep + 1);
   if (most + kExtra * units > 0x7fffffffull) return fail(BCP_ERR_CAPACITY, "%s: %u sequences of up to %u tokens are too many for one call", call, n_seqs, longest);
-  BCP_CUDA(launch_early(v.kernel, uint32_t(most < ctas ? most : ctas), kWarps * 32, v.smem, static_cast<cudaStream_t>(stream), a));
+  if (launch) BCP_CUDA(launch_early(v.kernel, uint32_t(most < ctas ? most : ctas), kWarps * 32, v.smem, static_cast<cudaStream_t>(stream), a));
   return BCP_OK;
+}
+
+}  // namespace bcp
+
+extern "C" int bcp_kv_attend(const bcp_kv_cache* c, const bcp_heads* q, const bcp_heads* out, float* lse, uint32_t n_seqs,
+                             const int32_t* block_table, int64_t table_stride, uint32_t table_width, const int32_t* lengths, float scale,
+                             uint32_t window, void* workspace, uint64_t workspace_bytes, void* stream) {
+  return attend("bcp_kv_attend", c, q, out, lse, n_seqs, block_table, table_stride, table_width, lengths, scale, window, workspace, workspace_bytes,
+                nullptr, true, stream);
 }

@@ -49,7 +49,7 @@ def _load_binding():
     module = importlib.util.module_from_spec(importlib.util.spec_from_file_location(loader.name, path, loader=loader))
     loader.exec_module(module)
     calls = ("bcp_rope", "bcp_rope_axes", "bcp_kv_write", "bcp_kv_write_axes", "bcp_kv_read", "bcp_kv_attend",
-             "bcp_verify_drafts", "bcp_last_error")
+             "bcp_kv_attend_shared", "bcp_verify_drafts", "bcp_last_error")
     module.bind(BcpError, *(C.cast(getattr(L.lib(), name), C.c_void_p).value for name in calls))
     return module
 
@@ -333,13 +333,14 @@ def bcp_kv_read(cache: KvCache, slots, out=None, dtype=None, stream=None):
 
 
 class KvWorkspace:
-    """Scratch memory of bcp_kv_attend for up to max_seqs sequences, zeroed on `stream`: a first use on another stream has to
+    """Scratch memory of bcp_kv_attend, and with shared=True of bcp_kv_attend_shared too, for up to max_seqs sequences, zeroed on `stream`: a first use on another stream has to
     be ordered behind that.  It serves one call at a time: calls that may overlap on the GPU (other streams without
     ordering) need a workspace each."""
 
-    def __init__(self, cache: KvCache, n_q_heads: int, max_seqs: int, stream=None):
+    def __init__(self, cache: KvCache, n_q_heads: int, max_seqs: int, stream=None, shared: bool = False):
         n = C.c_uint64()
-        _check(L.lib().bcp_kv_attend_workspace(cache.address, n_q_heads, max_seqs, C.byref(n)))
+        size = L.lib().bcp_kv_attend_shared_workspace if shared else L.lib().bcp_kv_attend_workspace
+        _check(size(cache.address, n_q_heads, max_seqs, C.byref(n)))
         with torch.cuda.stream(_torch_stream(stream, cache.k.device)):  # None: the current one
             self.memory = torch.zeros(n.value, dtype=torch.uint8, device=cache.k.device)
         self.address, self.bytes, self.device = self.memory.data_ptr(), n.value, cache.device
@@ -363,6 +364,26 @@ def bcp_kv_attend(cache: KvCache, q, block_table, lengths, scale: Optional[float
         _record(stream, q, out, lse, block_table, lengths, workspace.memory, *cache.tensors)
     return out, lse
 
+
+
+def bcp_kv_attend_shared(cache: KvCache, q, prefix_table, prefix_lengths, starts, block_table, lengths, scale: Optional[float] = None, out=None,
+                         lse=None, workspace: Optional[KvWorkspace] = None, stream=None):
+    """bcp_kv_attend for groups of sequences that share a prefix, which is read once for all of them: sequences starts[g] to starts[g + 1] - 1
+    (int32 [prefixes + 1], not decreasing) attend over the first prefix_lengths[g] (int32) tokens of the pages prefix_table[g] (int32 [prefixes,
+    width]) and then over their own first lengths[b] tokens in block_table[b].  Sequences that no group has, and groups of length 0, have no
+    prefix.  The drafted tokens of a sequence are such a group, the sequence's whole pages so far being the prefix.
+    Returns (out, lse) as bcp_kv_attend, over both parts together; `workspace` was made with shared=True."""
+    if out is None:
+        out = _empty(q, q.shape, q.dtype, stream)
+    if lse is None:
+        lse = _empty(q, q.shape[:2], torch.float32, stream)
+    if workspace is None:
+        workspace = KvWorkspace(cache, q.shape[1], q.shape[0], stream, shared=True)
+    _b.kv_attend_shared(cache.address, cache.device, q, out, lse, prefix_table, prefix_lengths, starts, block_table, lengths,
+                        cache.head_dim ** -0.5 if scale is None else scale, workspace.address, workspace.bytes, workspace.device, _raw(stream))
+    if stream is not None:
+        _record(stream, q, out, lse, prefix_table, prefix_lengths, starts, block_table, lengths, workspace.memory, *cache.tensors)
+    return out, lse
 
 
 # ------------------------------------------------------------------ drafted tokens
