@@ -99,19 +99,18 @@ __device__ __forceinline__ float query_at(const void* p, int i, bool bf16) {
   return bf16 ? __bfloat162float(static_cast<const __nv_bfloat16*>(p)[i]) : __half2float(static_cast<const __half*>(p)[i]);
 }
 
-// What attention over shared prefixes leaves for the attention over the sequences' own tokens: for every row (sequence, query head) the places
-// of its records; a record is sums relative to a reference: o = sum exp2(s - m) v and l = sum exp2(s - m).
-struct Prior {
-  const int4* rows;   // first record, the next part's, parts, from a record to the second one of the same part (0: it has one)
-  const float2* ml;   // reference and denominator of each record
-  const float* o;     // `dims` floats each
-  uint32_t dims, apart, records, parts;  // apart: records from one part to the next; records, parts: how many there can be
+// Where the attention over own tokens leaves its sums when a shared prefix is still to be joined: for every row (sequence, query head) a
+// reference and a denominator, ml = (m, l), l = sum exp2(s - m), and `dims` sums o = sum exp2(s - m) v.
+struct Records {
+  float2* ml;
+  float* o;
+  uint32_t dims;
 };
 
-// The attention over own tokens, joined with what `prior` has (csrc/kv_attend.cu).
+// The attention over own tokens (csrc/kv_attend.cu); with `records` into those, out and lse are not written.
 int attend(const char* call, const bcp_kv_cache* c, const bcp_heads* q, const bcp_heads* out, float* lse, uint32_t n_seqs, const int32_t* block_table,
            int64_t table_stride, uint32_t table_width, const int32_t* lengths, float scale, uint32_t window, void* workspace, uint64_t workspace_bytes,
-           const Prior* prior, bool launch, void* stream);  // launch false: the arguments are only looked at
+           const Records* records, bool launch, void* stream);  // launch false: the arguments are only looked at
 int check_group(const char* call, const bcp_kv_cache* c, uint32_t n_q_heads);
 
 }  // namespace bcp

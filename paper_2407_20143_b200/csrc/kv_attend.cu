@@ -64,7 +64,7 @@ struct AttendArgs {
   uint32_t* part_count;   // two per part: parts that have arrived, at the place of a unit's first part in a group
   uint32_t* group_count;  // two per part: groups that have arrived, at the place of the unit's first part
   float* parts;          // two places per part: sums, then references, then denominators
-  Prior prior;           // what a shared prefix has left to join (PRIOR)
+  Records records;       // where the sums go instead of out and lse (RECORD)
 };
 
 // Steps that a unit counts for besides its own.  Microseconds with 0 / 1 / 2 / 3: 64 ragged sequences of up to 4k tokens,
@@ -179,63 +179,7 @@ __device__ __forceinline__ void advance(Place& p, const AttendArgs& a, uint32_t 
   if (++p.b < a.n_seqs && more) p.span = span_of(a, p.b, extra);
 }
 
-// The sums of one row, x relative to m for the dimensions of this thread and den, joined with the records that its prefix left.  Sixteen
-// threads a row (sub: which), each with its own records to weigh; the order is that of the records.
-template <bool WIDE, int N>
-__device__ __forceinline__ void join_prior(const Prior& prior, const int4 row, uint32_t sub, uint32_t lane, float& m, float& den, float4 (&x)[N]) {
-  const uint32_t both = row.w ? 2 : 1, n = min(uint32_t(row.z), prior.parts) * both, half = 0xffffu << (lane & 16);
-  auto record = [&](uint32_t i) {
-    const uint32_t part = i / both, r = uint32_t(part ? row.y + (part - 1) * prior.apart : row.x) + (i % both) * uint32_t(row.w);
-    return r < prior.records ? r : prior.records;
-  };
-  if (!n) return;
-  float top = den > 0.f ? m : kNone;
-  for (uint32_t i = sub; i < n; i += 16) {
-    const uint32_t r = record(i);
-    if (r < prior.records) {
-      const float2 ml = __ldcg(prior.ml + r);
-      if (ml.y > 0.f) top = fmaxf(top, ml.x);
-    }
-  }
-#pragma unroll
-  for (int o = 1; o < 16; o <<= 1) top = fmaxf(top, __shfl_xor_sync(half, top, o));
-  const Factor<WIDE> own(den > 0.f ? m - top : kNone);
-  float sum = 0.f;
-#pragma unroll
-  for (int k = 0; k < N; ++k) x[k].x *= own.all, x[k].y *= own.all, x[k].z *= own.all, x[k].w *= own.all;
-  for (uint32_t i0 = 0; i0 < n; i0 += 16) {
-    float weight = 0.f;
-    uint32_t place = 0;
-    if (i0 + sub < n) {
-      const uint32_t r = record(i0 + sub);
-      if (r < prior.records) {
-        const float2 ml = __ldcg(prior.ml + r);
-        const Factor<WIDE> down(ml.y > 0.f ? ml.x - top : kNone);
-        sum += down.denominator(ml.y), weight = down.all, place = r;
-        if (ml.y != ml.y) sum = weight = ml.y;  // a NaN stays one
-      }
-    }
-    const uint32_t here = n - i0 < 16 ? n - i0 : 16;
-#pragma unroll 4
-    for (uint32_t j = 0; j < here; ++j) {
-      const float w = __shfl_sync(half, weight, (lane & 16) + j);
-      const float* const from = prior.o + uint64_t(__shfl_sync(half, place, (lane & 16) + j)) * prior.dims;
-      if (w == 0.f) continue;  // an empty record has no sums
-#pragma unroll
-      for (int k = 0; k < N; ++k) {
-        const uint32_t d = 64 * k + 4 * sub;
-        if (d >= prior.dims) break;
-        const float4 y = __ldcg(reinterpret_cast<const float4*>(from + d));
-        x[k].x += y.x * w, x[k].y += y.y * w, x[k].z += y.z * w, x[k].w += y.w * w;
-      }
-    }
-  }
-#pragma unroll
-  for (int o = 1; o < 16; o <<= 1) sum += __shfl_xor_sync(half, sum, o);
-  den = own.denominator(den) + sum, m = top;
-}
-
-template <int FMT, int DP, int NT, bool PRIOR>
+template <int FMT, int DP, int NT, bool RECORD>
 __global__ void __launch_bounds__(kWarps * 32, Shape<FMT, DP, NT>::CTAS) bcp_kv_attend_kernel(const AttendArgs a) {
   typedef Shape<FMT, DP, NT> S;
   constexpr bool kBf16 = FMT == BCP_BF16;  // type of the products; 8-bit caches are widened to binary16
@@ -706,10 +650,13 @@ __global__ void __launch_bounds__(kWarps * 32, Shape<FMT, DP, NT>::CTAS) bcp_kv_
           continue;
         }
         const uint32_t qh = h * a.group + row0 + col;
-        if constexpr (PRIOR) {
-          m -= kLift;
-          join_prior<S::quant>(a.prior, a.prior.rows[uint64_t(at.b) * (a.n_heads * a.group) + qh], sub, lane, m, den, x);
-          m += kLift;
+        if constexpr (RECORD) {
+          const uint64_t row = uint64_t(at.b) * (a.n_heads * a.group) + qh;
+#pragma unroll
+          for (int i = 0; i < DP / 64; ++i)
+            if (64 * i + 4 * sub < a.records.dims) __stcg(reinterpret_cast<float4*>(a.records.o + row * a.records.dims + 64 * i + 4 * sub), x[i]);
+          if (sub == 0) __stcg(a.records.ml + row, make_float2(m - kLift, den));
+          continue;
         }
         const float inv = den == 0.f ? 0.f : reciprocal_fast(den);  // up to 2^127, where the fast division gives zero
 #pragma unroll
@@ -766,24 +713,24 @@ struct Variant {
 };
 
 template <int FMT, int DP, int NT>
-Variant variant(bool prior) {
+Variant variant(bool record) {
   typedef Shape<FMT, DP, NT> S;
-  return Variant{prior ? bcp_kv_attend_kernel<FMT, DP, NT, true> : bcp_kv_attend_kernel<FMT, DP, NT, false>, S::SMEM, S::ROWS, S::PART};
+  return Variant{record ? bcp_kv_attend_kernel<FMT, DP, NT, true> : bcp_kv_attend_kernel<FMT, DP, NT, false>, S::SMEM, S::ROWS, S::PART};
 }
 template <int FMT>
-Variant variant_of(uint32_t head_dim, uint32_t group, bool prior) {
+Variant variant_of(uint32_t head_dim, uint32_t group, bool record) {
   // Query heads of a group beyond eight take a second column block (16 rows share each key and value that
   // was read); with 256 dimensions the sums of 16 rows would not fit the registers, more rows are more units.
-  if (head_dim <= 64) return group <= 8 ? variant<FMT, 64, 1>(prior) : variant<FMT, 64, 2>(prior);
-  if (head_dim <= 128) return group <= 8 ? variant<FMT, 128, 1>(prior) : variant<FMT, 128, 2>(prior);
-  return variant<FMT, 256, 1>(prior);
+  if (head_dim <= 64) return group <= 8 ? variant<FMT, 64, 1>(record) : variant<FMT, 64, 2>(record);
+  if (head_dim <= 128) return group <= 8 ? variant<FMT, 128, 1>(record) : variant<FMT, 128, 2>(record);
+  return variant<FMT, 256, 1>(record);
 }
-Variant variant_of(uint32_t format, uint32_t head_dim, uint32_t group, bool prior) {
+Variant variant_of(uint32_t format, uint32_t head_dim, uint32_t group, bool record) {
   switch (format) {
-    case BCP_BF16: return variant_of<BCP_BF16>(head_dim, group, prior);
-    case BCP_F16: return variant_of<BCP_F16>(head_dim, group, prior);
-    case BCP_E4M3: return variant_of<BCP_E4M3>(head_dim, group, prior);
-    default: return variant_of<BCP_I8>(head_dim, group, prior);
+    case BCP_BF16: return variant_of<BCP_BF16>(head_dim, group, record);
+    case BCP_F16: return variant_of<BCP_F16>(head_dim, group, record);
+    case BCP_E4M3: return variant_of<BCP_E4M3>(head_dim, group, record);
+    default: return variant_of<BCP_I8>(head_dim, group, record);
   }
 }
 
@@ -842,8 +789,8 @@ extern "C" int bcp_kv_attend_workspace(const bcp_kv_cache* cache, uint32_t n_q_h
   const uint32_t group = n_q_heads / cache->n_heads;
   (void)max_seqs;  // the parts are as many as CTAs, however many sequences they come from
   *bytes = 0;
-  for (bool prior : {false, true}) {  // for either form of the kernel
-    const Variant v = variant_of(cache->format, cache->head_dim, group, prior);
+  for (bool record : {false, true}) {  // for either form of the kernel
+    const Variant v = variant_of(cache->format, cache->head_dim, group, record);
     uint32_t ctas = 0;
     if (int rc = resident_ctas(v, &ctas)) return rc;
     const uint64_t n = workspace_bytes_of(ctas, v);
@@ -856,7 +803,7 @@ namespace bcp {
 
 int attend(const char* call, const bcp_kv_cache* c, const bcp_heads* q, const bcp_heads* out, float* lse, uint32_t n_seqs, const int32_t* block_table,
            int64_t table_stride, uint32_t table_width, const int32_t* lengths, float scale, uint32_t window, void* workspace, uint64_t workspace_bytes,
-           const Prior* prior, bool launch, void* stream) {
+           const Records* records, bool launch, void* stream) {
   if (int rc = check_cache(call, c)) return rc;
   if (int rc = check_heads(call, "q", q, false, c->head_dim, n_seqs)) return rc;
   if (int rc = check_heads(call, "out", out, true, c->head_dim, n_seqs)) return rc;
@@ -873,7 +820,7 @@ int attend(const char* call, const bcp_kv_cache* c, const bcp_heads* q, const bc
   if (!(scale == scale) || scale - scale != 0.f) return fail(BCP_ERR_INVALID, "%s: scale is not a finite number", call);
 
   const uint32_t group = q->n_heads / c->n_heads;
-  const Variant v = variant_of(c->format, c->head_dim, group, prior != nullptr);
+  const Variant v = variant_of(c->format, c->head_dim, group, records != nullptr);
   uint32_t ctas = 0;
   if (int rc = resident_ctas(v, &ctas)) return rc;
   AttendArgs a = {};
@@ -895,7 +842,7 @@ int attend(const char* call, const bcp_kv_cache* c, const bcp_heads* q, const bc
   a.q_is_bf16 = q->type == BCP_BF16, a.group = group, a.n_seqs = n_seqs;
   a.block_table = block_table, a.table_stride = table_stride, a.lengths = lengths;
   a.scale_log2 = scale * kLog2e, a.window = window;
-  if (prior) a.prior = *prior;
+  if (records) a.records = *records;
   char* const w = static_cast<char*>(workspace);
   a.part_count = reinterpret_cast<uint32_t*>(w);
   a.group_count = reinterpret_cast<uint32_t*>(w + kCounterBytes);

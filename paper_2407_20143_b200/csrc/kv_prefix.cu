@@ -15,6 +15,8 @@
 // Four warps bring tokens by 16-byte asynchronous copies through a ring of tiles (pages may have any size and place), a warp issues the products.
 //
 // Split.  The tiles of all groups, cache heads and 256 rows form one line that is cut into as many equal parts as there are SMs.
+#include <cuda.h>
+
 #include <mutex>
 
 #include "attend.cuh"
@@ -29,6 +31,8 @@ constexpr uint32_t kMeta = 16;              // tiles whose masks and scales are 
 constexpr uint64_t kMostNs = 2000000000ull; // a wait that takes longer gives up
 
 struct PrefixArgs {
+  CUtensorMap k_map, v_map;  // the cache as [page][head][token][element], boxes of `block` tokens
+  uint32_t block;            // 0: none
   const void *k, *v;
   const float *k_scale, *v_scale;
   uint32_t page_stride, head_stride, token_stride;
@@ -37,16 +41,16 @@ struct PrefixArgs {
   uint32_t* status;
   const void* q;
   int64_t q_token, q_head;
-  uint32_t q_is_bf16, n_seqs, n_groups;
+  uint32_t q_is_bf16, q_wide, n_seqs, n_groups;  // q_wide: its rows start on 16-byte boundaries
   FastDiv group;  // query heads of a cache head
   const int32_t* table;
   int64_t table_stride;
   uint32_t capacity;
   const int32_t *lengths, *starts;
   float scale_log2;
-  int4* rows;
-  float2* ml;
-  float* o;
+  int4* rows;   // of each row: its first record, the next part's, parts, from a record to the other one of the same part (0: it has one)
+  float2* ml;   // reference and denominator of each record: l = sum exp2(s - m)
+  float* o;     // its sums, o = sum exp2(s - m) v
 };
 
 template <int FMT, int DP>
@@ -64,8 +68,13 @@ struct Shape {
   static constexpr uint32_t NMETA = quant ? 8 : kMeta;
   static constexpr uint32_t SLOTS = DP == 64 ? 8 : quant ? 3 : 5;
   static constexpr uint32_t AHEAD = quant ? RAWS - 1 : 3;    // copies of so many tiles are under way
-  static constexpr uint32_t SMEM = STREAMS * Q + SLOTS * TILE + RAWS * RAW + NMETA * META + 8 * (2 * SLOTS + NMETA + 4 * STREAMS + 1) + 64 + 1024;
-  static constexpr uint32_t WARPS = 4 * STREAMS + kLoaders + 1, THREADS = 32 * WARPS;
+  static constexpr uint32_t SMEM = STREAMS * Q + SLOTS * TILE + RAWS * RAW + NMETA * META + 8 * (2 * SLOTS + NMETA + 6 * STREAMS + 4 * RAWS) + 64 + 1024;
+  // a warpgroup for each stream, one that copies, one of whose warps issues the products
+  static constexpr uint32_t WARPS = 4 * STREAMS + kLoaders + 4, THREADS = 32 * WARPS;
+  // Registers a thread: at launch, and after the groups have been given theirs (their sum is the launch's).
+  // With one stream there are enough for all.
+  static constexpr uint32_t REGS = 128, REGS_ROWS = 168, REGS_COPY = 104, REGS_PRODUCT = 72;
+  static_assert(2 * REGS_ROWS + REGS_COPY + REGS_PRODUCT <= 4 * REGS, "registers of the launch");
   static constexpr uint32_t S0 = 0, O0 = STREAMS * TOK;      // columns of tensor memory
   static_assert(O0 + STREAMS * DP <= 512, "tensor memory");
   static_assert(SMEM <= 232448, "shared memory");
@@ -74,8 +83,13 @@ struct Shape {
 
 // ------------------------------------------------------------------------------ instructions
 __device__ __forceinline__ void bar_arrive(uint32_t bar) { asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory"); }
+__device__ __forceinline__ bool bar_test(uint32_t bar, uint32_t parity) {  // without waiting
+  uint32_t ok;
+  asm volatile("{\n.reg .pred p;\nmbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\nselp.u32 %0, 1, 0, p;\n}" : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
+  return ok;
+}
 // False, in all lanes of a warp, if the wait ran out here or in another warp.
-__device__ __noinline__ bool bar_wait_slow(uint32_t bar, uint32_t parity, volatile uint32_t* stop) {
+__device__ __forceinline__ bool bar_wait_slow(uint32_t bar, uint32_t parity, volatile uint32_t* stop) {
   const uint64_t begin = global_timer_ns();
   while (!mbar_try_wait(bar, parity)) {
     if (*stop) return false;
@@ -104,15 +118,21 @@ __device__ __forceinline__ void tmem_store_wait() { asm volatile("tcgen05.wait::
 __device__ __forceinline__ void to_async_proxy() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 
 // 32 columns of this thread's row
-__device__ __forceinline__ void tmem_load32(uint32_t at, float (&x)[32]) {
-  uint32_t* r = reinterpret_cast<uint32_t*>(x);
+__device__ __forceinline__ void tmem_load32(uint32_t at, float* r) {
   asm volatile(
       "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, %17, %18, %19, %20, %21, %22, %23, "
       "%24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
-      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]),
-        "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]),
-        "=r"(r[23]), "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+      : "=f"(r[0]), "=f"(r[1]), "=f"(r[2]), "=f"(r[3]), "=f"(r[4]), "=f"(r[5]), "=f"(r[6]), "=f"(r[7]), "=f"(r[8]), "=f"(r[9]), "=f"(r[10]), "=f"(r[11]),
+        "=f"(r[12]), "=f"(r[13]), "=f"(r[14]), "=f"(r[15]), "=f"(r[16]), "=f"(r[17]), "=f"(r[18]), "=f"(r[19]), "=f"(r[20]), "=f"(r[21]), "=f"(r[22]),
+        "=f"(r[23]), "=f"(r[24]), "=f"(r[25]), "=f"(r[26]), "=f"(r[27]), "=f"(r[28]), "=f"(r[29]), "=f"(r[30]), "=f"(r[31])
       : "r"(at));
+}
+// Values are used only behind the wait for their loads.
+__device__ __forceinline__ void loaded32(float* r) {
+  asm volatile("" : "+f"(r[0]), "+f"(r[1]), "+f"(r[2]), "+f"(r[3]), "+f"(r[4]), "+f"(r[5]), "+f"(r[6]), "+f"(r[7]), "+f"(r[8]), "+f"(r[9]), "+f"(r[10]), "+f"(r[11]), "+f"(r[12]), "+f"(r[13]), "+f"(r[14]), "+f"(r[15]), "+f"(r[16]), "+f"(r[17]), "+f"(r[18]), "+f"(r[19]), "+f"(r[20]), "+f"(r[21]), "+f"(r[22]), "+f"(r[23]), "+f"(r[24]), "+f"(r[25]), "+f"(r[26]), "+f"(r[27]), "+f"(r[28]), "+f"(r[29]), "+f"(r[30]), "+f"(r[31]));
+}
+__device__ __forceinline__ void loaded16(float* r) {
+  asm volatile("" : "+f"(r[0]), "+f"(r[1]), "+f"(r[2]), "+f"(r[3]), "+f"(r[4]), "+f"(r[5]), "+f"(r[6]), "+f"(r[7]), "+f"(r[8]), "+f"(r[9]), "+f"(r[10]), "+f"(r[11]), "+f"(r[12]), "+f"(r[13]), "+f"(r[14]), "+f"(r[15]));
 }
 __device__ __forceinline__ void tmem_store16(uint32_t at, const uint32_t (&r)[16]) {
   asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};" ::"r"(at), "r"(r[0]),
@@ -120,31 +140,53 @@ __device__ __forceinline__ void tmem_store16(uint32_t at, const uint32_t (&r)[16
                "r"(r[14]), "r"(r[15])
                : "memory");
 }
-__device__ __forceinline__ void tmem_load16(uint32_t at, float (&x)[16]) {
-  uint32_t* r = reinterpret_cast<uint32_t*>(x);
+__device__ __forceinline__ void tmem_load16(uint32_t at, float* r) {
   asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
-               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]),
-                 "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+               : "=f"(r[0]), "=f"(r[1]), "=f"(r[2]), "=f"(r[3]), "=f"(r[4]), "=f"(r[5]), "=f"(r[6]), "=f"(r[7]), "=f"(r[8]), "=f"(r[9]), "=f"(r[10]),
+                 "=f"(r[11]), "=f"(r[12]), "=f"(r[13]), "=f"(r[14]), "=f"(r[15])
                : "r"(at));
 }
 
-// Shared-memory operands in rows of 128 bytes (64 elements), eight rows a swizzled block of 1024 bytes, blocks of rows one after the other.
-// Keys and queries (the sum runs along the row): `apart` is not used.  Values (the sum runs over rows): `apart` bytes from 64 columns to the next.
-__device__ __forceinline__ uint64_t operand(uint32_t at, uint32_t apart) {
-  return uint64_t(at >> 4 & 0x3fff) | uint64_t(apart >> 4) << 16 | uint64_t(1024 >> 4) << 32 | uint64_t(1) << 46 | uint64_t(2) << 61;
+__device__ __forceinline__ float2 add2(float2 a, float2 b) {
+  float2 r;
+  asm("{\n.reg .b64 x, y, z;\nmov.b64 x, {%2, %3};\nmov.b64 y, {%4, %5};\nadd.rn.f32x2 z, x, y;\nmov.b64 {%0, %1}, z;\n}"
+      : "=f"(r.x), "=f"(r.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+  return r;
 }
+__device__ __forceinline__ float largest(float a, float b, float c) {
+  float r;
+  asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+  return r;
+}
+__device__ __forceinline__ float minus_upper(float x) { return __uint_as_float((__float_as_uint(x) & 0xffff0000u) ^ 0x80000000u); }
+__device__ __forceinline__ bool elected() {
+  uint32_t yes;
+  asm volatile("{\n.reg .pred p;\nelect.sync _|p, 0xffffffff;\nselp.u32 %0, 1, 0, p;\n}" : "=r"(yes));
+  return yes;
+}
+template <uint32_t N>
+__device__ __forceinline__ void more_registers() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N)); }
+template <uint32_t N>
+__device__ __forceinline__ void fewer_registers() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N)); }
+
+// Shared-memory operands in rows of 128 bytes (64 elements), eight rows a swizzled block of 1024 bytes, blocks of rows one after the other; a
+// descriptor's lower half has the address and, for values (whose sum runs over rows), the bytes from 64 columns to the next; its upper half is the same for all.
+// Products follow one another at 64 cycles, about the time that one thread needs to issue one with all its numbers at hand: they are unrolled, and each
+// adds a constant to the lower half.
+__device__ __forceinline__ uint32_t operand(uint32_t at, uint32_t apart) { return (at >> 4 & 0x3fff) | (apart >> 4) << 16; }
+constexpr uint32_t kUpper = 1024 >> 4 | 1u << 14 | 2u << 29;
 // kind::f16 with binary32 sums, 128 rows, n columns; both operands bfloat16 or both binary16; the second one's rows along the sum or not
 __host__ __device__ constexpr uint32_t product(bool bf16, bool second_by_rows, uint32_t n) {
   return 1u << 4 | (bf16 ? 1u << 7 | 1u << 10 : 0u) | (second_by_rows ? 1u << 16 : 0u) | (n >> 3) << 17 | (kRows >> 4) << 24;
 }
-__device__ __forceinline__ void mma_shared(uint32_t d, uint64_t a, uint64_t b, uint32_t what, bool add) {
-  asm volatile("{\n.reg .pred p;\nsetp.ne.u32 p, %4, 0;\ntcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}" ::"r"(d), "l"(a), "l"(b), "r"(what),
-               "r"(uint32_t(add))
+__device__ __forceinline__ void mma_shared(uint32_t d, uint32_t a, uint32_t b, uint32_t what, bool add) {
+  asm volatile("{\n.reg .pred p;\n.reg .b64 x, y;\nsetp.ne.u32 p, %4, 0;\nmov.b64 x, {%1, %5};\nmov.b64 y, {%2, %5};\n"
+               "tcgen05.mma.cta_group::1.kind::f16 [%0], x, y, %3, p;\n}" ::"r"(d), "r"(a), "r"(b), "r"(what), "r"(uint32_t(add)), "n"(kUpper)
                : "memory");
 }
-__device__ __forceinline__ void mma_tensor(uint32_t d, uint32_t a, uint64_t b, uint32_t what, bool add) {
-  asm volatile("{\n.reg .pred p;\nsetp.ne.u32 p, %4, 0;\ntcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n}" ::"r"(d), "r"(a), "l"(b), "r"(what),
-               "r"(uint32_t(add))
+__device__ __forceinline__ void mma_tensor(uint32_t d, uint32_t a, uint32_t b, uint32_t what, bool add) {
+  asm volatile("{\n.reg .pred p;\n.reg .b64 y;\nsetp.ne.u32 p, %4, 0;\nmov.b64 y, {%2, %5};\ntcgen05.mma.cta_group::1.kind::f16 [%0], [%1], y, %3, p;\n}" ::"r"(d),
+               "r"(a), "r"(b), "r"(what), "r"(uint32_t(add)), "n"(kUpper)
                : "memory");
 }
 __device__ __forceinline__ void shared_store16(uint32_t at, uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
@@ -154,6 +196,28 @@ __device__ __forceinline__ uint4 shared_load16(uint32_t at) {
   uint4 v;
   asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(at) : "memory");
   return v;
+}
+
+__device__ __forceinline__ void copies_wait_all_but(uint32_t n) {
+  switch (n) {
+    case 0: copies_wait<0>(); break;
+    case 1: copies_wait<1>(); break;
+    case 2: copies_wait<2>(); break;
+    default: copies_wait<3>(); break;
+  }
+}
+
+// `block` tokens of 64 (16-bit) or all (8-bit) elements, from element x on
+__device__ __forceinline__ void box_load(uint32_t to, const CUtensorMap* map, uint32_t x, uint32_t token, uint32_t head, uint32_t page, uint32_t bar) {
+  asm volatile("cp.async.bulk.tensor.4d.shared::cta.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];" ::"r"(to), "l"(map),
+               "r"(x), "r"(token), "r"(head), "r"(page), "r"(bar)
+               : "memory");
+}
+
+__device__ __forceinline__ void store8(float* to, const float* x) {  // a whole sector of memory
+  asm volatile("st.global.v8.f32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(to), "f"(x[0]), "f"(x[1]), "f"(x[2]), "f"(x[3]), "f"(x[4]), "f"(x[5]),
+               "f"(x[6]), "f"(x[7])
+               : "memory");
 }
 
 // ------------------------------------------------------------------------------ the line
@@ -192,7 +256,7 @@ __device__ __forceinline__ void advance(Place& p, const PrefixArgs& a, uint32_t 
 }
 
 template <int FMT, int DP>
-__global__ void __launch_bounds__(Shape<FMT, DP>::THREADS, 1) bcp_kv_prefix_kernel(const PrefixArgs a) {
+__global__ void __launch_bounds__(Shape<FMT, DP>::THREADS, 1) bcp_kv_prefix_kernel(const __grid_constant__ PrefixArgs a) {
   typedef Shape<FMT, DP> S;
   extern __shared__ unsigned char raw_smem[];
   const uint32_t tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
@@ -202,12 +266,25 @@ __global__ void __launch_bounds__(Shape<FMT, DP>::THREADS, 1) bcp_kv_prefix_kern
   unsigned char* const meta_ptr = smem + (meta - base);
   const uint32_t bars = meta + S::NMETA * S::META;
   const uint32_t full = bars, empty = full + 8 * S::SLOTS, described = empty + 8 * S::SLOTS, q_full = described + 8 * S::NMETA, s_full = q_full + 8 * S::STREAMS,
-                 p_full = s_full + 8 * S::STREAMS, o_full = p_full + 8 * S::STREAMS, drained = o_full + 8 * S::STREAMS;
-  uint32_t* const words = reinterpret_cast<uint32_t*>(smem + (drained + 8 - base));  // tensor memory, stop, found[3], totals
+                 p_full = s_full + 8 * S::STREAMS, o_full = p_full + 16 * S::STREAMS, drained = o_full + 8 * S::STREAMS, raw_full = drained + 8 * S::STREAMS;
+  uint32_t* const words = reinterpret_cast<uint32_t*>(smem + (raw_full + 32 * S::RAWS - base));  // tensor memory, stop, found[8]
   volatile uint32_t* const stop = words + 1;
   uint32_t* const found = words + 2;
   uint32_t* const totals = reinterpret_cast<uint32_t*>(smem);  // before the tiles come
 
+  if (warp == S::WARPS - 4) tmem_alloc(uint32_t(__cvta_generic_to_shared(words)));
+  if (tid == 0) {
+    for (uint32_t i = 0; i < S::SLOTS; ++i) mbar_init(full + 8 * i, 32 * kLoaders), mbar_init(empty + 8 * i, 2);
+    for (uint32_t i = 0; i < S::NMETA; ++i) mbar_init(described + 8 * i, 32 * kLoaders);
+    for (uint32_t i = 0; i < S::STREAMS; ++i)
+      mbar_init(q_full + 8 * i, kRows), mbar_init(s_full + 8 * i, 1), mbar_init(p_full + 16 * i, kRows), mbar_init(p_full + 16 * i + 8, kRows), mbar_init(o_full + 8 * i, 1), mbar_init(drained + 8 * i, 1);
+    for (uint32_t i = 0; i < 4 * S::RAWS; ++i) mbar_init(raw_full + 8 * i, 1);
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  tmem_before();
+  __syncthreads();
+  tmem_after();
+  const uint32_t tmem = *static_cast<volatile uint32_t*>(words);
   after_previous();
   // ---- rows without a prefix have no records
   const uint32_t n_q_heads = a.n_heads * a.group.d;
@@ -253,10 +330,12 @@ __global__ void __launch_bounds__(Shape<FMT, DP>::THREADS, 1) bcp_kv_prefix_kern
     if (w < warp) before += totals[w];
     all += totals[w];
   }
-  if (!all) return;
   Cuts cuts;
-  cuts.cut(all, gridDim.x);
-  if (blockIdx.x >= cuts.parts) return;
+  if (all) cuts.cut(all, gridDim.x);
+  if (!all || blockIdx.x >= cuts.parts) {
+    if (warp == S::WARPS - 4) tmem_free(tmem);
+    return;
+  }
   const uint32_t s0 = cuts.begin(blockIdx.x), n_steps = cuts.begin(blockIdx.x + 1) - s0;
   if (s0 >= before && s0 < before + mine) {
     uint32_t pre = before, g = run0;
@@ -265,36 +344,27 @@ __global__ void __launch_bounds__(Shape<FMT, DP>::THREADS, 1) bcp_kv_prefix_kern
       const uint32_t n = x.steps * x.tiles * a.n_heads;
       if (s0 < pre + n) {
         found[0] = g, found[1] = (s0 - pre) / x.steps, found[2] = (s0 - pre) % x.steps;
+        found[3] = x.first, found[4] = x.rows, found[5] = x.len, found[6] = x.steps, found[7] = x.tiles;
         break;
       }
       pre += n;
     }
   }
-  if (tid == 0) {
-    for (uint32_t i = 0; i < S::SLOTS; ++i) mbar_init(full + 8 * i, 32 * kLoaders), mbar_init(empty + 8 * i, 1);
-    for (uint32_t i = 0; i < S::NMETA; ++i) mbar_init(described + 8 * i, 32 * kLoaders);
-    for (uint32_t i = 0; i < S::STREAMS; ++i)
-      mbar_init(q_full + 8 * i, kRows), mbar_init(s_full + 8 * i, 1), mbar_init(p_full + 8 * i, kRows), mbar_init(o_full + 8 * i, 1);
-    mbar_init(drained, 1);
-    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-  }
-  if (warp == S::WARPS - 1) tmem_alloc(uint32_t(__cvta_generic_to_shared(words)));
-  tmem_before();
   __syncthreads();
-  tmem_after();
-  const uint32_t tmem = *static_cast<volatile uint32_t*>(words);
   Place at;
   at.g = found[0], at.u = found[1], at.step = found[2];
-  at.group = group_of<S>(a, at.g);
+  at.group.first = found[3], at.group.rows = found[4], at.group.len = found[5], at.group.steps = found[6], at.group.tiles = found[7];
 
   uint32_t left = n_steps;
   if (warp < 4 * S::STREAMS) {
     // ================================================================ a stream's rows
+    if constexpr (S::STREAMS == 2) more_registers<S::REGS_ROWS>();
     const uint32_t stream = warp >> 2, row = tid & (kRows - 1);
     const uint32_t lanes = tmem + ((warp & 3) << 21);  // this warp's 32 rows
     const uint32_t s_at = lanes + S::S0 + stream * S::TOK, o_at = lanes + S::O0 + stream * DP;
     uint32_t n_scores = 0, n_ends = 0, tile0 = 0;
     const float scale = fabsf(a.scale_log2);
+    constexpr float kLeast = 0x1p-126f;  // a factor is not 0, so that a masked score stays below all others; any score times this counts as 0
     bool ok = true;
     while (left && ok) {
       const uint32_t n = min(at.group.steps - at.step, left);
@@ -308,30 +378,40 @@ __global__ void __launch_bounds__(Shape<FMT, DP>::THREADS, 1) bcp_kv_prefix_kern
       const bool any = both || stream < n;  // has tiles here
       float factor = scale;
       if (any) {
-        const uint2* const from = reinterpret_cast<const uint2*>(static_cast<const char*>(a.q) + (b * a.q_token + head * a.q_head) * 2);
+        // A warp's 32 rows, neighbouring lanes on neighbouring chunks of a row.
         const uint32_t flip = a.scale_log2 < 0.f ? 0x80008000u : 0u;  // the scale's sign goes into the query
-        const uint32_t to = q_at + stream * S::Q + row * 128;
-        float up = 1.f;
-        if constexpr (S::quant) {
-          uint32_t top = 0;
-          if (live)
-            for (uint32_t i = 0; i < a.head_dim / 4; ++i) {
-              const uint2 w = from[i];
-#pragma unroll
-              for (int j = 0; j < 4; ++j) top = max(top, __float_as_uint(query_at(&w, j, a.q_is_bf16)) & 0x7fffffffu);
-            }
-          const uint32_t e = top >> 23 == 254 ? 253 : top >> 23;
-          if (e >= 1 && e <= 253) up = __uint_as_float((254 - e) << 23), factor *= __uint_as_float(e << 23);
-        }
+        const int64_t from = live ? b * a.q_token + head * a.q_head : -1;
+        constexpr uint32_t kChunks = DP / 8, kTogether = 32 / kChunks;
+        const uint32_t c = lane % kChunks, mine = lane / kChunks;
 #pragma unroll 4
-        for (uint32_t c = 0; c < a.head_dim / 8; ++c) {
-          uint2 x = make_uint2(0, 0), y = x;
-          if (live) x = from[2 * c], y = from[2 * c + 1];
-          if constexpr (S::quant) {
-            auto two = [&](uint32_t w) { return pack16<false>(query_at(&w, 0, a.q_is_bf16) * up, query_at(&w, 1, a.q_is_bf16) * up); };
-            x = make_uint2(two(x.x), two(x.y)), y = make_uint2(two(y.x), two(y.y));
+        for (uint32_t i = 0; i < 32 / kTogether; ++i) {
+          const uint32_t owner = i * kTogether + mine, r = (warp & 3) * 32 + owner;
+          const int64_t at_row = __shfl_sync(0xffffffffu, from, owner);
+          uint4 x = make_uint4(0, 0, 0, 0);
+          if (at_row >= 0 && 8 * c < a.head_dim) {
+            const char* const p = static_cast<const char*>(a.q) + (at_row + 8 * c) * 2;
+            if (a.q_wide) {
+              x = *reinterpret_cast<const uint4*>(p);
+            } else {
+              const uint2 u = *reinterpret_cast<const uint2*>(p), v = *reinterpret_cast<const uint2*>(p + 8);
+              x = make_uint4(u.x, u.y, v.x, v.y);
+            }
           }
-          shared_store16(to + (c >> 3) * (kRows * 128) + ((c & 7 ^ row & 7) << 4), x.x ^ flip, x.y ^ flip, y.x ^ flip, y.y ^ flip);
+          if constexpr (S::quant) {
+            auto size = [&](uint32_t w) { return max(__float_as_uint(query_at(&w, 0, a.q_is_bf16)) & 0x7fffffffu, __float_as_uint(query_at(&w, 1, a.q_is_bf16)) & 0x7fffffffu); };
+            uint32_t top = max(max(size(x.x), size(x.y)), max(size(x.z), size(x.w)));
+#pragma unroll
+            for (uint32_t o = 1; o < kChunks; o <<= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
+            const uint32_t e = min(top >> 23, 253u + (top >> 23 == 255) * 2);  // (neither zeros nor what is not finite)
+            float up = 1.f, back = 1.f;
+            if (e >= 1 && e <= 253) up = __uint_as_float((254 - e) << 23), back = __uint_as_float(e << 23);
+            auto word = [&](uint32_t w) { return pack16<false>(query_at(&w, 0, a.q_is_bf16) * up, query_at(&w, 1, a.q_is_bf16) * up); };
+            x = make_uint4(word(x.x), word(x.y), word(x.z), word(x.w));
+            back = __shfl_sync(0xffffffffu, back, lane % kTogether * kChunks);
+            if (lane / kTogether == i) factor *= back;
+          }
+          if (8 * c < a.head_dim)
+            shared_store16(q_at + stream * S::Q + r * 128 + (c >> 3) * (kRows * 128) + ((c & 7 ^ r & 7) << 4), x.x ^ flip, x.y ^ flip, x.z ^ flip, x.w ^ flip);
         }
       }
       if (any) {
@@ -340,6 +420,7 @@ __global__ void __launch_bounds__(Shape<FMT, DP>::THREADS, 1) bcp_kv_prefix_kern
       }
 
       float ref = kNone, l = 0.f, top_scale = 0.f, unit = 1.f;  // unit: what the values' scales are multiplied by
+      factor = fmaxf(factor, kLeast);
       bool first = true;
       const uint32_t step = both ? 1 : S::STREAMS;
       uint32_t t = both ? 0 : stream;
@@ -350,108 +431,130 @@ __global__ void __launch_bounds__(Shape<FMT, DP>::THREADS, 1) bcp_kv_prefix_kern
         if (!ok) break;
         ++n_scores;
         tmem_after();
-        const uint4 alive = *reinterpret_cast<const uint4*>(about);
-        const uint32_t mask[4] = {alive.x, alive.y, alive.z, alive.w};
-        if (__any_sync(0xffffffffu, live)) {
-          // the largest score
-          float top = -INFINITY;
+        const bool work = __any_sync(0xffffffffu, live);
+        // 64 scores into registers; 8-bit keys: times their scales; masked ones below all others
+        float x[64];
+        auto read = [&](uint32_t half) {
+          tmem_load32(s_at + 64 * half, x), tmem_load32(s_at + 64 * half + 32, x + 32);
+          tmem_load_wait();
+          loaded32(x), loaded32(x + 32);
+          if constexpr (S::quant) {
 #pragma unroll
-          for (uint32_t c = 0; c < S::TOK / 32; ++c) {
-            float x[32];
-            tmem_load32(s_at + 32 * c, x);
-            tmem_load_wait();
-            if constexpr (S::quant) {
-#pragma unroll
-              for (int i = 0; i < 32; i += 4) {
-                const float4 ks = *reinterpret_cast<const float4*>(about + 16 + (32 * c + i) * 4);
-                x[i] *= ks.x, x[i + 1] *= ks.y, x[i + 2] *= ks.z, x[i + 3] *= ks.w;
-              }
-            }
-            if (mask[c] == 0xffffffffu) {
-#pragma unroll
-              for (int i = 0; i < 32; ++i) top = fmaxf(top, x[i]);
-            } else {
-#pragma unroll
-              for (int i = 0; i < 32; ++i)
-                if (mask[c] >> i & 1) top = fmaxf(top, x[i]);
+            for (int i = 0; i < 64; i += 4) {
+              const float4 ks = *reinterpret_cast<const float4*>(about + 16 + 256 * half + 4 * i);
+              const float2 u = mul2(make_float2(x[i], x[i + 1]), make_float2(ks.x, ks.y)), v = mul2(make_float2(x[i + 2], x[i + 3]), make_float2(ks.z, ks.w));
+              x[i] = u.x, x[i + 1] = u.y, x[i + 2] = v.x, x[i + 3] = v.y;
             }
           }
-          if (top > -INFINITY) top *= factor;
-          float down = 1.f, down_o = 1.f;
-          if (top > ref + 8.f) down = down_o = exp2_fast(ref - top), ref = top, l *= down;
+          const uint2 mask = *reinterpret_cast<const uint2*>(about + 8 * half);
+          if ((mask.x & mask.y) != 0xffffffffu) {
+#pragma unroll
+            for (int i = 0; i < 64; ++i)
+              if (!((i < 32 ? mask.x : mask.y) >> (i & 31) & 1)) x[i] = -INFINITY;
+          }
+        };
+        if (work) {
+          float top = -INFINITY;
+#pragma unroll 1
+          for (uint32_t half = 0; half < S::TOK / 64; ++half) {
+            read(half);
+            float tops[4] = {top, x[0], x[1], x[2]};
+#pragma unroll
+            for (uint32_t i = 2; i < 64; i += 2) tops[i / 2 % 4] = largest(tops[i / 2 % 4], x[i], x[i + 1]);
+            top = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3]));
+          }
+          top *= factor;
+          float down = 1.f;
+          if (top > ref + 8.f) down = exp2_fast(ref - top), ref = top, l *= down;
           if constexpr (S::quant) {
             // Weights times scales must neither overflow in the sums nor vanish: where scales beyond 2^60 turn up all are multiplied by 2^-40, while none
             // is above 2^-40 by 2^60.
             const float4 w = *reinterpret_cast<const float4*>(about + 16 + S::TOK * 8);
             top_scale = fmaxf(top_scale, fmaxf(fmaxf(w.x, w.y), fmaxf(w.z, w.w)));
             const float next = top_scale > 0x1p60f ? 0x1p-40f : top_scale < 0x1p-40f ? 0x1p60f : 1.f;
-            if (next != unit) down_o *= next / unit, unit = next;
+            if (next != unit) down *= next / unit, unit = next;
           }
-          if (!first && __any_sync(0xffffffffu, down_o != 1.f)) {
+          if (!first && __any_sync(0xffffffffu, down != 1.f)) {
 #pragma unroll 1
             for (uint32_t c = 0; c < a.head_dim; c += 16) {
-              float x[16];
+              float z[16];
               uint32_t y[16];
-              tmem_load16(o_at + c, x);
+              tmem_load16(o_at + c, z);
               tmem_load_wait();
+              loaded16(z);
 #pragma unroll
-              for (int i = 0; i < 16; ++i) y[i] = __float_as_uint(x[i] * down_o);
+              for (int i = 0; i < 16; ++i) y[i] = __float_as_uint(z[i] * down);
               tmem_store16(o_at + c, y);
             }
           }
-          // the weights
+        }
+        // The weights, in two halves: the products with one begin while the other is made.
+        constexpr float kLift = S::split ? 0.f : 6.f;  // binary16 weights underflow below 2^-24: lifted by 2^6 that is 2^-30
+        const float2 factors = make_float2(factor, factor), less = make_float2(kLift - ref, kLift - ref);
+        auto weights = [&](uint32_t at, float* z, const unsigned char* scales) {  // 32 of them
+          float2 sum[4] = {};  // four, so that no addition waits for the one before it
 #pragma unroll
-          for (uint32_t c = 0; c < S::TOK / 32; ++c) {
-            float x[32];
-            tmem_load32(s_at + 32 * c, x);
-            tmem_load_wait();
-            constexpr float kLift = S::split ? 0.f : 6.f;  // binary16 weights underflow below 2^-24: lifted by 2^6 that is 2^-30
-            const float less = kLift - ref;
-            if constexpr (S::quant) {
+          for (int i = 0; i < 32; i += 2) {
+            const float2 e = fma2(make_float2(z[i], z[i + 1]), factors, less);
+            z[i] = exp2_fast(e.x), z[i + 1] = exp2_fast(e.y);
+            sum[i / 2 & 3] = add2(sum[i / 2 & 3], make_float2(z[i], z[i + 1]));
+          }
+          sum[0] = add2(add2(sum[0], sum[1]), add2(sum[2], sum[3]));
+          l += sum[0].x + sum[0].y;
+          if constexpr (S::quant) {
+            const float2 units = make_float2(unit, unit);
 #pragma unroll
-              for (int i = 0; i < 32; i += 4) {
-                const float4 ks = *reinterpret_cast<const float4*>(about + 16 + (32 * c + i) * 4);
-                x[i] *= ks.x, x[i + 1] *= ks.y, x[i + 2] *= ks.z, x[i + 3] *= ks.w;
-              }
-            }
-#pragma unroll
-            for (int i = 0; i < 32; ++i) x[i] = exp2_fast(fmaf(x[i], factor, less));
-            if (mask[c] != 0xffffffffu) {
-#pragma unroll
-              for (int i = 0; i < 32; ++i)
-                if (!(mask[c] >> i & 1)) x[i] = 0.f;
-            }
-            // the sum as four, so that no addition waits for the one before it
-            float sum[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-            for (int i = 0; i < 32; ++i) sum[i & 3] += x[i];
-            l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
-            if constexpr (S::quant) {
-#pragma unroll
-              for (int i = 0; i < 32; i += 4) {
-                const float4 vs = *reinterpret_cast<const float4*>(about + 16 + S::TOK * 4 + (32 * c + i) * 4);
-                x[i] *= vs.x * unit, x[i + 1] *= vs.y * unit, x[i + 2] *= vs.z * unit, x[i + 3] *= vs.w * unit;
-              }
-            }
-            uint32_t y[16];
-            if constexpr (S::split) {
-#pragma unroll
-              for (int i = 0; i < 16; ++i) y[i] = upper_halves(x[2 * i], x[2 * i + 1]);
-              tmem_store16(s_at + 32 * c, y);
-#pragma unroll
-              for (int i = 0; i < 16; ++i) y[i] = pack16<true>(lower_half(x[2 * i]), lower_half(x[2 * i + 1]));
-              tmem_store16(s_at + 32 * c + 16, y);
-            } else {
-#pragma unroll
-              for (int i = 0; i < 16; ++i) y[i] = pack16<false>(x[2 * i], x[2 * i + 1]);
-              tmem_store16(s_at + 32 * c, y);
+            for (int i = 0; i < 32; i += 4) {
+              const float4 vs = *reinterpret_cast<const float4*>(scales + 4 * i);
+              const float2 u = mul2(mul2(make_float2(vs.x, vs.y), units), make_float2(z[i], z[i + 1]));
+              const float2 v = mul2(mul2(make_float2(vs.z, vs.w), units), make_float2(z[i + 2], z[i + 3]));
+              z[i] = u.x, z[i + 1] = u.y, z[i + 2] = v.x, z[i + 3] = v.y;
             }
           }
+          uint32_t y[16];
+          if constexpr (S::split) {
+            // the upper half as it stands, and what remains, made positive by 2^-20 of the weight: the products of both with an infinite value are that
+            // infinity
+#pragma unroll
+            for (int i = 0; i < 16; ++i) y[i] = upper_halves(z[2 * i], z[2 * i + 1]);
+            tmem_store16(at, y);
+            const float2 more = make_float2(1.f + 0x1p-20f, 1.f + 0x1p-20f);
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+              const float2 rest = fma2(make_float2(z[2 * i], z[2 * i + 1]), more, make_float2(minus_upper(z[2 * i]), minus_upper(z[2 * i + 1])));
+              y[i] = pack16<true>(rest.x, rest.y);
+            }
+            tmem_store16(at + 16, y);
+          } else {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) y[i] = pack16<false>(z[2 * i], z[2 * i + 1]);
+            tmem_store16(at, y);
+          }
+        };
+        auto ready = [&](uint32_t half) {
           tmem_store_wait();
+          tmem_before();
+          bar_arrive(p_full + 16 * stream + 8 * half);
+        };
+        if constexpr (S::TOK == 128) {
+          // the second half of the scores is still in registers: it is made first
+#pragma unroll 1
+          for (uint32_t half = 0; half < 2; ++half) {
+            if (work) {
+              const uint32_t at = 1 - half;
+              if (half) read(at);
+              weights(s_at + 64 * at, x, about + 16 + S::TOK * 4 + 256 * at);
+              weights(s_at + 64 * at + 32, x + 32, about + 16 + S::TOK * 4 + 256 * at + 128);
+            }
+            ready(half);
+          }
+        } else {
+          if (work) weights(s_at + 32, x + 32, about + 16 + S::TOK * 4 + 128);
+          ready(0);
+          if (work) weights(s_at, x, about + 16 + S::TOK * 4);
+          ready(1);
         }
         first = false;
-        tmem_before();
-        bar_arrive(p_full + 8 * stream);
       }
       tile0 += n;
       if (!ok) break;
@@ -471,10 +574,10 @@ __global__ void __launch_bounds__(Shape<FMT, DP>::THREADS, 1) bcp_kv_prefix_kern
             float x[16];
             tmem_load16(o_at + c, x);
             tmem_load_wait();
+            loaded16(x);
             if (live) {
-              float4* const to = reinterpret_cast<float4*>(a.o + uint64_t(record) * a.head_dim + c);
-#pragma unroll
-              for (int i = 0; i < 4; ++i) __stcg(to + i, make_float4(x[4 * i], x[4 * i + 1], x[4 * i + 2], x[4 * i + 3]));
+              float* const to = a.o + uint64_t(record) * a.head_dim + c;
+              store8(to, x), store8(to + 8, x + 8);
             }
           }
         }
@@ -498,65 +601,76 @@ __global__ void __launch_bounds__(Shape<FMT, DP>::THREADS, 1) bcp_kv_prefix_kern
     }
   } else if (warp < 4 * S::STREAMS + kLoaders) {
     // ================================================================ copies of keys and values
-    const uint32_t w = warp - 4 * S::STREAMS, id = w * 32 + lane;
-    constexpr uint32_t kEach = S::TOK / kLoaders;                 // rows of a tile that a warp copies
+    if constexpr (S::STREAMS == 2) fewer_registers<S::REGS_COPY>();
+    const uint32_t w = warp - 4 * S::STREAMS;
+    constexpr uint32_t kEach = S::TOK / kLoaders;                 // rows of a tile that a warp brings
     constexpr uint32_t kChunks = DP * (S::quant ? 1 : 2) / 16;    // 16-byte chunks of a row
     constexpr uint32_t kTogether = 32 / kChunks, kTurns = kEach / kTogether;
+    constexpr uint32_t kAll = kEach == 32 ? 0xffffffffu : (1u << (kEach & 31)) - 1;
     const uint32_t my_row = lane / kChunks, chunk = lane % kChunks;
     const bool inside = chunk * 16 < a.head_dim * (S::quant ? 1u : 2u);
-    uint32_t item = 0, tile0 = 0, landed = 0;
-    uint32_t kind[8];  // of the items under way: the tile whose keys they are, plus 1; 0: values
+    uint32_t item = 0, tile0 = 0, landed = 0, brought = 0;  // brought: tiles whose keys are under way or have landed
+    uint32_t kinds = 0, tile_landed = 0;  // a bit for each item: it is keys; tiles whose keys have landed
+    uint32_t boxes = 0, phases = 0;       // a bit for each item: it comes in boxes; for each place of 8-bit tiles: the parity of its barrier
+    // Where this warp's tokens of a tile lie (a row a lane); the page of the next tile's is looked up ahead.
+    int32_t page = -1, page_of[2] = {-1, -1};
+    uint32_t off = 0, off_of[2] = {0, 0}, alive_of[2] = {0, 0};
     const int64_t v_from_k = static_cast<const char*>(a.v) - static_cast<const char*>(a.k);
     bool ok = true;
 
-    // What has come in goes on: 16-bit tiles lie where they belong, 8-bit ones are widened.
+    // An 8-bit tile that has come in is widened into its place.
     auto land = [&]() {
       const uint32_t slot = landed % S::SLOTS, at_slot = ring + slot * S::TILE;
-      const uint32_t keys = kind[landed & 7];
+      const bool keys = kinds >> (landed & 31) & 1;
+      const uint32_t m_slot = tile_landed % S::NMETA;
       if constexpr (S::quant) {
+        const uint32_t stage = landed % S::RAWS;
+        if (boxes >> (landed & 31) & 1) {
+          ok = ok && bar_wait(raw_full + 8 * (4 * stage + w), phases >> stage & 1, stop);
+          phases ^= 1u << stage;
+        }
         if (landed >= S::SLOTS) ok = ok && bar_wait(empty + 8 * slot, landed / S::SLOTS - 1 & 1, stop);
-        const uint32_t from = raw + landed % S::RAWS * S::RAW + id * 16;
+        const uint32_t from = raw + stage * S::RAW + (w * kEach + my_row) * a.head_dim + chunk * 16;
+        if (inside && ok) {
 #pragma unroll 2
-        for (uint32_t i = 0; i < kTurns; ++i) {
-          const uint32_t r = w * kEach + i * kTogether + my_row;
-          const uint4 x = shared_load16(from + i * (kLoaders * 32 * 16));
-          uint32_t y[8];
-          const uint32_t in[4] = {x.x, x.y, x.z, x.w};
+          for (uint32_t i = 0; i < kTurns; ++i) {
+            const uint32_t r = w * kEach + i * kTogether + my_row;
+            const uint4 x = shared_load16(from + i * kTogether * a.head_dim);
+            uint32_t y[8];
+            const uint32_t in[4] = {x.x, x.y, x.z, x.w};
 #pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            widen4<FMT>(in[j], y[2 * j], y[2 * j + 1]);
-            if (!keys) {
+            for (int j = 0; j < 4; ++j) {
+              widen4<FMT>(in[j], y[2 * j], y[2 * j + 1]);
+              if (!keys) {
 #pragma unroll
-              for (int e = 0; e < 2; ++e) {
-                const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&y[2 * j + e]));
-                y[2 * j + e] = pack16<true>(f.x, f.y);
+                for (int e = 0; e < 2; ++e) {
+                  const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&y[2 * j + e]));
+                  y[2 * j + e] = pack16<true>(f.x, f.y);
+                }
               }
             }
+            const uint32_t to = at_slot + (chunk >> 2) * (S::TOK * 128) + r * 128, c = 2 * (chunk & 3);
+            shared_store16(to + ((c ^ r & 7) << 4), y[0], y[1], y[2], y[3]);
+            shared_store16(to + ((c + 1 ^ r & 7) << 4), y[4], y[5], y[6], y[7]);
           }
-          const uint32_t to = at_slot + (chunk >> 2) * (S::TOK * 128) + r * 128, c = 2 * (chunk & 3);
-          shared_store16(to + ((c ^ r & 7) << 4), y[0], y[1], y[2], y[3]);
-          shared_store16(to + ((c + 1 ^ r & 7) << 4), y[4], y[5], y[6], y[7]);
         }
         if (keys) {  // the largest of the values' scales
-          unsigned char* const about = meta_ptr + (keys - 1) % S::NMETA * S::META;
+          unsigned char* const about = meta_ptr + m_slot * S::META;
           float top = lane < kEach ? *reinterpret_cast<volatile float*>(about + 16 + S::TOK * 4 + (w * kEach + lane) * 4) : 0.f;
 #pragma unroll
           for (int o = 16; o; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
           if (lane == 0) *reinterpret_cast<volatile float*>(about + 16 + S::TOK * 8 + w * 4) = top;
-          __syncwarp();
         }
+        __syncwarp();  // the place of the 8-bit tile is read out, too
       }
-      if (keys) bar_arrive(described + 8 * ((keys - 1) % S::NMETA));
+      if (keys) bar_arrive(described + 8 * m_slot), ++tile_landed;
       to_async_proxy();
       bar_arrive(full + 8 * slot);
       ++landed;
     };
-    // One tile of keys (or values) of cache head h, tokens pos0 on.
-    auto bring = [&](uint32_t tile, uint32_t pos0, uint32_t h, bool keys) {
-      if (!ok) return;
+    auto look_up = [&](uint32_t pos0) {
       const uint32_t pos = pos0 + w * kEach + (lane & (kEach - 1));
-      int32_t page = -1;
-      uint32_t off = 0;
+      page = -1;
       if (pos < at.group.len) {
         const uint32_t n = a.page_size.div(pos);
         off = pos - n * a.page_size.d;
@@ -566,51 +680,92 @@ __global__ void __launch_bounds__(Shape<FMT, DP>::THREADS, 1) bcp_kv_prefix_kern
           page = -1;
         }
       }
-      const bool on = page >= 0;
-      const uint64_t row = on ? uint64_t(uint32_t(page)) * a.page_stride + uint64_t(h) * a.head_stride + uint64_t(off) * a.token_stride : 0;
-      const uint32_t alive = __ballot_sync(0xffffffffu, on);
-      const uint32_t slot = item % S::SLOTS;
-      const char* const from = static_cast<const char*>(a.k) + (keys ? 0 : v_from_k);
-      uint32_t to = ring + slot * S::TILE;
-      if constexpr (S::quant) {
-        to = raw + item % S::RAWS * S::RAW + id * 16;
-      } else if (item >= S::SLOTS) {
-        ok = bar_wait(empty + 8 * slot, item / S::SLOTS - 1 & 1, stop);
-        if (!ok) return;
-      }
-#pragma unroll 4
-      for (uint32_t i = 0; i < kTurns; ++i) {
-        const uint32_t r = i * kTogether + my_row;
-        const uint64_t x = __shfl_sync(0xffffffffu, row, r) * (S::quant ? 1 : 2) + chunk * 16;
-        const bool copy = (alive >> r & 1) && inside;
-        uint32_t place;
-        if constexpr (S::quant) {
-          place = to + i * (kLoaders * 32 * 16);
-        } else {
-          const uint32_t tile_row = w * kEach + r;
-          place = to + (chunk >> 3) * (S::TOK * 128) + tile_row * 128 + ((chunk & 7 ^ tile_row & 7) << 4);
-        }
-        copy16(place, from + (copy ? x : 0), copy);
-      }
+    };
+    // A tile of keys, whose pages have been looked up, or of values of cache head h; `next`: where the tile after it begins, 0: none.
+    auto bring = [&](uint32_t tile, uint32_t next, uint32_t h, bool keys) {
+      if (!ok) return;
       if (keys) {
+        page_of[1] = page_of[0], off_of[1] = off_of[0], alive_of[1] = alive_of[0];
+        page_of[0] = page, off_of[0] = off, alive_of[0] = __ballot_sync(0xffffffffu, page >= 0) & kAll;
+        ++brought;
         unsigned char* const about = meta_ptr + tile % S::NMETA * S::META;
         if (lane == 0) {
-          if (kEach == 32) reinterpret_cast<volatile uint32_t*>(about)[w] = alive;
-          if (kEach == 16) reinterpret_cast<volatile uint16_t*>(about)[w] = uint16_t(alive);
-        }
-        if constexpr (S::quant) {
-          if (lane < kEach) {
-            const uint64_t n = (uint64_t(uint32_t(on ? page : 0)) * a.n_heads + h) * a.page_size.d + off;
-            const uint32_t there = meta + tile % S::NMETA * S::META + 16 + (w * kEach + lane) * 4;
-            copy4(there, a.k_scale + n, on);
-            copy4(there + S::TOK * 4, a.v_scale + n, on);
-          }
+          if (kEach == 32) reinterpret_cast<volatile uint32_t*>(about)[w] = alive_of[0];
+          if (kEach == 16) reinterpret_cast<volatile uint16_t*>(about)[w] = uint16_t(alive_of[0]);
         }
       }
+      // values come behind the next tile's keys where the streams take turns
+      const bool older = !keys && tile + 1 < brought;
+      const int32_t my_page = older ? page_of[1] : page_of[0];
+      const uint32_t my_off = older ? off_of[1] : off_of[0], alive = older ? alive_of[1] : alive_of[0];
+      const uint32_t slot = item % S::SLOTS, stage = S::quant ? item % S::RAWS : 0;
+      uint32_t bar = full + 8 * slot;
+      if constexpr (S::quant) {
+        bar = raw_full + 8 * (4 * stage + w);
+      } else if (item >= S::SLOTS) {
+        const uint32_t parity = item / S::SLOTS - 1 & 1;
+        // copies that are under way go on to the products while this tile's place is still taken
+        while (landed < item && !__all_sync(0xffffffffu, bar_test(empty + 8 * slot, parity))) {
+          copies_wait_all_but(item - landed - 1);
+          land();
+        }
+        ok = bar_wait(empty + 8 * slot, parity, stop);
+        if (!ok) return;
+      }
+      const bool box = a.block && alive == kAll;
+      if (box) {
+        // a warp's tokens in boxes, each inside one page
+        const CUtensorMap* const map = keys ? &a.k_map : &a.v_map;
+        if constexpr (S::quant) {
+          if (lane == 0) mbar_expect_tx(bar, kEach * a.head_dim);
+          __syncwarp();
+          if (lane < kEach && (lane & (a.block - 1)) == 0)
+            box_load(raw + stage * S::RAW + (w * kEach + lane) * a.head_dim, map, 0, my_off, h, uint32_t(my_page), bar);
+        } else {
+          const uint32_t wide = (a.head_dim + 63) / 64;
+          if (lane == 0) mbar_expect_tx(bar, kEach * 128 * wide);
+          __syncwarp();
+          if (lane < kEach && (lane & (a.block - 1)) == 0)
+            for (uint32_t i = 0; i < wide; ++i)
+              box_load(ring + slot * S::TILE + i * (S::TOK * 128) + (w * kEach + lane) * 128, map, 64 * i, my_off, h, uint32_t(my_page), bar);
+        }
+      } else {
+        const uint64_t row = my_page >= 0 ? uint64_t(uint32_t(my_page)) * a.page_stride + uint64_t(h) * a.head_stride + uint64_t(my_off) * a.token_stride : 0;
+        const char* const from = static_cast<const char*>(a.k) + (keys ? 0 : v_from_k);
+        const uint32_t to = S::quant ? raw + stage * S::RAW + w * kEach * a.head_dim : ring + slot * S::TILE;
+#pragma unroll 4
+        for (uint32_t i = 0; i < kTurns; ++i) {
+          const uint32_t r = i * kTogether + my_row;
+          const uint64_t x = __shfl_sync(0xffffffffu, row, r) * (S::quant ? 1 : 2) + chunk * 16;
+          const bool copy = (alive >> r & 1) && inside;
+          const uint32_t tile_row = w * kEach + r;
+          const uint32_t place = S::quant ? r * a.head_dim + chunk * 16 : (chunk >> 3) * (S::TOK * 128) + tile_row * 128 + ((chunk & 7 ^ tile_row & 7) << 4);
+          if (!S::quant || inside) copy16(to + place, from + (copy ? x : 0), copy);
+        }
+      }
+      if (S::quant && keys && lane < kEach) {
+        const uint64_t n = (uint64_t(uint32_t(page >= 0 ? page : 0)) * a.n_heads + h) * a.page_size.d + off;
+        const uint32_t there = meta + tile % S::NMETA * S::META + 16 + (w * kEach + lane) * 4;
+        copy4(there, a.k_scale + n, page >= 0);
+        copy4(there + S::TOK * 4, a.v_scale + n, page >= 0);
+      }
       copies_end();
-      kind[item & 7] = keys ? tile + 1 : 0;
+      if (next) look_up(next);
+      kinds = (kinds & ~(1u << (item & 31))) | uint32_t(keys) << (item & 31);
+      boxes = (boxes & ~(1u << (item & 31))) | uint32_t(box) << (item & 31);
       ++item;
-      if (item - landed > S::AHEAD) {
+      if (S::quant) {
+        if (item - landed > S::AHEAD) {
+          copies_wait<S::AHEAD>();
+          land();
+        }
+      } else if (a.block) {
+        // boxes count themselves; rows that had to be copied one by one, at the end of a prefix, are waited for at once
+        if (!box) copies_wait<0>(), to_async_proxy();
+        if (keys) bar_arrive(described + 8 * (tile % S::NMETA));
+        if (!box || lane) bar_arrive(bar);
+        landed = item;
+      } else if (item - landed > S::AHEAD) {
         copies_wait<S::AHEAD>();
         land();
       }
@@ -619,9 +774,10 @@ __global__ void __launch_bounds__(Shape<FMT, DP>::THREADS, 1) bcp_kv_prefix_kern
       const uint32_t n = min(at.group.steps - at.step, left), h = at.u / at.group.tiles;
       const uint32_t row0 = (at.u - h * at.group.tiles) * S::ROWS;
       const uint32_t ahead = min(at.group.rows - row0, S::ROWS) > kRows ? 1 : S::STREAMS;  // keys come so many tiles before values
+      look_up(at.step * S::TOK);
       for (uint32_t t = 0; t < n + ahead; ++t) {
-        if (t >= ahead) bring(tile0 + t - ahead, (at.step + t - ahead) * S::TOK, h, false);
-        if (t < n) bring(tile0 + t, (at.step + t) * S::TOK, h, true);
+        if (t >= ahead && t - ahead < n) bring(tile0 + t - ahead, 0, h, false);
+        if (t < n) bring(tile0 + t, t + 1 < n ? (at.step + t + 1) * S::TOK : 0, h, true);
       }
       tile0 += n;
       left -= n;
@@ -629,100 +785,105 @@ __global__ void __launch_bounds__(Shape<FMT, DP>::THREADS, 1) bcp_kv_prefix_kern
     }
     copies_wait<0>();
     while (landed < item && ok) land();
+    // (boxes under way are waited for by the products, or, if a wait ran out, by what follows)
+    if (!ok) {
+      const uint64_t begin = global_timer_ns();
+      while (global_timer_ns() - begin < kMostNs / 100) {
+      }
+    }
   } else {
     // ================================================================ the products
-    uint32_t item = 0, n_weights[2] = {0, 0}, n_queries[2] = {0, 0};
-    const uint32_t depth = a.head_dim / 16;
-    const uint32_t scores = product(FMT == BCP_BF16, false, S::TOK), sums = product(S::split, true, a.head_dim);
-    bool ok = true;
-    auto score = [&](uint32_t stream, uint32_t slot) {
-      if (lane == 0) {
-        const uint32_t q = q_at + stream * S::Q, k = ring + slot * S::TILE;
-        for (uint32_t i = 0; i < depth; ++i)
-          mma_shared(tmem + S::S0 + stream * S::TOK, operand(q + (i >> 2) * (kRows * 128) + (i & 3) * 32, 0), operand(k + (i >> 2) * (S::TOK * 128) + (i & 3) * 32, 0),
-                     scores, i > 0);
-        tmem_commit(s_full + 8 * stream);
-      }
-      __syncwarp();
-    };
-    auto weigh = [&](uint32_t stream, uint32_t slot, bool add) {
-      if (lane == 0) {
-        const uint32_t v = ring + slot * S::TILE, p = tmem + S::S0 + stream * S::TOK, o = tmem + S::O0 + stream * DP;
-        for (uint32_t i = 0; i < S::TOK / 16; ++i) {
-          const uint32_t from = p + (i >> 1) * 32 + (i & 1) * 8;
-          mma_tensor(o, from, operand(v + i * 2048, S::TOK * 128), sums, add || i > 0);
-          if (S::split) mma_tensor(o, from + 16, operand(v + i * 2048, S::TOK * 128), sums, true);
+    // A warp for each stream: one thread of it issues, which next to the busy warps takes about as long as the products themselves.
+    if constexpr (S::STREAMS == 2) fewer_registers<S::REGS_PRODUCT>();
+    const uint32_t stream = warp - (4 * S::STREAMS + kLoaders);
+    if (stream < S::STREAMS) {
+      uint32_t item = 0, n_weights = 0, n_queries = 0;  // item: the place of the stretch's first tile in the ring's order
+      const uint32_t depth = a.head_dim / 16;
+      const uint32_t scores = product(FMT == BCP_BF16, false, S::TOK), sums = product(S::split, true, a.head_dim);
+      const bool chosen = elected();
+      bool ok = true;
+      auto same = [](uint32_t x) { return __shfl_sync(0xffffffffu, x, 0); };  // (the compiler cannot know that it is)
+      auto score = [&](uint32_t i) {  // with the keys of item i
+        const uint32_t q = same(operand(q_at + stream * S::Q, 0)), k = same(operand(ring + i % S::SLOTS * S::TILE, 0)), d = same(tmem + S::S0 + stream * S::TOK);
+        if (chosen) {
+#pragma unroll
+          for (uint32_t j = 0; j < DP / 16; ++j)
+            if (j < depth) mma_shared(d, q + ((j >> 2) * (kRows * 128) + (j & 3) * 32) / 16, k + ((j >> 2) * (S::TOK * 128) + (j & 3) * 32) / 16, scores, j > 0);
+          tmem_commit(s_full + 8 * stream);
         }
-      }
-      __syncwarp();
-    };
-    auto commit = [&](uint32_t bar) {
-      if (lane == 0) tmem_commit(bar);
-      __syncwarp();
-    };
-    auto arrived = [&](uint32_t bar, uint32_t parity) {
-      ok = ok && bar_wait(bar, parity, stop);
-      tmem_after();
-      return ok;
-    };
-    auto have = [&](uint32_t i) { return arrived(full + 8 * (i % S::SLOTS), i / S::SLOTS & 1); };
-    while (left && ok) {
-      const uint32_t n = min(at.group.steps - at.step, left);
-      const uint32_t row0 = at.u % at.group.tiles * S::ROWS;
-      const bool both = min(at.group.rows - row0, S::ROWS) > kRows;
-      for (uint32_t s = 0; s < S::STREAMS; ++s)
-        if ((both || s < n) && !arrived(q_full + 8 * s, n_queries[s]++ & 1)) break;
-      if (!ok) break;
-      if (both) {
-        // every tile for both streams
-        if (!have(item)) break;
-        for (uint32_t s = 0; s < S::STREAMS; ++s) score(s, item % S::SLOTS);
-        commit(empty + 8 * (item++ % S::SLOTS));
-        for (uint32_t t = 0; t < n && ok; ++t) {
-          const uint32_t values = item, keys = item + 1;
+        __syncwarp();
+      };
+      auto weigh = [&](uint32_t i, bool add, uint32_t half) {  // half of the values of item i
+        const uint32_t first = (1 - half) * (S::TOK / 32);
+        const uint32_t v = same(operand(ring + i % S::SLOTS * S::TILE + first * 2048, S::TOK * 128));
+        const uint32_t p = same(tmem + S::S0 + stream * S::TOK + first * 16), o = same(tmem + S::O0 + stream * DP);
+        if (chosen) {
+#pragma unroll
+          for (uint32_t j = 0; j < S::TOK / 32; ++j) {
+            const uint32_t from = p + (j >> 1) * 32 + (j & 1) * 8;
+            mma_tensor(o, from, v + j * (2048 / 16), sums, j > 0 || add || half);
+            if (S::split) mma_tensor(o, from + 16, v + j * (2048 / 16), sums, true);
+          }
+        }
+        __syncwarp();
+      };
+      // An item is free when both streams are done with it; where they take turns the one that used it says so twice.
+      auto done = [&](uint32_t i, bool twice) {
+        if (chosen) {
+          tmem_commit(empty + 8 * (i % S::SLOTS));
+          if (twice) tmem_commit(empty + 8 * (i % S::SLOTS));
+        }
+        __syncwarp();
+      };
+      auto arrived = [&](uint32_t bar, uint32_t parity) {
+        ok = ok && bar_wait(bar, parity, stop);
+        tmem_after();
+        return ok;
+      };
+      auto have = [&](uint32_t i) { return arrived(full + 8 * (i % S::SLOTS), i / S::SLOTS & 1); };
+      while (left && ok) {
+        const uint32_t n = min(at.group.steps - at.step, left);
+        const uint32_t row0 = at.u % at.group.tiles * S::ROWS;
+        const bool both = min(at.group.rows - row0, S::ROWS) > kRows;
+        // Tiles first, first + step, .. are this stream's.  The ring's order: the keys of `ahead` tiles, then the values of a tile and the keys of the one `ahead` of it in turn.
+        const uint32_t step = both ? 1 : S::STREAMS, ahead = both ? 1 : S::STREAMS, first = both ? 0 : stream;
+        const uint32_t early = min(n, ahead);
+        auto keys_of = [&](uint32_t t) { return item + (t < ahead ? t : ahead + 2 * (t - ahead) + 1); };
+        auto values_of = [&](uint32_t t) { return item + early + (t + ahead <= n ? 2 * t : 2 * (n - early) + (t - (n - early))); };
+        if (first < n) {
+          if (!arrived(q_full + 8 * stream, n_queries++ & 1) || !have(keys_of(first))) break;
+          score(keys_of(first));
+          done(keys_of(first), !both || S::STREAMS == 1);
+        }
+        for (uint32_t t = first; t < n && ok; t += step) {
+          const uint32_t parity = n_weights++ & 1, values = values_of(t);
           if (!have(values)) break;
-          for (uint32_t s = 0; s < S::STREAMS; ++s) {
-            if (!arrived(p_full + 8 * s, n_weights[s]++ & 1)) break;
-            weigh(s, values % S::SLOTS, t > 0);
-            if (s == S::STREAMS - 1) commit(empty + 8 * (values % S::SLOTS));
-            if (t + 1 < n) {
-              if (!have(keys)) break;
-              score(s, keys % S::SLOTS);
-              if (s == S::STREAMS - 1) commit(empty + 8 * (keys % S::SLOTS));
-            } else {
-              commit(o_full + 8 * s);
-            }
+#pragma unroll 1
+          for (uint32_t half = 0; half < 2; ++half) {
+            if (!arrived(p_full + 16 * stream + 8 * half, parity)) break;
+            weigh(values, t > first, half);
           }
-          item += t + 1 < n ? 2 : 1;
-        }
-      } else {
-        // the streams take turns
-        for (uint32_t t = 0; t < min(n, S::STREAMS) && ok; ++t) {
-          if (!have(item)) break;
-          score(t, item % S::SLOTS);
-          commit(empty + 8 * (item++ % S::SLOTS));
-        }
-        for (uint32_t t = 0; t < n && ok; ++t) {
-          const uint32_t s = t % S::STREAMS;
-          if (!have(item) || !arrived(p_full + 8 * s, n_weights[s]++ & 1)) break;
-          weigh(s, item % S::SLOTS, t >= S::STREAMS);
-          commit(empty + 8 * (item++ % S::SLOTS));
-          if (t + S::STREAMS < n) {
-            if (!have(item)) break;
-            score(s, item % S::SLOTS);
-            commit(empty + 8 * (item++ % S::SLOTS));
-          } else {
-            commit(o_full + 8 * s);
+          if (!ok) break;
+          done(values, !both || S::STREAMS == 1);
+          if (t + step < n) {
+            if (!have(keys_of(t + step))) break;
+            score(keys_of(t + step));
+            done(keys_of(t + step), !both || S::STREAMS == 1);
+          } else if (chosen) {
+            tmem_commit(o_full + 8 * stream);
           }
+          __syncwarp();
         }
+        item += 2 * n;
+        left -= n;
+        advance<S>(at, a, n, left != 0);
       }
-      left -= n;
-      advance<S>(at, a, n, left != 0);
-    }
-    if (!ok) {  // what was issued comes to its end before the tensor memory is given back
-      commit(drained);
-      const uint64_t begin = global_timer_ns();
-      while (!mbar_try_wait(drained, 0) && global_timer_ns() - begin < kMostNs) {
+      if (!ok) {  // what was issued comes to its end before the tensor memory is given back
+        if (chosen) tmem_commit(drained + 8 * stream);
+        __syncwarp();
+        const uint64_t begin = global_timer_ns();
+        while (!mbar_try_wait(drained + 8 * stream, 0) && global_timer_ns() - begin < kMostNs) {
+        }
       }
     }
   }
@@ -730,18 +891,157 @@ __global__ void __launch_bounds__(Shape<FMT, DP>::THREADS, 1) bcp_kv_prefix_kern
   __syncthreads();
   if (tid == 0 && *stop) raise(a.status, BCP_TIMED_OUT);
   tmem_after();
-  if (warp == S::WARPS - 1) tmem_free(tmem);
+  if (warp == S::WARPS - 4) tmem_free(tmem);
+}
+
+// ------------------------------------------------------------------------------ the end
+// The records of a row, that of its own tokens first and then its prefix's in the order of the parts, become its result.  Four warps: rows with few
+// records have a warp each, rows with many all four.
+struct JoinArgs {
+  const int4* rows;
+  const float2* ml;
+  const float* o;
+  uint32_t n_rows, n_q_heads, dims, apart, own, records, parts;  // own: the record of row 0's own tokens; apart: records from one part to the next
+  void* out;
+  float* lse;
+  int64_t out_token, out_head;
+  uint32_t is_bf16;
+};
+constexpr uint32_t kJoinRows = 4;
+constexpr uint32_t kFew = 33;  // records that a warp takes alone
+
+template <int DP>
+__global__ void __launch_bounds__(128) bcp_kv_join_kernel(const JoinArgs a) {
+  after_previous();
+  constexpr int N = (DP + 127) / 128;  // vectors of four dimensions a lane
+  const uint32_t tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  __shared__ float4 sums[kJoinRows][N][32];
+  __shared__ float2 about[kJoinRows];
+  const uint32_t row0 = blockIdx.x * kJoinRows;
+  int4 d = make_int4(0, 0, 0, 0);
+  if (row0 + warp < a.n_rows) d = __ldcg(a.rows + row0 + warp);
+  const uint32_t both = d.w ? 2 : 1;
+  const uint32_t mine = 1 + min(uint32_t(d.z), a.parts) * both;
+  const bool together = __syncthreads_or(mine > kFew);
+
+  // records first, first + step, .. of row r: largest reference, denominator, sums
+  float m, den;
+  float4 x[N];
+  auto add_up = [&](uint32_t r, const int4 d, uint32_t n, uint32_t first, uint32_t step) {
+    const uint32_t both = d.w ? 2 : 1;
+    auto record = [&](uint32_t i) {
+      if (i == 0) return a.own + r;
+      const uint32_t part = (i - 1) / both;
+      const uint32_t place = (part ? uint32_t(d.y) + (part - 1) * a.apart : uint32_t(d.x)) + (i - 1) % both * uint32_t(d.w);
+      return place < a.records ? place : a.own + r;  // (a row that two groups claim: whatever comes out)
+    };
+    m = kNone, den = 0.f;
+#pragma unroll
+    for (int k = 0; k < N; ++k) x[k] = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (uint32_t i0 = first; i0 < n; i0 += 32 * step) {
+      // a record a lane
+      const uint32_t i = i0 + lane * step;
+      float2 ml = make_float2(kNone, 0.f);
+      uint32_t place = a.own + r;
+      if (i < n) place = record(i), ml = __ldcg(a.ml + place);
+      float top = ml.y > 0.f ? ml.x : kNone;
+#pragma unroll
+      for (int o = 16; o; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+      top = fmaxf(top, m);
+      const Factor<true> before(m - top);
+      den = before.denominator(den), m = top;
+#pragma unroll
+      for (int k = 0; k < N; ++k) x[k].x *= before.all, x[k].y *= before.all, x[k].z *= before.all, x[k].w *= before.all;
+      const Factor<true> down(ml.y > 0.f ? ml.x - top : kNone);
+      float weight = down.all, sum = down.denominator(ml.y);
+      if (ml.y != ml.y) weight = sum = ml.y;  // a NaN stays one
+#pragma unroll
+      for (int o = 16; o; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+      den += sum;
+      const uint32_t here = min(32u, (n - i0 + step - 1) / step);
+#pragma unroll 1
+      for (uint32_t j0 = 0; j0 < here; j0 += 8) {
+        float4 y[8][N];
+        float w[8];
+#pragma unroll
+        for (uint32_t j = 0; j < 8; ++j) {
+          w[j] = __shfl_sync(0xffffffffu, weight, j0 + j);
+          const float* const from = a.o + uint64_t(__shfl_sync(0xffffffffu, place, j0 + j)) * a.dims;
+          if (j0 + j >= here) w[j] = 0.f;
+#pragma unroll
+          for (int k = 0; k < N; ++k)
+            if (w[j] != 0.f && 128 * k + 4 * lane < a.dims) y[j][k] = __ldcg(reinterpret_cast<const float4*>(from + 128 * k + 4 * lane));
+        }
+#pragma unroll
+        for (uint32_t j = 0; j < 8; ++j) {
+          if (w[j] == 0.f) continue;  // an empty record has no sums
+#pragma unroll
+          for (int k = 0; k < N; ++k)
+            x[k].x += y[j][k].x * w[j], x[k].y += y[j][k].y * w[j], x[k].z += y[j][k].z * w[j], x[k].w += y[j][k].w * w[j];
+        }
+      }
+    }
+  };
+  auto finish = [&](uint32_t r) {
+    const float inv = den == 0.f ? 0.f : reciprocal_fast(den);
+    const uint32_t b = r / a.n_q_heads, h = r - b * a.n_q_heads;
+#pragma unroll
+    for (int k = 0; k < N; ++k) {
+      const uint32_t e = 128 * k + 4 * lane;
+      if (e >= a.dims) break;
+      uint2 y;
+      y.x = a.is_bf16 ? pack16<true>(x[k].x * inv, x[k].y * inv) : pack16<false>(x[k].x * inv, x[k].y * inv);
+      y.y = a.is_bf16 ? pack16<true>(x[k].z * inv, x[k].w * inv) : pack16<false>(x[k].z * inv, x[k].w * inv);
+      *reinterpret_cast<uint2*>(static_cast<char*>(a.out) + (b * a.out_token + h * a.out_head + e) * 2) = y;
+    }
+    if (lane == 0 && a.lse) a.lse[r] = den == 0.f ? -INFINITY : (m + log2_fast(den)) * 0.6931471805599453f;
+  };
+
+  if (!together) {
+    if (row0 + warp >= a.n_rows) return;
+    add_up(row0 + warp, d, mine, 0, 1);
+    finish(row0 + warp);
+    return;
+  }
+  for (uint32_t i = 0; i < kJoinRows && row0 + i < a.n_rows; ++i) {
+    const int4 e = __ldcg(a.rows + row0 + i);
+    const uint32_t n = 1 + min(uint32_t(e.z), a.parts) * (e.w ? 2 : 1);
+    add_up(row0 + i, e, n, warp, 4);
+#pragma unroll
+    for (int k = 0; k < N; ++k) sums[warp][k][lane] = x[k];
+    if (lane == 0) about[warp] = make_float2(m, den);
+    __syncthreads();
+    if (warp == (i & 3)) {
+      float top = kNone;
+      for (uint32_t w = 0; w < 4; ++w) top = fmaxf(top, about[w].x);
+      m = top, den = 0.f;
+#pragma unroll
+      for (int k = 0; k < N; ++k) x[k] = make_float4(0.f, 0.f, 0.f, 0.f);
+      for (uint32_t w = 0; w < 4; ++w) {
+        const Factor<true> down(about[w].x - top);
+        den += down.denominator(about[w].y);
+#pragma unroll
+        for (int k = 0; k < N; ++k) {
+          const float4 y = sums[w][k][lane];
+          x[k].x += y.x * down.all, x[k].y += y.y * down.all, x[k].z += y.z * down.all, x[k].w += y.w * down.all;
+        }
+      }
+      finish(row0 + i);
+    }
+    __syncthreads();
+  }
 }
 
 // ------------------------------------------------------------------------------ launch
 struct Variant {
   void (*kernel)(PrefixArgs);
-  uint32_t smem, threads, rows, tokens;
+  void (*join)(JoinArgs);
+  uint32_t smem, threads, rows, tokens, registers;
 };
 template <int FMT, int DP>
 Variant variant() {
   typedef Shape<FMT, DP> S;
-  return Variant{bcp_kv_prefix_kernel<FMT, DP>, S::SMEM, S::THREADS, S::ROWS, S::TOK};
+  return Variant{bcp_kv_prefix_kernel<FMT, DP>, DP <= 128 ? bcp_kv_join_kernel<128> : bcp_kv_join_kernel<256>, S::SMEM, S::THREADS, S::ROWS, S::TOK, S::STREAMS == 2 ? S::REGS : 0};
 }
 template <int FMT>
 Variant variant_of(uint32_t head_dim) {
@@ -774,10 +1074,55 @@ int prepare(const Variant& v, uint32_t* sms) {
       *sms = known[i].sms;
       return BCP_OK;
     }
+  // the warpgroups hand registers to one another: what they hand on has to be there
+  cudaFuncAttributes about;
+  BCP_CUDA(cudaFuncGetAttributes(&about, v.kernel));
+  if (v.registers && about.numRegs != int(v.registers)) return fail(BCP_ERR_CUDA, "bcp_kv_attend_shared: the kernel has %d registers a thread, not %u", about.numRegs, v.registers);
   BCP_CUDA(cudaFuncSetAttribute(v.kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, int(v.smem)));
   BCP_CUDA(cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, device));
   *sms = uint32_t(n);
   if (n_known < 256) known[n_known++] = {v.kernel, device, *sms};
+  return BCP_OK;
+}
+
+typedef CUresult (*EncodeTiled)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*,
+                                const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+int encode_tiled(EncodeTiled* out) {
+  static std::mutex mu;
+  static EncodeTiled known = nullptr;
+  std::lock_guard<std::mutex> lock(mu);
+  if (!known) {
+    void* sym = nullptr;
+    cudaDriverEntryPointQueryResult q;
+    BCP_CUDA(cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &sym, cudaEnableDefault, &q));
+    if (q != cudaDriverEntryPointSuccess || !sym) return fail(BCP_ERR_CUDA, "cuTensorMapEncodeTiled is not available in this driver");
+    known = reinterpret_cast<EncodeTiled>(sym);
+  }
+  *out = known;
+  return BCP_OK;
+}
+// Keys and values as tensors of whose tokens a warp's share of a tile is brought in boxes: of as many tokens as divide a page, a power of two of at least
+// eight.  Smaller ones would be more commands than the copies take, and vectors under 64 elements do not fill a box: those are copied row by row.
+int make_maps(const bcp_kv_cache* c, const Variant& v, PrefixArgs* a) {
+  uint32_t block = v.tokens / kLoaders;
+  while (c->page_size % block) block /= 2;
+  const bool wide = is_8bit(c->format);
+  a->block = 0;
+  if (block < 8 || (!wide && c->head_dim < 64)) return BCP_OK;
+  EncodeTiled encode = nullptr;
+  if (int rc = encode_tiled(&encode)) return rc;
+  const uint64_t es = type_size(c->format);
+  const cuuint64_t dims[4] = {c->head_dim, c->page_size, c->n_heads, c->n_pages};
+  const cuuint64_t strides[3] = {uint64_t(c->token_stride) * es, uint64_t(c->head_stride) * es, uint64_t(c->page_stride) * es};
+  const cuuint32_t box[4] = {wide ? c->head_dim : 64, block, 1, 1}, ones[4] = {1, 1, 1, 1};
+  const CUtensorMapDataType type = wide ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : CU_TENSOR_MAP_DATA_TYPE_UINT16;
+  for (int side = 0; side < 2; ++side) {
+    const CUresult rc = encode(side ? &a->v_map : &a->k_map, type, 4, side ? c->v : c->k, dims, strides, box, ones, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                               wide ? CU_TENSOR_MAP_SWIZZLE_NONE : CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                               CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    if (rc != CUDA_SUCCESS) return BCP_OK;  // strides that a tensor map cannot have
+  }
+  a->block = block;
   return BCP_OK;
 }
 
@@ -787,7 +1132,7 @@ struct Layout {
   uint64_t rows, ml, o, end, records;
   Layout(uint64_t begin, const Variant& v, uint32_t sms, uint64_t n_seqs, uint32_t n_q_heads, uint32_t head_dim) {
     const uint64_t every = n_seqs * n_q_heads;
-    records = 2 * every + 2ull * sms * v.rows;
+    records = 3 * every + 2ull * sms * v.rows;  // whole units (two streams), parts, own tokens
     rows = aligned(begin), ml = aligned(rows + every * sizeof(int4)), o = aligned(ml + records * sizeof(float2)), end = o + records * head_dim * 4;
   }
 };
@@ -849,17 +1194,28 @@ extern "C" int bcp_kv_attend_shared(const bcp_kv_cache* c, const bcp_heads* q, c
   a.page_size = FastDiv(c->page_size);
   a.status = c->status;
   a.q = q->data, a.q_token = q->token_stride, a.q_head = q->head_stride;
-  a.q_is_bf16 = q->type == BCP_BF16, a.n_seqs = n_seqs, a.n_groups = n_prefixes, a.group = FastDiv(group);
+  a.q_is_bf16 = q->type == BCP_BF16, a.q_wide = rows_aligned(q, 16), a.n_seqs = n_seqs, a.n_groups = n_prefixes, a.group = FastDiv(group);
   a.table = prefix_table, a.table_stride = prefix_stride;
   a.lengths = prefix_lengths, a.starts = starts;
   a.scale_log2 = scale * kLog2e;
+  if (int rc = make_maps(c, v, &a)) return rc;
   char* const w = static_cast<char*>(workspace);
   a.rows = reinterpret_cast<int4*>(w + at.rows), a.ml = reinterpret_cast<float2*>(w + at.ml), a.o = reinterpret_cast<float*>(w + at.o);
-  const Prior prior = {a.rows, a.ml, a.o, c->head_dim, 2 * v.rows, uint32_t(at.records), sms};
-  // the second call's arguments are looked at before the first kernel is launched
-  if (int rc = attend(call, c, q, out, lse, n_seqs, block_table, table_stride, table_width, lengths, scale, 0, workspace, own, &prior, false, stream))
+  const uint64_t own_at = at.records - uint64_t(n_seqs) * q->n_heads;
+  const Records records = {a.ml + own_at, a.o + own_at * c->head_dim, c->head_dim};
+  // the second kernel's arguments are looked at before the first is launched
+  if (int rc = attend(call, c, q, out, lse, n_seqs, block_table, table_stride, table_width, lengths, scale, 0, workspace, own, &records, false, stream))
     return rc;
   const uint64_t most = tiles * c->n_heads * steps;
-  BCP_CUDA(launch_early(v.kernel, uint32_t(most < sms ? most : sms), v.threads, v.smem, static_cast<cudaStream_t>(stream), a));
-  return attend(call, c, q, out, lse, n_seqs, block_table, table_stride, table_width, lengths, scale, 0, workspace, own, &prior, true, stream);
+  cudaStream_t const st = static_cast<cudaStream_t>(stream);
+  BCP_CUDA(launch_early(v.kernel, uint32_t(most < sms ? most : sms), v.threads, v.smem, st, a));
+  if (int rc = attend(call, c, q, out, lse, n_seqs, block_table, table_stride, table_width, lengths, scale, 0, workspace, own, &records, true, stream))
+    return rc;
+  JoinArgs j = {};
+  j.rows = a.rows, j.ml = a.ml, j.o = a.o;
+  j.n_rows = n_seqs * q->n_heads, j.n_q_heads = q->n_heads, j.dims = c->head_dim;
+  j.apart = 2 * v.rows, j.own = uint32_t(own_at), j.records = uint32_t(own_at), j.parts = sms;
+  j.out = out->data, j.lse = lse, j.out_token = out->token_stride, j.out_head = out->head_stride, j.is_bf16 = out->type == BCP_BF16;
+  BCP_CUDA(launch_early(v.join, (j.n_rows + kJoinRows - 1) / kJoinRows, 128, 0, st, j));
+  return BCP_OK;
 }
