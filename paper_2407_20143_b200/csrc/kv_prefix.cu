@@ -68,13 +68,12 @@ struct Shape {
   static constexpr uint32_t NMETA = quant ? 8 : kMeta;
   static constexpr uint32_t SLOTS = DP == 64 ? 8 : quant ? 3 : 5;
   static constexpr uint32_t AHEAD = quant ? RAWS - 1 : 3;    // copies of so many tiles are under way
-  static constexpr uint32_t SMEM = STREAMS * Q + SLOTS * TILE + RAWS * RAW + NMETA * META + 8 * (2 * SLOTS + NMETA + 6 * STREAMS + 4 * RAWS) + 64 + 1024;
-  // a warpgroup for each stream, one that copies, one of whose warps issues the products
-  static constexpr uint32_t WARPS = 4 * STREAMS + kLoaders + 4, THREADS = 32 * WARPS;
-  // Registers a thread: at launch, and after the groups have been given theirs (their sum is the launch's).
-  // With one stream there are enough for all.
-  static constexpr uint32_t REGS = 128, REGS_ROWS = 168, REGS_COPY = 104, REGS_PRODUCT = 72;
-  static_assert(2 * REGS_ROWS + REGS_COPY + REGS_PRODUCT <= 4 * REGS, "registers of the launch");
+  static constexpr uint32_t SMEM = STREAMS * Q + SLOTS * TILE + RAWS * RAW + NMETA * META + 8 * (2 * SLOTS + NMETA + 7 * STREAMS + 4 * RAWS) + STREAMS * 1024 + 48;
+  // two warpgroups for each stream (a thread has half of a row's scores), one that copies, one of whose warps issue the products
+  static constexpr uint32_t WARPS = 8 * STREAMS + kLoaders + 4, THREADS = 32 * WARPS, COLS = TOK / 2;
+  // Registers a thread: at launch, and after the groups have been given theirs (their sum is the launch's).  With one stream there are enough for all.
+  static constexpr uint32_t REGS = 80, REGS_ROWS = 88, REGS_COPY = 72, REGS_PRODUCT = 56;
+  static_assert(4 * REGS_ROWS + REGS_COPY + REGS_PRODUCT <= 6 * REGS, "registers of the launch");
   static constexpr uint32_t S0 = 0, O0 = STREAMS * TOK;      // columns of tensor memory
   static_assert(O0 + STREAMS * DP <= 512, "tensor memory");
   static_assert(SMEM <= 232448, "shared memory");
@@ -88,10 +87,16 @@ __device__ __forceinline__ bool bar_test(uint32_t bar, uint32_t parity) {  // wi
   asm volatile("{\n.reg .pred p;\nmbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\nselp.u32 %0, 1, 0, p;\n}" : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
   return ok;
 }
+// Sleeps until the phase is complete, a millisecond at most.
+__device__ __forceinline__ bool bar_sleep(uint32_t bar, uint32_t parity) {
+  uint32_t ok;
+  asm volatile("{\n.reg .pred p;\nmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, 1000000;\nselp.u32 %0, 1, 0, p;\n}" : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
+  return ok;
+}
 // False, in all lanes of a warp, if the wait ran out here or in another warp.
 __device__ __forceinline__ bool bar_wait_slow(uint32_t bar, uint32_t parity, volatile uint32_t* stop) {
   const uint64_t begin = global_timer_ns();
-  while (!mbar_try_wait(bar, parity)) {
+  while (!bar_sleep(bar, parity)) {
     if (*stop) return false;
     if (global_timer_ns() - begin > kMostNs) {
       *stop = 1;
@@ -101,7 +106,7 @@ __device__ __forceinline__ bool bar_wait_slow(uint32_t bar, uint32_t parity, vol
   return true;
 }
 __device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity, volatile uint32_t* stop) {
-  return __all_sync(0xffffffffu, mbar_try_wait(bar, parity) || bar_wait_slow(bar, parity, stop));
+  return __all_sync(0xffffffffu, bar_sleep(bar, parity) || bar_wait_slow(bar, parity, stop));
 }
 
 __device__ __forceinline__ void tmem_alloc(uint32_t to) { asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(to) : "memory"); }
@@ -159,6 +164,9 @@ __device__ __forceinline__ float largest(float a, float b, float c) {
   return r;
 }
 __device__ __forceinline__ float minus_upper(float x) { return __uint_as_float((__float_as_uint(x) & 0xffff0000u) ^ 0x80000000u); }
+// A number that all lanes have, in a form in which the compiler knows that they do: it then lies in a uniform register, where the operands of
+// tcgen05 instructions have to be, and branches on it keep the warp together.
+__device__ __forceinline__ uint32_t same(uint32_t x) { return __reduce_or_sync(0xffffffffu, x); }
 __device__ __forceinline__ bool elected() {
   uint32_t yes;
   asm volatile("{\n.reg .pred p;\nelect.sync _|p, 0xffffffff;\nselp.u32 %0, 1, 0, p;\n}" : "=r"(yes));
@@ -179,14 +187,17 @@ constexpr uint32_t kUpper = 1024 >> 4 | 1u << 14 | 2u << 29;
 __host__ __device__ constexpr uint32_t product(bool bf16, bool second_by_rows, uint32_t n) {
   return 1u << 4 | (bf16 ? 1u << 7 | 1u << 10 : 0u) | (second_by_rows ? 1u << 16 : 0u) | (n >> 3) << 17 | (kRows >> 4) << 24;
 }
-__device__ __forceinline__ void mma_shared(uint32_t d, uint32_t a, uint32_t b, uint32_t what, bool add) {
-  asm volatile("{\n.reg .pred p;\n.reg .b64 x, y;\nsetp.ne.u32 p, %4, 0;\nmov.b64 x, {%1, %5};\nmov.b64 y, {%2, %5};\n"
-               "tcgen05.mma.cta_group::1.kind::f16 [%0], x, y, %3, p;\n}" ::"r"(d), "r"(a), "r"(b), "r"(what), "r"(uint32_t(add)), "n"(kUpper)
+// (Only the instruction itself is left to one lane: the numbers around it are made by the whole warp.)
+__device__ __forceinline__ void mma_shared(bool chosen, uint32_t d, uint32_t a, uint32_t b, uint32_t what, bool add) {
+  asm volatile("{\n.reg .pred p, q;\n.reg .b64 x, y;\nsetp.ne.u32 p, %4, 0;\nsetp.ne.u32 q, %6, 0;\nmov.b64 x, {%1, %5};\nmov.b64 y, {%2, %5};\n"
+               "@q tcgen05.mma.cta_group::1.kind::f16 [%0], x, y, %3, p;\n}" ::"r"(d), "r"(a), "r"(b), "r"(what), "r"(uint32_t(add)), "n"(kUpper),
+               "r"(uint32_t(chosen))
                : "memory");
 }
-__device__ __forceinline__ void mma_tensor(uint32_t d, uint32_t a, uint32_t b, uint32_t what, bool add) {
-  asm volatile("{\n.reg .pred p;\n.reg .b64 y;\nsetp.ne.u32 p, %4, 0;\nmov.b64 y, {%2, %5};\ntcgen05.mma.cta_group::1.kind::f16 [%0], [%1], y, %3, p;\n}" ::"r"(d),
-               "r"(a), "r"(b), "r"(what), "r"(uint32_t(add)), "n"(kUpper)
+__device__ __forceinline__ void mma_tensor(bool chosen, uint32_t d, uint32_t a, uint32_t b, uint32_t what, bool add) {
+  asm volatile("{\n.reg .pred p, q;\n.reg .b64 y;\nsetp.ne.u32 p, %4, 0;\nsetp.ne.u32 q, %6, 0;\nmov.b64 y, {%2, %5};\n"
+               "@q tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], y, %3, p;\n}" ::"r"(d), "r"(a), "r"(b), "r"(what), "r"(uint32_t(add)), "n"(kUpper),
+               "r"(uint32_t(chosen))
                : "memory");
 }
 __device__ __forceinline__ void shared_store16(uint32_t at, uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
@@ -258,26 +269,30 @@ __device__ __forceinline__ void advance(Place& p, const PrefixArgs& a, uint32_t 
 template <int FMT, int DP>
 __global__ void __launch_bounds__(Shape<FMT, DP>::THREADS, 1) bcp_kv_prefix_kernel(const __grid_constant__ PrefixArgs a) {
   typedef Shape<FMT, DP> S;
-  extern __shared__ unsigned char raw_smem[];
-  const uint32_t tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-  unsigned char* const smem = raw_smem + (1024 - (uint32_t(__cvta_generic_to_shared(raw_smem)) & 1023) & 1023);
+  extern __shared__ __align__(1024) unsigned char smem[];  // swizzled blocks lie on 1024-byte boundaries
+  const uint32_t tid = threadIdx.x, warp = same(tid >> 5), lane = tid & 31;
   const uint32_t base = uint32_t(__cvta_generic_to_shared(smem));
   const uint32_t q_at = base, ring = q_at + S::STREAMS * S::Q, raw = ring + S::SLOTS * S::TILE, meta = raw + S::RAWS * S::RAW;
   unsigned char* const meta_ptr = smem + (meta - base);
   const uint32_t bars = meta + S::NMETA * S::META;
   const uint32_t full = bars, empty = full + 8 * S::SLOTS, described = empty + 8 * S::SLOTS, q_full = described + 8 * S::NMETA, s_full = q_full + 8 * S::STREAMS,
-                 p_full = s_full + 8 * S::STREAMS, o_full = p_full + 16 * S::STREAMS, drained = o_full + 8 * S::STREAMS, raw_full = drained + 8 * S::STREAMS;
-  uint32_t* const words = reinterpret_cast<uint32_t*>(smem + (raw_full + 32 * S::RAWS - base));  // tensor memory, stop, found[8]
+                 p_full = s_full + 8 * S::STREAMS, o_full = p_full + 16 * S::STREAMS, drained = o_full + 8 * S::STREAMS, turn = drained + 8 * S::STREAMS, raw_full = turn + 8 * S::STREAMS;
+  uint32_t* const words = reinterpret_cast<uint32_t*>(smem + (raw_full + 32 * S::RAWS + S::STREAMS * 1024 - base));  // tensor memory, stop, found[8]
+  volatile float* const swap = reinterpret_cast<volatile float*>(smem + (raw_full + 32 * S::RAWS - base));  // [stream][half][row]
   volatile uint32_t* const stop = words + 1;
   uint32_t* const found = words + 2;
   uint32_t* const totals = reinterpret_cast<uint32_t*>(smem);  // before the tiles come
 
+  if (base & 1023) {  // no room is left to move them there
+    if (tid == 0) raise(a.status, BCP_TIMED_OUT);
+    return;
+  }
   if (warp == S::WARPS - 4) tmem_alloc(uint32_t(__cvta_generic_to_shared(words)));
   if (tid == 0) {
     for (uint32_t i = 0; i < S::SLOTS; ++i) mbar_init(full + 8 * i, 32 * kLoaders), mbar_init(empty + 8 * i, 2);
     for (uint32_t i = 0; i < S::NMETA; ++i) mbar_init(described + 8 * i, 32 * kLoaders);
     for (uint32_t i = 0; i < S::STREAMS; ++i)
-      mbar_init(q_full + 8 * i, kRows), mbar_init(s_full + 8 * i, 1), mbar_init(p_full + 16 * i, kRows), mbar_init(p_full + 16 * i + 8, kRows), mbar_init(o_full + 8 * i, 1), mbar_init(drained + 8 * i, 1);
+      mbar_init(q_full + 8 * i, 2 * kRows), mbar_init(s_full + 8 * i, 1), mbar_init(p_full + 16 * i, 2 * kRows), mbar_init(p_full + 16 * i + 8, 2 * kRows), mbar_init(o_full + 8 * i, 1), mbar_init(drained + 8 * i, 1), mbar_init(turn + 8 * i, 1);
     for (uint32_t i = 0; i < 4 * S::RAWS; ++i) mbar_init(raw_full + 8 * i, 1);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
@@ -356,114 +371,131 @@ __global__ void __launch_bounds__(Shape<FMT, DP>::THREADS, 1) bcp_kv_prefix_kern
   at.group.first = found[3], at.group.rows = found[4], at.group.len = found[5], at.group.steps = found[6], at.group.tiles = found[7];
 
   uint32_t left = n_steps;
-  if (warp < 4 * S::STREAMS) {
+  if (warp < 8 * S::STREAMS) {
     // ================================================================ a stream's rows
     if constexpr (S::STREAMS == 2) more_registers<S::REGS_ROWS>();
-    const uint32_t stream = warp >> 2, row = tid & (kRows - 1);
-    const uint32_t lanes = tmem + ((warp & 3) << 21);  // this warp's 32 rows
-    const uint32_t s_at = lanes + S::S0 + stream * S::TOK, o_at = lanes + S::O0 + stream * DP;
+    const uint32_t stream = warp >> 3, part = warp >> 2 & 1, quarter = warp & 3, row = quarter * 32 + lane;
+    const uint32_t lanes = tmem + (quarter << 21);  // this warp's 32 rows
+    const uint32_t s_at = lanes + S::S0 + stream * S::TOK + part * S::COLS, o_at = lanes + S::O0 + stream * DP;
     uint32_t n_scores = 0, n_ends = 0, tile0 = 0;
     const float scale = fabsf(a.scale_log2);
     constexpr float kLeast = 0x1p-126f;  // a factor is not 0, so that a masked score stays below all others; any score times this counts as 0
     bool ok = true;
+    // The two warps of 32 rows wait for each other; the two threads of a row see each other's number.  (A warp that gives up arrives once more, below, so that
+    // the other does not wait for it.)
+    const uint32_t pair = 1 + 4 * stream + quarter;
+    auto meet = [&]() { asm volatile("bar.sync %0, 64;" ::"r"(pair) : "memory"); };
+    auto other = [&](float mine) {
+      swap[(stream * 2 + part) * kRows + row] = mine;
+      meet();
+      return swap[(stream * 2 + 1 - part) * kRows + row];
+    };
     while (left && ok) {
       const uint32_t n = min(at.group.steps - at.step, left);
       const uint32_t h = at.u / at.group.tiles, row0 = (at.u - h * at.group.tiles) * S::ROWS, rows = min(at.group.rows - row0, S::ROWS);
       const bool both = rows > kRows;  // the streams have rows of their own, else they take turns
       const uint32_t r = row0 + (both ? stream * kRows : 0) + row;
-      const bool live = r < row0 + rows;
+      const bool live = r < row0 + rows, work = __any_sync(0xffffffffu, live);
       const uint32_t seq = a.group.div(live ? r : 0), head = h * a.group.d + (live ? r : 0) - seq * a.group.d, b = at.group.first + seq;
-
-      // ---- the query into shared memory; over 8-bit caches a power of two brings its largest element into [1, 2), so that it fits binary16
       const bool any = both || stream < n;  // has tiles here
       float factor = scale;
       if (any) {
-        // A warp's 32 rows, neighbouring lanes on neighbouring chunks of a row.
+        // The queries into shared memory, neighbouring lanes on neighbouring chunks of a row; a warp has 16 of its 32 rows, the other part's the rest.  Over 8-bit
+        // caches a power of two brings a row's largest element into [1, 2), so that it fits binary16.
         const uint32_t flip = a.scale_log2 < 0.f ? 0x80008000u : 0u;  // the scale's sign goes into the query
         const int64_t from = live ? b * a.q_token + head * a.q_head : -1;
-        constexpr uint32_t kChunks = DP / 8, kTogether = 32 / kChunks;
+        constexpr uint32_t kChunks = DP / 8, kTogether = 32 / kChunks, kTurns = 16 / kTogether, kAtOnce = 8;
         const uint32_t c = lane % kChunks, mine = lane / kChunks;
-#pragma unroll 4
-        for (uint32_t i = 0; i < 32 / kTogether; ++i) {
-          const uint32_t owner = i * kTogether + mine, r = (warp & 3) * 32 + owner;
-          const int64_t at_row = __shfl_sync(0xffffffffu, from, owner);
-          uint4 x = make_uint4(0, 0, 0, 0);
-          if (at_row >= 0 && 8 * c < a.head_dim) {
-            const char* const p = static_cast<const char*>(a.q) + (at_row + 8 * c) * 2;
-            if (a.q_wide) {
-              x = *reinterpret_cast<const uint4*>(p);
-            } else {
-              const uint2 u = *reinterpret_cast<const uint2*>(p), v = *reinterpret_cast<const uint2*>(p + 8);
-              x = make_uint4(u.x, u.y, v.x, v.y);
+#pragma unroll 1
+        for (uint32_t i0 = 0; i0 < kTurns; i0 += kAtOnce) {
+          uint4 x[kAtOnce];
+#pragma unroll
+          for (uint32_t i = 0; i < kAtOnce; ++i) {
+            x[i] = make_uint4(0, 0, 0, 0);
+            const int64_t at_row = __shfl_sync(0xffffffffu, from, part * 16 + (i0 + i) % kTurns * kTogether + mine);
+            if (at_row >= 0 && 8 * c < a.head_dim && i0 + i < kTurns) {
+              const char* const p = static_cast<const char*>(a.q) + (at_row + 8 * c) * 2;
+              if (a.q_wide) {
+                x[i] = *reinterpret_cast<const uint4*>(p);
+              } else {
+                const uint2 u = *reinterpret_cast<const uint2*>(p), v = *reinterpret_cast<const uint2*>(p + 8);
+                x[i] = make_uint4(u.x, u.y, v.x, v.y);
+              }
             }
           }
-          if constexpr (S::quant) {
-            auto size = [&](uint32_t w) { return max(__float_as_uint(query_at(&w, 0, a.q_is_bf16)) & 0x7fffffffu, __float_as_uint(query_at(&w, 1, a.q_is_bf16)) & 0x7fffffffu); };
-            uint32_t top = max(max(size(x.x), size(x.y)), max(size(x.z), size(x.w)));
 #pragma unroll
-            for (uint32_t o = 1; o < kChunks; o <<= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
-            const uint32_t e = min(top >> 23, 253u + (top >> 23 == 255) * 2);  // (neither zeros nor what is not finite)
-            float up = 1.f, back = 1.f;
-            if (e >= 1 && e <= 253) up = __uint_as_float((254 - e) << 23), back = __uint_as_float(e << 23);
-            auto word = [&](uint32_t w) { return pack16<false>(query_at(&w, 0, a.q_is_bf16) * up, query_at(&w, 1, a.q_is_bf16) * up); };
-            x = make_uint4(word(x.x), word(x.y), word(x.z), word(x.w));
-            back = __shfl_sync(0xffffffffu, back, lane % kTogether * kChunks);
-            if (lane / kTogether == i) factor *= back;
+          for (uint32_t i = 0; i < kAtOnce; ++i) {
+            if (i0 + i >= kTurns) break;
+            const uint32_t r = quarter * 32 + part * 16 + (i0 + i) * kTogether + mine;
+            if constexpr (S::quant) {
+              auto size = [&](uint32_t w) { return max(__float_as_uint(query_at(&w, 0, a.q_is_bf16)) & 0x7fffffffu, __float_as_uint(query_at(&w, 1, a.q_is_bf16)) & 0x7fffffffu); };
+              uint32_t top = max(max(size(x[i].x), size(x[i].y)), max(size(x[i].z), size(x[i].w)));
+#pragma unroll
+              for (uint32_t o = 1; o < kChunks; o <<= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
+              const uint32_t e = top >> 23 == 254 ? 253 : top >> 23;
+              float up = 1.f, back = 1.f;
+              if (e >= 1 && e <= 253) up = __uint_as_float((254 - e) << 23), back = __uint_as_float(e << 23);
+              auto word = [&](uint32_t w) { return pack16<false>(query_at(&w, 0, a.q_is_bf16) * up, query_at(&w, 1, a.q_is_bf16) * up); };
+              x[i] = make_uint4(word(x[i].x), word(x[i].y), word(x[i].z), word(x[i].w));
+              // both threads of the row get to know it
+              if (c < 2) swap[(stream * 2 + c) * kRows + r] = back;
+            }
+            if (8 * c < a.head_dim)
+              shared_store16(q_at + stream * S::Q + r * 128 + (c >> 3) * (kRows * 128) + ((c & 7 ^ r & 7) << 4), x[i].x ^ flip, x[i].y ^ flip, x[i].z ^ flip, x[i].w ^ flip);
           }
-          if (8 * c < a.head_dim)
-            shared_store16(q_at + stream * S::Q + r * 128 + (c >> 3) * (kRows * 128) + ((c & 7 ^ r & 7) << 4), x.x ^ flip, x.y ^ flip, x.z ^ flip, x.w ^ flip);
         }
-      }
-      if (any) {
         to_async_proxy();
         bar_arrive(q_full + 8 * stream);
+        if constexpr (S::quant) {
+          meet();
+          factor *= swap[(stream * 2 + part) * kRows + row];
+        }
       }
+      factor = fmaxf(factor, kLeast);
 
       float ref = kNone, l = 0.f, top_scale = 0.f, unit = 1.f;  // unit: what the values' scales are multiplied by
-      factor = fmaxf(factor, kLeast);
       bool first = true;
       const uint32_t step = both ? 1 : S::STREAMS;
-      uint32_t t = both ? 0 : stream;
-      for (; t < n; t += step) {
+      for (uint32_t t = both ? 0 : stream; t < n; t += step) {
         const uint32_t m_slot = (tile0 + t) % S::NMETA;
         const unsigned char* const about = meta_ptr + m_slot * S::META;
         ok = bar_wait(described + 8 * m_slot, (tile0 + t) / S::NMETA & 1, stop) && bar_wait(s_full + 8 * stream, n_scores & 1, stop);
         if (!ok) break;
         ++n_scores;
         tmem_after();
-        const bool work = __any_sync(0xffffffffu, live);
-        // 64 scores into registers; 8-bit keys: times their scales; masked ones below all others
-        float x[64];
-        auto read = [&](uint32_t half) {
-          tmem_load32(s_at + 64 * half, x), tmem_load32(s_at + 64 * half + 32, x + 32);
-          tmem_load_wait();
-          loaded32(x), loaded32(x + 32);
-          if constexpr (S::quant) {
-#pragma unroll
-            for (int i = 0; i < 64; i += 4) {
-              const float4 ks = *reinterpret_cast<const float4*>(about + 16 + 256 * half + 4 * i);
-              const float2 u = mul2(make_float2(x[i], x[i + 1]), make_float2(ks.x, ks.y)), v = mul2(make_float2(x[i + 2], x[i + 3]), make_float2(ks.z, ks.w));
-              x[i] = u.x, x[i + 1] = u.y, x[i + 2] = v.x, x[i + 3] = v.y;
-            }
-          }
-          const uint2 mask = *reinterpret_cast<const uint2*>(about + 8 * half);
-          if ((mask.x & mask.y) != 0xffffffffu) {
-#pragma unroll
-            for (int i = 0; i < 64; ++i)
-              if (!((i < 32 ? mask.x : mask.y) >> (i & 31) & 1)) x[i] = -INFINITY;
-          }
-        };
         if (work) {
+          // 32 scores into registers; 8-bit keys: times their scales; masked ones below all others
+          float x[32];
+          auto read = [&](uint32_t c) {
+            tmem_load32(s_at + 32 * c, x);
+            tmem_load_wait();
+            loaded32(x);
+            const uint32_t column = part * S::COLS + 32 * c;
+            if constexpr (S::quant) {
+#pragma unroll
+              for (int i = 0; i < 32; i += 4) {
+                const float4 ks = *reinterpret_cast<const float4*>(about + 16 + 4 * (column + i));
+                x[i] *= ks.x, x[i + 1] *= ks.y, x[i + 2] *= ks.z, x[i + 3] *= ks.w;
+              }
+            }
+            const uint32_t mask = *reinterpret_cast<const uint32_t*>(about + column / 8);
+            if (mask != 0xffffffffu) {
+#pragma unroll
+              for (int i = 0; i < 32; ++i)
+                if (!(mask >> i & 1)) x[i] = -INFINITY;
+            }
+          };
+          // the largest; the last 32 stay in registers
           float top = -INFINITY;
-#pragma unroll 1
-          for (uint32_t half = 0; half < S::TOK / 64; ++half) {
-            read(half);
+#pragma unroll
+          for (uint32_t c = 0; c < S::COLS / 32; ++c) {
+            read(c);
             float tops[4] = {top, x[0], x[1], x[2]};
 #pragma unroll
-            for (uint32_t i = 2; i < 64; i += 2) tops[i / 2 % 4] = largest(tops[i / 2 % 4], x[i], x[i + 1]);
+            for (uint32_t i = 2; i < 32; i += 2) tops[i / 2 % 4] = largest(tops[i / 2 % 4], x[i], x[i + 1]);
             top = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3]));
           }
-          top *= factor;
+          top = fmaxf(top, other(top)) * factor;
           float down = 1.f;
           if (top > ref + 8.f) down = exp2_fast(ref - top), ref = top, l *= down;
           if constexpr (S::quant) {
@@ -476,7 +508,7 @@ __global__ void __launch_bounds__(Shape<FMT, DP>::THREADS, 1) bcp_kv_prefix_kern
           }
           if (!first && __any_sync(0xffffffffu, down != 1.f)) {
 #pragma unroll 1
-            for (uint32_t c = 0; c < a.head_dim; c += 16) {
+            for (uint32_t c = 16 * part; c < a.head_dim; c += 32) {
               float z[16];
               uint32_t y[16];
               tmem_load16(o_at + c, z);
@@ -487,72 +519,46 @@ __global__ void __launch_bounds__(Shape<FMT, DP>::THREADS, 1) bcp_kv_prefix_kern
               tmem_store16(o_at + c, y);
             }
           }
-        }
-        // The weights, in two halves: the products with one begin while the other is made.
-        constexpr float kLift = S::split ? 0.f : 6.f;  // binary16 weights underflow below 2^-24: lifted by 2^6 that is 2^-30
-        const float2 factors = make_float2(factor, factor), less = make_float2(kLift - ref, kLift - ref);
-        auto weights = [&](uint32_t at, float* z, const unsigned char* scales) {  // 32 of them
-          float2 sum[4] = {};  // four, so that no addition waits for the one before it
+          // the weights; the products with the last 32 columns of either part begin while those with the others are made
+          constexpr float kLift = S::split ? 0.f : 6.f;  // binary16 weights underflow below 2^-24: lifted by 2^6 that is 2^-30
+          const float2 factors = make_float2(factor, factor), less = make_float2(kLift - ref, kLift - ref);
 #pragma unroll
-          for (int i = 0; i < 32; i += 2) {
-            const float2 e = fma2(make_float2(z[i], z[i + 1]), factors, less);
-            z[i] = exp2_fast(e.x), z[i + 1] = exp2_fast(e.y);
-            sum[i / 2 & 3] = add2(sum[i / 2 & 3], make_float2(z[i], z[i + 1]));
-          }
-          sum[0] = add2(add2(sum[0], sum[1]), add2(sum[2], sum[3]));
-          l += sum[0].x + sum[0].y;
-          if constexpr (S::quant) {
-            const float2 units = make_float2(unit, unit);
+          for (uint32_t j = 0; j < S::COLS / 32; ++j) {
+            const uint32_t c = S::COLS / 32 - 1 - j;
+            if (j) read(c);
+            float2 sum[4] = {};  // four, so that no addition waits for the one before it
+            uint32_t y[16], rest[16];
 #pragma unroll
-            for (int i = 0; i < 32; i += 4) {
-              const float4 vs = *reinterpret_cast<const float4*>(scales + 4 * i);
-              const float2 u = mul2(mul2(make_float2(vs.x, vs.y), units), make_float2(z[i], z[i + 1]));
-              const float2 v = mul2(mul2(make_float2(vs.z, vs.w), units), make_float2(z[i + 2], z[i + 3]));
-              z[i] = u.x, z[i + 1] = u.y, z[i + 2] = v.x, z[i + 3] = v.y;
+            for (int i = 0; i < 32; i += 2) {
+              const float2 e = fma2(make_float2(x[i], x[i + 1]), factors, less);
+              float2 p = make_float2(exp2_fast(e.x), exp2_fast(e.y));
+              sum[i / 2 & 3] = add2(sum[i / 2 & 3], p);
+              if constexpr (S::quant) {
+                const float2 vs = *reinterpret_cast<const float2*>(about + 16 + S::TOK * 4 + 4 * (part * S::COLS + 32 * c + i));
+                p = mul2(p, mul2(vs, make_float2(unit, unit)));
+              }
+              if constexpr (S::split) {
+                // the upper half as it stands, and what remains, made positive by 2^-20 of the weight: the products of both with an infinite value are
+                // that infinity
+                y[i / 2] = upper_halves(p.x, p.y);
+                const float2 r = fma2(p, make_float2(1.f + 0x1p-20f, 1.f + 0x1p-20f), make_float2(minus_upper(p.x), minus_upper(p.y)));
+                rest[i / 2] = pack16<true>(r.x, r.y);
+              } else {
+                y[i / 2] = pack16<false>(p.x, p.y);
+              }
             }
-          }
-          uint32_t y[16];
-          if constexpr (S::split) {
-            // the upper half as it stands, and what remains, made positive by 2^-20 of the weight: the products of both with an infinite value are that
-            // infinity
-#pragma unroll
-            for (int i = 0; i < 16; ++i) y[i] = upper_halves(z[2 * i], z[2 * i + 1]);
-            tmem_store16(at, y);
-            const float2 more = make_float2(1.f + 0x1p-20f, 1.f + 0x1p-20f);
-#pragma unroll
-            for (int i = 0; i < 16; ++i) {
-              const float2 rest = fma2(make_float2(z[2 * i], z[2 * i + 1]), more, make_float2(minus_upper(z[2 * i]), minus_upper(z[2 * i + 1])));
-              y[i] = pack16<true>(rest.x, rest.y);
-            }
-            tmem_store16(at + 16, y);
-          } else {
-#pragma unroll
-            for (int i = 0; i < 16; ++i) y[i] = pack16<false>(z[2 * i], z[2 * i + 1]);
-            tmem_store16(at, y);
-          }
-        };
-        auto ready = [&](uint32_t half) {
-          tmem_store_wait();
-          tmem_before();
-          bar_arrive(p_full + 16 * stream + 8 * half);
-        };
-        if constexpr (S::TOK == 128) {
-          // the second half of the scores is still in registers: it is made first
-#pragma unroll 1
-          for (uint32_t half = 0; half < 2; ++half) {
-            if (work) {
-              const uint32_t at = 1 - half;
-              if (half) read(at);
-              weights(s_at + 64 * at, x, about + 16 + S::TOK * 4 + 256 * at);
-              weights(s_at + 64 * at + 32, x + 32, about + 16 + S::TOK * 4 + 256 * at + 128);
-            }
-            ready(half);
+            sum[0] = add2(add2(sum[0], sum[1]), add2(sum[2], sum[3]));
+            l += sum[0].x + sum[0].y;
+            tmem_store16(s_at + 32 * c, y);
+            if constexpr (S::split) tmem_store16(s_at + 32 * c + 16, rest);
+            tmem_store_wait();
+            tmem_before();
+            bar_arrive(p_full + 16 * stream + 8 * j);
           }
         } else {
-          if (work) weights(s_at + 32, x + 32, about + 16 + S::TOK * 4 + 128);
-          ready(0);
-          if (work) weights(s_at, x, about + 16 + S::TOK * 4);
-          ready(1);
+          tmem_before();
+#pragma unroll
+          for (uint32_t j = 0; j < S::COLS / 32; ++j) bar_arrive(p_full + 16 * stream + 8 * j);
         }
         first = false;
       }
@@ -568,9 +574,9 @@ __global__ void __launch_bounds__(Shape<FMT, DP>::THREADS, 1) bcp_kv_prefix_kern
         if (!ok) break;
         ++n_ends;
         tmem_after();
-        if (__any_sync(0xffffffffu, live)) {
+        if (work) {
 #pragma unroll 1
-          for (uint32_t c = 0; c < a.head_dim; c += 16) {
+          for (uint32_t c = 16 * part; c < a.head_dim; c += 32) {
             float x[16];
             tmem_load16(o_at + c, x);
             tmem_load_wait();
@@ -580,10 +586,12 @@ __global__ void __launch_bounds__(Shape<FMT, DP>::THREADS, 1) bcp_kv_prefix_kern
               store8(to, x), store8(to + 8, x + 8);
             }
           }
+          l += other(l);
+          if (S::quant) meet();  // what the next queries bring is written only when this has been read
         }
         tmem_before();
       }
-      if (live) {
+      if (live && part == 0) {
         constexpr float kLift = S::split ? 0.f : 6.f;
         // a reference with the scales' unit in it, as sums over values have it
         const float shift = unit == 1.f ? 0.f : unit > 1.f ? 60.f : -40.f;
@@ -599,10 +607,11 @@ __global__ void __launch_bounds__(Shape<FMT, DP>::THREADS, 1) bcp_kv_prefix_kern
       left -= n;
       advance<S>(at, a, n, left != 0);
     }
-  } else if (warp < 4 * S::STREAMS + kLoaders) {
+    if (!ok) asm volatile("bar.arrive %0, 64;" ::"r"(pair) : "memory");
+  } else if (warp < 8 * S::STREAMS + kLoaders) {
     // ================================================================ copies of keys and values
     if constexpr (S::STREAMS == 2) fewer_registers<S::REGS_COPY>();
-    const uint32_t w = warp - 4 * S::STREAMS;
+    const uint32_t w = warp - 8 * S::STREAMS;
     constexpr uint32_t kEach = S::TOK / kLoaders;                 // rows of a tile that a warp brings
     constexpr uint32_t kChunks = DP * (S::quant ? 1 : 2) / 16;    // 16-byte chunks of a row
     constexpr uint32_t kTogether = 32 / kChunks, kTurns = kEach / kTogether;
@@ -795,86 +804,90 @@ __global__ void __launch_bounds__(Shape<FMT, DP>::THREADS, 1) bcp_kv_prefix_kern
     // ================================================================ the products
     // A warp for each stream: one thread of it issues, which next to the busy warps takes about as long as the products themselves.
     if constexpr (S::STREAMS == 2) fewer_registers<S::REGS_PRODUCT>();
-    const uint32_t stream = warp - (4 * S::STREAMS + kLoaders);
+    const uint32_t stream = warp - (8 * S::STREAMS + kLoaders);
     if (stream < S::STREAMS) {
-      uint32_t item = 0, n_weights = 0, n_queries = 0;  // item: the place of the stretch's first tile in the ring's order
+      uint32_t item = 0, n_weights = 0, n_queries = 0, n_turns = 0;  // item: the place in the ring's order
       const uint32_t depth = a.head_dim / 16;
       const uint32_t scores = product(FMT == BCP_BF16, false, S::TOK), sums = product(S::split, true, a.head_dim);
       const bool chosen = elected();
       bool ok = true;
-      auto same = [](uint32_t x) { return __shfl_sync(0xffffffffu, x, 0); };  // (the compiler cannot know that it is)
       auto score = [&](uint32_t i) {  // with the keys of item i
         const uint32_t q = same(operand(q_at + stream * S::Q, 0)), k = same(operand(ring + i % S::SLOTS * S::TILE, 0)), d = same(tmem + S::S0 + stream * S::TOK);
-        if (chosen) {
 #pragma unroll
-          for (uint32_t j = 0; j < DP / 16; ++j)
-            if (j < depth) mma_shared(d, q + ((j >> 2) * (kRows * 128) + (j & 3) * 32) / 16, k + ((j >> 2) * (S::TOK * 128) + (j & 3) * 32) / 16, scores, j > 0);
-          tmem_commit(s_full + 8 * stream);
-        }
+        for (uint32_t j = 0; j < DP / 16; ++j)
+          if ((DP > 64 && j < DP / 32) || j < depth) mma_shared(chosen, d, q + ((j >> 2) * (kRows * 128) + (j & 3) * 32) / 16, k + ((j >> 2) * (S::TOK * 128) + (j & 3) * 32) / 16, scores, j > 0);
+        if (chosen) tmem_commit(s_full + 8 * stream);
         __syncwarp();
       };
-      auto weigh = [&](uint32_t i, bool add, uint32_t half) {  // half of the values of item i
-        const uint32_t first = (1 - half) * (S::TOK / 32);
-        const uint32_t v = same(operand(ring + i % S::SLOTS * S::TILE + first * 2048, S::TOK * 128));
-        const uint32_t p = same(tmem + S::S0 + stream * S::TOK + first * 16), o = same(tmem + S::O0 + stream * DP);
-        if (chosen) {
+      // The values of item i with the weights of columns 32 c and on of either part.
+      auto weigh = [&](uint32_t i, bool add, uint32_t c) {
+        const uint32_t v = same(operand(ring + i % S::SLOTS * S::TILE + c * 4096, S::TOK * 128));
+        const uint32_t p = same(tmem + S::S0 + stream * S::TOK + 32 * c), o = same(tmem + S::O0 + stream * DP);
 #pragma unroll
-          for (uint32_t j = 0; j < S::TOK / 32; ++j) {
-            const uint32_t from = p + (j >> 1) * 32 + (j & 1) * 8;
-            mma_tensor(o, from, v + j * (2048 / 16), sums, j > 0 || add || half);
-            if (S::split) mma_tensor(o, from + 16, v + j * (2048 / 16), sums, true);
-          }
+        for (uint32_t j = 0; j < 4; ++j) {
+          const uint32_t from = p + (j >> 1) * S::COLS + (j & 1) * 8, values = v + ((j >> 1) * S::COLS * 128 + (j & 1) * 2048) / 16;
+          mma_tensor(chosen, o, from, values, sums, j > 0 || add);
+          if (S::split) mma_tensor(chosen, o, from + 16, values, sums, true);
         }
-        __syncwarp();
-      };
-      // An item is free when both streams are done with it; where they take turns the one that used it says so twice.
-      auto done = [&](uint32_t i, bool twice) {
-        if (chosen) {
-          tmem_commit(empty + 8 * (i % S::SLOTS));
-          if (twice) tmem_commit(empty + 8 * (i % S::SLOTS));
-        }
-        __syncwarp();
       };
       auto arrived = [&](uint32_t bar, uint32_t parity) {
         ok = ok && bar_wait(bar, parity, stop);
         tmem_after();
         return ok;
       };
-      auto have = [&](uint32_t i) { return arrived(full + 8 * (i % S::SLOTS), i / S::SLOTS & 1); };
-      while (left && ok) {
-        const uint32_t n = min(at.group.steps - at.step, left);
+      for (left = same(left); left && ok;) {
+        const uint32_t n = same(min(at.group.steps - at.step, left));
         const uint32_t row0 = at.u % at.group.tiles * S::ROWS;
-        const bool both = min(at.group.rows - row0, S::ROWS) > kRows;
-        // Tiles first, first + step, .. are this stream's.  The ring's order: the keys of `ahead` tiles, then the values of a tile and the keys of the one `ahead` of it in turn.
-        const uint32_t step = both ? 1 : S::STREAMS, ahead = both ? 1 : S::STREAMS, first = both ? 0 : stream;
-        const uint32_t early = min(n, ahead);
-        auto keys_of = [&](uint32_t t) { return item + (t < ahead ? t : ahead + 2 * (t - ahead) + 1); };
-        auto values_of = [&](uint32_t t) { return item + early + (t + ahead <= n ? 2 * t : 2 * (n - early) + (t - (n - early))); };
-        if (first < n) {
-          if (!arrived(q_full + 8 * stream, n_queries++ & 1) || !have(keys_of(first))) break;
-          score(keys_of(first));
-          done(keys_of(first), !both || S::STREAMS == 1);
-        }
-        for (uint32_t t = first; t < n && ok; t += step) {
-          const uint32_t parity = n_weights++ & 1, values = values_of(t);
-          if (!have(values)) break;
-#pragma unroll 1
-          for (uint32_t half = 0; half < 2; ++half) {
-            if (!arrived(p_full + 16 * stream + 8 * half, parity)) break;
-            weigh(values, t > first, half);
+        const bool both = same(min(at.group.rows - row0, S::ROWS)) > kRows;
+        // Tiles first, first + step, .. are this stream's.  Both warps go through all items of the ring, in its order: the keys of `early` tiles, then the values of
+        // a tile and the keys of the next in turn, and an item is free when both are done with it.
+        const uint32_t step = both ? 1 : S::STREAMS, first = both ? 0 : stream, early = min(n, step);
+        if (first < n && !arrived(q_full + 8 * stream, n_queries++ & 1)) break;
+        auto there = [&](uint32_t i) { return arrived(full + 8 * (i % S::SLOTS), i / S::SLOTS & 1); };
+        auto done = [&](uint32_t i) {
+          if (chosen) {
+            tmem_commit(empty + 8 * (i % S::SLOTS));
+            if (S::STREAMS == 1) tmem_commit(empty + 8 * (i % S::SLOTS));
           }
-          if (!ok) break;
-          done(values, !both || S::STREAMS == 1);
-          if (t + step < n) {
-            if (!have(keys_of(t + step))) break;
-            score(keys_of(t + step));
-            done(keys_of(t + step), !both || S::STREAMS == 1);
-          } else if (chosen) {
-            tmem_commit(o_full + 8 * stream);
+        };
+        for (uint32_t i = 0; i < 2 * n && ok; ++i, ++item) {
+          const uint32_t j = i - early;
+          const bool keys = i < early || (j < 2 * (n - early) && (j & 1));
+          const uint32_t t = i < early ? i : keys ? early + j / 2 : j < 2 * (n - early) ? j / 2 : j - (n - early);
+          if (!there(item)) break;
+          if (!both && t % S::STREAMS != stream) {
+            if (chosen) bar_arrive(empty + 8 * (item % S::SLOTS));
+            __syncwarp();
+            continue;
           }
+          if (keys) {
+            score(item);
+            done(item);
+            __syncwarp();
+            continue;
+          }
+          // Values, and where both streams take every tile the next keys right behind them.  One stream's products after the other's: side by side both
+          // would be done late, and both streams would make weights, then wait, at the same time.
+          const bool more = both && t + 1 < n;
+          if (more && !there(item + 1)) break;
+          if (!arrived(p_full + 16 * stream, n_weights & 1)) break;
+          if (both && (stream || n_turns)) {
+            if (!arrived(turn + 8 * stream, (stream ? n_turns : n_turns - 1) & 1)) break;
+          }
+          n_turns += both;
+          weigh(item, t > first, S::COLS / 32 - 1);
+          if constexpr (S::COLS == 64) {
+            if (!arrived(p_full + 16 * stream + 8, n_weights & 1)) break;
+            weigh(item, true, 0);
+          }
+          ++n_weights;
+          if (more) score(item + 1);
+          if (both && chosen) bar_arrive(turn + 8 * (1 - stream));
+          done(item);
+          if (more) done(item + 1), ++item, ++i;
+          if (chosen && t + step >= n) tmem_commit(o_full + 8 * stream);
           __syncwarp();
         }
-        item += 2 * n;
         left -= n;
         advance<S>(at, a, n, left != 0);
       }
