@@ -306,9 +306,11 @@ struct Angles {
 // stream ends (launch_early), and begin with after_previous(): the next kernel may do the same, and
 // nothing is read or written before the one before has completed and its memory is visible.  (No load takes the
 // read-only path: what one kernel reads may be written while its blocks already wait.)
+__device__ __forceinline__ void next_may_start() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+__device__ __forceinline__ void wait_for_previous() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 __device__ __forceinline__ void after_previous() {
-  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-  asm volatile("griddepcontrol.wait;" ::: "memory");
+  next_may_start();
+  wait_for_previous();
 }
 template <typename Args>
 cudaError_t launch_early(void (*kernel)(Args), uint32_t blocks, uint32_t threads, uint32_t shared_bytes, cudaStream_t stream, const Args& args) {

@@ -197,7 +197,9 @@ __global__ void __launch_bounds__(kWarps * 32, Shape<FMT, DP, NT>::CTAS) bcp_kv_
   float* const sums = reinterpret_cast<float*>(smem + kWarps * S::STAGES * S::STAGE);  // a part's worth for each warp
   uint32_t* const shared_word = reinterpret_cast<uint32_t*>(sums + kWarps * S::PART);
 
-  after_previous();
+  // With records, the kernel before this one is that of the prefixes, whose results are of no concern here: it lets this one start when what came before it
+  // is complete, and this one only has to end after it (what follows needs both).
+  if constexpr (RECORD) next_may_start(); else after_previous();
   // ---- the line, and this CTA's part of it
   const uint32_t units = a.n_heads * a.row_tiles;
   // every thread counts the steps of a run of sequences; an exclusive scan over the threads
@@ -231,7 +233,10 @@ __global__ void __launch_bounds__(kWarps * 32, Shape<FMT, DP, NT>::CTAS) bcp_kv_
     mine += extra * (run1 - run0), before += extra * run0;
     cuts.cut((all + extra * a.n_seqs) * units, gridDim.x);
   }
-  if (blockIdx.x >= cuts.parts) return;
+  if (blockIdx.x >= cuts.parts) {
+    if constexpr (RECORD) wait_for_previous();
+    return;
+  }
   const uint32_t s0 = cuts.begin(blockIdx.x), n_steps = cuts.begin(blockIdx.x + 1) - s0;
   Place at;
   {
@@ -703,6 +708,7 @@ __global__ void __launch_bounds__(kWarps * 32, Shape<FMT, DP, NT>::CTAS) bcp_kv_
     at.step += n - 1;
     advance(at, a, units, extra, done < n_steps);
   }
+  if constexpr (RECORD) wait_for_previous();
 }
 
 // ------------------------------------------------------------------------------ launch

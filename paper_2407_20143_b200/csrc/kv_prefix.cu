@@ -300,29 +300,10 @@ __global__ void __launch_bounds__(Shape<FMT, DP>::THREADS, 1) bcp_kv_prefix_kern
   __syncthreads();
   tmem_after();
   const uint32_t tmem = *static_cast<volatile uint32_t*>(words);
-  after_previous();
-  // ---- rows without a prefix have no records
-  const uint32_t n_q_heads = a.n_heads * a.group.d;
-  for (uint32_t b = blockIdx.x * S::THREADS + tid; b < a.n_seqs; b += gridDim.x * S::THREADS) {
-    uint32_t lo = 0, hi = a.n_groups;  // the last group that starts at or before b
-    while (lo < hi) {
-      const uint32_t mid = (lo + hi) / 2;
-      if (a.starts[mid] <= int32_t(b)) lo = mid + 1; else hi = mid;
-    }
-    bool has = false;
-    if (lo) {
-      const Group x = group_of<S>(a, lo - 1);
-      has = b >= x.first && b - x.first < x.rows / a.group.d && x.steps;
-    }
-    if (!has)
-      for (uint32_t h = 0; h < n_q_heads; ++h) a.rows[uint64_t(b) * n_q_heads + h] = make_int4(0, 0, 0, 0);
-  }
-  if (a.status && blockIdx.x == 0)
-    for (uint32_t g = tid; g < a.n_groups; g += S::THREADS)
-      if (a.lengths[g] > int32_t(a.capacity) || a.starts[g] < 0 || a.starts[g + 1] < a.starts[g] || a.starts[g + 1] > int32_t(a.n_seqs))
-        raise(a.status, BCP_BAD_LENGTH);
-
+  wait_for_previous();
+  next_may_start();  // the kernel of the own tokens, which needs nothing of this one, but what came before
   // ---- the line, and this CTA's part of it
+  const uint32_t n_q_heads = a.n_heads * a.group.d;
   const uint32_t run = (a.n_groups + S::THREADS - 1) / S::THREADS;
   const uint32_t run0 = min(tid * run, a.n_groups), run1 = min(run0 + run, a.n_groups);
   uint32_t mine = 0, before;
@@ -347,7 +328,30 @@ __global__ void __launch_bounds__(Shape<FMT, DP>::THREADS, 1) bcp_kv_prefix_kern
   }
   Cuts cuts;
   if (all) cuts.cut(all, gridDim.x);
+  // Rows without a prefix have no records: two warps that have nothing else to do look at all of them.
+  auto look_at_rows = [&]() {
+    const uint32_t id = blockIdx.x * 64 + (tid & 63), step = gridDim.x * 64;
+    for (uint32_t b = id; b < a.n_seqs; b += step) {
+      uint32_t lo = 0, hi = a.n_groups;  // the last group that starts at or before b
+      while (lo < hi) {
+        const uint32_t mid = (lo + hi) / 2;
+        if (a.starts[mid] <= int32_t(b)) lo = mid + 1; else hi = mid;
+      }
+      bool has = false;
+      if (lo) {
+        const Group x = group_of<S>(a, lo - 1);
+        has = b >= x.first && b - x.first < x.rows / a.group.d && x.steps;
+      }
+      if (!has)
+        for (uint32_t h = 0; h < n_q_heads; ++h) a.rows[uint64_t(b) * n_q_heads + h] = make_int4(0, 0, 0, 0);
+    }
+    if (a.status)
+      for (uint32_t g = id; g < a.n_groups; g += step)
+        if (a.lengths[g] > int32_t(a.capacity) || a.starts[g] < 0 || a.starts[g + 1] < a.starts[g] || a.starts[g + 1] > int32_t(a.n_seqs))
+          raise(a.status, BCP_BAD_LENGTH);
+  };
   if (!all || blockIdx.x >= cuts.parts) {
+    if (warp >= S::WARPS - 2) look_at_rows();
     if (warp == S::WARPS - 4) tmem_free(tmem);
     return;
   }
@@ -805,6 +809,7 @@ __global__ void __launch_bounds__(Shape<FMT, DP>::THREADS, 1) bcp_kv_prefix_kern
     // A warp for each stream: one thread of it issues, which next to the busy warps takes about as long as the products themselves.
     if constexpr (S::STREAMS == 2) fewer_registers<S::REGS_PRODUCT>();
     const uint32_t stream = warp - (8 * S::STREAMS + kLoaders);
+    if (stream >= 2) look_at_rows();
     if (stream < S::STREAMS) {
       uint32_t item = 0, n_weights = 0, n_queries = 0, n_turns = 0;  // item: the place in the ring's order
       const uint32_t depth = a.head_dim / 16;
@@ -908,8 +913,7 @@ __global__ void __launch_bounds__(Shape<FMT, DP>::THREADS, 1) bcp_kv_prefix_kern
 }
 
 // ------------------------------------------------------------------------------ the end
-// The records of a row, that of its own tokens first and then its prefix's in the order of the parts, become its result.  Four warps: rows with few
-// records have a warp each, rows with many all four.
+// The records of a row, that of its own tokens first and then its prefix's in the order of the parts, become its result.
 struct JoinArgs {
   const int4* rows;
   const float2* ml;
@@ -920,28 +924,23 @@ struct JoinArgs {
   int64_t out_token, out_head;
   uint32_t is_bf16;
 };
-constexpr uint32_t kJoinRows = 4;
-constexpr uint32_t kFew = 33;  // records that a warp takes alone
+constexpr uint32_t kFewRows = 600;
 
-template <int DP>
-__global__ void __launch_bounds__(128) bcp_kv_join_kernel(const JoinArgs a) {
+// TOGETHER: eight warps take a row, else a warp does.
+template <int DP, bool TOGETHER>
+__global__ void __launch_bounds__(256) bcp_kv_join_kernel(const JoinArgs a) {
   after_previous();
   constexpr int N = (DP + 127) / 128;  // vectors of four dimensions a lane
   const uint32_t tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-  __shared__ float4 sums[kJoinRows][N][32];
-  __shared__ float2 about[kJoinRows];
-  const uint32_t row0 = blockIdx.x * kJoinRows;
-  int4 d = make_int4(0, 0, 0, 0);
-  if (row0 + warp < a.n_rows) d = __ldcg(a.rows + row0 + warp);
-  const uint32_t both = d.w ? 2 : 1;
-  const uint32_t mine = 1 + min(uint32_t(d.z), a.parts) * both;
-  const bool together = __syncthreads_or(mine > kFew);
+  const uint32_t r = TOGETHER ? blockIdx.x : blockIdx.x * 8 + warp;
+  if (r >= a.n_rows) return;
+  const int4 d = __ldcg(a.rows + r);
+  const uint32_t both = d.w ? 2 : 1, n = 1 + min(uint32_t(d.z), a.parts) * both;
 
   // records first, first + step, .. of row r: largest reference, denominator, sums
   float m, den;
   float4 x[N];
-  auto add_up = [&](uint32_t r, const int4 d, uint32_t n, uint32_t first, uint32_t step) {
-    const uint32_t both = d.w ? 2 : 1;
+  auto add_up = [&](uint32_t first, uint32_t step) {
     auto record = [&](uint32_t i) {
       if (i == 0) return a.own + r;
       const uint32_t part = (i - 1) / both;
@@ -995,7 +994,7 @@ __global__ void __launch_bounds__(128) bcp_kv_join_kernel(const JoinArgs a) {
       }
     }
   };
-  auto finish = [&](uint32_t r) {
+  auto finish = [&]() {
     const float inv = den == 0.f ? 0.f : reciprocal_fast(den);
     const uint32_t b = r / a.n_q_heads, h = r - b * a.n_q_heads;
 #pragma unroll
@@ -1010,51 +1009,47 @@ __global__ void __launch_bounds__(128) bcp_kv_join_kernel(const JoinArgs a) {
     if (lane == 0 && a.lse) a.lse[r] = den == 0.f ? -INFINITY : (m + log2_fast(den)) * 0.6931471805599453f;
   };
 
-  if (!together) {
-    if (row0 + warp >= a.n_rows) return;
-    add_up(row0 + warp, d, mine, 0, 1);
-    finish(row0 + warp);
-    return;
-  }
-  for (uint32_t i = 0; i < kJoinRows && row0 + i < a.n_rows; ++i) {
-    const int4 e = __ldcg(a.rows + row0 + i);
-    const uint32_t n = 1 + min(uint32_t(e.z), a.parts) * (e.w ? 2 : 1);
-    add_up(row0 + i, e, n, warp, 4);
+  if constexpr (!TOGETHER) {
+    add_up(0, 1);
+    finish();
+  } else {
+    __shared__ float4 sums[8][N][32];
+    __shared__ float2 about[8];
+    add_up(warp, 8);
 #pragma unroll
     for (int k = 0; k < N; ++k) sums[warp][k][lane] = x[k];
     if (lane == 0) about[warp] = make_float2(m, den);
     __syncthreads();
-    if (warp == (i & 3)) {
-      float top = kNone;
-      for (uint32_t w = 0; w < 4; ++w) top = fmaxf(top, about[w].x);
-      m = top, den = 0.f;
+    if (warp) return;
+    m = kNone, den = 0.f;
+    for (uint32_t w = 0; w < 8; ++w) m = fmaxf(m, about[w].x);
 #pragma unroll
-      for (int k = 0; k < N; ++k) x[k] = make_float4(0.f, 0.f, 0.f, 0.f);
-      for (uint32_t w = 0; w < 4; ++w) {
-        const Factor<true> down(about[w].x - top);
-        den += down.denominator(about[w].y);
+    for (int k = 0; k < N; ++k) x[k] = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
-        for (int k = 0; k < N; ++k) {
-          const float4 y = sums[w][k][lane];
-          x[k].x += y.x * down.all, x[k].y += y.y * down.all, x[k].z += y.z * down.all, x[k].w += y.w * down.all;
-        }
+    for (uint32_t w = 0; w < 8; ++w) {
+      const Factor<true> down(about[w].x - m);
+      den += down.denominator(about[w].y);
+#pragma unroll
+      for (int k = 0; k < N; ++k) {
+        const float4 y = sums[w][k][lane];
+        x[k].x += y.x * down.all, x[k].y += y.y * down.all, x[k].z += y.z * down.all, x[k].w += y.w * down.all;
       }
-      finish(row0 + i);
     }
-    __syncthreads();
+    finish();
   }
 }
 
 // ------------------------------------------------------------------------------ launch
 struct Variant {
   void (*kernel)(PrefixArgs);
-  void (*join)(JoinArgs);
+  void (*join[2])(JoinArgs);  // a warp a row; eight
   uint32_t smem, threads, rows, tokens, registers;
 };
 template <int FMT, int DP>
 Variant variant() {
   typedef Shape<FMT, DP> S;
-  return Variant{bcp_kv_prefix_kernel<FMT, DP>, DP <= 128 ? bcp_kv_join_kernel<128> : bcp_kv_join_kernel<256>, S::SMEM, S::THREADS, S::ROWS, S::TOK, S::STREAMS == 2 ? S::REGS : 0};
+  constexpr int JOIN = DP <= 128 ? 128 : 256;
+  return Variant{bcp_kv_prefix_kernel<FMT, DP>, {bcp_kv_join_kernel<JOIN, false>, bcp_kv_join_kernel<JOIN, true>}, S::SMEM, S::THREADS, S::ROWS, S::TOK, S::STREAMS == 2 ? S::REGS : 0};
 }
 template <int FMT>
 Variant variant_of(uint32_t head_dim) {
@@ -1229,6 +1224,7 @@ extern "C" int bcp_kv_attend_shared(const bcp_kv_cache* c, const bcp_heads* q, c
   j.n_rows = n_seqs * q->n_heads, j.n_q_heads = q->n_heads, j.dims = c->head_dim;
   j.apart = 2 * v.rows, j.own = uint32_t(own_at), j.records = uint32_t(own_at), j.parts = sms;
   j.out = out->data, j.lse = lse, j.out_token = out->token_stride, j.out_head = out->head_stride, j.is_bf16 = out->type == BCP_BF16;
-  BCP_CUDA(launch_early(v.join, (j.n_rows + kJoinRows - 1) / kJoinRows, 128, 0, st, j));
+  const bool together = j.n_rows <= kFewRows;
+  BCP_CUDA(launch_early(v.join[together], together ? j.n_rows : (j.n_rows + 7) / 8, 256, 0, st, j));
   return BCP_OK;
 }
