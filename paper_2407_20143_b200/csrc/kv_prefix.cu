@@ -26,7 +26,6 @@ namespace bcp {
 namespace {
 
 constexpr uint32_t kRows = 128;             // rows of a stream
-constexpr uint32_t kLoaders = 4;            // warps that copy
 constexpr uint32_t kMeta = 16;              // tiles whose masks and scales are kept
 constexpr uint64_t kMostNs = 2000000000ull; // a wait that takes longer gives up
 
@@ -64,16 +63,18 @@ struct Shape {
   static constexpr uint32_t Q = kRows * DP * 2;
   static constexpr uint32_t RAW = quant ? TOK * DP : 0;      // of a tile as it lies in an 8-bit cache
   static constexpr uint32_t RAWS = quant ? 3 : 0;
-  static constexpr uint32_t META = quant ? 16 + TOK * 8 + 16 : 16;
+  // Warps that bring tokens; 8-bit ones have to be widened by them, too.
+  static constexpr uint32_t LOADERS = quant && STREAMS == 2 ? 8 : 4;
+  static constexpr uint32_t META = quant ? 16 + TOK * 8 + 32 : 16;
   static constexpr uint32_t NMETA = quant ? 8 : kMeta;
   static constexpr uint32_t SLOTS = DP == 64 ? 8 : quant ? 3 : 5;
   static constexpr uint32_t AHEAD = quant ? RAWS - 1 : 3;    // copies of so many tiles are under way
-  static constexpr uint32_t SMEM = STREAMS * Q + SLOTS * TILE + RAWS * RAW + NMETA * META + 8 * (2 * SLOTS + NMETA + 7 * STREAMS + 4 * RAWS) + STREAMS * 1024 + 48;
+  static constexpr uint32_t SMEM = STREAMS * Q + SLOTS * TILE + RAWS * RAW + NMETA * META + 8 * (2 * SLOTS + NMETA + 7 * STREAMS + LOADERS * RAWS) + STREAMS * 1024 + 48;
   // two warpgroups for each stream (a thread has half of a row's scores), one that copies, one of whose warps issue the products
-  static constexpr uint32_t WARPS = 8 * STREAMS + kLoaders + 4, THREADS = 32 * WARPS, COLS = TOK / 2;
+  static constexpr uint32_t WARPS = 8 * STREAMS + LOADERS + 4, THREADS = 32 * WARPS, COLS = TOK / 2;
   // Registers a thread: at launch, and after the groups have been given theirs (their sum is the launch's).  With one stream there are enough for all.
-  static constexpr uint32_t REGS = 80, REGS_ROWS = 88, REGS_COPY = 72, REGS_PRODUCT = 56;
-  static_assert(4 * REGS_ROWS + REGS_COPY + REGS_PRODUCT <= 6 * REGS, "registers of the launch");
+  static constexpr uint32_t REGS = quant ? 72 : 80, REGS_ROWS = quant ? 80 : 88, REGS_COPY = quant ? 64 : 72, REGS_PRODUCT = 56;
+  static_assert(4 * REGS_ROWS + LOADERS / 4 * REGS_COPY + REGS_PRODUCT <= (5 + LOADERS / 4) * REGS || STREAMS == 1, "registers of the launch");
   static constexpr uint32_t S0 = 0, O0 = STREAMS * TOK;      // columns of tensor memory
   static_assert(O0 + STREAMS * DP <= 512, "tensor memory");
   static_assert(SMEM <= 232448, "shared memory");
@@ -277,8 +278,8 @@ __global__ void __launch_bounds__(Shape<FMT, DP>::THREADS, 1) bcp_kv_prefix_kern
   const uint32_t bars = meta + S::NMETA * S::META;
   const uint32_t full = bars, empty = full + 8 * S::SLOTS, described = empty + 8 * S::SLOTS, q_full = described + 8 * S::NMETA, s_full = q_full + 8 * S::STREAMS,
                  p_full = s_full + 8 * S::STREAMS, o_full = p_full + 16 * S::STREAMS, drained = o_full + 8 * S::STREAMS, turn = drained + 8 * S::STREAMS, raw_full = turn + 8 * S::STREAMS;
-  uint32_t* const words = reinterpret_cast<uint32_t*>(smem + (raw_full + 32 * S::RAWS + S::STREAMS * 1024 - base));  // tensor memory, stop, found[8]
-  volatile float* const swap = reinterpret_cast<volatile float*>(smem + (raw_full + 32 * S::RAWS - base));  // [stream][half][row]
+  uint32_t* const words = reinterpret_cast<uint32_t*>(smem + (raw_full + 8 * S::LOADERS * S::RAWS + S::STREAMS * 1024 - base));  // tensor memory, stop, found[8]
+  volatile float* const swap = reinterpret_cast<volatile float*>(smem + (raw_full + 8 * S::LOADERS * S::RAWS - base));  // [stream][half][row]
   volatile uint32_t* const stop = words + 1;
   uint32_t* const found = words + 2;
   uint32_t* const totals = reinterpret_cast<uint32_t*>(smem);  // before the tiles come
@@ -289,11 +290,11 @@ __global__ void __launch_bounds__(Shape<FMT, DP>::THREADS, 1) bcp_kv_prefix_kern
   }
   if (warp == S::WARPS - 4) tmem_alloc(uint32_t(__cvta_generic_to_shared(words)));
   if (tid == 0) {
-    for (uint32_t i = 0; i < S::SLOTS; ++i) mbar_init(full + 8 * i, 32 * kLoaders), mbar_init(empty + 8 * i, 2);
-    for (uint32_t i = 0; i < S::NMETA; ++i) mbar_init(described + 8 * i, 32 * kLoaders);
+    for (uint32_t i = 0; i < S::SLOTS; ++i) mbar_init(full + 8 * i, 32 * S::LOADERS), mbar_init(empty + 8 * i, 2);
+    for (uint32_t i = 0; i < S::NMETA; ++i) mbar_init(described + 8 * i, 32 * S::LOADERS);
     for (uint32_t i = 0; i < S::STREAMS; ++i)
       mbar_init(q_full + 8 * i, 2 * kRows), mbar_init(s_full + 8 * i, 1), mbar_init(p_full + 16 * i, 2 * kRows), mbar_init(p_full + 16 * i + 8, 2 * kRows), mbar_init(o_full + 8 * i, 1), mbar_init(drained + 8 * i, 1), mbar_init(turn + 8 * i, 1);
-    for (uint32_t i = 0; i < 4 * S::RAWS; ++i) mbar_init(raw_full + 8 * i, 1);
+    for (uint32_t i = 0; i < S::LOADERS * S::RAWS; ++i) mbar_init(raw_full + 8 * i, 1);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   tmem_before();
@@ -505,8 +506,11 @@ __global__ void __launch_bounds__(Shape<FMT, DP>::THREADS, 1) bcp_kv_prefix_kern
           if constexpr (S::quant) {
             // Weights times scales must neither overflow in the sums nor vanish: where scales beyond 2^60 turn up all are multiplied by 2^-40, while none
             // is above 2^-40 by 2^60.
-            const float4 w = *reinterpret_cast<const float4*>(about + 16 + S::TOK * 8);
-            top_scale = fmaxf(top_scale, fmaxf(fmaxf(w.x, w.y), fmaxf(w.z, w.w)));
+#pragma unroll
+            for (uint32_t i = 0; i < S::LOADERS; i += 4) {
+              const float4 w = *reinterpret_cast<const float4*>(about + 16 + S::TOK * 8 + 4 * i);
+              top_scale = fmaxf(top_scale, fmaxf(fmaxf(w.x, w.y), fmaxf(w.z, w.w)));
+            }
             const float next = top_scale > 0x1p60f ? 0x1p-40f : top_scale < 0x1p-40f ? 0x1p60f : 1.f;
             if (next != unit) down *= next / unit, unit = next;
           }
@@ -612,11 +616,11 @@ __global__ void __launch_bounds__(Shape<FMT, DP>::THREADS, 1) bcp_kv_prefix_kern
       advance<S>(at, a, n, left != 0);
     }
     if (!ok) asm volatile("bar.arrive %0, 64;" ::"r"(pair) : "memory");
-  } else if (warp < 8 * S::STREAMS + kLoaders) {
+  } else if (warp < 8 * S::STREAMS + S::LOADERS) {
     // ================================================================ copies of keys and values
     if constexpr (S::STREAMS == 2) fewer_registers<S::REGS_COPY>();
     const uint32_t w = warp - 8 * S::STREAMS;
-    constexpr uint32_t kEach = S::TOK / kLoaders;                 // rows of a tile that a warp brings
+    constexpr uint32_t kEach = S::TOK / S::LOADERS;                 // rows of a tile that a warp brings
     constexpr uint32_t kChunks = DP * (S::quant ? 1 : 2) / 16;    // 16-byte chunks of a row
     constexpr uint32_t kTogether = 32 / kChunks, kTurns = kEach / kTogether;
     constexpr uint32_t kAll = kEach == 32 ? 0xffffffffu : (1u << (kEach & 31)) - 1;
@@ -627,6 +631,7 @@ __global__ void __launch_bounds__(Shape<FMT, DP>::THREADS, 1) bcp_kv_prefix_kern
     uint32_t boxes = 0, phases = 0;       // a bit for each item: it comes in boxes; for each place of 8-bit tiles: the parity of its barrier
     // Where this warp's tokens of a tile lie (a row a lane); the page of the next tile's is looked up ahead.
     int32_t page = -1, page_of[2] = {-1, -1};
+    bool inside_prefix = false;
     uint32_t off = 0, off_of[2] = {0, 0}, alive_of[2] = {0, 0};
     const int64_t v_from_k = static_cast<const char*>(a.v) - static_cast<const char*>(a.k);
     bool ok = true;
@@ -639,7 +644,7 @@ __global__ void __launch_bounds__(Shape<FMT, DP>::THREADS, 1) bcp_kv_prefix_kern
       if constexpr (S::quant) {
         const uint32_t stage = landed % S::RAWS;
         if (boxes >> (landed & 31) & 1) {
-          ok = ok && bar_wait(raw_full + 8 * (4 * stage + w), phases >> stage & 1, stop);
+          ok = ok && bar_wait(raw_full + 8 * (S::LOADERS * stage + w), phases >> stage & 1, stop);
           phases ^= 1u << stage;
         }
         if (landed >= S::SLOTS) ok = ok && bar_wait(empty + 8 * slot, landed / S::SLOTS - 1 & 1, stop);
@@ -681,123 +686,117 @@ __global__ void __launch_bounds__(Shape<FMT, DP>::THREADS, 1) bcp_kv_prefix_kern
       bar_arrive(full + 8 * slot);
       ++landed;
     };
-    auto look_up = [&](uint32_t pos0) {
+    auto look_up = [&](uint32_t pos0) {  // (nothing looks at what was loaded before it is used)
       const uint32_t pos = pos0 + w * kEach + (lane & (kEach - 1));
-      page = -1;
-      if (pos < at.group.len) {
+      page = -1, inside_prefix = pos < at.group.len;
+      if (inside_prefix) {
         const uint32_t n = a.page_size.div(pos);
         off = pos - n * a.page_size.d;
         page = a.table[at.g * a.table_stride + n];
-        if (uint32_t(page) >= a.n_pages) {
-          raise(a.status, BCP_BAD_PAGE);
-          page = -1;
-        }
       }
     };
-    // A tile of keys, whose pages have been looked up, or of values of cache head h; `next`: where the tile after it begins, 0: none.
-    auto bring = [&](uint32_t tile, uint32_t next, uint32_t h, bool keys) {
-      if (!ok) return;
-      if (keys) {
-        page_of[1] = page_of[0], off_of[1] = off_of[0], alive_of[1] = alive_of[0];
-        page_of[0] = page, off_of[0] = off, alive_of[0] = __ballot_sync(0xffffffffu, page >= 0) & kAll;
-        ++brought;
-        unsigned char* const about = meta_ptr + tile % S::NMETA * S::META;
-        if (lane == 0) {
-          if (kEach == 32) reinterpret_cast<volatile uint32_t*>(about)[w] = alive_of[0];
-          if (kEach == 16) reinterpret_cast<volatile uint16_t*>(about)[w] = uint16_t(alive_of[0]);
+    // One loop with one piece of code for each thing to do: the warps that bring and those that weigh share the instruction cache.
+    uint32_t n = 0, h = 0, early = 0, i = 0;
+    bool at_end = false;
+    while (ok) {
+      if (!at_end && i == 2 * n) {  // the next stretch
+        if (n) {
+          tile0 += n, left -= n;
+          advance<S>(at, a, n, left != 0);
         }
-      }
-      // values come behind the next tile's keys where the streams take turns
-      const bool older = !keys && tile + 1 < brought;
-      const int32_t my_page = older ? page_of[1] : page_of[0];
-      const uint32_t my_off = older ? off_of[1] : off_of[0], alive = older ? alive_of[1] : alive_of[0];
-      const uint32_t slot = item % S::SLOTS, stage = S::quant ? item % S::RAWS : 0;
-      uint32_t bar = full + 8 * slot;
-      if constexpr (S::quant) {
-        bar = raw_full + 8 * (4 * stage + w);
-      } else if (item >= S::SLOTS) {
-        const uint32_t parity = item / S::SLOTS - 1 & 1;
-        // copies that are under way go on to the products while this tile's place is still taken
-        while (landed < item && !__all_sync(0xffffffffu, bar_test(empty + 8 * slot, parity))) {
-          copies_wait_all_but(item - landed - 1);
-          land();
-        }
-        ok = bar_wait(empty + 8 * slot, parity, stop);
-        if (!ok) return;
-      }
-      const bool box = a.block && alive == kAll;
-      if (box) {
-        // a warp's tokens in boxes, each inside one page
-        const CUtensorMap* const map = keys ? &a.k_map : &a.v_map;
-        if constexpr (S::quant) {
-          if (lane == 0) mbar_expect_tx(bar, kEach * a.head_dim);
-          __syncwarp();
-          if (lane < kEach && (lane & (a.block - 1)) == 0)
-            box_load(raw + stage * S::RAW + (w * kEach + lane) * a.head_dim, map, 0, my_off, h, uint32_t(my_page), bar);
+        if (left) {
+          n = min(at.group.steps - at.step, left), h = at.u / at.group.tiles, i = 0;
+          const uint32_t row0 = (at.u - h * at.group.tiles) * S::ROWS;
+          early = min(n, min(at.group.rows - row0, S::ROWS) > kRows ? 1u : S::STREAMS);  // the keys of so many tiles come before values
+          look_up(at.step * S::TOK);
         } else {
-          const uint32_t wide = (a.head_dim + 63) / 64;
-          if (lane == 0) mbar_expect_tx(bar, kEach * 128 * wide);
+          at_end = true;
+        }
+      }
+      if (at_end && landed == item) break;
+      const uint32_t slot = item % S::SLOTS, stage = S::quant ? item % S::RAWS : 0;
+      bool land_now = at_end;
+      if (!S::quant && !at_end && item >= S::SLOTS) {
+        // copies that are under way go on to the products while this tile's place is still taken
+        const uint32_t parity = item / S::SLOTS - 1 & 1;
+        land_now = landed < item && !__all_sync(0xffffffffu, bar_test(empty + 8 * slot, parity));
+        if (!land_now) ok = bar_wait(empty + 8 * slot, parity, stop);
+        if (!ok) break;
+      }
+      if (!land_now) {
+        // An item of the stretch: the keys of the first tiles, then values and keys in turn, then the values that are left.
+        const uint32_t j = i - early;
+        const bool keys = i < early || (j < 2 * (n - early) && (j & 1));
+        const uint32_t t = i < early ? i : keys ? early + j / 2 : j < 2 * (n - early) ? j / 2 : j - (n - early), tile = tile0 + t;
+        if (keys) {
+          if (uint32_t(page) >= a.n_pages) {
+            if (inside_prefix) raise(a.status, BCP_BAD_PAGE);
+            page = -1;
+          }
+          page_of[1] = page_of[0], off_of[1] = off_of[0], alive_of[1] = alive_of[0];
+          page_of[0] = page, off_of[0] = off, alive_of[0] = __ballot_sync(0xffffffffu, page >= 0) & kAll;
+          ++brought;
+          unsigned char* const about = meta_ptr + tile % S::NMETA * S::META;
+          if (lane == 0) {
+            if (kEach == 32) reinterpret_cast<volatile uint32_t*>(about)[w] = alive_of[0];
+            if (kEach == 16) reinterpret_cast<volatile uint16_t*>(about)[w] = uint16_t(alive_of[0]);
+          }
+        }
+        // values come behind the next tile's keys where the streams take turns
+        const bool older = !keys && tile + 1 < brought;
+        const int32_t my_page = older ? page_of[1] : page_of[0];
+        const uint32_t my_off = older ? off_of[1] : off_of[0], alive = older ? alive_of[1] : alive_of[0];
+        const uint32_t bar = S::quant ? raw_full + 8 * (S::LOADERS * stage + w) : full + 8 * slot;
+        const bool box = a.block && alive == kAll;
+        if (box) {
+          // a warp's tokens in boxes, each inside one page
+          const CUtensorMap* const map = keys ? &a.k_map : &a.v_map;
+          const uint32_t wide = S::quant ? 1 : (a.head_dim + 63) / 64;
+          if (lane == 0) mbar_expect_tx(bar, kEach * (S::quant ? a.head_dim : 128 * wide));
           __syncwarp();
+          const uint32_t to = S::quant ? raw + stage * S::RAW + (w * kEach + lane) * a.head_dim : ring + slot * S::TILE + (w * kEach + lane) * 128;
           if (lane < kEach && (lane & (a.block - 1)) == 0)
-            for (uint32_t i = 0; i < wide; ++i)
-              box_load(ring + slot * S::TILE + i * (S::TOK * 128) + (w * kEach + lane) * 128, map, 64 * i, my_off, h, uint32_t(my_page), bar);
+            for (uint32_t x = 0; x < wide; ++x) box_load(to + x * (S::TOK * 128), map, 64 * x, my_off, h, uint32_t(my_page), bar);
+        } else {
+          const uint64_t row = my_page >= 0 ? uint64_t(uint32_t(my_page)) * a.page_stride + uint64_t(h) * a.head_stride + uint64_t(my_off) * a.token_stride : 0;
+          const char* const from = static_cast<const char*>(a.k) + (keys ? 0 : v_from_k);
+          const uint32_t to = S::quant ? raw + stage * S::RAW + w * kEach * a.head_dim : ring + slot * S::TILE;
+#pragma unroll 2
+          for (uint32_t k = 0; k < kTurns; ++k) {
+            const uint32_t r = k * kTogether + my_row;
+            const uint64_t x = __shfl_sync(0xffffffffu, row, r) * (S::quant ? 1 : 2) + chunk * 16;
+            const bool copy = (alive >> r & 1) && inside;
+            const uint32_t tile_row = w * kEach + r;
+            const uint32_t place = S::quant ? r * a.head_dim + chunk * 16 : (chunk >> 3) * (S::TOK * 128) + tile_row * 128 + ((chunk & 7 ^ tile_row & 7) << 4);
+            if (!S::quant || inside) copy16(to + place, from + (copy ? x : 0), copy);
+          }
         }
-      } else {
-        const uint64_t row = my_page >= 0 ? uint64_t(uint32_t(my_page)) * a.page_stride + uint64_t(h) * a.head_stride + uint64_t(my_off) * a.token_stride : 0;
-        const char* const from = static_cast<const char*>(a.k) + (keys ? 0 : v_from_k);
-        const uint32_t to = S::quant ? raw + stage * S::RAW + w * kEach * a.head_dim : ring + slot * S::TILE;
-#pragma unroll 4
-        for (uint32_t i = 0; i < kTurns; ++i) {
-          const uint32_t r = i * kTogether + my_row;
-          const uint64_t x = __shfl_sync(0xffffffffu, row, r) * (S::quant ? 1 : 2) + chunk * 16;
-          const bool copy = (alive >> r & 1) && inside;
-          const uint32_t tile_row = w * kEach + r;
-          const uint32_t place = S::quant ? r * a.head_dim + chunk * 16 : (chunk >> 3) * (S::TOK * 128) + tile_row * 128 + ((chunk & 7 ^ tile_row & 7) << 4);
-          if (!S::quant || inside) copy16(to + place, from + (copy ? x : 0), copy);
+        if (S::quant && keys && lane < kEach) {
+          const uint64_t at_scale = (uint64_t(uint32_t(page >= 0 ? page : 0)) * a.n_heads + h) * a.page_size.d + off;
+          const uint32_t there = meta + tile % S::NMETA * S::META + 16 + (w * kEach + lane) * 4;
+          copy4(there, a.k_scale + at_scale, page >= 0);
+          copy4(there + S::TOK * 4, a.v_scale + at_scale, page >= 0);
         }
+        copies_end();
+        if (keys && t + 1 < n) look_up((at.step + t + 1) * S::TOK);
+        kinds = (kinds & ~(1u << (item & 31))) | uint32_t(keys) << (item & 31);
+        boxes = (boxes & ~(1u << (item & 31))) | uint32_t(box) << (item & 31);
+        ++item, ++i;
+        if (!S::quant && a.block) {
+          // boxes count themselves; rows that had to be copied one by one, at the end of a prefix, are waited for at once
+          if (!box) copies_wait<0>(), to_async_proxy();
+          if (keys) bar_arrive(described + 8 * (tile % S::NMETA));
+          if (!box || lane) bar_arrive(bar);
+          landed = item;
+        }
+        land_now = item - landed > S::AHEAD;
       }
-      if (S::quant && keys && lane < kEach) {
-        const uint64_t n = (uint64_t(uint32_t(page >= 0 ? page : 0)) * a.n_heads + h) * a.page_size.d + off;
-        const uint32_t there = meta + tile % S::NMETA * S::META + 16 + (w * kEach + lane) * 4;
-        copy4(there, a.k_scale + n, page >= 0);
-        copy4(there + S::TOK * 4, a.v_scale + n, page >= 0);
-      }
-      copies_end();
-      if (next) look_up(next);
-      kinds = (kinds & ~(1u << (item & 31))) | uint32_t(keys) << (item & 31);
-      boxes = (boxes & ~(1u << (item & 31))) | uint32_t(box) << (item & 31);
-      ++item;
-      if (S::quant) {
-        if (item - landed > S::AHEAD) {
-          copies_wait<S::AHEAD>();
-          land();
-        }
-      } else if (a.block) {
-        // boxes count themselves; rows that had to be copied one by one, at the end of a prefix, are waited for at once
-        if (!box) copies_wait<0>(), to_async_proxy();
-        if (keys) bar_arrive(described + 8 * (tile % S::NMETA));
-        if (!box || lane) bar_arrive(bar);
-        landed = item;
-      } else if (item - landed > S::AHEAD) {
-        copies_wait<S::AHEAD>();
+      if (land_now) {
+        copies_wait_all_but(item - landed - 1);
         land();
       }
-    };
-    while (left && ok) {
-      const uint32_t n = min(at.group.steps - at.step, left), h = at.u / at.group.tiles;
-      const uint32_t row0 = (at.u - h * at.group.tiles) * S::ROWS;
-      const uint32_t ahead = min(at.group.rows - row0, S::ROWS) > kRows ? 1 : S::STREAMS;  // keys come so many tiles before values
-      look_up(at.step * S::TOK);
-      for (uint32_t t = 0; t < n + ahead; ++t) {
-        if (t >= ahead && t - ahead < n) bring(tile0 + t - ahead, 0, h, false);
-        if (t < n) bring(tile0 + t, t + 1 < n ? (at.step + t + 1) * S::TOK : 0, h, true);
-      }
-      tile0 += n;
-      left -= n;
-      advance<S>(at, a, n, left != 0);
     }
     copies_wait<0>();
-    while (landed < item && ok) land();
     // (boxes under way are waited for by the products, or, if a wait ran out, by what follows)
     if (!ok) {
       const uint64_t begin = global_timer_ns();
@@ -808,7 +807,7 @@ __global__ void __launch_bounds__(Shape<FMT, DP>::THREADS, 1) bcp_kv_prefix_kern
     // ================================================================ the products
     // A warp for each stream: one thread of it issues, which next to the busy warps takes about as long as the products themselves.
     if constexpr (S::STREAMS == 2) fewer_registers<S::REGS_PRODUCT>();
-    const uint32_t stream = warp - (8 * S::STREAMS + kLoaders);
+    const uint32_t stream = warp - (8 * S::STREAMS + S::LOADERS);
     if (stream >= 2) look_at_rows();
     if (stream < S::STREAMS) {
       uint32_t item = 0, n_weights = 0, n_queries = 0, n_turns = 0;  // item: the place in the ring's order
@@ -1043,13 +1042,13 @@ __global__ void __launch_bounds__(256) bcp_kv_join_kernel(const JoinArgs a) {
 struct Variant {
   void (*kernel)(PrefixArgs);
   void (*join[2])(JoinArgs);  // a warp a row; eight
-  uint32_t smem, threads, rows, tokens, registers;
+  uint32_t smem, threads, rows, tokens, registers, each;  // each: tokens of a tile that a warp brings
 };
 template <int FMT, int DP>
 Variant variant() {
   typedef Shape<FMT, DP> S;
   constexpr int JOIN = DP <= 128 ? 128 : 256;
-  return Variant{bcp_kv_prefix_kernel<FMT, DP>, {bcp_kv_join_kernel<JOIN, false>, bcp_kv_join_kernel<JOIN, true>}, S::SMEM, S::THREADS, S::ROWS, S::TOK, S::STREAMS == 2 ? S::REGS : 0};
+  return Variant{bcp_kv_prefix_kernel<FMT, DP>, {bcp_kv_join_kernel<JOIN, false>, bcp_kv_join_kernel<JOIN, true>}, S::SMEM, S::THREADS, S::ROWS, S::TOK, S::STREAMS == 2 ? S::REGS : 0, S::TOK / S::LOADERS};
 }
 template <int FMT>
 Variant variant_of(uint32_t head_dim) {
@@ -1112,7 +1111,7 @@ int encode_tiled(EncodeTiled* out) {
 // Keys and values as tensors of whose tokens a warp's share of a tile is brought in boxes: of as many tokens as divide a page, a power of two of at least
 // eight.  Smaller ones would be more commands than the copies take, and vectors under 64 elements do not fill a box: those are copied row by row.
 int make_maps(const bcp_kv_cache* c, const Variant& v, PrefixArgs* a) {
-  uint32_t block = v.tokens / kLoaders;
+  uint32_t block = v.each;
   while (c->page_size % block) block /= 2;
   const bool wide = is_8bit(c->format);
   a->block = 0;
