@@ -22,8 +22,10 @@ namespace cg = cooperative_groups;
 
 namespace {
 
-constexpr uint32_t kThreads = 256, kWarps = kThreads / 32;
+constexpr uint32_t kThreads = 256, kManyThreads = 1024;  // of a CTA: four an SM, or one where the sequences leave SMs without work
+constexpr uint32_t kParts = 8;                           // warps that share a row's part, at most
 constexpr uint32_t kSegment = 256;  // tokens of a stretch that is summed for the draw: eight a lane
+constexpr int32_t kNoToken = -(1 << 30);
 constexpr float kLog2e = 1.4426950408889634f;
 
 struct VerifyArgs {
@@ -48,16 +50,13 @@ __device__ __forceinline__ float exp2_fast(float x) {
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
 }
-__device__ __forceinline__ float reference(float m) { return m == -INFINITY ? 0.f : m; }
-
-__device__ __forceinline__ RowSum join(const RowSum& a, const RowSum& b, float c) {
-  RowSum r;
-  r.m = fmaxf(a.m, b.m);
-  const float ref = reference(r.m);
-  r.s = a.s * exp2_fast((a.m - ref) * c) + b.s * exp2_fast((b.m - ref) * c);
-  r.index = a.m > b.m || (a.m == b.m && a.index < b.index) ? a.index : b.index;
+__device__ __forceinline__ float2 add2(float2 a, float2 b) {
+  float2 r;
+  asm("{\n.reg .b64 x, y, z;\nmov.b64 x, {%2, %3};\nmov.b64 y, {%4, %5};\nadd.rn.f32x2 z, x, y;\nmov.b64 {%0, %1}, z;\n}"
+      : "=f"(r.x), "=f"(r.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
   return r;
 }
+__device__ __forceinline__ float reference(float m) { return m == -INFINITY ? 0.f : m; }
 
 // A row in units of eight elements that start on 16-byte boundaries: unit v has elements 8 v - shift and on, of which those outside
 // 0 .. n - 1 are not the row's.
@@ -70,60 +69,87 @@ struct Row {
     units = (n + shift + 7) / 8;
   }
   __device__ __forceinline__ int32_t first(uint32_t v) const { return int32_t(8 * v) - int32_t(shift); }
-  // Eight elements from e on, `none` where the row has none; aligned: e is a unit's first.
-  __device__ __forceinline__ void load(int32_t e, bool aligned, float none, float (&x)[8]) const {
-    if (aligned && e >= 0 && uint32_t(e) + 8 <= n) {
-      Raw<T, 8> r;
-      r.load(p + e);
-#pragma unroll
-      for (int i = 0; i < 8; ++i) x[i] = to_f32(r.get(i));
+  // Unit v as it lies in memory; `none` where the row has no elements, and from unit `end` on.
+  __device__ __forceinline__ void raw(uint32_t v, uint32_t end, float none, Raw<T, 8>& x) const {
+    const int32_t e = first(v);
+    if (v < end && e >= 0 && uint32_t(e) + 8 <= n) {
+      x.load(p + e);
     } else {
 #pragma unroll
-      for (int i = 0; i < 8; ++i) x[i] = e + i >= 0 && uint32_t(e + i) < n ? to_f32(p[e + i]) : none;
+      for (int i = 0; i < 8; ++i) x.set(i, v < end && e + i >= 0 && uint32_t(e + i) < n ? p[e + i] : from_f32<T>(none));
     }
   }
 };
 
-// The part of a row that this thread sees: units first, first + kThreads, .. below end.
+__device__ __forceinline__ float largest8(const Raw<float, 8>& r) {
+  float m = r.get(0);
+#pragma unroll
+  for (int i = 1; i < 8; ++i) m = fmaxf(m, r.get(i));
+  return m;
+}
+template <typename T, typename T2>
+__device__ __forceinline__ float largest_of_pairs(const Raw<T, 8>& r) {
+  T2 p[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) p[i] = *reinterpret_cast<const T2*>(&r.w[i]);
+  const T2 m = __hmax2(__hmax2(p[0], p[1]), __hmax2(p[2], p[3]));
+  return fmaxf(to_f32(m.x), to_f32(m.y));
+}
+__device__ __forceinline__ float largest8(const Raw<__nv_bfloat16, 8>& r) { return largest_of_pairs<__nv_bfloat16, __nv_bfloat162>(r); }
+__device__ __forceinline__ float largest8(const Raw<__half, 8>& r) { return largest_of_pairs<__half, __half2>(r); }
+
+// Units first, first + 32, .. below end of a row, as this lane sees them.  (Terms are exp2((z - m) c): with one fused z c - m c the largest would be off by the
+// rounding of m c, which low temperatures make large.)
 template <typename T>
 __device__ __forceinline__ RowSum look_over(const Row<T>& row, uint32_t first, uint32_t end, float c, bool greedy) {
   RowSum r = {-INFINITY, 0xffffffffu, 0.0};
-  constexpr int kAhead = 4;
-  for (uint32_t v0 = first; v0 < end; v0 += kAhead * kThreads) {
-    float x[kAhead][8];
+  constexpr int kAhead = sizeof(T) == 2 ? 4 : 2;
+  for (uint32_t v0 = first; v0 < end; v0 += kAhead * 32) {
+    Raw<T, 8> x[kAhead];
 #pragma unroll
-    for (int j = 0; j < kAhead; ++j) {
-      const uint32_t v = v0 + j * kThreads;
-      if (v < end) {
-        row.load(row.first(v), true, -INFINITY, x[j]);
-      } else {
+    for (int j = 0; j < kAhead; ++j) row.raw(v0 + j * 32, end, -INFINITY, x[j]);
+    float top = largest8(x[0]);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) x[j][i] = -INFINITY;
-      }
-    }
+    for (int j = 1; j < kAhead; ++j) top = fmaxf(top, largest8(x[j]));
+    if (greedy) {
+      if (top > r.m) {
+        r.m = top;
 #pragma unroll
-    for (int j = 0; j < kAhead; ++j) {
-      float top = x[j][0];
-#pragma unroll
-      for (int i = 1; i < 8; ++i) top = fmaxf(top, x[j][i]);
-      if (greedy) {
-        if (top > r.m) {
-          r.m = top;
+        for (int j = kAhead - 1; j >= 0; --j)
 #pragma unroll
           for (int i = 7; i >= 0; --i)
-            if (x[j][i] == top) r.index = uint32_t(row.first(v0 + j * kThreads) + i);
-        }
-        continue;
+            if (to_f32(x[j].get(i)) == top) r.index = uint32_t(row.first(v0 + j * 32) + i);
       }
-      if (top > r.m) r.s *= exp2_fast((r.m - top) * c), r.m = top;
-      const float ref = reference(r.m);
-      float s = 0.f;
-#pragma unroll
-      for (int i = 0; i < 8; ++i) s += exp2_fast((x[j][i] - ref) * c);
-      r.s += s;
+      continue;
     }
+    if (top > r.m) r.s *= exp2_fast((r.m - top) * c), r.m = top;
+    const float ref = reference(r.m);
+    const float2 less = make_float2(-ref, -ref), c2 = make_float2(c, c);
+    float2 s[4] = {};
+#pragma unroll
+    for (int j = 0; j < kAhead; ++j)
+#pragma unroll
+      for (int i = 0; i < 8; i += 2) {
+        const float2 e = mul2(add2(make_float2(to_f32(x[j].get(i)), to_f32(x[j].get(i + 1))), less), c2);
+        s[i / 2] = add2(s[i / 2], make_float2(exp2_fast(e.x), exp2_fast(e.y)));
+      }
+    s[0] = add2(add2(s[0], s[1]), add2(s[2], s[3]));
+    r.s += s[0].x + s[0].y;
   }
   return r;
+}
+// The same of `lanes` lanes together, in all of them.
+__device__ __forceinline__ RowSum join(RowSum r, float c, bool greedy, uint32_t lanes) {
+  float m = r.m;
+  for (uint32_t o = lanes / 2; o; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+  if (greedy) {
+    uint32_t index = r.m == m ? r.index : 0xffffffffu;
+    for (uint32_t o = lanes / 2; o; o >>= 1) index = min(index, __shfl_xor_sync(0xffffffffu, index, o));
+    return RowSum{m, index, 0.0};
+  }
+  double s = r.s * exp2_fast((r.m - reference(m)) * c);
+  for (uint32_t o = lanes / 2; o; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+  return RowSum{m, 0, s};
 }
 
 // What turns an element into a probability.
@@ -136,36 +162,55 @@ struct Weights {  // of the row that is drawn from
   Row<T> p, q;
   Scale ps, qs;
   bool use_q, same;   // subtract q's; its units begin where p's do
-  int64_t without;    // a token that counts nothing
+  int32_t without;    // a token that counts nothing
   __device__ __forceinline__ static float probability(float z, const Scale& s) {
     return PROB ? z : exp2_fast((z - s.m) * s.c) * s.inverse;
   }
-  __device__ __forceinline__ void load(int32_t e, float (&w)[8]) const {
-    p.load(e, true, PROB ? 0.f : -INFINITY, w);
+  // Elements of units v, v + apart, .. of p, and of q at the same tokens.
+  template <uint32_t N>
+  __device__ __forceinline__ void read(uint32_t v, uint32_t apart, Raw<T, 8> (&x)[N], Raw<T, 8> (&y)[N]) const {
+    constexpr float none = PROB ? 0.f : -INFINITY;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) w[i] = probability(w[i], ps);
+    for (uint32_t j = 0; j < N; ++j) p.raw(v + j * apart, p.units, none, x[j]);
     if (use_q) {
-      float y[8];
-      q.load(e, same, PROB ? 0.f : -INFINITY, y);
 #pragma unroll
-      for (int i = 0; i < 8; ++i) w[i] = fmaxf(w[i] - probability(y[i], qs), 0.f);
+      for (uint32_t j = 0; j < N; ++j) {
+        if (same) {
+          q.raw(v + j * apart, p.units, none, y[j]);
+        } else {
+          const int32_t e = p.first(v + j * apart);
+#pragma unroll
+          for (int i = 0; i < 8; ++i) y[j].set(i, e + i >= 0 && uint32_t(e + i) < p.n ? q.p[e + i] : from_f32<T>(none));
+        }
+      }
     }
+  }
+  __device__ __forceinline__ void weigh(int32_t e, const Raw<T, 8>& x, const Raw<T, 8>& y, float (&w)[8]) const {
 #pragma unroll
-    for (int i = 0; i < 8; ++i)
-      if (w[i] < 0.f || e + i == without || e + i < 0 || uint32_t(e + i) >= p.n) w[i] = 0.f;
+    for (int i = 0; i < 8; ++i) {
+      w[i] = probability(to_f32(x.get(i)), ps);
+      if (use_q) w[i] = fmaxf(w[i] - probability(to_f32(y.get(i)), qs), 0.f);
+      if (PROB && w[i] < 0.f) w[i] = 0.f;
+    }
+    const int32_t skip = without - e;
+    if (e < 0 || uint32_t(e) + 8 > p.n || uint32_t(skip) < 8) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        if (i == skip || e + i < 0 || uint32_t(e + i) >= p.n) w[i] = 0.f;
+    }
   }
 };
 
 template <typename T, bool PROB>
-__global__ void __launch_bounds__(kThreads, 4) bcp_verify_kernel(const VerifyArgs a) {
+__global__ void __launch_bounds__(kManyThreads, 1) bcp_verify_kernel(const VerifyArgs a) {
   after_previous();
   cg::cluster_group cluster = cg::this_cluster();
   const uint32_t ctas = cluster.num_blocks(), rank = cluster.block_rank();
-  const uint32_t b = blockIdx.x / ctas, tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const uint32_t b = blockIdx.x / ctas, tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, warps = blockDim.x >> 5;
   const uint32_t most_rows = 2 * a.n_drafts + 1;
   extern __shared__ __align__(16) unsigned char smem[];
-  RowSum* const by_warp = reinterpret_cast<RowSum*>(smem);       // [rows][warps]
-  RowSum* const mine = by_warp + most_rows * kWarps;             // [rows]: of this CTA's part, read by the others
+  RowSum* const by_warp = reinterpret_cast<RowSum*>(smem);       // [rows][parts]
+  RowSum* const mine = by_warp + most_rows * kParts;             // [rows]: of this CTA's part, read by the others
   RowSum* const whole = mine + most_rows;                        // [rows]
   double* const total = reinterpret_cast<double*>(whole + most_rows);  // [2]: of this CTA's weights, read by the others
   uint32_t* const good = reinterpret_cast<uint32_t*>(total + 2);       // [n_drafts + 1]
@@ -177,64 +222,66 @@ __global__ void __launch_bounds__(kThreads, 4) bcp_verify_kernel(const VerifyArg
   const bool greedy = !PROB && !(t > 1e-30f);
   t = fminf(t, 1e30f);
   const float c = kLog2e / t;
-  // drafts of this sequence: up to the first negative one
-  if (tid <= a.n_drafts) good[tid] = tid < a.n_drafts && drafts[tid] >= 0;
+  auto target = [&](uint32_t i) { return Row<T>(a.target, b * a.t_seq + i * a.t_row, a.vocab); };
+  auto draft = [&](uint32_t i) { return Row<T>(a.draft, b * a.d_seq + i * a.d_row, a.vocab); };
+  // Drafts of this sequence: up to the first negative one.  A thread has each, with what its rows say about it.
+  int64_t my_draft = -1;
+  float my_p = 0.f, my_q = 0.f, my_u = 0.f;
+  if (tid < a.n_drafts) {
+    my_draft = drafts[tid], my_u = uniform[tid];
+    if (my_draft >= 0 && my_draft < int64_t(a.vocab)) {
+      my_p = to_f32(target(tid).p[my_draft]);
+      if (!a.certain) my_q = to_f32(draft(tid).p[my_draft]);
+    }
+  }
+  if (tid <= a.n_drafts) good[tid] = my_draft >= 0;
   __syncthreads();
   uint32_t n = 0;
   while (n < a.n_drafts && good[n]) ++n;
   __syncthreads();
 
-  auto target = [&](uint32_t i) { return Row<T>(a.target, b * a.t_seq + i * a.t_row, a.vocab); };
-  auto draft = [&](uint32_t i) { return Row<T>(a.draft, b * a.d_seq + i * a.d_row, a.vocab); };
-
   // ---- maxima and sums of all rows: the target's 0 .. n, then the drafts'
   const uint32_t n_rows = n + 1 + (a.certain || greedy ? 0 : n);
   if (!PROB) {
-    for (uint32_t i = 0; i < n_rows; ++i) {
+    // A row's part is cut for as many warps as have a batch of loads each, so that short rows are read side by side.
+    const uint32_t most = (a.vocab / 8 + ctas) / ctas, parts = most >= 1024 ? 8 : most >= 512 ? 4 : most >= 256 ? 2 : 1;
+    for (uint32_t task = warp; task < n_rows * parts; task += warps) {
+      const uint32_t i = task / parts, part = task % parts;
       const Row<T> row = i <= n ? target(i) : draft(i - n - 1);
-      const uint32_t each = (row.units + ctas - 1) / ctas, begin = rank * each;
-      RowSum r = look_over(row, begin + tid, min(begin + each, row.units), c, greedy);
-#pragma unroll
-      for (int o = 16; o; o >>= 1) {
-        RowSum other;
-        other.m = __shfl_xor_sync(0xffffffffu, r.m, o);
-        other.index = __shfl_xor_sync(0xffffffffu, r.index, o);
-        other.s = __shfl_xor_sync(0xffffffffu, r.s, o);
-        r = join(r, other, c);
-      }
-      if (lane == 0) by_warp[i * kWarps + warp] = r;
+      const uint32_t each = (row.units + ctas - 1) / ctas, begin = min(rank * each, row.units), end = min(begin + each, row.units);
+      const uint32_t some = (end - begin + parts - 1) / parts, from = min(begin + part * some, end), to = min(from + some, end);
+      const RowSum r = join(look_over(row, from + lane, to, c, greedy), c, greedy, 32);
+      if (lane == 0) by_warp[i * kParts + part] = r;
     }
     __syncthreads();
-    for (uint32_t i = tid; i < n_rows; i += kThreads) {
-      RowSum r = by_warp[i * kWarps];
-      for (uint32_t w = 1; w < kWarps; ++w) r = join(r, by_warp[i * kWarps + w], c);
-      mine[i] = r;
+    // warps join what their CTA has of a row, a lane a part, then what all CTAs have, a lane a CTA
+    const RowSum nothing = {-INFINITY, 0xffffffffu, 0.0};
+    for (uint32_t i = warp; i < n_rows; i += warps) {
+      const RowSum r = join(lane < parts ? by_warp[i * kParts + lane] : nothing, c, greedy, 8);
+      if (lane == 0) mine[i] = r;
     }
     cluster.sync();
-    for (uint32_t i = tid; i < n_rows; i += kThreads) {
-      RowSum r = cluster.map_shared_rank(mine, 0)[i];
-      for (uint32_t w = 1; w < ctas; ++w) r = join(r, cluster.map_shared_rank(mine, w)[i], c);
-      whole[i] = r;
+    for (uint32_t i = warp; i < n_rows; i += warps) {
+      const RowSum r = join(lane < ctas ? cluster.map_shared_rank(mine, lane)[i] : nothing, c, greedy, 16);
+      if (lane == 0) whole[i] = r;
     }
     __syncthreads();
   }
 
   // ---- every draft is judged by a thread; the same in all CTAs
   const double nan = __longlong_as_double(0x7ff8000000000000ll);
-  auto probability = [&](const Row<T>& row, uint32_t i, int64_t x) -> double {  // of token x in row i
-    const float z = to_f32(row.p[x]);
+  auto probability = [&](float z, uint32_t i) -> double {  // of an element of row i
     if (PROB) return z;
     const double s = whole[i].s;
     return s > 0 && s < INFINITY ? exp((double(z) - double(whole[i].m)) / double(t)) / s : nan;
   };
   if (tid < n) {
-    const int64_t x = drafts[tid];
-    bool ok = x < int64_t(a.vocab);
+    bool ok = my_draft < int64_t(a.vocab);
     if (ok && greedy) {
-      ok = whole[tid].index == uint32_t(x);
+      ok = whole[tid].index == uint32_t(my_draft);
     } else if (ok) {
-      const double p = probability(target(tid), tid, x), q = a.certain ? 1.0 : probability(draft(tid), n + 1 + tid, x);
-      ok = double(uniform[tid]) * q < p;
+      const double p = probability(my_p, tid), q = a.certain ? 1.0 : probability(my_q, n + 1 + tid);
+      ok = double(my_u) * q < p;
     }
     good[tid] = ok;
   }
@@ -243,7 +290,7 @@ __global__ void __launch_bounds__(kThreads, 4) bcp_verify_kernel(const VerifyArg
   while (k < n && good[k]) ++k;
   int64_t* const tokens = a.tokens + uint64_t(b) * (a.n_drafts + 1);
   if (rank == 0) {
-    for (uint32_t i = tid; i <= a.n_drafts; i += kThreads)
+    for (uint32_t i = tid; i <= a.n_drafts; i += blockDim.x)
       if (i != k) tokens[i] = i < k ? drafts[i] : -1;
     if (tid == 0) a.accepted[b] = int32_t(k);
     if (greedy && tid == 0) tokens[k] = whole[k].m > -INFINITY ? int64_t(whole[k].index) : -1;
@@ -260,7 +307,7 @@ __global__ void __launch_bounds__(kThreads, 4) bcp_verify_kernel(const VerifyArg
       return s;
     };
     const bool rejected = k < n;
-    Weights<T, PROB> w = {target(k), target(k), scale(k), scale(k), rejected && !a.certain, false, rejected && a.certain ? drafts[k] : -1};
+    Weights<T, PROB> w = {target(k), target(k), scale(k), scale(k), rejected && !a.certain, false, rejected && a.certain && drafts[k] < int64_t(a.vocab) ? int32_t(drafts[k]) : kNoToken};
     if (w.use_q) {
       w.q = draft(k), w.qs = scale(n + 1 + k);
       w.same = w.q.shift == w.p.shift;
@@ -271,15 +318,25 @@ __global__ void __launch_bounds__(kThreads, 4) bcp_verify_kernel(const VerifyArg
     const double u = uniform[a.n_drafts];
     // what is left after q may be nothing at all (p and q alike, a draft outside its own row): then p itself counts
     for (int round = 0;; ++round) {
-      for (uint32_t s = s0 + warp; s < s1; s += kWarps) {
-        float x[8];
-        w.load(w.p.first(s * (kSegment / 8) + lane), x);
-        double sum = 0.0;
+      // four stretches at a time, so that their loads are under way together
+      constexpr uint32_t kTogether = sizeof(T) == 2 ? 4 : 2;
+      for (uint32_t s = s0 + warp; s < s1; s += warps * kTogether) {
+        Raw<T, 8> p[kTogether], q[kTogether];
+        w.read(s * (kSegment / 8) + lane, warps * (kSegment / 8), p, q);
+        float sum[kTogether];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) sum += x[i];
+        for (uint32_t j = 0; j < kTogether; ++j) {
+          float x[8];
+          w.weigh(w.p.first((s + j * warps) * (kSegment / 8) + lane), p[j], q[j], x);
+          sum[j] = ((x[0] + x[1]) + (x[2] + x[3])) + ((x[4] + x[5]) + (x[6] + x[7]));
+        }
 #pragma unroll
-        for (int o = 16; o; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-        if (lane == 0) segments[s - s0] = sum;
+        for (int o = 16; o; o >>= 1)
+#pragma unroll
+          for (uint32_t j = 0; j < kTogether; ++j) sum[j] += __shfl_xor_sync(0xffffffffu, sum[j], o);
+#pragma unroll
+        for (uint32_t j = 0; j < kTogether; ++j)
+          if (lane == 0 && s + j * warps < s1) segments[s + j * warps - s0] = sum[j];
       }
       __syncthreads();
       if (warp == 0) {
@@ -290,23 +347,22 @@ __global__ void __launch_bounds__(kThreads, 4) bcp_verify_kernel(const VerifyArg
         if (lane == 0) total[round] = sum;
       }
       cluster.sync();
-      // the CTA that holds the place; if rounding has left none, the last that has any weight
-      double all = 0.0, base = 0.0;
-      for (uint32_t r = 0; r < ctas; ++r) all += cluster.map_shared_rank(total, r)[round];
-      const double place = u * all;
-      uint32_t owner = 0xffffffffu;
-      double line = 0.0;
-      for (uint32_t r = 0; r < ctas; ++r) {
-        const double next = line + cluster.map_shared_rank(total, r)[round];
-        if (next > line) {
-          owner = r, base = line;
-          if (next > place) break;
-        }
-        line = next;
+      // a lane a CTA: all weights, what lies before, and the CTA that holds the place; if rounding has left none, the last that has any weight
+      const double held = lane < ctas ? cluster.map_shared_rank(total, lane)[round] : 0.0;
+      double line = held;
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const double y = __shfl_up_sync(0xffffffffu, line, o);
+        if (int(lane) >= o) line += y;
       }
+      const double all = __shfl_sync(0xffffffffu, line, 31);
+      const double place = u * all;
+      const uint32_t behind = __ballot_sync(0xffffffffu, held > 0.0 && line > place), heavy = __ballot_sync(0xffffffffu, held > 0.0);
+      const uint32_t owner = behind ? __ffs(behind) - 1 : 31 - __clz(heavy | 1);
+      const double base = __shfl_sync(0xffffffffu, line - held, owner);
       const bool any = all > 0.0 && all < INFINITY;
       if (!any && round == 0 && rejected) {
-        w.use_q = false, w.without = -1;
+        w.use_q = false, w.without = kNoToken;
         __syncthreads();  // segments are written again
         continue;
       }
@@ -345,8 +401,11 @@ __global__ void __launch_bounds__(kThreads, 4) bcp_verify_kernel(const VerifyArg
         const uint32_t stretch = __shfl_sync(0xffffffffu, found, from);
         const double start = __shfl_sync(0xffffffffu, found_base, from);
         float x[8];
-        const int32_t e = w.p.first((s0 + stretch) * (kSegment / 8) + lane);
-        w.load(e, x);
+        const uint32_t v = (s0 + stretch) * (kSegment / 8) + lane;
+        const int32_t e = w.p.first(v);
+        Raw<T, 8> xp[1], xq[1];
+        w.read(v, 0, xp, xq);
+        w.weigh(e, xp[0], xq[0], x);
         sum = 0.0;
 #pragma unroll
         for (int i = 0; i < 8; ++i) sum += x[i];
@@ -381,7 +440,7 @@ __global__ void __launch_bounds__(kThreads, 4) bcp_verify_kernel(const VerifyArg
 }
 
 template <typename T, bool PROB>
-cudaError_t launch(const VerifyArgs& a, uint32_t n_seqs, uint32_t ctas, uint32_t smem, cudaStream_t stream) {
+cudaError_t launch(const VerifyArgs& a, uint32_t n_seqs, uint32_t ctas, uint32_t threads, uint32_t smem, cudaStream_t stream) {
   void (*const kernel)(VerifyArgs) = bcp_verify_kernel<T, PROB>;
   cudaError_t e = cudaSuccess;
   if (ctas > 8) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
@@ -392,13 +451,13 @@ cudaError_t launch(const VerifyArgs& a, uint32_t n_seqs, uint32_t ctas, uint32_t
   attributes[1].id = cudaLaunchAttributeClusterDimension;
   attributes[1].val.clusterDim.x = ctas, attributes[1].val.clusterDim.y = 1, attributes[1].val.clusterDim.z = 1;
   cudaLaunchConfig_t config = {};
-  config.gridDim = dim3(n_seqs * ctas), config.blockDim = dim3(kThreads), config.dynamicSmemBytes = smem, config.stream = stream;
+  config.gridDim = dim3(n_seqs * ctas), config.blockDim = dim3(threads), config.dynamicSmemBytes = smem, config.stream = stream;
   config.attrs = attributes, config.numAttrs = 2;
   return cudaLaunchKernelEx(&config, kernel, a);
 }
 template <typename T>
-cudaError_t launch(const VerifyArgs& a, bool prob, uint32_t n_seqs, uint32_t ctas, uint32_t smem, cudaStream_t stream) {
-  return prob ? launch<T, true>(a, n_seqs, ctas, smem, stream) : launch<T, false>(a, n_seqs, ctas, smem, stream);
+cudaError_t launch(const VerifyArgs& a, bool prob, uint32_t n_seqs, uint32_t ctas, uint32_t threads, uint32_t smem, cudaStream_t stream) {
+  return prob ? launch<T, true>(a, n_seqs, ctas, threads, smem, stream) : launch<T, false>(a, n_seqs, ctas, threads, smem, stream);
 }
 
 int check_rows(const char* call, const char* name, const bcp_vocab_rows* r) {
@@ -447,10 +506,11 @@ extern "C" int bcp_verify_drafts(const bcp_vocab_rows* target, const bcp_vocab_r
   uint32_t ctas = 16;
   while (ctas > 1 && (uint64_t(n_seqs) * ctas > uint64_t(sms) * 4 || vocab / ctas < 2048) && vocab / ctas < (1u << 18)) ctas /= 2;
   const uint32_t rows = 2 * n_drafts + 1, segments = (vocab + 7) / kSegment + 2;
-  const uint32_t smem = uint32_t(sizeof(RowSum)) * rows * (kWarps + 2) + 8 * (2 + (n_drafts + 2) / 2 + (segments + ctas - 1) / ctas);
+  const uint32_t smem = uint32_t(sizeof(RowSum)) * rows * (kParts + 2) + 8 * (2 + (n_drafts + 2) / 2 + (segments + ctas - 1) / ctas);
+  const uint32_t threads = uint64_t(n_seqs) * ctas <= uint64_t(sms) ? kManyThreads : kThreads;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
-  if (target->type == BCP_F32) BCP_CUDA(launch<float>(a, probabilities != 0, n_seqs, ctas, smem, st));
-  if (target->type == BCP_BF16) BCP_CUDA(launch<__nv_bfloat16>(a, probabilities != 0, n_seqs, ctas, smem, st));
-  if (target->type == BCP_F16) BCP_CUDA(launch<__half>(a, probabilities != 0, n_seqs, ctas, smem, st));
+  if (target->type == BCP_F32) BCP_CUDA(launch<float>(a, probabilities != 0, n_seqs, ctas, threads, smem, st));
+  if (target->type == BCP_BF16) BCP_CUDA(launch<__nv_bfloat16>(a, probabilities != 0, n_seqs, ctas, threads, smem, st));
+  if (target->type == BCP_F16) BCP_CUDA(launch<__half>(a, probabilities != 0, n_seqs, ctas, threads, smem, st));
   return BCP_OK;
 }
