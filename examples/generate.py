@@ -6,7 +6,10 @@ generate tokens: keys are rotated and written into a paged cache as they are mad
 are rotated (bcp_rope) and attend over the cache (bcp_kv_attend).  Sequences enter the batch one after the other, so
 their lengths differ; one that has not begun has length 0 and its slot is negative.
 
-    python examples/generate.py [--cache bf16|e4m3|int8] [--steps 64]
+With --drafts, what followed the last occurrence of a sequence's newest token is drafted, all drafts of a sequence go through the
+model at once, attending over the sequence's cache as a shared prefix (bcp_kv_attend_shared), and are verified (bcp_verify_drafts).
+
+    python examples/generate.py [--cache bf16|e4m3|int8] [--steps 64] [--drafts 4]
 """
 from __future__ import annotations
 
@@ -66,24 +69,47 @@ class Decoder:
         self.block_table = torch.randperm(max_seqs * pages, generator=torch.Generator().manual_seed(1)).int().view(max_seqs, pages).cuda()
         self.work = bcp.KvWorkspace(self.caches[0], Q_HEADS, max_seqs)
         self.rows = torch.arange(max_seqs, device="cuda")
+        self.shared, self.shared_rows = None, 0  # scratch memory of step_drafts
 
-    def step(self, tokens, positions):
-        """Logits (float32) after one more token for every sequence; a position of -1: the sequence has not begun."""
-        slots = self.caches[0].slots(self.block_table, self.rows, positions)
-        lengths = (positions + 1).int()
-        n = tokens.shape[0]
-        x = self.w["embed_tokens.weight"][tokens]
+    def _layers(self, x, positions, slots, attend):
+        """Logits (float32) of tokens whose embeddings are x; attend(cache, q) is the attention over a layer's cache."""
+        n = x.shape[0]
         for i, cache in enumerate(self.caches):
             p = f"layers.{i}."
             qkv = (norm(x, self.w[p + "input_norm.weight"]) @ self.w[p + "attn.qkv.weight"].T).view(n, Q_HEADS + 2 * KV_HEADS, HEAD_DIM)
             q, k, v = qkv.split([Q_HEADS, KV_HEADS, KV_HEADS], 1)
             bcp.bcp_rope(q, self.rope, positions, out=q)
             bcp.bcp_kv_write(cache, k, v, slots, rope=self.rope, positions=positions)
-            out, _ = bcp.bcp_kv_attend(cache, q, self.block_table, lengths, workspace=self.work)
-            x = x + out.view(n, HIDDEN) @ self.w[p + "attn.o.weight"].T
+            x = x + attend(cache, q).view(n, HIDDEN) @ self.w[p + "attn.o.weight"].T
             gate, up = (norm(x, self.w[p + "post_norm.weight"]) @ self.w[p + "mlp.gate_up.weight"].T).split(FFN, -1)
             x = x + (torch.nn.functional.silu(gate) * up) @ self.w[p + "mlp.down.weight"].T
         return (norm(x, self.w["final_norm.weight"]) @ self.w["lm_head.weight"].T).float()
+
+    def step(self, tokens, positions):
+        """Logits (float32) after one more token for every sequence; a position of -1: the sequence has not begun."""
+        slots = self.caches[0].slots(self.block_table, self.rows, positions)
+        lengths = (positions + 1).int()
+        return self._layers(self.w["embed_tokens.weight"][tokens], positions, slots,
+                            lambda cache, q: bcp.bcp_kv_attend(cache, q, self.block_table, lengths, workspace=self.work)[0])
+
+    def step_drafts(self, tokens, cached):
+        """Logits (float32) [sequences, m, vocabulary] after tokens [sequences, m], of which the first follows cached[b] (int64) tokens of each sequence.
+        A negative token (no draft) is computed as if it were 0, and what it writes is written over later."""
+        b, m = tokens.shape
+        page, width = self.caches[0].page_size, self.block_table.shape[1]
+        positions = (cached[:, None] + torch.arange(m, device=cached.device)).flatten()
+        slots = self.caches[0].slots(self.block_table, self.rows[:b].repeat_interleave(m), positions)
+        # whole pages are the prefix that the tokens of a sequence share; the rest of the last page and the tokens themselves are their own
+        whole = cached // page
+        columns = (whole[:, None] + torch.arange((page + m - 2) // page + 1, device=cached.device)).clamp_max(width - 1)
+        own = self.block_table[:b].gather(1, columns).repeat_interleave(m, 0)
+        lengths = (positions + 1 - (whole * page).repeat_interleave(m)).int()
+        starts = torch.arange(b + 1, dtype=torch.int32, device=cached.device) * m
+        if self.shared is None or self.shared_rows < b * m:
+            self.shared, self.shared_rows = bcp.KvWorkspace(self.caches[0], Q_HEADS, b * m, shared=True), b * m
+        logits = self._layers(self.w["embed_tokens.weight"][tokens.clamp_min(0).flatten()], positions, slots, lambda cache, q: bcp.bcp_kv_attend_shared(
+            cache, q, self.block_table[:b], (whole * page).int(), starts, own, lengths, workspace=self.shared)[0])
+        return logits.view(b, m, -1)
 
     def check(self):
         self.rope.check()
@@ -104,14 +130,56 @@ def generate(decoder: Decoder, first_tokens, steps: int, stagger: int = 3):
     return trace
 
 
+def look_up(history, lengths, n: int):
+    """n drafts for each sequence (int64 [sequences, n]): what followed the last earlier occurrence of its newest token; -1 where there is none."""
+    at = torch.arange(history.shape[1], device=history.device)
+    newest = history.gather(1, lengths[:, None] - 1)
+    seen = torch.where((history == newest) & (at < lengths[:, None] - 1), at, -1).amax(1)
+    take = seen[:, None] + 1 + torch.arange(n, device=history.device)
+    drafts = history.gather(1, take.clamp_max(history.shape[1] - 1))
+    known = (seen[:, None] >= 0) & (take < lengths[:, None])
+    return torch.where(known.long().cumprod(1).bool(), drafts, -1)
+
+
+def generate_with_drafts(decoder: Decoder, first_tokens, steps: int, drafts: int, temperature=None, seed: int = 0):
+    """Generation with looked-up drafts until every sequence has `steps` tokens behind its first one.  temperature (float32 [sequences], None: greedy)
+    goes for all drawn tokens.  Returns (tokens [sequences, steps + 1], rounds through the model)."""
+    b, device = len(first_tokens), first_tokens.device
+    history = torch.full((b, steps + drafts + 2), -2, dtype=torch.int64, device=device)
+    history[:, 0] = first_tokens
+    lengths = torch.ones(b, dtype=torch.int64, device=device)
+    temperature = torch.zeros(b, device=device) if temperature is None else temperature
+    random, rounds = torch.Generator(device=device).manual_seed(seed), 0
+    at = torch.arange(drafts + 1, device=device)
+    while int(lengths.min()) <= steps:
+        guess = torch.where(lengths[:, None] + at[:-1] < steps, look_up(history, lengths, drafts), -1)  # none past the end
+        going = lengths <= steps
+        tokens = torch.cat([history.gather(1, lengths[:, None] - 1), guess], 1)
+        logits = decoder.step_drafts(tokens, lengths - 1)
+        new, accepted = bcp.bcp_verify_drafts(logits, guess, torch.rand(b, drafts + 1, generator=random, device=device), temperature=temperature)
+        place = lengths[:, None] + at
+        keep = (new >= 0) & going[:, None]
+        history.scatter_(1, place.clamp_max(history.shape[1] - 1), torch.where(keep, new, history.gather(1, place.clamp_max(history.shape[1] - 1))))
+        lengths = lengths + torch.where(going, accepted.long() + 1, 0)
+        rounds += 1
+    return history[:, : steps + 1], rounds
+
+
 def main():
     ap = argparse.ArgumentParser(description=__doc__.split("\n")[0])
     ap.add_argument("--cache", choices=sorted(CACHES), default="e4m3")
     ap.add_argument("--steps", type=int, default=64)
     ap.add_argument("--sequences", type=int, default=8)
+    ap.add_argument("--drafts", type=int, default=0)
     a = ap.parse_args()
-    decoder = Decoder(merged_parameters(), a.sequences, a.steps, a.cache)
+    decoder = Decoder(merged_parameters(), a.sequences, a.steps + a.drafts + 1, a.cache)
     first = torch.arange(a.sequences, device="cuda") * 17 % VOCAB
+    if a.drafts:
+        tokens, rounds = generate_with_drafts(decoder, first, a.steps, a.drafts)
+        decoder.check()
+        print(f"{a.sequences} sequences, {a.steps} tokens each in {rounds} rounds of up to {a.drafts} drafts, {a.cache} cache")
+        print("sequence 0:", tokens[0].tolist())
+        return
     generate(decoder, first, min(a.steps, 4))
     torch.cuda.synchronize()
     t = time.perf_counter()
