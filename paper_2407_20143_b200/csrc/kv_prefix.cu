@@ -815,18 +815,20 @@ __global__ void __launch_bounds__(Shape<FMT, DP>::THREADS, 1) bcp_kv_prefix_kern
       const uint32_t scores = product(FMT == BCP_BF16, false, S::TOK), sums = product(S::split, true, a.head_dim);
       const bool chosen = elected();
       bool ok = true;
-      auto score = [&](uint32_t i) {  // with the keys of item i
-        const uint32_t q = same(operand(q_at + stream * S::Q, 0)), k = same(operand(ring + i % S::SLOTS * S::TILE, 0)), d = same(tmem + S::S0 + stream * S::TOK);
+      const uint32_t q = same(operand(q_at + stream * S::Q, 0)), s_at = same(tmem + S::S0 + stream * S::TOK), o = same(tmem + S::O0 + stream * DP);
+      const uint32_t keys_at = same(operand(ring, 0)), values_at = same(operand(ring, S::TOK * 128));
+      auto score = [&](uint32_t slot) {  // with the keys in a place of the ring
+        const uint32_t k = keys_at + slot * (S::TILE / 16);
 #pragma unroll
         for (uint32_t j = 0; j < DP / 16; ++j)
-          if ((DP > 64 && j < DP / 32) || j < depth) mma_shared(chosen, d, q + ((j >> 2) * (kRows * 128) + (j & 3) * 32) / 16, k + ((j >> 2) * (S::TOK * 128) + (j & 3) * 32) / 16, scores, j > 0);
+          if ((DP > 64 && j < DP / 32) || j < depth)
+            mma_shared(chosen, s_at, q + ((j >> 2) * (kRows * 128) + (j & 3) * 32) / 16, k + ((j >> 2) * (S::TOK * 128) + (j & 3) * 32) / 16, scores, j > 0);
         if (chosen) tmem_commit(s_full + 8 * stream);
         __syncwarp();
       };
-      // The values of item i with the weights of columns 32 c and on of either part.
-      auto weigh = [&](uint32_t i, bool add, uint32_t c) {
-        const uint32_t v = same(operand(ring + i % S::SLOTS * S::TILE + c * 4096, S::TOK * 128));
-        const uint32_t p = same(tmem + S::S0 + stream * S::TOK + 32 * c), o = same(tmem + S::O0 + stream * DP);
+      // The values in a place of the ring with the weights of columns 32 c and on of either part.
+      auto weigh = [&](uint32_t slot, bool add, uint32_t c) {
+        const uint32_t v = values_at + (slot * S::TILE + c * 4096) / 16, p = s_at + 32 * c;
 #pragma unroll
         for (uint32_t j = 0; j < 4; ++j) {
           const uint32_t from = p + (j >> 1) * S::COLS + (j & 1) * 8, values = v + ((j >> 1) * S::COLS * 128 + (j & 1) * 2048) / 16;
@@ -864,8 +866,9 @@ __global__ void __launch_bounds__(Shape<FMT, DP>::THREADS, 1) bcp_kv_prefix_kern
             __syncwarp();
             continue;
           }
+          const uint32_t slot = same(item % S::SLOTS);
           if (keys) {
-            score(item);
+            score(slot);
             done(item);
             __syncwarp();
             continue;
@@ -874,18 +877,18 @@ __global__ void __launch_bounds__(Shape<FMT, DP>::THREADS, 1) bcp_kv_prefix_kern
           // would be done late, and both streams would make weights, then wait, at the same time.
           const bool more = both && t + 1 < n;
           if (more && !there(item + 1)) break;
-          if (!arrived(p_full + 16 * stream, n_weights & 1)) break;
           if (both && (stream || n_turns)) {
             if (!arrived(turn + 8 * stream, (stream ? n_turns : n_turns - 1) & 1)) break;
           }
           n_turns += both;
-          weigh(item, t > first, S::COLS / 32 - 1);
+          if (!arrived(p_full + 16 * stream, n_weights & 1)) break;
+          weigh(slot, t > first, S::COLS / 32 - 1);
           if constexpr (S::COLS == 64) {
             if (!arrived(p_full + 16 * stream + 8, n_weights & 1)) break;
-            weigh(item, true, 0);
+            weigh(slot, true, 0);
           }
           ++n_weights;
-          if (more) score(item + 1);
+          if (more) score(slot + 1 == S::SLOTS ? 0 : slot + 1);
           if (both && chosen) bar_arrive(turn + 8 * (1 - stream));
           done(item);
           if (more) done(item + 1), ++item, ++i;
