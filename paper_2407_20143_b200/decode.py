@@ -147,14 +147,14 @@ class RopeTable:
         self.tensors = (table, self.status)
         self.c = L.RopeTableC(table.data_ptr(), table.shape[0], 2 * table.shape[2], _LAYOUTS[layout], self.status.data_ptr())
         self.address = C.addressof(self.c)
-        self.axes, self.axes_address = None, None
+        self.axes, self.axes_args = None, ()  # what the binding takes besides, where a table has axes
         if axes is not None:
             self.axes = tuple(axes)
             if len(self.axes) != table.shape[2] or not all(a in range(MAX_AXES) for a in self.axes):
                 raise _invalid(f"axes {self.axes}: one from 0 to {MAX_AXES - 1} for each of {table.shape[2]} pairs expected")
             self._of_pair = (C.c_uint8 * max(1, len(self.axes)))(*self.axes)
             self.axes_c = L.RopeAxesC(C.addressof(self._of_pair), 0, 1 + max(self.axes, default=0), 0)
-            self.axes_address = C.addressof(self.axes_c)
+            self.axes_args = (C.addressof(self.axes_c),)
 
     @classmethod
     def build(cls, frequencies: Sequence[float], n_positions: int, *, layout: str = "half", attention_factor: float = 1.0,
@@ -170,19 +170,13 @@ class RopeTable:
         _check_status(self.status, stream)
 
 
-def _axes_of(table) -> tuple:
-    """What the binding takes besides, where a table has axes."""
-    axes = getattr(table, "axes_address", None)
-    return () if axes is None else (axes,)
-
-
 def _rope(x, table: RopeTable, positions, out, transpose: bool, stream):
     if isinstance(x, torch.Tensor):
         if out is None:
             out = _empty(x, x.shape, x.dtype, stream)
         elif not isinstance(out, torch.Tensor):
             out, = out
-        _b.rope(table.address, table.device, x, None, out, None, positions, transpose, _raw(stream), *_axes_of(table))
+        _b.rope(table.address, table.device, x, None, out, None, positions, transpose, _raw(stream), *getattr(table, "axes_args", ()))
         if stream is not None:
             _record(stream, x, out, positions, *table.tensors)
         return out
@@ -191,7 +185,7 @@ def _rope(x, table: RopeTable, positions, out, transpose: bool, stream):
     q, k = x
     if out is None:
         out = (_empty(q, q.shape, q.dtype, stream), _empty(k, k.shape, k.dtype, stream))
-    _b.rope(table.address, table.device, q, k, out[0], out[1], positions, transpose, _raw(stream), *_axes_of(table))
+    _b.rope(table.address, table.device, q, k, out[0], out[1], positions, transpose, _raw(stream), *getattr(table, "axes_args", ()))
     if stream is not None:
         _record(stream, q, k, *out, positions, *table.tensors)
     return out
@@ -314,7 +308,7 @@ def bcp_kv_write(cache: KvCache, k, v, slots, rope: Optional[RopeTable] = None, 
     if rope is None:
         _b.kv_write(cache.address, cache.device, k, v, slots, None, cache.device, positions, _raw(stream), cache.k, cache.v)
     else:
-        _b.kv_write(cache.address, cache.device, k, v, slots, rope.address, rope.device, positions, _raw(stream), cache.k, cache.v, *_axes_of(rope))
+        _b.kv_write(cache.address, cache.device, k, v, slots, rope.address, rope.device, positions, _raw(stream), cache.k, cache.v, *rope.axes_args)
     if stream is not None:
         _record(stream, k, v, slots, positions, *cache.tensors, *(() if rope is None else rope.tensors))
 
