@@ -1,20 +1,29 @@
 // Attention of groups of sequences over the prefix that each group shares, computed once for all of them.
 //
 // Mathematics.  The query rows of a group under one cache head, (sequence, query head) by (sequence, query head), are the rows of S = Q K^T and O = P V
-// with P = exp2(S c - m), c = scale log2 e.  m is a row's reference: when a score exceeds it by more than 8, the row's sums are brought to the new
-// one.  What is left of the prefix are records (o, m, l) a row, which the attention over the sequences' own tokens joins (kv_attend.cu).
+// with P = exp2(c S - m), c = scale log2 e.  m is a row's reference: when a score exceeds it by more than 8, the row's sums are brought to the new
+// one.  What is left of the prefix are records (o, m, l) a row; the attention over the sequences' own tokens (kv_attend.cu) leaves one more, and a third
+// kernel joins a row's records.
 //
-// What bounds it: up to 256 rows a cache head, reading the prefix once (a byte of a 16-bit cache meets 256 rows in 512 multiply-adds,
-// 1024 with the second product of the weights); beyond that the products, the exponentials and the rounding of the weights.
+// Both products are tcgen05.mma with 128 rows.  A CTA has two streams, each with 128 rows whose scores and output lie in tensor memory (one stream with more
+// than 128 dimensions): with more than 128 rows in a tile both take every 128 tokens, else they take turns with the same rows.  Two threads have half of a row's
+// scores each (one thread a row: 3.5 us for a tile of both streams, two: 2.9, bfloat16).  Weights go back to tensor memory in place of the scores and are the first
+// operand of the second product from there.  Over bfloat16 and 8-bit caches a weight is the sum of two bfloat16 numbers (2^-16 of it), as one alone would be
+// rounded as coarsely as the result; 8-bit values are widened to bfloat16, keys to binary16, both exactly, the value's scale goes into the weight.  Over binary16
+// caches a weight is one binary16 number (2^-11).
 //
-// Both products are tcgen05.mma with 128 rows.  A CTA has two streams, each a warpgroup with 128 rows (a thread a row), their scores and their output in
-// tensor memory: with more than 128 rows in a tile both take every 128 tokens, else they take turns with the same rows; one works on its weights while the
-// tensor cores work for the other.  Weights go back to tensor memory in place of the scores and are the first operand of the second
-// product from there.  Over bfloat16 and 8-bit caches a weight is the sum of two bfloat16 numbers (2^-16 of it), as one alone would be rounded as
-// coarsely as the result; 8-bit values are widened to bfloat16, keys to binary16, both exactly, the value's scale goes into the weight.
-// Four warps bring tokens by 16-byte asynchronous copies through a ring of tiles (pages may have any size and place), a warp issues the products.
+// Tokens come as boxes of a tensor map (pages of a multiple of eight tokens) or by 16-byte asynchronous copies (other pages, the end of a prefix) into a ring
+// of tiles; a warp for each stream issues its products, the products of one stream behind those of the other: side by side both end late, and both streams
+// make weights, then wait, at the same time (256 sequences over 32,768 tokens, binary16, without own tokens: 164 us, 181 side by side).
 //
-// Split.  The tiles of all groups, cache heads and 256 rows form one line that is cut into as many equal parts as there are SMs.
+// Split.  The tiles of all groups, cache heads and 256 rows form one line that is cut into as many equal parts as there are SMs, so a part
+// is one or two stretches of a unit.  The kernel of the own tokens needs nothing of this one and starts while it ends.
+//
+// What bounds it: the chain of a tile.  Scores of 128 x 128, their largest, the exchange between a row's two threads, 64 exponentials a thread in two halves, products:
+// 2.9 us for both streams with weights of two numbers and 2.4 with one, where the tensor cores need 1.56 and 1.04, exponentials 1.04, and the tile's 64 KB 1.5 at the
+// copy bandwidth.  8-bit caches wait for the warps that widen them (about 4 us a tile of 128 tokens).  Measured on one B200, launches of all three kernels
+// in a row in a CUDA graph, 32 / 8 heads of 128: 5 drafted tokens over 4096, bfloat16: 14.8 us (without prefix and own tokens the three launches take 7.5); 64
+// sequences over 32,768 and up to 600 own tokens, bfloat16: 89 us; 70 over 5 prefixes of up to 9000, e4m3, pages of 24: 98 us; 256 over 32,768, binary16: 220 us.
 #include <cuda.h>
 
 #include <mutex>
@@ -72,7 +81,7 @@ struct Shape {
   static constexpr uint32_t SMEM = STREAMS * Q + SLOTS * TILE + RAWS * RAW + NMETA * META + 8 * (2 * SLOTS + NMETA + 7 * STREAMS + LOADERS * RAWS) + STREAMS * 1024 + 48;
   // two warpgroups for each stream (a thread has half of a row's scores), one that copies, one of whose warps issue the products
   static constexpr uint32_t WARPS = 8 * STREAMS + LOADERS + 4, THREADS = 32 * WARPS, COLS = TOK / 2;
-  // Registers a thread: at launch, and after the groups have been given theirs (their sum is the launch's).  With one stream there are enough for all.
+  // Registers a thread: at launch, and after the groups have been given theirs (their sum is at most the launch's).  With one stream there are enough for all.
   static constexpr uint32_t REGS = quant ? 72 : 80, REGS_ROWS = quant ? 80 : 88, REGS_COPY = quant ? 64 : 72, REGS_PRODUCT = 56;
   static_assert(4 * REGS_ROWS + LOADERS / 4 * REGS_COPY + REGS_PRODUCT <= (5 + LOADERS / 4) * REGS || STREAMS == 1, "registers of the launch");
   static constexpr uint32_t S0 = 0, O0 = STREAMS * TOK;      // columns of tensor memory

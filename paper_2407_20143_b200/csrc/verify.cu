@@ -5,11 +5,16 @@
 // all weights.  Rows of logits stand for p(j) = exp((z_j - m) / T) / S, so each is read once for m and S (a running maximum, the sum
 // brought to a new one where it grows) before the first draft can be judged.
 //
-// What bounds it: reading the rows for few drafts or many sequences, latency for a single sequence.  A cluster of CTAs takes a
-// sequence, each CTA a stretch of the vocabulary in all rows; maxima and sums are exchanged through the cluster's shared memory, every CTA
+// A cluster of CTAs takes a sequence, each CTA a stretch of the vocabulary in all rows; maxima and sums are exchanged through the cluster's shared memory, every CTA
 // judges all drafts itself, and the weights of the one row that is drawn from (two with drafts' rows; still in the L2 cache) are
 // summed by stretches of 256 tokens.  The CTA in whose stretch the drawn place lies goes over those 256 again.  One launch, no
 // workspace, no atomics: the same bits on every run.
+//
+// What bounds it: an exponential for every element (16 a clock and SM: 74 million take 16 us) beside reading the rows, and for few sequences the chain of phases.
+// Measured on one B200, among other calls: 64 sequences of 4 drafts over 128,256 tokens, bfloat16, 148 MB: 60 us, of which the maxima and sums take 30, and SMs with four CTAs
+// end 15 us after those with three; one sequence of 4 drafts over 32,768: 16 us; 200 rows of 50,304 sampled, binary16: 23 us; 37 sequences of up to 7 looked-up drafts
+// over 50,257 probabilities, binary32: 11.4 us (only the row that is drawn from is read).  CTAs of 1024 threads where all sequences' fit one an SM: one
+// sequence 16.1 us, 17.8 with 256.
 //
 // Precision: a token hangs on a comparison, so sums are held in 64 bits and the probability of a drafted token is computed in 64 bits
 // from its logit; the terms of the sums are binary32 (2^-22 of each).
