@@ -13,8 +13,7 @@
 // What bounds it: an exponential for every element (16 a clock and SM: 74 million take 16 us) beside reading the rows, and for few sequences the chain of phases.
 // Measured on one B200, among other calls: 64 sequences of 4 drafts over 128,256 tokens, bfloat16, 148 MB: 60 us, of which the maxima and sums take 30, and SMs with four CTAs
 // end 15 us after those with three; one sequence of 4 drafts over 32,768: 16 us; 200 rows of 50,304 sampled, binary16: 23 us; 37 sequences of up to 7 looked-up drafts
-// over 50,257 probabilities, binary32: 11.4 us (only the row that is drawn from is read).  CTAs of 1024 threads where all sequences' fit one an SM: one
-// sequence 16.1 us, 17.8 with 256.
+// over 50,257 probabilities, binary32: 7 us (only the row that is drawn from is read).
 //
 // Precision: a token hangs on a comparison, so sums are held in 64 bits and the probability of a drafted token is computed in 64 bits
 // from its logit; the terms of the sums are binary32 (2^-22 of each).
@@ -27,7 +26,9 @@ namespace cg = cooperative_groups;
 
 namespace {
 
-constexpr uint32_t kThreads = 256, kManyThreads = 1024;  // of a CTA: four an SM, or one where the sequences leave SMs without work
+// Of a CTA, four an SM.  (1024 and one an SM for few sequences: 8 of 4 drafts over 128,256 tokens 42.9 us, 26.2 with 256; one over 32,768 16.5 and 15.2; 512 for
+// many: 64 sequences 67.8 and 57.7.)
+constexpr uint32_t kThreads = 256;
 constexpr uint32_t kParts = 8;                           // warps that share a row's part, at most
 constexpr uint32_t kSegment = 256;  // tokens of a stretch that is summed for the draw: eight a lane
 constexpr int32_t kNoToken = -(1 << 30);
@@ -207,11 +208,11 @@ struct Weights {  // of the row that is drawn from
 };
 
 template <typename T, bool PROB>
-__global__ void __launch_bounds__(kManyThreads, 1) bcp_verify_kernel(const VerifyArgs a) {
+__global__ void __launch_bounds__(kThreads, 4) bcp_verify_kernel(const VerifyArgs a) {
   after_previous();
   cg::cluster_group cluster = cg::this_cluster();
   const uint32_t ctas = cluster.num_blocks(), rank = cluster.block_rank();
-  const uint32_t b = blockIdx.x / ctas, tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, warps = blockDim.x >> 5;
+  const uint32_t b = blockIdx.x / ctas, tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, warps = kThreads / 32;
   const uint32_t most_rows = 2 * a.n_drafts + 1;
   extern __shared__ __align__(16) unsigned char smem[];
   RowSum* const by_warp = reinterpret_cast<RowSum*>(smem);       // [rows][parts]
@@ -295,7 +296,7 @@ __global__ void __launch_bounds__(kManyThreads, 1) bcp_verify_kernel(const Verif
   while (k < n && good[k]) ++k;
   int64_t* const tokens = a.tokens + uint64_t(b) * (a.n_drafts + 1);
   if (rank == 0) {
-    for (uint32_t i = tid; i <= a.n_drafts; i += blockDim.x)
+    for (uint32_t i = tid; i <= a.n_drafts; i += kThreads)
       if (i != k) tokens[i] = i < k ? drafts[i] : -1;
     if (tid == 0) a.accepted[b] = int32_t(k);
     if (greedy && tid == 0) tokens[k] = whole[k].m > -INFINITY ? int64_t(whole[k].index) : -1;
@@ -445,7 +446,7 @@ __global__ void __launch_bounds__(kManyThreads, 1) bcp_verify_kernel(const Verif
 }
 
 template <typename T, bool PROB>
-cudaError_t launch(const VerifyArgs& a, uint32_t n_seqs, uint32_t ctas, uint32_t threads, uint32_t smem, cudaStream_t stream) {
+cudaError_t launch(const VerifyArgs& a, uint32_t n_seqs, uint32_t ctas, uint32_t smem, cudaStream_t stream) {
   void (*const kernel)(VerifyArgs) = bcp_verify_kernel<T, PROB>;
   cudaError_t e = cudaSuccess;
   if (ctas > 8) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
@@ -456,13 +457,13 @@ cudaError_t launch(const VerifyArgs& a, uint32_t n_seqs, uint32_t ctas, uint32_t
   attributes[1].id = cudaLaunchAttributeClusterDimension;
   attributes[1].val.clusterDim.x = ctas, attributes[1].val.clusterDim.y = 1, attributes[1].val.clusterDim.z = 1;
   cudaLaunchConfig_t config = {};
-  config.gridDim = dim3(n_seqs * ctas), config.blockDim = dim3(threads), config.dynamicSmemBytes = smem, config.stream = stream;
+  config.gridDim = dim3(n_seqs * ctas), config.blockDim = dim3(kThreads), config.dynamicSmemBytes = smem, config.stream = stream;
   config.attrs = attributes, config.numAttrs = 2;
   return cudaLaunchKernelEx(&config, kernel, a);
 }
 template <typename T>
-cudaError_t launch(const VerifyArgs& a, bool prob, uint32_t n_seqs, uint32_t ctas, uint32_t threads, uint32_t smem, cudaStream_t stream) {
-  return prob ? launch<T, true>(a, n_seqs, ctas, threads, smem, stream) : launch<T, false>(a, n_seqs, ctas, threads, smem, stream);
+cudaError_t launch(const VerifyArgs& a, bool prob, uint32_t n_seqs, uint32_t ctas, uint32_t smem, cudaStream_t stream) {
+  return prob ? launch<T, true>(a, n_seqs, ctas, smem, stream) : launch<T, false>(a, n_seqs, ctas, smem, stream);
 }
 
 int check_rows(const char* call, const char* name, const bcp_vocab_rows* r) {
@@ -506,16 +507,18 @@ extern "C" int bcp_verify_drafts(const bcp_vocab_rows* target, const bcp_vocab_r
   int sms = 0, device = 0;
   BCP_CUDA(cudaGetDevice(&device));
   BCP_CUDA(cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, device));
-  // CTAs of a sequence: as long as the GPU has room for four of them an SM, and each has 2048 tokens; of a huge vocabulary a CTA has at
-  // most 2^19 tokens, whose sums fit its shared memory.
+  // CTAs of a sequence: as long as the GPU has room for four of them an SM, and each has 2048 tokens, or 4096 of probabilities, which are read once; of a huge
+  // vocabulary a CTA has at most 2^19 tokens, whose sums fit its shared memory.  Microseconds with room for two / four / eight: 64 sequences of 4 drafts over
+  // 128,256 tokens 82 / 57.5 / 71, 200 rows of 50,304 sampled 28.5 / 21.9 / 25.1, 30 rows of 128,256 16.0 / 13.5 / 13.7; with 2048 and 4096 tokens: 37
+  // rows of 50,257 probabilities 11.0 / 7.1, one sequence of 4 drafts over 32,768 16.5 / 17.1.
+  const uint32_t least = probabilities ? 4096 : 2048;
   uint32_t ctas = 16;
-  while (ctas > 1 && (uint64_t(n_seqs) * ctas > uint64_t(sms) * 4 || vocab / ctas < 2048) && vocab / ctas < (1u << 18)) ctas /= 2;
+  while (ctas > 1 && (uint64_t(n_seqs) * ctas > uint64_t(sms) * 4 || vocab / ctas < least) && vocab / ctas < (1u << 18)) ctas /= 2;
   const uint32_t rows = 2 * n_drafts + 1, segments = (vocab + 7) / kSegment + 2;
   const uint32_t smem = uint32_t(sizeof(RowSum)) * rows * (kParts + 2) + 8 * (2 + (n_drafts + 2) / 2 + (segments + ctas - 1) / ctas);
-  const uint32_t threads = uint64_t(n_seqs) * ctas <= uint64_t(sms) ? kManyThreads : kThreads;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
-  if (target->type == BCP_F32) BCP_CUDA(launch<float>(a, probabilities != 0, n_seqs, ctas, threads, smem, st));
-  if (target->type == BCP_BF16) BCP_CUDA(launch<__nv_bfloat16>(a, probabilities != 0, n_seqs, ctas, threads, smem, st));
-  if (target->type == BCP_F16) BCP_CUDA(launch<__half>(a, probabilities != 0, n_seqs, ctas, threads, smem, st));
+  if (target->type == BCP_F32) BCP_CUDA(launch<float>(a, probabilities != 0, n_seqs, ctas, smem, st));
+  if (target->type == BCP_BF16) BCP_CUDA(launch<__nv_bfloat16>(a, probabilities != 0, n_seqs, ctas, smem, st));
+  if (target->type == BCP_F16) BCP_CUDA(launch<__half>(a, probabilities != 0, n_seqs, ctas, smem, st));
   return BCP_OK;
 }

@@ -265,6 +265,24 @@ def test_streams_graphs_and_outputs(cuda_device):
     assert none[0].shape == (0, 4) and none[1].shape == (0,)
 
 
+@pytest.mark.parametrize("b,v", [(1, 40001), (5, 128256), (70, 33000)])
+def test_clusters_of_every_size_in_graphs_and_on_two_streams(cuda_device, b, v):
+    # 16, 8 or fewer CTAs a sequence; two captured calls without anything between them, two streams at once
+    z, drafts, u, q = _batch(b, 3, v, 41, BF16)
+    want = bcp.bcp_verify_drafts(z, drafts, u, draft=q)
+    out, torch_graph = [], torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(torch_graph):
+        out = [bcp.bcp_verify_drafts(z, drafts, u, draft=q) for _ in range(2)]
+    torch_graph.replay()
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    for s in streams:
+        s.wait_stream(torch.cuda.current_stream())
+    out += [bcp.bcp_verify_drafts(z, drafts, u, draft=q, stream=streams[i % 2]) for i in range(4)]
+    torch.cuda.synchronize()
+    assert all(torch.equal(x, want[0]) and torch.equal(y, want[1]) for x, y in out)
+
+
 def test_refusals(cuda_device):
     z, drafts, u, q = _batch(3, 2, 50, 37)
     bcp.bcp_verify_drafts(z, drafts, u, draft=q)
