@@ -21,9 +21,9 @@
 //
 // What bounds it: the chain of a tile.  Scores of 128 x 128, their largest, the exchange between a row's two threads, 64 exponentials a thread in two halves, products:
 // 2.9 us for both streams with weights of two numbers and 2.4 with one, where the tensor cores need 1.56 and 1.04, exponentials 1.04, and the tile's 64 KB 1.5 at the
-// copy bandwidth.  8-bit caches wait for the warps that widen them (about 4 us a tile of 128 tokens).  Measured on one B200, launches of all three kernels
+// copy bandwidth.  8-bit caches wait for the warps that widen them (about 2.9 us a tile of 128 tokens).  Measured on one B200, launches of all three kernels
 // in a row in a CUDA graph, 32 / 8 heads of 128: 5 drafted tokens over 4096, bfloat16: 14.8 us (without prefix and own tokens the three launches take 7.5); 64
-// sequences over 32,768 and up to 600 own tokens, bfloat16: 89 us; 70 over 5 prefixes of up to 9000, e4m3, pages of 24: 98 us; 256 over 32,768, binary16: 220 us.
+// sequences over 32,768 and up to 600 own tokens, bfloat16: 88 us; 70 over 5 prefixes of up to 9000, e4m3, pages of 24: 96 us; 256 over 32,768, binary16: 220 us.
 #include <cuda.h>
 
 #include <mutex>
@@ -72,13 +72,14 @@ struct Shape {
   static constexpr uint32_t Q = kRows * DP * 2;
   static constexpr uint32_t RAW = quant ? TOK * DP : 0;      // of a tile as it lies in an 8-bit cache
   static constexpr uint32_t RAWS = quant ? 3 : 0;
-  // Warps that bring tokens; 8-bit ones have to be widened by them, too.
+  // Warps that bring tokens; 8-bit ones have to be widened by them, too (70 sequences over 5 prefixes of up to 9000 tokens, e4m3: 104 us with four, 98 with eight on
+  // every tile, 96 with four for keys and four for values).
   static constexpr uint32_t LOADERS = quant && STREAMS == 2 ? 8 : 4;
-  static constexpr uint32_t META = quant ? 16 + TOK * 8 + 32 : 16;
+  static constexpr uint32_t META = quant ? 16 + TOK * 8 + 16 : 16;
   static constexpr uint32_t NMETA = quant ? 8 : kMeta;         // (more than the tiles that can be on their way past one that is still worked on)
   static constexpr uint32_t SLOTS = DP == 64 ? 8 : quant ? 3 : 5;  // tiles in 16 bits: what shared memory has room for
   static constexpr uint32_t AHEAD = quant ? RAWS - 1 : 3;    // copies of so many tiles are under way
-  static constexpr uint32_t SMEM = STREAMS * Q + SLOTS * TILE + RAWS * RAW + NMETA * META + 8 * (2 * SLOTS + NMETA + 7 * STREAMS + LOADERS * RAWS) + STREAMS * 1024 + 48;
+  static constexpr uint32_t SMEM = STREAMS * Q + SLOTS * TILE + RAWS * RAW + NMETA * META + 8 * (2 * SLOTS + NMETA + 7 * STREAMS + 4 * RAWS) + STREAMS * 1024 + 48;
   // two warpgroups for each stream (a thread has half of a row's scores), one that copies, one of whose warps issue the products
   static constexpr uint32_t WARPS = 8 * STREAMS + LOADERS + 4, THREADS = 32 * WARPS, COLS = TOK / 2;
   // Registers a thread: at launch, and after the groups have been given theirs (their sum is at most the launch's).  With one stream there are enough for all.
@@ -287,8 +288,8 @@ __global__ void __launch_bounds__(Shape<FMT, DP>::THREADS, 1) bcp_kv_prefix_kern
   const uint32_t bars = meta + S::NMETA * S::META;
   const uint32_t full = bars, empty = full + 8 * S::SLOTS, described = empty + 8 * S::SLOTS, q_full = described + 8 * S::NMETA, s_full = q_full + 8 * S::STREAMS,
                  p_full = s_full + 8 * S::STREAMS, o_full = p_full + 16 * S::STREAMS, drained = o_full + 8 * S::STREAMS, turn = drained + 8 * S::STREAMS, raw_full = turn + 8 * S::STREAMS;
-  uint32_t* const words = reinterpret_cast<uint32_t*>(smem + (raw_full + 8 * S::LOADERS * S::RAWS + S::STREAMS * 1024 - base));  // tensor memory, stop, found[8]
-  volatile float* const swap = reinterpret_cast<volatile float*>(smem + (raw_full + 8 * S::LOADERS * S::RAWS - base));  // [stream][half][row]
+  uint32_t* const words = reinterpret_cast<uint32_t*>(smem + (raw_full + 32 * S::RAWS + S::STREAMS * 1024 - base));  // tensor memory, stop, found[8]
+  volatile float* const swap = reinterpret_cast<volatile float*>(smem + (raw_full + 32 * S::RAWS - base));  // [stream][half][row]
   volatile uint32_t* const stop = words + 1;
   uint32_t* const found = words + 2;
   uint32_t* const totals = reinterpret_cast<uint32_t*>(smem);  // before the tiles come
@@ -299,11 +300,11 @@ __global__ void __launch_bounds__(Shape<FMT, DP>::THREADS, 1) bcp_kv_prefix_kern
   }
   if (warp == S::WARPS - 4) tmem_alloc(uint32_t(__cvta_generic_to_shared(words)));
   if (tid == 0) {
-    for (uint32_t i = 0; i < S::SLOTS; ++i) mbar_init(full + 8 * i, 32 * S::LOADERS), mbar_init(empty + 8 * i, 2);
-    for (uint32_t i = 0; i < S::NMETA; ++i) mbar_init(described + 8 * i, 32 * S::LOADERS);
+    for (uint32_t i = 0; i < S::SLOTS; ++i) mbar_init(full + 8 * i, kRows), mbar_init(empty + 8 * i, 2);
+    for (uint32_t i = 0; i < S::NMETA; ++i) mbar_init(described + 8 * i, kRows);
     for (uint32_t i = 0; i < S::STREAMS; ++i)
       mbar_init(q_full + 8 * i, 2 * kRows), mbar_init(s_full + 8 * i, 1), mbar_init(p_full + 16 * i, 2 * kRows), mbar_init(p_full + 16 * i + 8, 2 * kRows), mbar_init(o_full + 8 * i, 1), mbar_init(drained + 8 * i, 1), mbar_init(turn + 8 * i, 1);
-    for (uint32_t i = 0; i < S::LOADERS * S::RAWS; ++i) mbar_init(raw_full + 8 * i, 1);
+    for (uint32_t i = 0; i < 4 * S::RAWS; ++i) mbar_init(raw_full + 8 * i, 1);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   tmem_before();
@@ -515,11 +516,8 @@ __global__ void __launch_bounds__(Shape<FMT, DP>::THREADS, 1) bcp_kv_prefix_kern
           if constexpr (S::quant) {
             // Weights times scales must neither overflow in the sums nor vanish: where scales beyond 2^60 turn up all are multiplied by 2^-40, while none
             // is above 2^-40 by 2^60.
-#pragma unroll
-            for (uint32_t i = 0; i < S::LOADERS; i += 4) {
-              const float4 w = *reinterpret_cast<const float4*>(about + 16 + S::TOK * 8 + 4 * i);
-              top_scale = fmaxf(top_scale, fmaxf(fmaxf(w.x, w.y), fmaxf(w.z, w.w)));
-            }
+            const float4 w = *reinterpret_cast<const float4*>(about + 16 + S::TOK * 8);
+            top_scale = fmaxf(top_scale, fmaxf(fmaxf(w.x, w.y), fmaxf(w.z, w.w)));
             const float next = top_scale > 0x1p60f ? 0x1p-40f : top_scale < 0x1p-40f ? 0x1p60f : 1.f;
             if (next != unit) down *= next / unit, unit = next;
           }
@@ -628,16 +626,23 @@ __global__ void __launch_bounds__(Shape<FMT, DP>::THREADS, 1) bcp_kv_prefix_kern
   } else if (warp < 8 * S::STREAMS + S::LOADERS) {
     // ================================================================ copies of keys and values
     if constexpr (S::STREAMS == 2) fewer_registers<S::REGS_COPY>();
-    const uint32_t w = warp - 8 * S::STREAMS;
-    constexpr uint32_t kEach = S::TOK / S::LOADERS;                 // rows of a tile that a warp brings
+    // Four warps share a tile.  With eight (8-bit caches, whose tiles have to be widened) four bring keys and four bring values.
+    const uint32_t w = warp - 8 * S::STREAMS & 3;
+    constexpr bool kTeams = S::LOADERS == 8;
+    const bool keys_team = warp - 8 * S::STREAMS < 4;
+    constexpr uint32_t kEach = S::TOK / 4;                        // rows of a tile that a warp brings
     constexpr uint32_t kChunks = DP * (S::quant ? 1 : 2) / 16;    // 16-byte chunks of a row
     constexpr uint32_t kTogether = 32 / kChunks, kTurns = kEach / kTogether;
     constexpr uint32_t kAll = kEach == 32 ? 0xffffffffu : (1u << (kEach & 31)) - 1;
     const uint32_t my_row = lane / kChunks, chunk = lane % kChunks;
     const bool inside = chunk * 16 < a.head_dim * (S::quant ? 1u : 2u);
-    uint32_t item = 0, tile0 = 0, landed = 0, brought = 0;  // brought: tiles whose keys are under way or have landed
-    uint32_t kinds = 0, tile_landed = 0;  // a bit for each item: it is keys; tiles whose keys have landed
-    uint32_t boxes = 0, phases = 0;       // a bit for each item: it comes in boxes; for each place of 8-bit tiles: the parity of its barrier
+    uint32_t item = 0, tile0 = 0, brought = 0;  // item: of the ring; brought: tiles whose keys have been seen
+    uint32_t queued = 0, landed = 0;            // of this team's items: those under way or landed, those landed
+    uint32_t items[2] = {0, 0};                 // with teams: the last two of them that are queued, the newer one first
+    uint32_t kinds = 0, tile_landed = 0;        // a bit for each queued item: it is keys; tiles whose keys have landed
+    uint32_t boxes = 0, phases = 0;             // a bit for each queued item: it comes in boxes; for each place of 8-bit tiles: the parity of its barrier
+    auto stage_of = [&](uint32_t n) { return !S::quant ? 0 : kTeams ? keys_team ? n & 1 : 2 : n % S::RAWS; };  // of the n-th queued item
+    const uint32_t ahead = kTeams ? keys_team : S::AHEAD;
     // Where this warp's tokens of a tile lie (a row a lane); the page of the next tile's is looked up ahead.
     int32_t page = -1, page_of[2] = {-1, -1};
     bool inside_prefix = false;
@@ -647,16 +652,17 @@ __global__ void __launch_bounds__(Shape<FMT, DP>::THREADS, 1) bcp_kv_prefix_kern
 
     // An 8-bit tile that has come in is widened into its place.
     auto land = [&]() {
-      const uint32_t slot = landed % S::SLOTS, at_slot = ring + slot * S::TILE;
+      const uint32_t this_item = !kTeams ? landed : queued - landed > 1 ? items[1] : items[0];
+      const uint32_t slot = this_item % S::SLOTS, at_slot = ring + slot * S::TILE;
       const bool keys = kinds >> (landed & 31) & 1;
       const uint32_t m_slot = tile_landed % S::NMETA;
       if constexpr (S::quant) {
-        const uint32_t stage = landed % S::RAWS;
+        const uint32_t stage = stage_of(landed);
         if (boxes >> (landed & 31) & 1) {
-          ok = ok && bar_wait(raw_full + 8 * (S::LOADERS * stage + w), phases >> stage & 1, stop);
+          ok = ok && bar_wait(raw_full + 8 * (4 * stage + w), phases >> stage & 1, stop);
           phases ^= 1u << stage;
         }
-        if (landed >= S::SLOTS) ok = ok && bar_wait(empty + 8 * slot, landed / S::SLOTS - 1 & 1, stop);
+        if (this_item >= S::SLOTS) ok = ok && bar_wait(empty + 8 * slot, this_item / S::SLOTS - 1 & 1, stop);
         const uint32_t from = raw + stage * S::RAW + (w * kEach + my_row) * a.head_dim + chunk * 16;
         if (inside && ok) {
 #pragma unroll 2
@@ -722,13 +728,13 @@ __global__ void __launch_bounds__(Shape<FMT, DP>::THREADS, 1) bcp_kv_prefix_kern
           at_end = true;
         }
       }
-      if (at_end && landed == item) break;
-      const uint32_t slot = item % S::SLOTS, stage = S::quant ? item % S::RAWS : 0;
+      if (at_end && landed == queued) break;
+      const uint32_t slot = item % S::SLOTS, stage = stage_of(queued);
       bool land_now = at_end;
       if (!S::quant && !at_end && item >= S::SLOTS) {
         // copies that are under way go on to the products while this tile's place is still taken
         const uint32_t parity = item / S::SLOTS - 1 & 1;
-        land_now = landed < item && !__all_sync(0xffffffffu, bar_test(empty + 8 * slot, parity));
+        land_now = landed < queued && !__all_sync(0xffffffffu, bar_test(empty + 8 * slot, parity));
         if (!land_now) ok = bar_wait(empty + 8 * slot, parity, stop);
         if (!ok) break;
       }
@@ -746,16 +752,21 @@ __global__ void __launch_bounds__(Shape<FMT, DP>::THREADS, 1) bcp_kv_prefix_kern
           page_of[0] = page, off_of[0] = off, alive_of[0] = __ballot_sync(0xffffffffu, page >= 0) & kAll;
           ++brought;
           unsigned char* const about = meta_ptr + tile % S::NMETA * S::META;
-          if (lane == 0) {
+          if (lane == 0 && keys_team) {
             if (kEach == 32) reinterpret_cast<volatile uint32_t*>(about)[w] = alive_of[0];
             if (kEach == 16) reinterpret_cast<volatile uint16_t*>(about)[w] = uint16_t(alive_of[0]);
           }
+        }
+        if (kTeams && keys != keys_team) {
+          if (keys && t + 1 < n) look_up((at.step + t + 1) * S::TOK);
+          ++item, ++i;
+          continue;
         }
         // values come behind the next tile's keys where the streams take turns
         const bool older = !keys && tile + 1 < brought;
         const int32_t my_page = older ? page_of[1] : page_of[0];
         const uint32_t my_off = older ? off_of[1] : off_of[0], alive = older ? alive_of[1] : alive_of[0];
-        const uint32_t bar = S::quant ? raw_full + 8 * (S::LOADERS * stage + w) : full + 8 * slot;
+        const uint32_t bar = S::quant ? raw_full + 8 * (4 * stage + w) : full + 8 * slot;
         const bool box = a.block && alive == kAll;
         if (box) {
           // a warp's tokens in boxes, each inside one page
@@ -788,20 +799,21 @@ __global__ void __launch_bounds__(Shape<FMT, DP>::THREADS, 1) bcp_kv_prefix_kern
         }
         copies_end();
         if (keys && t + 1 < n) look_up((at.step + t + 1) * S::TOK);
-        kinds = (kinds & ~(1u << (item & 31))) | uint32_t(keys) << (item & 31);
-        boxes = (boxes & ~(1u << (item & 31))) | uint32_t(box) << (item & 31);
-        ++item, ++i;
+        kinds = (kinds & ~(1u << (queued & 31))) | uint32_t(keys) << (queued & 31);
+        boxes = (boxes & ~(1u << (queued & 31))) | uint32_t(box) << (queued & 31);
+        items[1] = items[0], items[0] = item;
+        ++queued, ++item, ++i;
         if (!S::quant && a.block) {
           // boxes count themselves; rows that had to be copied one by one, at the end of a prefix, are waited for at once
           if (!box) copies_wait<0>(), to_async_proxy();
           if (keys) bar_arrive(described + 8 * (tile % S::NMETA));
           if (!box || lane) bar_arrive(bar);
-          landed = item;
+          landed = queued;
         }
-        land_now = item - landed > S::AHEAD;
+        land_now = queued - landed > ahead;
       }
       if (land_now) {
-        copies_wait_all_but(item - landed - 1);
+        copies_wait_all_but(queued - landed - 1);
         land();
       }
     }
@@ -1061,7 +1073,7 @@ template <int FMT, int DP>
 Variant variant() {
   typedef Shape<FMT, DP> S;
   constexpr int JOIN = DP <= 128 ? 128 : 256;
-  return Variant{bcp_kv_prefix_kernel<FMT, DP>, {bcp_kv_join_kernel<JOIN, false>, bcp_kv_join_kernel<JOIN, true>}, S::SMEM, S::THREADS, S::ROWS, S::TOK, S::STREAMS == 2 ? S::REGS : 0, S::TOK / S::LOADERS};
+  return Variant{bcp_kv_prefix_kernel<FMT, DP>, {bcp_kv_join_kernel<JOIN, false>, bcp_kv_join_kernel<JOIN, true>}, S::SMEM, S::THREADS, S::ROWS, S::TOK, S::STREAMS == 2 ? S::REGS : 0, S::TOK / 4};
 }
 template <int FMT>
 Variant variant_of(uint32_t head_dim) {

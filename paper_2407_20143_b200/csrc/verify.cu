@@ -12,7 +12,7 @@
 //
 // What bounds it: an exponential for every element (16 a clock and SM: 74 million take 16 us) beside reading the rows, and for few sequences the chain of phases.
 // Measured on one B200, among other calls: 64 sequences of 4 drafts over 128,256 tokens, bfloat16, 148 MB: 60 us, of which the maxima and sums take 30, and SMs with four CTAs
-// end 15 us after those with three; one sequence of 4 drafts over 32,768: 16 us; 200 rows of 50,304 sampled, binary16: 23 us; 37 sequences of up to 7 looked-up drafts
+// end 15 us after those with three; one sequence of 4 drafts over 32,768: 15 us; 200 rows of 50,304 sampled, binary16: 23 us; 37 sequences of up to 7 looked-up drafts
 // over 50,257 probabilities, binary32: 7 us (only the row that is drawn from is read).
 //
 // Precision: a token hangs on a comparison, so sums are held in 64 bits and the probability of a drafted token is computed in 64 bits

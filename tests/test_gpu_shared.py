@@ -348,6 +348,39 @@ def test_streams_and_graphs(cuda_device):
     assert all(torch.equal(x, out) and torch.equal(y, lse) for x, y in got)
 
 
+@pytest.mark.parametrize("page", [64, 7])
+def test_offsets_past_32_bits(cuda_device, page):
+    # the last pages of a cache whose elements lie beyond 2^32; boxes and copies
+    n_pages = (1 << 32) // (page * 128) + 40
+    k, v = (torch.zeros((n_pages, 1, page, 128), dtype=I8, device="cuda") for _ in range(2))
+    cache = bcp.KvCache(k, v, *(torch.zeros((n_pages, 1, page), device="cuda") for _ in range(2)))
+    last = torch.arange(n_pages - 40, n_pages, device="cuda")
+    slots = (last[:, None] * page + torch.arange(page, device="cuda")).flatten()
+    bcp.bcp_kv_write(cache, _randn((len(slots), 1, 128), 1), _randn((len(slots), 1, 128), 2), slots)
+    table = last[torch.randperm(40, generator=torch.Generator().manual_seed(1)).cuda()].int()
+    prefix_table, own, lengths = table[None, :30], table[30:].view(5, 2), [page + 3] * 5
+    q = _randn((5, 4, 128), 9, BF16)
+    out, lse = bcp.bcp_kv_attend_shared(cache, q, prefix_table, _int([30 * page - 5]), _int([0, 5]), own, _int(lengths))
+    cache.check()
+    assert_attended(out, lse, cache, q, prefix_table, [30 * page - 5], [0, 5], own, lengths)
+
+
+def test_small_work_between_other_kernels(cuda_device):
+    # queries, lengths and pages are written by kernels right before, outputs read right behind, without anything waiting between
+    prefix_table, table, n_pages = _tables([300], [30] * 9, 16, 5)
+    cache = _cache(n_pages, 2, 16, 128, BF16)
+    work, got = bcp.KvWorkspace(cache, 8, 9, shared=True), []
+    lengths, prefix = _int([0] * 9), _int([0])
+    for i in range(20):
+        q = _randn((9, 8, 128), 100 + i, BF16)
+        lengths.fill_(1 + i), prefix.fill_(15 * i)
+        out, lse = bcp.bcp_kv_attend_shared(cache, q, prefix_table, prefix, _int([0, 9]), table, lengths, workspace=work)
+        got.append((q, out * 1, lse * 1))
+        out.zero_()
+    for i, (q, out, lse) in enumerate(got):
+        assert_attended(out, lse, cache, q, prefix_table, [15 * i], [0, 9], table, [1 + i] * 9)
+
+
 def test_refusals(cuda_device):
     prefix_table, table, n_pages = _tables([150], [9] * 5, 16, 5)
     cache = _cache(n_pages, 2, 16, 64, BF16)
