@@ -292,7 +292,7 @@ __global__ void __launch_bounds__(Shape<FMT, DP>::THREADS, 1) bcp_kv_prefix_kern
   volatile float* const swap = reinterpret_cast<volatile float*>(smem + (raw_full + 32 * S::RAWS - base));  // [stream][half][row]
   volatile uint32_t* const stop = words + 1;
   uint32_t* const found = words + 2;
-  uint32_t* const totals = reinterpret_cast<uint32_t*>(smem);  // before the tiles come
+  uint64_t* const totals = reinterpret_cast<uint64_t*>(smem);  // before the tiles come
 
   if (base & 1023) {  // no room is left to move them there
     if (tid == 0) raise(a.status, BCP_TIMED_OUT);
@@ -317,26 +317,29 @@ __global__ void __launch_bounds__(Shape<FMT, DP>::THREADS, 1) bcp_kv_prefix_kern
   const uint32_t n_q_heads = a.n_heads * a.group.d;
   const uint32_t run = (a.n_groups + S::THREADS - 1) / S::THREADS;
   const uint32_t run0 = min(tid * run, a.n_groups), run1 = min(run0 + run, a.n_groups);
-  uint32_t mine = 0, before;
+  // (The host has made sure that the steps of groups without common sequences fit 32 bits; what starts says may be anything.)
+  uint64_t mine64 = 0;
   for (uint32_t g = run0; g < run1; ++g) {
     const Group x = group_of<S>(a, g);
-    mine += x.steps * x.tiles * a.n_heads;
+    mine64 += uint64_t(x.steps) * x.tiles * a.n_heads;
   }
-  before = mine;
+  uint64_t before64 = mine64;
 #pragma unroll
   for (uint32_t o = 1; o < 32; o <<= 1) {
-    const uint32_t x = __shfl_up_sync(0xffffffffu, before, o);
-    if (lane >= o) before += x;
+    const uint64_t x = __shfl_up_sync(0xffffffffu, before64, o);
+    if (lane >= o) before64 += x;
   }
-  if (lane == 31) totals[warp] = before;
+  if (lane == 31) totals[warp] = before64;
   if (tid == 0) *stop = 0;
   __syncthreads();
-  uint32_t all = 0;
-  before -= mine;
+  uint64_t all64 = 0;
+  before64 -= mine64;
   for (uint32_t w = 0; w < S::WARPS; ++w) {
-    if (w < warp) before += totals[w];
-    all += totals[w];
+    if (w < warp) before64 += totals[w];
+    all64 += totals[w];
   }
+  const bool sound = all64 <= 0x7fffffffull;
+  const uint32_t all = sound ? uint32_t(all64) : 0, mine = uint32_t(mine64), before = uint32_t(before64);
   Cuts cuts;
   if (all) cuts.cut(all, gridDim.x);
   // Rows without a prefix have no records: two warps that have nothing else to do look at all of them.
@@ -351,7 +354,7 @@ __global__ void __launch_bounds__(Shape<FMT, DP>::THREADS, 1) bcp_kv_prefix_kern
       bool has = false;
       if (lo) {
         const Group x = group_of<S>(a, lo - 1);
-        has = b >= x.first && b - x.first < x.rows / a.group.d && x.steps;
+        has = sound && b >= x.first && b - x.first < x.rows / a.group.d && x.steps;
       }
       if (!has)
         for (uint32_t h = 0; h < n_q_heads; ++h) a.rows[uint64_t(b) * n_q_heads + h] = make_int4(0, 0, 0, 0);

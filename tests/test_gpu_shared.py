@@ -283,6 +283,21 @@ def test_bad_pages_lengths_and_starts(cuda_device):
         cache.check()
 
 
+def test_starts_that_claim_every_sequence_again_and_again(cuda_device):
+    # 300,000 prefixes of 16 tiles, half of which claim all of 65,536 sequences (1024 tiles of rows): 2.4e9 steps, more than the kernel counts; no prefix is used and
+    # the status says so
+    cache = _cache(130, 1, 16, 64, BF16)
+    n, groups = 65536, 300000
+    starts = torch.tensor([0, n] * (groups // 2) + [0], dtype=torch.int32, device="cuda")
+    prefix_table = torch.arange(125, dtype=torch.int32, device="cuda").expand(groups, -1).contiguous()
+    q, table = _randn((n, 4, 64), 9, BF16), torch.full((n, 1), 127, dtype=torch.int32, device="cuda")
+    out, _ = bcp.bcp_kv_attend_shared(cache, q, prefix_table, _int([2000] * groups), starts, table, _int([9] * n))
+    with pytest.raises(bcp.BcpError) as e:
+        cache.check()
+    assert "length" in str(e.value)
+    assert_attended(out[:3], bcp.bcp_kv_attend(cache, q[:3], table[:3], _int([9] * 3))[1], cache, q[:3], prefix_table[:0], [], [], table[:3], [9] * 3)
+
+
 def test_one_workspace_for_calls_of_different_shapes(cuda_device):
     cache = _cache(60, 2, 16, 128, E4M3)
     work = bcp.KvWorkspace(cache, 8, 50, shared=True)
