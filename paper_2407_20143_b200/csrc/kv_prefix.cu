@@ -1161,16 +1161,20 @@ int make_maps(const bcp_kv_cache* c, const Variant& v, PrefixArgs* a) {
   return BCP_OK;
 }
 
-uint64_t aligned(uint64_t n) { return (n + 255) / 256 * 256; }
-// The workspace: that of the attention over own tokens, then rows, references and sums of the records.
+constexpr uint64_t kBoundary = 256;
+uint64_t aligned(uint64_t n) { return (n + kBoundary - 1) / kBoundary * kBoundary; }
+// The workspace: that of the attention over own tokens, then rows, references and sums of the records.  These lie on boundaries of memory (sums are stored 32
+// bytes at a time), the workspace itself on one of 16 bytes: `skew` is what is missing to the next boundary where it begins.
 struct Layout {
   uint64_t rows, ml, o, end, records;
-  Layout(uint64_t begin, const Variant& v, uint32_t sms, uint64_t n_seqs, uint32_t n_q_heads, uint32_t head_dim) {
+  Layout(uint64_t begin, uint64_t skew, const Variant& v, uint32_t sms, uint64_t n_seqs, uint32_t n_q_heads, uint32_t head_dim) {
     const uint64_t every = n_seqs * n_q_heads;
     records = 3 * every + 2ull * sms * v.rows;  // whole units (two streams), parts, own tokens
-    rows = aligned(begin), ml = aligned(rows + every * sizeof(int4)), o = aligned(ml + records * sizeof(float2)), end = o + records * head_dim * 4;
+    rows = aligned(begin) + skew, ml = rows + aligned(every * sizeof(int4)), o = ml + aligned(records * sizeof(float2)), end = o + records * head_dim * 4;
   }
 };
+constexpr uint64_t kMostSkew = kBoundary - 16;
+uint64_t skew_of(const void* workspace) { return (0 - reinterpret_cast<uintptr_t>(workspace)) & (kBoundary - 1); }
 
 }  // namespace
 }  // namespace bcp
@@ -1184,7 +1188,7 @@ extern "C" int bcp_kv_attend_shared_workspace(const bcp_kv_cache* cache, uint32_
   const Variant v = variant_of(cache->format, cache->head_dim);
   uint32_t sms = 0;
   if (int rc = prepare(v, &sms)) return rc;
-  const Layout at(own, v, sms, max_seqs, n_q_heads, cache->head_dim);
+  const Layout at(own, kMostSkew, v, sms, max_seqs, n_q_heads, cache->head_dim);
   if (at.records > 0x7fffffffull) return fail(BCP_ERR_CAPACITY, "%s: %u sequences of %u query heads are too many for one call", call, max_seqs, n_q_heads);
   *bytes = at.end;
   return BCP_OK;
@@ -1211,8 +1215,8 @@ extern "C" int bcp_kv_attend_shared(const bcp_kv_cache* c, const bcp_heads* q, c
   const Variant v = variant_of(c->format, c->head_dim);
   uint32_t sms = 0;
   if (int rc = prepare(v, &sms)) return rc;
-  const Layout at(own, v, sms, n_seqs, q->n_heads, c->head_dim);
   if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 15)) return fail(BCP_ERR_INVALID, "%s: workspace is NULL or not 16-byte aligned", call);
+  const Layout at(own, skew_of(workspace), v, sms, n_seqs, q->n_heads, c->head_dim);
   if (workspace_bytes < at.end)
     return fail(BCP_ERR_CAPACITY, "%s: a workspace of %llu bytes, %llu needed", call, (unsigned long long)workspace_bytes, (unsigned long long)at.end);
   const uint32_t group = q->n_heads / c->n_heads;
