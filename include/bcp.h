@@ -629,7 +629,7 @@ typedef struct {
 #define BCP_BAD_SLOT 2u
 #define BCP_BAD_PAGE 4u
 #define BCP_BAD_LENGTH 8u
-#define BCP_TIMED_OUT 16u   /* a wait inside a kernel ran out (two seconds): the call's results are not to be used */
+#define BCP_TIMED_OUT 16u   /* a wait inside a kernel ran out (BCP_WAIT_NS, see bcp_wait_limit): the call's results are not to be used */
 
 /*
  * Rotates the heads of n_tokens tokens: (y1, y2) = (x1 c - x2 s, x2 c + x1 s) for every pair, with
@@ -762,6 +762,14 @@ BCP_API int bcp_verify_drafts(const bcp_vocab_rows* target, const bcp_vocab_rows
  * stream sets meanwhile stay for the next call), and returns BCP_OK or BCP_ERR_BOUNDS with a message that names the bits.
  */
 BCP_API int bcp_decode_status(uint32_t* status, void* stream);
+
+/*
+ * How long a wait inside the kernel of bcp_kv_attend_shared may take before it gives up (BCP_TIMED_OUT), in calls and captures of this process from now on.
+ * No wait in a sound call takes more than microseconds of the GPU's time; a GPU that leaves a kernel for a debugger or for other processes may need more.
+ * With 0 a wait gives up where it would have to sleep.
+ */
+#define BCP_WAIT_NS 2000000000u
+BCP_API int bcp_wait_limit(uint32_t nanoseconds);
 
 #ifdef __cplusplus
 }

@@ -167,6 +167,7 @@ _PROTOS = {
                                        C.c_float, _VP, C.c_uint64, _VP]),
     "bcp_verify_drafts": (C.c_int, [_VP, _VP, C.c_uint32, C.c_uint32, C.c_uint32, _VP, _VP, _VP, C.c_int, _VP, _VP, _VP]),
     "bcp_decode_status": (C.c_int, [_VP, _VP]),
+    "bcp_wait_limit": (C.c_int, [C.c_uint32]),
     "bcp_pack_static": (C.c_int, [C.POINTER(_VP), C.POINTER(PackMetaC), C.c_size_t, _VP, C.c_uint64, _VP]),
 }
 

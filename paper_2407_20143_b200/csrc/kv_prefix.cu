@@ -26,6 +26,7 @@
 // sequences over 32,768 and up to 600 own tokens, bfloat16: 88 us; 70 over 5 prefixes of up to 9000, e4m3, pages of 24: 96 us; 256 over 32,768, binary16: 220 us.
 #include <cuda.h>
 
+#include <atomic>
 #include <mutex>
 
 #include "attend.cuh"
@@ -36,7 +37,9 @@ namespace {
 
 constexpr uint32_t kRows = 128;             // rows of a stream
 constexpr uint32_t kMeta = 16;              // tiles whose masks and scales are kept
-constexpr uint64_t kMostNs = 2000000000ull; // a wait that takes longer gives up
+constexpr uint32_t kMostNs = BCP_WAIT_NS;   // a wait that takes longer gives up, unless the host has said otherwise
+std::atomic<uint32_t> g_limit{kMostNs};
+constexpr uint32_t kDrainNs = 20000000u;    // copies under way have landed after that
 
 struct PrefixArgs {
   CUtensorMap k_map, v_map;  // the cache as [page][head][token][element], boxes of `block` tokens
@@ -59,6 +62,7 @@ struct PrefixArgs {
   int4* rows;   // of each row: its first record, the next part's, parts, from a record to the other one of the same part (0: it has one)
   float2* ml;   // reference and denominator of each record: l = sum exp2(s - m)
   float* o;     // its sums, o = sum exp2(s - m) v
+  uint32_t limit;  // nanoseconds of a wait
 };
 
 template <int FMT, int DP>
@@ -98,26 +102,30 @@ __device__ __forceinline__ bool bar_test(uint32_t bar, uint32_t parity) {  // wi
   asm volatile("{\n.reg .pred p;\nmbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\nselp.u32 %0, 1, 0, p;\n}" : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
   return ok;
 }
-// Sleeps until the phase is complete, a millisecond at most.
-__device__ __forceinline__ bool bar_sleep(uint32_t bar, uint32_t parity) {
-  uint32_t ok;
-  asm volatile("{\n.reg .pred p;\nmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, 1000000;\nselp.u32 %0, 1, 0, p;\n}" : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
-  return ok;
+// What a wait may take, and the word that says that one has taken longer.
+struct Limit {
+  volatile uint32_t* stop;
+  const uint32_t& ns;
+};
+// Sleeps until the phase is complete, for four microseconds (measured; the hardware's choice) at most; with a limit of zero it only looks.  (To be told how long to sleep
+// takes a register at every wait.  64 sequences over 32,768 tokens and 5 over 4096: 88.5 and 15.4 us, with a constant 89.1 and 15.7, with an argument 92.8 and 16.1.)
+__device__ __forceinline__ bool bar_try(uint32_t bar, uint32_t parity, const Limit& limit) {
+  return limit.ns ? mbar_try_wait(bar, parity) : bar_test(bar, parity);
 }
 // False, in all lanes of a warp, if the wait ran out here or in another warp.
-__device__ __forceinline__ bool bar_wait_slow(uint32_t bar, uint32_t parity, volatile uint32_t* stop) {
+__device__ __forceinline__ bool bar_wait_slow(uint32_t bar, uint32_t parity, const Limit& limit) {
   const uint64_t begin = global_timer_ns();
-  while (!bar_sleep(bar, parity)) {
-    if (*stop) return false;
-    if (global_timer_ns() - begin > kMostNs) {
-      *stop = 1;
+  while (!bar_try(bar, parity, limit)) {
+    if (*limit.stop) return false;
+    if (global_timer_ns() - begin > limit.ns) {
+      *limit.stop = 1;
       return false;
     }
   }
   return true;
 }
-__device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity, volatile uint32_t* stop) {
-  return __all_sync(0xffffffffu, bar_sleep(bar, parity) || bar_wait_slow(bar, parity, stop));
+__device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity, const Limit& limit) {
+  return __all_sync(0xffffffffu, bar_try(bar, parity, limit) || bar_wait_slow(bar, parity, limit));
 }
 
 __device__ __forceinline__ void tmem_alloc(uint32_t to) { asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(to) : "memory"); }
@@ -291,10 +299,12 @@ __global__ void __launch_bounds__(Shape<FMT, DP>::THREADS, 1) bcp_kv_prefix_kern
   uint32_t* const words = reinterpret_cast<uint32_t*>(smem + (raw_full + 32 * S::RAWS + S::STREAMS * 1024 - base));  // tensor memory, stop, found[8]
   volatile float* const swap = reinterpret_cast<volatile float*>(smem + (raw_full + 32 * S::RAWS - base));  // [stream][half][row]
   volatile uint32_t* const stop = words + 1;
+  const Limit limit = {stop, a.limit};
   uint32_t* const found = words + 2;
   uint64_t* const totals = reinterpret_cast<uint64_t*>(smem);  // before the tiles come
 
   if (base & 1023) {  // no room is left to move them there
+    wait_for_previous();
     if (tid == 0) raise(a.status, BCP_TIMED_OUT);
     return;
   }
@@ -399,10 +409,12 @@ __global__ void __launch_bounds__(Shape<FMT, DP>::THREADS, 1) bcp_kv_prefix_kern
     const float scale = fabsf(a.scale_log2);
     constexpr float kLeast = 0x1p-126f;  // a factor is not 0, so that a masked score stays below all others; any score times this counts as 0
     bool ok = true;
-    // The two warps of 32 rows wait for each other; the two threads of a row see each other's number.  (A warp that gives up arrives once more, below, so that
-    // the other does not wait for it.)
+    // The two warps of 32 rows wait for each other; the two threads of a row see each other's number.  That wait has no limit, so a warp that gives up arrives
+    // once more, below, and the other must not wait for it twice: behind the meeting over a tile's scores it gets no further than the wait for the next products,
+    // which need the weights of both; where one meeting follows another without that, it looks whether a wait has run out (together).
     const uint32_t pair = 1 + 4 * stream + quarter;
     auto meet = [&]() { asm volatile("bar.sync %0, 64;" ::"r"(pair) : "memory"); };
+    auto together = [&]() { return !__any_sync(0xffffffffu, *stop); };
     auto other = [&](float mine) {
       swap[(stream * 2 + part) * kRows + row] = mine;
       meet();
@@ -466,6 +478,8 @@ __global__ void __launch_bounds__(Shape<FMT, DP>::THREADS, 1) bcp_kv_prefix_kern
         bar_arrive(q_full + 8 * stream);
         if constexpr (S::quant) {
           meet();
+          ok = together();
+          if (!ok) break;
           factor *= swap[(stream * 2 + part) * kRows + row];
         }
       }
@@ -477,7 +491,7 @@ __global__ void __launch_bounds__(Shape<FMT, DP>::THREADS, 1) bcp_kv_prefix_kern
       for (uint32_t t = both ? 0 : stream; t < n; t += step) {
         const uint32_t m_slot = (tile0 + t) % S::NMETA;
         const unsigned char* const about = meta_ptr + m_slot * S::META;
-        ok = bar_wait(described + 8 * m_slot, (tile0 + t) / S::NMETA & 1, stop) && bar_wait(s_full + 8 * stream, n_scores & 1, stop);
+        ok = bar_wait(described + 8 * m_slot, (tile0 + t) / S::NMETA & 1, limit) && bar_wait(s_full + 8 * stream, n_scores & 1, limit);
         if (!ok) break;
         ++n_scores;
         tmem_after();
@@ -588,7 +602,7 @@ __global__ void __launch_bounds__(Shape<FMT, DP>::THREADS, 1) bcp_kv_prefix_kern
       uint32_t record = b * n_q_heads + head + (!both && stream ? every : 0);
       if (!whole) record = 2 * every + (2 * blockIdx.x + (place != s0)) * S::ROWS + stream * kRows + row;
       if (any) {
-        ok = bar_wait(o_full + 8 * stream, n_ends & 1, stop);
+        ok = bar_wait(o_full + 8 * stream, n_ends & 1, limit);
         if (!ok) break;
         ++n_ends;
         tmem_after();
@@ -605,7 +619,13 @@ __global__ void __launch_bounds__(Shape<FMT, DP>::THREADS, 1) bcp_kv_prefix_kern
             }
           }
           l += other(l);
-          if (S::quant) meet();  // what the next queries bring is written only when this has been read
+          if constexpr (S::quant) {  // what the next queries bring is written only when this has been read
+            ok = together();
+            if (!ok) break;
+            meet();
+            ok = together();
+            if (!ok) break;
+          }
         }
         tmem_before();
       }
@@ -662,10 +682,10 @@ __global__ void __launch_bounds__(Shape<FMT, DP>::THREADS, 1) bcp_kv_prefix_kern
       if constexpr (S::quant) {
         const uint32_t stage = stage_of(landed);
         if (boxes >> (landed & 31) & 1) {
-          ok = ok && bar_wait(raw_full + 8 * (4 * stage + w), phases >> stage & 1, stop);
+          ok = ok && bar_wait(raw_full + 8 * (4 * stage + w), phases >> stage & 1, limit);
           phases ^= 1u << stage;
         }
-        if (this_item >= S::SLOTS) ok = ok && bar_wait(empty + 8 * slot, this_item / S::SLOTS - 1 & 1, stop);
+        if (this_item >= S::SLOTS) ok = ok && bar_wait(empty + 8 * slot, this_item / S::SLOTS - 1 & 1, limit);
         const uint32_t from = raw + stage * S::RAW + (w * kEach + my_row) * a.head_dim + chunk * 16;
         if (inside && ok) {
 #pragma unroll 2
@@ -738,7 +758,7 @@ __global__ void __launch_bounds__(Shape<FMT, DP>::THREADS, 1) bcp_kv_prefix_kern
         // copies that are under way go on to the products while this tile's place is still taken
         const uint32_t parity = item / S::SLOTS - 1 & 1;
         land_now = landed < queued && !__all_sync(0xffffffffu, bar_test(empty + 8 * slot, parity));
-        if (!land_now) ok = bar_wait(empty + 8 * slot, parity, stop);
+        if (!land_now) ok = bar_wait(empty + 8 * slot, parity, limit);
         if (!ok) break;
       }
       if (!land_now) {
@@ -821,12 +841,6 @@ __global__ void __launch_bounds__(Shape<FMT, DP>::THREADS, 1) bcp_kv_prefix_kern
       }
     }
     copies_wait<0>();
-    // (boxes under way are waited for by the products, or, if a wait ran out, by what follows)
-    if (!ok) {
-      const uint64_t begin = global_timer_ns();
-      while (global_timer_ns() - begin < kMostNs / 100) {
-      }
-    }
   } else {
     // ================================================================ the products
     // A warp for each stream: one thread of it issues, which next to the busy warps takes about as long as the products themselves.
@@ -861,7 +875,7 @@ __global__ void __launch_bounds__(Shape<FMT, DP>::THREADS, 1) bcp_kv_prefix_kern
         }
       };
       auto arrived = [&](uint32_t bar, uint32_t parity) {
-        ok = ok && bar_wait(bar, parity, stop);
+        ok = ok && bar_wait(bar, parity, limit);
         tmem_after();
         return ok;
       };
@@ -922,18 +936,26 @@ __global__ void __launch_bounds__(Shape<FMT, DP>::THREADS, 1) bcp_kv_prefix_kern
         left -= n;
         advance<S>(at, a, n, left != 0);
       }
-      if (!ok) {  // what was issued comes to its end before the tensor memory is given back
-        if (chosen) tmem_commit(drained + 8 * stream);
-        __syncwarp();
-        const uint64_t begin = global_timer_ns();
-        while (!mbar_try_wait(drained + 8 * stream, 0) && global_timer_ns() - begin < kMostNs) {
-        }
-      }
     }
   }
   tmem_before();
   __syncthreads();
-  if (tid == 0 && *stop) raise(a.status, BCP_TIMED_OUT);
+  if (*stop) {
+    // A wait has run out in some warp (all others are done, too, so nobody changes the word any more): products and boxes that nobody has waited for come to
+    // their end before the memory they use is given back.
+    const uint32_t stream = warp - (8 * S::STREAMS + S::LOADERS);
+    const uint64_t begin = global_timer_ns();
+    if (stream < S::STREAMS) {
+      if (elected()) tmem_commit(drained + 8 * stream);
+      __syncwarp();
+      while (!mbar_try_wait(drained + 8 * stream, 0) && global_timer_ns() - begin < kMostNs) {
+      }
+    }
+    while (global_timer_ns() - begin < kDrainNs) {
+    }
+    if (tid == 0) raise(a.status, BCP_TIMED_OUT);
+    __syncthreads();
+  }
   tmem_after();
   if (warp == S::WARPS - 4) tmem_free(tmem);
 }
@@ -1181,6 +1203,11 @@ uint64_t skew_of(const void* workspace) { return (0 - reinterpret_cast<uintptr_t
 
 using namespace bcp;
 
+extern "C" int bcp_wait_limit(uint32_t nanoseconds) {
+  g_limit.store(nanoseconds, std::memory_order_relaxed);
+  return BCP_OK;
+}
+
 extern "C" int bcp_kv_attend_shared_workspace(const bcp_kv_cache* cache, uint32_t n_q_heads, uint32_t max_seqs, uint64_t* bytes) {
   const char* call = "bcp_kv_attend_shared_workspace";
   uint64_t own = 0;
@@ -1237,6 +1264,7 @@ extern "C" int bcp_kv_attend_shared(const bcp_kv_cache* c, const bcp_heads* q, c
   a.table = prefix_table, a.table_stride = prefix_stride;
   a.lengths = prefix_lengths, a.starts = starts;
   a.scale_log2 = scale * kLog2e;
+  a.limit = g_limit.load(std::memory_order_relaxed);
   if (int rc = make_maps(c, v, &a)) return rc;
   char* const w = static_cast<char*>(workspace);
   a.rows = reinterpret_cast<int4*>(w + at.rows), a.ml = reinterpret_cast<float2*>(w + at.ml), a.o = reinterpret_cast<float*>(w + at.o);
