@@ -239,7 +239,9 @@ extern "C" int bcp_decode_status(uint32_t* status, void* stream_) {
   }
   if (e != cudaSuccess) return fail(BCP_ERR_CUDA, "bcp_decode_status: %s", cudaGetErrorString(e));
   if (!bits) return BCP_OK;
-  return fail(BCP_ERR_BOUNDS, "an index was outside its range and was left out:%s%s%s%s%s", bits & BCP_BAD_POSITION ? " position" : "",
-              bits & BCP_BAD_SLOT ? " slot" : "", bits & BCP_BAD_PAGE ? " page" : "", bits & BCP_BAD_LENGTH ? " length" : "",
-              bits & BCP_TIMED_OUT ? " (a wait inside a kernel ran out)" : "");
+  const char* const ran_out = bits & BCP_TIMED_OUT ? "a wait inside a kernel ran out, the results of its call are not to be used" : "";
+  if (!(bits & ~BCP_TIMED_OUT)) return fail(BCP_ERR_BOUNDS, "%s", ran_out);
+  return fail(BCP_ERR_BOUNDS, "%s%san index was outside its range and was left out:%s%s%s%s", ran_out, *ran_out ? "; " : "",
+              bits & BCP_BAD_POSITION ? " position" : "", bits & BCP_BAD_SLOT ? " slot" : "", bits & BCP_BAD_PAGE ? " page" : "",
+              bits & BCP_BAD_LENGTH ? " length" : "");
 }

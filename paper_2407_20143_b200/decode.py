@@ -35,7 +35,7 @@ from .api import ERR_INVALID, BcpError, _check
 
 F32, BF16, F16, E4M3, I8 = 1, 2, 3, 4, 5
 ROPE_HALF, ROPE_PAIRS = 0, 1
-BAD_POSITION, BAD_SLOT, BAD_PAGE, BAD_LENGTH = 1, 2, 4, 8
+BAD_POSITION, BAD_SLOT, BAD_PAGE, BAD_LENGTH, TIMED_OUT = 1, 2, 4, 8, 16
 MAX_HEAD_DIM, MAX_AXES = 256, 4
 _LAYOUTS = {"half": ROPE_HALF, "pairs": ROPE_PAIRS}
 

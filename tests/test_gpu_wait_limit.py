@@ -5,7 +5,7 @@ import torch
 
 import paper_2407_20143_b200 as bcp
 from paper_2407_20143_b200 import _lib as L
-from paper_2407_20143_b200 import api
+from paper_2407_20143_b200 import api, decode
 
 pytestmark = pytest.mark.gpu
 
@@ -51,3 +51,15 @@ def test_waits_that_run_out_end_the_call(cuda_device, limit, dtype, dim, seqs, p
         cache.check()
         assert torch.equal(out, want[0]) and torch.equal(lse, want[1])
     assert ran_out > 0
+
+
+def test_what_the_status_word_is_reported_as(cuda_device):
+    cache = bcp.KvCache.empty(1, 1, 16, 64)
+    outside = "an index was outside its range and was left out:"
+    for bits, says, not_says in ((decode.TIMED_OUT, ["a wait", "ran out"], [outside]), (decode.BAD_PAGE, [outside + " page"], ["wait", "slot"]),
+                                 (decode.TIMED_OUT | decode.BAD_LENGTH | decode.BAD_SLOT, ["a wait", "ran out", outside + " slot length"], ["page"])):
+        cache.status.fill_(bits)
+        with pytest.raises(bcp.BcpError) as e:
+            cache.check()
+        assert e.value.code == api.ERR_BOUNDS and all(x in str(e.value) for x in says) and not any(x in str(e.value) for x in not_says)
+        cache.check()
