@@ -738,7 +738,7 @@ BCP_API int bcp_kv_attend_shared(const bcp_kv_cache* cache, const bcp_heads* q, 
  * certain (looked up, say), q_i is 1 at x_i and 0 elsewhere.  Rows are logits, p = softmax(z / temperature[b]) (temperature NULL: 1; above
  * 1e30: that; not above 1e-30: greedy, p is 1 at the lowest index of the largest logit), or, with probabilities != 0, weights that are taken as they are.
  * Draft i is accepted iff all before it are and uniform[b*(n_drafts+1) + i] * q_i(x_i) < p_i(x_i); a draft past the vocabulary is not.  At the first
- * one that is not, r = max(p_i - q_i, 0) (p_i, if that is zero throughout); if all n are, r = p_n.  The next token is the lowest j with
+ * one that is not, r = max(p_i - q_i, 0) (p_i, if that is zero throughout, or if q_i holds a NaN); if all n are, r = p_n.  The next token is the lowest j with
  * sum_{l<=j} r(l) > uniform[b*(n_drafts+1) + n_drafts] * sum_l r(l) (should rounding leave none, the last with r > 0).
  * tokens[b*(n_drafts+1) ..]: the accepted drafts, the next token, then -1.  accepted[b]: how many drafts.  The next token is -1 where its
  * row has no weight, or one that is no finite number (all logits -infinity, a NaN, a logit of +infinity).

@@ -62,6 +62,12 @@ __device__ __forceinline__ float2 add2(float2 a, float2 b) {
       : "=f"(r.x), "=f"(r.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
   return r;
 }
+// The larger one; a NaN if either is one (which fmaxf would pass over).
+__device__ __forceinline__ float largest(float a, float b) {
+  float r;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+  return r;
+}
 __device__ __forceinline__ float reference(float m) { return m == -INFINITY ? 0.f : m; }
 
 // A row in units of eight elements that start on 16-byte boundaries: unit v has elements 8 v - shift and on, of which those outside
@@ -195,14 +201,14 @@ struct Weights {  // of the row that is drawn from
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       w[i] = probability(to_f32(x.get(i)), ps);
-      if (use_q) w[i] = fmaxf(w[i] - probability(to_f32(y.get(i)), qs), 0.f);
+      if (use_q) w[i] = largest(w[i] - probability(to_f32(y.get(i)), qs), 0.f);
       if (PROB && w[i] < 0.f) w[i] = 0.f;
     }
     const int32_t skip = without - e;
     if (e < 0 || uint32_t(e) + 8 > p.n || uint32_t(skip) < 8) {
 #pragma unroll
       for (int i = 0; i < 8; ++i)
-        if (i == skip || e + i < 0 || uint32_t(e + i) >= p.n) w[i] = 0.f;
+        if ((i == skip && !(PROB && w[i] != w[i])) || e + i < 0 || uint32_t(e + i) >= p.n) w[i] = 0.f;
     }
   }
 };
@@ -322,7 +328,7 @@ __global__ void __launch_bounds__(kThreads, 4) bcp_verify_kernel(const VerifyArg
     const uint32_t n_segments = (w.p.units + kSegment / 8 - 1) / (kSegment / 8), each = (n_segments + ctas - 1) / ctas;
     const uint32_t s0 = min(rank * each, n_segments), s1 = min(s0 + each, n_segments);
     const double u = uniform[a.n_drafts];
-    // what is left after q may be nothing at all (p and q alike, a draft outside its own row): then p itself counts
+    // what is left after q may be nothing at all (p and q alike, a draft outside its own row), or q's row holds no number: then p itself counts
     for (int round = 0;; ++round) {
       // four stretches at a time, so that their loads are under way together
       constexpr uint32_t kTogether = sizeof(T) == 2 ? 4 : 2;
