@@ -741,7 +741,8 @@ BCP_API int bcp_kv_attend_shared(const bcp_kv_cache* cache, const bcp_heads* q, 
  * one that is not, r = max(p_i - q_i, 0) (p_i, if that is zero throughout, or if q_i holds a NaN); if all n are, r = p_n.  The next token is the lowest j with
  * sum_{l<=j} r(l) > uniform[b*(n_drafts+1) + n_drafts] * sum_l r(l) (should rounding leave none, the last with r > 0).
  * tokens[b*(n_drafts+1) ..]: the accepted drafts, the next token, then -1.  accepted[b]: how many drafts.  The next token is -1 where its
- * row has no weight, or one that is no finite number (all logits -infinity, a NaN, a logit of +infinity).
+ * row has no weight, or one that is no finite number (all logits -infinity, a NaN, a logit of +infinity).  Greedy rows have one weight, so of these only all
+ * logits -infinity and a NaN: +infinity is the largest logit.  A draft whose row of logits holds a NaN is not accepted.
  * Sums are held in 64 bits, their terms in 32.  Random numbers are at least 0 and below 1.
  */
 #define BCP_MAX_DRAFTS 64u

@@ -44,7 +44,7 @@ struct VerifyArgs {
   int32_t* accepted;
 };
 
-// What is known of a row, or a part of it: the largest value and the sum of exp2((z - m) c); greedy: the index of the largest.
+// What is known of a row, or a part of it: the largest value and the sum of exp2((z - m) c); greedy: the index of the largest (m a NaN: the row holds one).
 struct RowSum {
   float m;
   uint32_t index;
@@ -96,7 +96,7 @@ struct Row {
 __device__ __forceinline__ float largest8(const Raw<float, 8>& r) {
   float m = r.get(0);
 #pragma unroll
-  for (int i = 1; i < 8; ++i) m = fmaxf(m, r.get(i));
+  for (int i = 1; i < 8; ++i) m = largest(m, r.get(i));
   return m;
 }
 template <typename T, typename T2>
@@ -104,8 +104,8 @@ __device__ __forceinline__ float largest_of_pairs(const Raw<T, 8>& r) {
   T2 p[4];
 #pragma unroll
   for (int i = 0; i < 4; ++i) p[i] = *reinterpret_cast<const T2*>(&r.w[i]);
-  const T2 m = __hmax2(__hmax2(p[0], p[1]), __hmax2(p[2], p[3]));
-  return fmaxf(to_f32(m.x), to_f32(m.y));
+  const T2 m = __hmax2_nan(__hmax2_nan(p[0], p[1]), __hmax2_nan(p[2], p[3]));
+  return largest(to_f32(m.x), to_f32(m.y));
 }
 __device__ __forceinline__ float largest8(const Raw<__nv_bfloat16, 8>& r) { return largest_of_pairs<__nv_bfloat16, __nv_bfloat162>(r); }
 __device__ __forceinline__ float largest8(const Raw<__half, 8>& r) { return largest_of_pairs<__half, __half2>(r); }
@@ -122,10 +122,10 @@ __device__ __forceinline__ RowSum look_over(const Row<T>& row, uint32_t first, u
     for (int j = 0; j < kAhead; ++j) row.raw(v0 + j * 32, end, -INFINITY, x[j]);
     float top = largest8(x[0]);
 #pragma unroll
-    for (int j = 1; j < kAhead; ++j) top = fmaxf(top, largest8(x[j]));
+    for (int j = 1; j < kAhead; ++j) top = largest(top, largest8(x[j]));
     if (greedy) {
-      if (top > r.m) {
-        r.m = top;
+      if (!(top <= r.m) && r.m == r.m) {  // larger, or a NaN, which stays and is at no index
+        r.m = top, r.index = 0xffffffffu;
 #pragma unroll
         for (int j = kAhead - 1; j >= 0; --j)
 #pragma unroll
@@ -153,7 +153,7 @@ __device__ __forceinline__ RowSum look_over(const Row<T>& row, uint32_t first, u
 // The same of `lanes` lanes together, in all of them.
 __device__ __forceinline__ RowSum join(RowSum r, float c, bool greedy, uint32_t lanes) {
   float m = r.m;
-  for (uint32_t o = lanes / 2; o; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+  for (uint32_t o = lanes / 2; o; o >>= 1) m = largest(m, __shfl_xor_sync(0xffffffffu, m, o));
   if (greedy) {
     uint32_t index = r.m == m ? r.index : 0xffffffffu;
     for (uint32_t o = lanes / 2; o; o >>= 1) index = min(index, __shfl_xor_sync(0xffffffffu, index, o));

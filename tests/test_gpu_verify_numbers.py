@@ -53,3 +53,30 @@ def test_weights_that_are_no_numbers(cuda_device, dtype, v):
     broken[0, 1, 11] = math.nan
     for draft in (q, None):
         assert _verify(broken, draft, u=(0.0, 0.4), draft=6, probabilities=True) == ([6, -1], 1)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F16, F32])
+@pytest.mark.parametrize("v", [9, 1000, 40001, 128256])
+def test_greedy_rows_that_hold_no_numbers(cuda_device, dtype, v):
+    # a NaN: no logit is the largest, so no draft is it either; +infinity is the largest logit
+    b, greedy = 6, torch.zeros(6, device="cuda")
+    z = torch.randn((b, 2, v), generator=torch.Generator(device="cuda").manual_seed(3), device="cuda").to(dtype)
+    best, behind = (torch.where(z == z.amax(-1, keepdim=True), torch.arange(v, device="cuda"), v).amin(-1)).unbind(1)
+    for at in (0, 3, v // 2, v - 1):
+        broken, drafts = z.clone(), best[:, None].clone()
+        broken[0, 0, at] = math.nan
+        broken[1, 0, at] = -math.nan
+        broken[2, 0, at] = math.inf
+        broken[3, 0, at], drafts[3] = math.inf, at
+        broken[4, 1, at] = math.nan                        # behind the accepted draft
+        broken[5, 0, :] = -math.inf
+        broken[5, 0, at], drafts[5] = math.nan, at         # nothing but a NaN
+        for draft in (None, z[:, :1]):
+            tokens, accepted = bcp.bcp_verify_drafts(broken, drafts, torch.full((b, 2), 0.5, device="cuda"), draft=draft, temperature=greedy)
+            second = at if int(best[2]) != at else int(behind[2])
+            hit = int(best[2]) == at
+            assert accepted.tolist() == [0, 0, int(hit), 1, 1, 0]
+            assert tokens.tolist() == [[-1, -1], [-1, -1], [at, second] if hit else [at, -1], [at, int(behind[3])], [int(best[4]), -1], [-1, -1]]
+    # warm rows of the same batch: a NaN or +infinity anywhere
+    warm, _ = bcp.bcp_verify_drafts(broken, drafts, torch.full((b, 2), 0.5, device="cuda"))
+    assert warm[[0, 1, 2, 5], 0].tolist() == [-1] * 4
