@@ -16,8 +16,11 @@
 // over 50,257 probabilities, binary32: 7 us (only the row that is drawn from is read).
 //
 // Precision: a token hangs on a comparison, so sums are held in 64 bits and the probability of a drafted token is computed in 64 bits
-// from its logit; the terms of the sums are binary32 (2^-22 of each).
+// from its logit; the terms of the sums are binary32 (2^-22 of each).  Of terms made from logits 32 (rows) or 256 (the draw) are added in binary32 first, at most
+// eight additions deep (2^-21); weights that are given are added in 64 bits from the first on.
 #include <cooperative_groups.h>
+
+#include <type_traits>
 
 #include "decode.cuh"
 
@@ -168,6 +171,11 @@ __device__ __forceinline__ RowSum join(RowSum r, float c, bool greedy, uint32_t 
 struct Scale {
   float m, c, inverse;
 };
+
+// What a stretch's weights are added up in.  Given ones are exact and may be of any size; those made from logits are at most 1 and off by 2^-22 each, and the
+// eight additions of binary32 that one goes through add 2^-21.
+template <bool PROB>
+using Sum = std::conditional_t<PROB, double, float>;
 
 template <typename T, bool PROB>
 struct Weights {  // of the row that is drawn from
@@ -335,12 +343,15 @@ __global__ void __launch_bounds__(kThreads, 4) bcp_verify_kernel(const VerifyArg
       for (uint32_t s = s0 + warp; s < s1; s += warps * kTogether) {
         Raw<T, 8> p[kTogether], q[kTogether];
         w.read(s * (kSegment / 8) + lane, warps * (kSegment / 8), p, q);
-        float sum[kTogether];
+        Sum<PROB> sum[kTogether];
 #pragma unroll
         for (uint32_t j = 0; j < kTogether; ++j) {
           float x[8];
           w.weigh(w.p.first((s + j * warps) * (kSegment / 8) + lane), p[j], q[j], x);
-          sum[j] = ((x[0] + x[1]) + (x[2] + x[3])) + ((x[4] + x[5]) + (x[6] + x[7]));
+          Sum<PROB> y[8];
+#pragma unroll
+          for (int i = 0; i < 8; ++i) y[i] = x[i];
+          sum[j] = ((y[0] + y[1]) + (y[2] + y[3])) + ((y[4] + y[5]) + (y[6] + y[7]));
         }
 #pragma unroll
         for (int o = 16; o; o >>= 1)

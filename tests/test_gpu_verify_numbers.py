@@ -80,3 +80,41 @@ def test_greedy_rows_that_hold_no_numbers(cuda_device, dtype, v):
     # warm rows of the same batch: a NaN or +infinity anywhere
     warm, _ = bcp.bcp_verify_drafts(broken, drafts, torch.full((b, 2), 0.5, device="cuda"))
     assert warm[[0, 1, 2, 5], 0].tolist() == [-1] * 4
+
+
+def _sampled(weights, u):
+    """The token that each random number draws from one row of weights (float32 [v], probabilities=True)."""
+    n = len(u)
+    tokens, _ = bcp.bcp_verify_drafts(weights.cuda().expand(n, 1, -1), torch.zeros((n, 0), dtype=torch.int64, device="cuda"),
+                                      torch.tensor(u, dtype=F32, device="cuda")[:, None], probabilities=True)
+    return tokens[:, 0].tolist()
+
+
+def _want(weights, u):
+    """The same in 64 bits.  Sums of whole numbers below 2^53, and their products with numbers of 24 bits below 2^29, are exact in any order."""
+    line = weights.double().cumsum(0)
+    return torch.searchsorted(line, torch.tensor(u, dtype=F32).double() * line[-1], right=True).tolist()
+
+
+@pytest.mark.parametrize("v,big,border", [(512, 2 ** 24, 256), (600, 2 ** 24, 512), (5000, 2 ** 25, 1024), (40001, 2 ** 24, 20224)])
+def test_sums_of_weights_are_held_in_64_bits(cuda_device, v, big, border):
+    # ones beside weights of 2^24 and more, which sums of 32 bits round away; places one apart around the end of a stretch of 256 tokens
+    weights = torch.ones(v)
+    weights[border - 256] = weights[border] = big
+    line = weights.double().cumsum(0)
+    at = torch.tensor([float(line[border - 1]) + d for d in range(-300, 40, 3)], dtype=torch.float64) / float(line[-1])
+    u = at.float().clamp(0, 1 - 2.0 ** -24).tolist()
+    want = _want(weights, u)
+    assert sum(border - 256 < w < border for w in want) > 20 and border in want  # (on both sides)
+    assert _sampled(weights, u) == want
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("v", [8, 300, 40001])
+def test_large_weights(cuda_device, dtype, v):
+    # any two add up to more than binary32 holds
+    u = [0.0, 0.2503, 0.7501, 1 - 2.0 ** -24]
+    n = len(u)
+    weights = torch.full((1, 1, v), torch.finfo(dtype).max, dtype=dtype, device="cuda").expand(n, 1, v)
+    tokens, _ = bcp.bcp_verify_drafts(weights, torch.zeros((n, 0), dtype=torch.int64, device="cuda"), torch.tensor(u, device="cuda")[:, None], probabilities=True)
+    assert tokens[:, 0].tolist() == [int(torch.tensor(x, dtype=F32).double() * v) for x in u]
