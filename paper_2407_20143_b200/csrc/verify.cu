@@ -483,6 +483,15 @@ cudaError_t launch(const VerifyArgs& a, bool prob, uint32_t n_seqs, uint32_t cta
   return prob ? launch<T, true>(a, n_seqs, ctas, smem, stream) : launch<T, false>(a, n_seqs, ctas, smem, stream);
 }
 
+struct Span {
+  const void* at;
+  uint64_t bytes;
+  bool meets(const Span& o) const {
+    const uintptr_t x = reinterpret_cast<uintptr_t>(at), y = reinterpret_cast<uintptr_t>(o.at);
+    return bytes && o.bytes && x < y + o.bytes && y < x + bytes;
+  }
+};
+
 int check_rows(const char* call, const char* name, const bcp_vocab_rows* r) {
   if (!r) return fail(BCP_ERR_INVALID, "%s: %s is NULL", call, name);
   if (r->type != BCP_F32 && r->type != BCP_BF16 && r->type != BCP_F16)
@@ -513,6 +522,15 @@ extern "C" int bcp_verify_drafts(const bcp_vocab_rows* target, const bcp_vocab_r
     if (draft->type != target->type) return fail(BCP_ERR_MISMATCH, "%s: target and draft have different types", call);
   }
   if ((n_drafts && !drafts) || !uniform || !tokens || !accepted) return fail(BCP_ERR_INVALID, "%s: drafts, uniform, tokens or accepted is NULL", call);
+
+  // one CTA writes while others of its cluster, and other sequences', may still read
+  const uint64_t places = uint64_t(n_seqs) * (n_drafts + 1);
+  const Span in[] = {{drafts, (places - n_seqs) * sizeof *drafts}, {uniform, places * sizeof *uniform}, {temperature, temperature ? n_seqs * sizeof *temperature : 0}};
+  const Span out[] = {{tokens, places * sizeof *tokens}, {accepted, n_seqs * sizeof *accepted}};
+  for (const Span& o : out)
+    for (const Span& i : in)
+      if (o.meets(i)) return fail(BCP_ERR_DST_ALIAS, "%s: tokens or accepted overlap drafts, uniform or temperature", call);
+  if (out[0].meets(out[1])) return fail(BCP_ERR_DST_ALIAS, "%s: tokens and accepted overlap", call);
 
   VerifyArgs a = {};
   a.target = target->data, a.t_seq = target->seq_stride, a.t_row = target->row_stride;
