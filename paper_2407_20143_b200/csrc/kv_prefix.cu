@@ -1131,10 +1131,11 @@ int prepare(const Variant& v, uint32_t* sms) {
       *sms = known[i].sms;
       return BCP_OK;
     }
-  // the warpgroups hand registers to one another: what they hand on has to be there
+  // The warpgroups hand registers to one another, and with fewer than they count on some would wait forever.  A kernel that hands them on is launched with the most that
+  // its launch bounds allow, whatever it needs, so this refuses nothing but the work of a compiler that does otherwise.
   cudaFuncAttributes about;
   BCP_CUDA(cudaFuncGetAttributes(&about, v.kernel));
-  if (v.registers && about.numRegs != int(v.registers)) return fail(BCP_ERR_CUDA, "bcp_kv_attend_shared: the kernel has %d registers a thread, not %u", about.numRegs, v.registers);
+  if (v.registers && about.numRegs < int(v.registers)) return fail(BCP_ERR_CUDA, "bcp_kv_attend_shared: the kernel has %d registers a thread, not %u", about.numRegs, v.registers);
   BCP_CUDA(cudaFuncSetAttribute(v.kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, int(v.smem)));
   BCP_CUDA(cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, device));
   *sms = uint32_t(n);
