@@ -715,7 +715,7 @@ BCP_API int bcp_kv_attend(const bcp_kv_cache* cache, const bcp_heads* q, const b
  * bcp_kv_attend for groups of sequences that share a prefix, which is read and multiplied once for all sequences of a group (samples of
  * one prompt, questions about one document; the drafted tokens of one sequence, whose own tokens so far are the prefix).
  * Sequences starts[g] <= b < starts[g+1] (n_prefixes + 1 numbers that do not decrease) attend over the first prefix_lengths[g] tokens of prefix g,
- * whose pages are row g of prefix_table, and then over their own lengths[b] tokens, whose pages are row b of block_table: softmax and lse are
+ * whose pages are row g of prefix_table (prefix_stride 0: all groups have one row), and then over their own lengths[b] tokens, whose pages are row b of block_table: softmax and lse are
  * those over both.  Sequences before starts[0] or from starts[n_prefixes] on have no prefix.  Everything else is as for bcp_kv_attend, without a
  * window; of the prefix, weights over a bfloat16 or 8-bit cache are the sum of two bfloat16 numbers (2^-16; below 2^-86 of the largest they may count
  * as nothing), over binary16 ones binary16.

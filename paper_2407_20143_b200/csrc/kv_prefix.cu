@@ -1231,7 +1231,7 @@ extern "C" int bcp_kv_attend_shared(const bcp_kv_cache* c, const bcp_heads* q, c
   if (int rc = check_heads(call, "q", q, false, c->head_dim, n_seqs)) return rc;
   if (int rc = check_group(call, c, q->n_heads)) return rc;
   if (n_seqs > 0x7fffffffu || n_prefixes > 0x7fffffffu) return fail(BCP_ERR_INVALID, "%s: %u sequences, %u prefixes", call, n_seqs, n_prefixes);
-  if (n_prefixes && (!prefix_table || !prefix_lengths || !starts || prefix_stride < 0 || (n_prefixes > 1 && prefix_stride < int64_t(prefix_width))))
+  if (n_prefixes && (!prefix_table || !prefix_lengths || !starts || prefix_stride < 0 || (n_prefixes > 1 && prefix_stride && prefix_stride < int64_t(prefix_width))))
     return fail(BCP_ERR_INVALID, "%s: prefix_table, prefix_lengths or starts is NULL, or rows of the table overlap", call);
   if (!(scale == scale) || scale - scale != 0.f) return fail(BCP_ERR_INVALID, "%s: scale is not a finite number", call);
   uint64_t own = 0;

@@ -1,4 +1,5 @@
-"""Workspaces of the attention over shared prefixes as its declaration allows them: anywhere on a 16-byte boundary, exactly as large as asked for."""
+"""Arguments of the attention over shared prefixes as its declaration allows them: workspaces anywhere on a 16-byte boundary, exactly as large as asked for; one row
+of the prefixes' table for all groups."""
 import pytest
 import torch
 
@@ -47,3 +48,21 @@ def test_a_workspace_that_is_too_small_or_off_the_boundary_is_refused(cuda_devic
     for work.address, work.bytes in ((address + 8, n - 8), (address + 4, n - 4), (address + 16, n - 512)):
         with pytest.raises(bcp.BcpError):
             call()
+
+
+@pytest.mark.parametrize("groups", [1, 2, 5])
+def test_one_row_of_the_table_for_all_prefixes(cuda_device, groups):
+    # prefixes of different lengths over the same pages
+    cache = bcp.KvCache.empty(30, 2, 16, 64, torch.bfloat16)
+    g = torch.Generator(device="cuda").manual_seed(1)
+    k, v = (torch.randn((480, 2, 64), generator=g, device="cuda") for _ in range(2))
+    bcp.bcp_kv_write(cache, k, v, torch.arange(480, device="cuda"))
+    q = torch.randn((10, 8, 64), generator=g, device="cuda").bfloat16()
+    row = torch.randperm(20, generator=torch.Generator().manual_seed(1)).int().cuda()[None]
+    lengths, starts = _int([320 - 37 * i for i in range(groups)]), _int([10 * i // groups for i in range(groups + 1)])
+    more = (lengths, starts, _int([[20 + i] for i in range(10)]), _int([7] * 10))
+    expanded = row.expand(groups, -1)
+    out, lse = bcp.bcp_kv_attend_shared(cache, q, expanded, *more)
+    want, sums = bcp.bcp_kv_attend_shared(cache, q, expanded.contiguous(), *more)
+    cache.check()
+    assert torch.equal(out, want) and torch.equal(lse, sums)
