@@ -76,8 +76,9 @@ struct Shape {
   static constexpr uint32_t Q = kRows * DP * 2;
   static constexpr uint32_t RAW = quant ? TOK * DP : 0;      // of a tile as it lies in an 8-bit cache
   static constexpr uint32_t RAWS = quant ? 3 : 0;
-  // Warps that bring tokens; 8-bit ones have to be widened by them, too (70 sequences over 5 prefixes of up to 9000 tokens, e4m3: 104 us with four, 98 with eight on
-  // every tile, 96 with four for keys and four for values).
+  // Warps that bring tokens; 8-bit ones have to be widened by them, too.  Microseconds with four on every tile and with four for keys and four for values (e4m3, pages of
+  // 24): 70 sequences over 5 prefixes of up to 9000 tokens 98.7 and 96.7, 5 sequences over one 37.0 and 35.9, 64 over one 76.0 and 79.2; pages of 7 102.4, 37.9, 77.7
+  // and 98.9, 36.6, 80.0.
   static constexpr uint32_t LOADERS = quant && STREAMS == 2 ? 8 : 4;
   static constexpr uint32_t META = quant ? 16 + TOK * 8 + 16 : 16;
   static constexpr uint32_t NMETA = quant ? 8 : kMeta;         // (more than the tiles that can be on their way past one that is still worked on)
@@ -972,8 +973,9 @@ struct JoinArgs {
   int64_t out_token, out_head;
   uint32_t is_bf16;
 };
-// Rows for which eight warps each are more than a warp each: 160 rows of 33 records 14.8 us (all three kernels), 26 with a warp; 2048 of 21 104 and 96.
-constexpr uint32_t kFewRows = 600;
+// Rows for which eight warps each are faster than a warp each.  Microseconds (all three kernels, 128 dimensions) with eight and with one over a prefix of 4096: 160 rows 14.7
+// and 20.8, 480 20.4 and 24.2, 800 22.3 and 25.7, 1216 28.4 and 26.0, 2048 34.5 and 27.8; over 32,768: 800 rows 48.9 and 53.6, 1216 59.4 and 56.9.
+constexpr uint32_t kFewRows = 1000;
 
 // TOGETHER: eight warps take a row, else a warp does.
 template <int DP, bool TOGETHER>
