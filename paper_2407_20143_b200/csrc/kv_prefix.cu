@@ -21,9 +21,10 @@
 //
 // What bounds it: the chain of a tile.  Scores of 128 x 128, their largest, the exchange between a row's two threads, 64 exponentials a thread in two halves, products:
 // 2.9 us for both streams with weights of two numbers and 2.4 with one, where the tensor cores need 1.56 and 1.04, exponentials 1.04, and the tile's 64 KB 1.5 at the
-// copy bandwidth.  8-bit caches wait for the warps that widen them (about 2.9 us a tile of 128 tokens).  Measured on one B200, launches of all three kernels
-// in a row in a CUDA graph, 32 / 8 heads of 128: 5 drafted tokens over 4096, bfloat16: 14.8 us (without prefix and own tokens the three launches take 7.5); 64
-// sequences over 32,768 and up to 600 own tokens, bfloat16: 88 us; 70 over 5 prefixes of up to 9000, e4m3, pages of 24: 96 us; 256 over 32,768, binary16: 220 us.
+// copy bandwidth.  8-bit caches wait for the warps that widen them (about 2.9 us a tile of 128 tokens).  Measured on one B200, all three kernels, 32 / 8 heads of 128,
+// among other calls with inputs that change (in brackets: the same call over and over in a CUDA graph): 5 drafted tokens over 4096, bfloat16: 15.7 us (15.4; without
+// prefix and own tokens the three launches take 7.5); 64 sequences over 32,768 and up to 600 own tokens, bfloat16: 95 us (88); 70 over 5 prefixes of up to 9000, e4m3,
+// pages of 24: 107 us (97); 256 over 32,768, binary16: 254 us (217).  With 256 dimensions, 64 sequences over 16,384: bfloat16 136 us, binary16 127, e4m3 160.
 #include <cuda.h>
 
 #include <atomic>

@@ -388,7 +388,8 @@ def bcp_verify_drafts(target, drafts, uniform, draft=None, temperature=None, pro
     behind the last one.  draft [sequences, n, vocabulary] is what the drafts were drawn from (None: they were certain); temperature
     (float32 [sequences]; 0: greedy) goes for both.  n may be 0: the next token is sampled.
     Returns (tokens int64 [sequences, n + 1]: the accepted drafts, the next token, then -1; accepted int32 [sequences]: how many drafts).  The
-    next token is -1 where its row has no weight or holds no number."""
+    next token is -1 where its row has no weight or holds a NaN (or infinite weight; among greedy logits +infinity is the largest).  `out` and `accepted`
+    must not share memory with the inputs."""
     if not isinstance(target, torch.Tensor):
         raise _invalid("target is not a tensor")
     if out is None:
