@@ -743,7 +743,8 @@ BCP_API int bcp_kv_attend_shared(const bcp_kv_cache* cache, const bcp_heads* q, 
  * tokens[b*(n_drafts+1) ..]: the accepted drafts, the next token, then -1.  accepted[b]: how many drafts.  The next token is -1 where its
  * row has no weight, or one that is no finite number (all logits -infinity, a NaN, a logit of +infinity).  Greedy rows have one weight, so of these only all
  * logits -infinity and a NaN: +infinity is the largest logit.  A draft whose row of logits holds a NaN is not accepted.
- * Sums are held in 64 bits, their terms in 32 (of terms made from logits up to 256 are added in 32 bits first).  Random numbers are at least 0 and below 1.
+ * Sums are held in 64 bits, their terms in 32 (of terms made from logits up to 256 are added in 32 bits first; of p_i - q_i what is below 2^-21 of p_i is not
+ * certain, nor its sign, which only counts where p_i and q_i are that close throughout).  Random numbers are at least 0 and below 1.
  * tokens and accepted overlap neither each other nor drafts, uniform and temperature (BCP_ERR_DST_ALIAS).
  */
 #define BCP_MAX_DRAFTS 64u
